@@ -478,6 +478,128 @@ void goldy_graph_free(goldy_graph* g);
 goldy_status goldy_gemm_noalloc(const goldy_gemm_desc* desc, int variant, const void* A,
                                 const void* B, void* C, void* stream);
 
+/* ---- a linear layer, plain or grouped by expert ---------------------------
+ * The products of Y = act(X W + b) + R and of its backward pass, each one
+ * kernel with the work around the product in its epilogue.  X is rows x in, W
+ * is in x out, Y is rows x out, row-major; X, W and dY are bf16, products are
+ * accumulated in fp32, and every result is rounded once, to nearest even.
+ *
+ * groups = 0: one W for all rows.  groups = E >= 1: E experts with weights
+ * W + e * stride_w and packed biases b + e * out; rows offsets[e] ..
+ * offsets[e+1] - 1 belong to expert e.  offsets: E + 1 non-decreasing 32-bit
+ * integers in device memory, read by the kernels (so they may be written by
+ * an earlier kernel of the stream, and no host copy is needed).  Experts may
+ * be empty; rows before offsets[0] and from offsets[E] on belong to none and
+ * their results are left as they are.  Offsets are clamped to [0, rows], and
+ * where they decrease the rows concerned are assigned in an unspecified way
+ * (nothing outside the arrays is touched).
+ *
+ * Row strides are in elements.  ldx: X and dX; ldw: W and dW; ldy: Y, dY and
+ * dZ; ldz: Z (0: the stride of the call's result, ldy or ldx); ldr: R (0: the
+ * same).  X, W and dY start on 16-byte boundaries and their strides are
+ * multiples of 8 where a product reads them; results, R, Z and biases need
+ * only their element's alignment, with faster accesses where base and row
+ * stride are multiples of 16 bytes.  in, out and rows are arbitrary, 0
+ * included (an empty sum is 0).
+ *
+ * Results must not overlap inputs, except that R may be the result itself
+ * (Y += ..., same stride). */
+typedef enum goldy_act {
+  GOLDY_ACT_NONE = 0,
+  GOLDY_ACT_RELU = 1,       /* max(z, 0); slope 0 at 0 */
+  GOLDY_ACT_GELU = 2,       /* z (1 + erf(z / sqrt 2)) / 2 */
+  GOLDY_ACT_GELU_TANH = 3,  /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2 */
+  GOLDY_ACT_SILU = 4        /* z / (1 + exp(-z)) */
+} goldy_act;
+
+#define GOLDY_MAX_GROUPS 4096
+
+typedef struct goldy_linear_desc {
+  int64_t rows, in, out;
+  int64_t ldx, ldw, ldy;
+  int64_t ldz, ldr;
+  int64_t stride_w;         /* elements between two experts' W (and dW): >= in * ldw, a multiple of 8 */
+  int32_t groups;           /* 0, or experts 1 .. GOLDY_MAX_GROUPS */
+  int32_t act;              /* goldy_act of this layer (forward, bias gradient) */
+  int32_t act_x;            /* goldy_act that made X (input gradient) */
+  int32_t y_dtype, dx_dtype, dw_dtype;   /* of Y, dX, dW (and of the R added to them) */
+  int32_t bias_dtype;
+  int32_t reserved;         /* must be 0 */
+} goldy_linear_desc;
+
+/* Device workspace that covers every call with this descriptor (host only; 0
+ * if none is needed).  A workspace is 256-byte aligned and zero-filled by the
+ * caller before its first use; its first 64 KiB are zero again after every
+ * complete call.  One workspace of the largest size serves all layer
+ * operators (these, goldy_layernorm_backward) of one stream; calls that may
+ * overlap on the GPU need one each. */
+goldy_status goldy_linear_query(const goldy_linear_desc* desc, size_t* workspace_bytes);
+
+/* Y = act(X W + bias) + R.  bias and R may be null; Z (bf16, rows x out), if
+ * not null, receives X W + bias for the backward pass (act uses the unrounded
+ * value).  Asynchronous on `stream`, like all calls below: no allocation, no
+ * synchronisation.  A stream of an SM partition runs the call inside the
+ * partition.  Errors: GOLDY_ERR_INVALID_ARG, GOLDY_ERR_UNSUPPORTED (types),
+ * GOLDY_ERR_NOMEM (workspace smaller than this call needs), GOLDY_ERR_CUDA; a
+ * kernel that gave up a bounded wait shows up in goldy_device_error(), and
+ * the workspace is then to be zero-filled again. */
+goldy_status goldy_linear_forward(const goldy_linear_desc* desc, const int32_t* offsets, const void* X, const void* W,
+                                  const void* bias, const void* R, void* Z, void* Y, void* workspace,
+                                  size_t workspace_bytes, void* stream);
+
+/* dX = (dY W^T) * act_x'(Z) + R: the gradient of this layer's input, carried
+ * through the activation that made X (X = act_x(Z); Z is bf16, rows x in, and
+ * null exactly when act_x is GOLDY_ACT_NONE).  R (may be null) is a gradient
+ * that reaches X another way. */
+goldy_status goldy_linear_input_grad(const goldy_linear_desc* desc, const int32_t* offsets, const void* dY,
+                                     const void* W, const void* Z, const void* R, void* dX, void* workspace,
+                                     size_t workspace_bytes, void* stream);
+
+/* dW = X^T dY (per expert over its rows; 0 for an empty expert), added to
+ * what dW holds when accumulate is 1. */
+goldy_status goldy_linear_weight_grad(const goldy_linear_desc* desc, const int32_t* offsets, const void* X,
+                                      const void* dY, void* dW, int accumulate, void* workspace,
+                                      size_t workspace_bytes, void* stream);
+
+/* db = sum of dZ over the rows (per expert; fp32, packed), dZ = dY * act'(Z).
+ * Z null: dZ = dY and dZ is null too; otherwise dZ (bf16, stride ldy; may be
+ * dY itself) is written: the gradient the other two calls take as their dY
+ * when the layer has an activation that no later layer's input gradient has
+ * gone through.  The sum takes dZ before it is rounded. */
+goldy_status goldy_linear_bias_grad(const goldy_linear_desc* desc, const int32_t* offsets, const void* dY,
+                                    const void* Z, void* dZ, float* db, int accumulate, void* workspace,
+                                    size_t workspace_bytes, void* stream);
+
+/* ---- layer norm -------------------------------------------------------------
+ * y = (x - mean) * rstd * gamma + beta per row of n elements, mean = sum(x) /
+ * n, rstd = 1 / sqrt(sum((x - mean)^2) / n + eps), in fp32.  X, Y, dX and dY
+ * share `dtype` (any row strides >= n, element alignment; ldx: X and dX, ldy:
+ * Y and dY); gamma and beta have param_dtype and may be null (1 and 0). */
+typedef struct goldy_layernorm_desc {
+  int64_t rows, n;
+  int64_t ldx, ldy;
+  int32_t dtype;            /* GOLDY_BF16 or GOLDY_F32 */
+  int32_t param_dtype;
+  float eps;                /* >= 0 */
+  int32_t reserved;         /* must be 0 */
+} goldy_layernorm_desc;
+
+/* Device workspace of the backward call (see goldy_linear_query; the forward
+ * call needs none). */
+goldy_status goldy_layernorm_query(const goldy_layernorm_desc* desc, size_t* workspace_bytes);
+
+/* mean and rstd (fp32, one per row) may be null when no backward pass needs
+ * them.  Y may be X itself. */
+goldy_status goldy_layernorm_forward(const goldy_layernorm_desc* desc, const void* X, const void* gamma,
+                                     const void* beta, void* Y, float* mean, float* rstd, void* stream);
+
+/* dX; and dgamma, dbeta (fp32, n each, either may be null), added to what
+ * they hold when accumulate is 1.  dX may be dY or X itself (same stride). */
+goldy_status goldy_layernorm_backward(const goldy_layernorm_desc* desc, const void* dY, const void* X,
+                                      const void* gamma, const float* mean, const float* rstd, void* dX,
+                                      float* dgamma, float* dbeta, int accumulate, void* workspace,
+                                      size_t workspace_bytes, void* stream);
+
 /* Error word the kernels set when a bounded wait gives up (0 = none; the
  * first failure wins): 1 a load-role wait, 2 an MMA-thread wait, 3 an
  * epilogue wait, 4 a split-K cluster-exchange wait.  Reads it synchronously

@@ -1,0 +1,228 @@
+// Bias gradient of a linear layer, with the activation's gradient fused in:
+//   dZ = dY * act'(Z)  (bf16, when Z is given),  db[e] = sum of dZ (or dY) over the rows of group e.
+//
+// HBM-bound: dY (and Z) are read once, dZ is written once.  A CTA sums a slice
+// of the rows for 256 columns (8 warps, 8 columns per lane: 512-byte rows per
+// warp access, several rows in flight), warps taking every eighth row, and
+// writes one fp32 partial row per group its slice meets.  Slice s and group e
+// use partial row s + e: along increasing rows slice and group numbers only
+// grow, so the sums are distinct.  The last slice to arrive at a column block
+// adds the partials in slice order.  Sums are fp32 in a fixed order (rows of a
+// warp, warps, slices), taken before dZ is rounded.
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <string>
+
+#include "goldy_internal.h"
+#include "layer_internal.h"
+#include "layer_math.cuh"
+#include "sm103_ptx.cuh"
+
+namespace goldy {
+namespace {
+
+constexpr int kCols = 256;         // columns per CTA
+constexpr int kWarps = 8;
+constexpr int kUnroll = 4;         // rows in flight per warp
+constexpr int kMinRows = 64;       // rows per slice, at least
+constexpr int kTargetCtas = 608;   // 4 per SM
+
+int slices_for(int64_t rows, int64_t cols) {
+  const int64_t blocks = std::max<int64_t>(1, ceil_div(cols, kCols));
+  const int64_t want = std::max<int64_t>(1, kTargetCtas / blocks);
+  return int(std::max<int64_t>(1, std::min<int64_t>(want, ceil_div(rows, kMinRows))));
+}
+
+template <bool ACT>
+__global__ void __launch_bounds__(kWarps * 32) bias_grad_kernel(const BiasGradParams p) {
+  __shared__ float part[kWarps][kCols];
+  __shared__ unsigned arrived;
+  ptx::griddep_launch_dependents();
+  ptx::griddep_wait();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int c0 = blockIdx.x * kCols;
+  const int col = c0 + lane * 8;
+  const int n = max(0, min(8, p.cols - col));
+  const bool vec = p.vec && n == 8;
+  const int height = (p.rows + p.slices - 1) / p.slices;
+  const int row_lo = min(p.rows, int(blockIdx.y) * height), row_hi = min(p.rows, row_lo + height);
+
+  auto first_row = [&](int e) { return p.offsets ? min(max(__ldg(p.offsets + e), 0), p.rows) : (e == 0 ? 0 : p.rows); };
+  // the first group that ends behind row_lo
+  int e = 0;
+  if (p.offsets) {
+    int hi = p.groups;
+    while (e < hi) {
+      const int mid = (e + hi) >> 1;
+      if (first_row(mid + 1) > row_lo) hi = mid;
+      else e = mid + 1;
+    }
+  }
+  for (; e < p.groups; ++e) {
+    const int a = max(first_row(e), row_lo), b = min(first_row(e + 1), row_hi);
+    if (first_row(e) >= row_hi) break;
+    if (a >= b) continue;
+    float sum[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum[k] = 0.0f;
+    auto load = [&](const void* base, int64_t ld, int r, float (&f)[8]) {
+      const uint16_t* at = static_cast<const uint16_t*>(base) + int64_t(r) * ld + col;
+      if (vec) {
+        unpack8(*reinterpret_cast<const uint4*>(at), f);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) f[k] = k < n ? load_bf16(at, k) : 0.0f;
+      }
+    };
+    auto take = [&](int r, float (&f)[8], const float (&z)[8]) {
+      if (ACT) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) f[k] *= act_slope(z[k], p.act);
+        uint16_t* to = static_cast<uint16_t*>(p.dz) + int64_t(r) * p.lddz + col;
+        if (vec) {
+          *reinterpret_cast<uint4*>(to) = pack8(f);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            if (k < n) store_bf16(to, k, f[k]);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (k < n) sum[k] += f[k];
+    };
+    int r = a + warp;
+    for (; r + (kUnroll - 1) * kWarps < b; r += kUnroll * kWarps) {
+      float f[kUnroll][8], z[kUnroll][8];
+#pragma unroll
+      for (int i = 0; i < kUnroll; ++i) {
+        load(p.dy, p.lddy, r + i * kWarps, f[i]);
+        if (ACT) load(p.z, p.ldz, r + i * kWarps, z[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < kUnroll; ++i) take(r + i * kWarps, f[i], z[i]);
+    }
+    for (; r < b; r += kWarps) {
+      float f[8], z[8];
+      load(p.dy, p.lddy, r, f);
+      if (ACT) load(p.z, p.ldz, r, z);
+      take(r, f, z);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) part[warp][lane * 8 + k] = sum[k];
+    __syncthreads();
+    if (c0 + int(threadIdx.x) < p.cols) {
+      float s = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) s += part[w][threadIdx.x];
+      __stcg(p.part + int64_t(blockIdx.y + e) * p.cols + c0 + threadIdx.x, s);
+    }
+    __syncthreads();
+  }
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) arrived = atomicAdd(p.cnt + blockIdx.x, 1u);
+  __syncthreads();
+  if (arrived != unsigned(p.slices - 1)) return;
+  __threadfence();
+  if (threadIdx.x == 0) p.cnt[blockIdx.x] = 0u;
+  // one thread per column; groups in turn, slices of a group in order
+  const int c = c0 + threadIdx.x;
+  if (c >= p.cols) return;
+  for (int g = 0; g < p.groups; ++g) {
+    const int a = first_row(g), b = first_row(g + 1);
+    float s = 0.0f;
+    if (a < b) {
+      const int last = (b - 1) / height;
+#pragma unroll 8
+      for (int i = a / height; i <= last; ++i) s += __ldcg(p.part + int64_t(i + g) * p.cols + c);
+    }
+    float* to = p.db + int64_t(g) * p.cols + c;
+    *to = p.accumulate ? *to + s : s;
+  }
+}
+
+goldy_status bad(const std::string& why) { return fail(GOLDY_ERR_INVALID_ARG, why); }
+bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+
+struct BiasCall {
+  BiasGradParams p;
+  void* stream;
+};
+
+goldy_status launch_bias_grad(const LayerContext&, void* arg) {
+  BiasCall& call = *static_cast<BiasCall*>(arg);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(unsigned(ceil_div(call.p.cols, kCols)), unsigned(call.p.slices));
+  cfg.blockDim = dim3(kWarps * 32);
+  cfg.stream = static_cast<cudaStream_t>(call.stream);
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  void* args[] = {&call.p};
+  const void* fn = call.p.z ? reinterpret_cast<const void*>(&bias_grad_kernel<true>)
+                            : reinterpret_cast<const void*>(&bias_grad_kernel<false>);
+  const cudaError_t e = cudaLaunchKernelExC(&cfg, fn, args);
+  if (e != cudaSuccess) return fail(GOLDY_ERR_CUDA, std::string("bias gradient launch: ") + cudaGetErrorString(e));
+  return GOLDY_OK;
+}
+
+}  // namespace
+
+size_t bias_grad_part_bytes(const goldy_linear_desc& d) {
+  if (d.out == 0) return 0;
+  return size_t(slices_for(d.rows, d.out) + std::max(1, d.groups)) * size_t(d.out) * sizeof(float);
+}
+
+}  // namespace goldy
+
+using namespace goldy;
+
+extern "C" goldy_status goldy_linear_bias_grad(const goldy_linear_desc* desc, const int32_t* offsets, const void* dY,
+                                               const void* Z, void* dZ, float* db, int accumulate, void* workspace,
+                                               size_t workspace_bytes, void* stream) {
+  goldy_status st = check_linear(desc);
+  if (st == GOLDY_OK) st = check_offsets(*desc, offsets);
+  if (st != GOLDY_OK) return st;
+  if (accumulate != 0 && accumulate != 1) return bad("linear layer: accumulate must be 0 or 1");
+  if ((Z != nullptr) != (dZ != nullptr)) return bad("linear layer: Z and dZ come together");
+  if (Z && desc->act == GOLDY_ACT_NONE) return bad("linear layer: Z given, but act is GOLDY_ACT_NONE");
+  if (desc->out == 0) return ok();
+  if (ceil_div(desc->out, kCols) > int64_t(kLayerCounterBytes / sizeof(unsigned)))
+    return fail(GOLDY_ERR_UNSUPPORTED, "bias gradient: too many columns");
+  if (!db || !aligned(db, 4)) return bad("linear layer: db null or misaligned");
+  const int64_t ldz = desc->ldz ? desc->ldz : desc->ldy;
+  if (desc->rows > 0 && (!dY || !aligned(dY, 2) || !aligned(Z, 2) || !aligned(dZ, 2)))
+    return bad("linear layer: dY null, or dY, Z or dZ misaligned");
+  if (Z && ldz < desc->out) return bad("linear layer: the row stride of Z is smaller than its row");
+  const size_t need = kLayerCounterBytes + bias_grad_part_bytes(*desc);
+  if (!workspace || !aligned(workspace, 256)) return bad("linear layer: the workspace must be a 256-byte aligned device pointer");
+  if (workspace_bytes < need)
+    return fail(GOLDY_ERR_NOMEM, "linear layer: workspace of " + std::to_string(workspace_bytes) + " bytes, " +
+                                     std::to_string(need) + " needed");
+  BiasCall call{};
+  BiasGradParams& p = call.p;
+  p.dy = dY;
+  p.z = Z;
+  p.dz = dZ;
+  p.db = db;
+  p.offsets = offsets;
+  p.cnt = static_cast<unsigned*>(workspace);
+  p.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + kLayerCounterBytes);
+  p.lddy = desc->ldy;
+  p.ldz = ldz;
+  p.lddz = desc->ldy;
+  p.rows = int32_t(desc->rows);
+  p.cols = int32_t(desc->out);
+  p.groups = std::max(1, desc->groups);
+  p.act = desc->act;
+  p.slices = slices_for(desc->rows, desc->out);
+  p.vec = aligned(dY, 16) && desc->ldy % 8 == 0 && (!Z || (aligned(Z, 16) && ldz % 8 == 0 && aligned(dZ, 16)));
+  p.accumulate = accumulate;
+  call.stream = stream;
+  st = with_layer_context(stream, launch_bias_grad, &call);
+  return st == GOLDY_OK ? ok() : st;
+}

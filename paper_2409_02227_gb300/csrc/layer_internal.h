@@ -1,0 +1,127 @@
+// Internal types of the layer operators (linear-layer products, bias
+// gradient, layer norm): kernel parameter blocks shared by the host code and
+// the kernels, and the launch context the launch manager provides.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <cstddef>
+#include <cstdint>
+
+#include "../../include/goldy.h"
+
+namespace goldy {
+
+// ---- launch context (runtime.cu) --------------------------------------------
+typedef CUresult (*TensorMapEncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                      const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                                      CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                                      CUtensorMapFloatOOBfill);
+struct LayerContext {
+  int device;             // current device
+  int sm_count;           // SMs the stream may use (its partition's, or the device's)
+  int* err_word;          // the kernels' error word (goldy_device_error)
+  TensorMapEncodeFn encode;
+};
+// Run `body(ctx, arg)` with the SM partition of `stream` (if it has one)
+// current on this thread.
+goldy_status with_layer_context(void* stream, goldy_status (*body)(const LayerContext&, void*), void* arg);
+
+// One workspace serves every layer operator: a fixed counter area in front
+// (zero between calls), fp32 partial results behind it.
+constexpr size_t kLayerCounterBytes = 64 * 1024;
+
+// ---- linear-layer products (linear_kernel.cuh, linear.cu) -------------------
+// All three passes compute C[r][c] with c, the contiguous index of C, along
+// the tensor cores' M dimension and r along their N dimension:
+//   forward      C = Y  (rows x out): c an output feature, r a row, reduction over input features
+//   input grad   C = dX (rows x in):  c an input feature,  r a row, reduction over output features
+//   weight grad  C = dW (in x out):   c an output feature, r an input feature, reduction over rows
+constexpr int kLinForward = 0;
+constexpr int kLinInputGrad = 1;
+constexpr int kLinWeightGrad = 2;
+constexpr int kLinThreads = 320;          // load warp, MMA warp, 8 epilogue warps
+constexpr int kLinEpiWarps = 8;
+constexpr int kLinStageK = 64;            // reduction elements per pipeline stage
+constexpr int kLinMaxStages = 12;
+constexpr int kLinRowBand = 8;            // row tiles walked before the next column tile
+constexpr int kLinPromote = 8;            // stages accumulated in tensor memory for fp32 results
+constexpr int kLinStagingBytes = kLinEpiWarps * 4096;
+constexpr int kLinSmemBudget = 232448;    // 227 KB
+
+struct LinearParams {
+  CUtensorMap ta;          // operand along c (weights, or dY of the weight gradient)
+  CUtensorMap tb;          // operand along r, one box per full tile
+  CUtensorMap tb_part;     // the same in boxes of part_box rows, for narrower tiles
+  const int* offsets;      // groups + 1 row offsets, or null
+  int32_t groups;          // >= 1
+  int32_t rows;            // rows of X and Y
+  int32_t size_c;          // columns of C
+  int32_t size_r;          // rows of C (weight gradient), else = rows
+  int32_t red;             // reduction length (forward, input gradient)
+  int32_t tile_r;          // rows of C per tile, at most
+  int32_t tiles_c;         // column tiles
+  int32_t split;           // reduction split over this many units
+  int32_t stages;
+  int32_t stage_bytes;
+  int32_t part_box;        // rows per box of tb_part
+  int32_t part_chunks;     // 32-row chunks per epilogue warp in a partial
+  int32_t act;
+  int32_t bias_f32;
+  int32_t vec_c, vec_r, vec_z;   // 16-byte accesses possible
+  int32_t loads;           // 0: empty reduction, no tensor maps
+  void* c;
+  int64_t ldc, c_group;    // row stride and group stride of C (group stride: weight gradient)
+  const void* bias;        // [groups][size_c] or null
+  const void* res;         // added to the result, same type and layout rules as C, or null
+  int64_t ldr, r_group;
+  const void* z_in;        // bf16: multiply by act'(z_in) instead of applying act
+  void* z_out;             // bf16: receives the value before act
+  int64_t ldz;
+  float* part;             // split partials
+  unsigned* cnt;           // arrival counters, zero between calls
+  int* err;
+};
+static_assert(sizeof(LinearParams) <= 4096, "kernel parameter block");
+
+// Host stub of the kernel for a pass; pair: CTA-pair tiles of 256 columns, else 128.
+const void* linear_kernel_fn(int pass, int pair, int out_f32);
+
+// ---- bias gradient and layer norm -------------------------------------------
+struct BiasGradParams {
+  const void* dy;
+  const void* z;           // null: no activation gradient
+  void* dz;
+  float* db;               // [groups][cols]
+  const int* offsets;
+  float* part;
+  unsigned* cnt;
+  int64_t lddy, ldz, lddz;
+  int32_t rows, cols, groups, act, slices, vec, accumulate;
+};
+
+// Argument checks shared by the linear-layer entry points (linear.cu), and the
+// bias gradient's workspace behind the counters (bias_grad.cu).
+goldy_status check_linear(const goldy_linear_desc* d);
+goldy_status check_offsets(const goldy_linear_desc& d, const int32_t* offsets);
+size_t bias_grad_part_bytes(const goldy_linear_desc& d);
+
+struct NormParams {
+  const void* x;
+  const void* dy;
+  const void* gamma;       // null: 1
+  const void* beta;        // null: 0
+  void* out;               // Y, or dX
+  float* mean;             // forward: written, may be null
+  float* rstd;
+  float* part;             // backward: [grid][2][n] partial dgamma, dbeta (null: not wanted)
+  int64_t ldx, ldy;        // row strides: X and dX; Y and dY
+  int64_t rows;
+  int32_t n;
+  int32_t param_f32;
+  float eps;
+  float inv_n;
+};
+
+}  // namespace goldy

@@ -1,0 +1,406 @@
+// Host side of the linear-layer operators: argument checks, tensor maps, the
+// choice of tile and split, launches.  Nothing here allocates device memory
+// or synchronises; the choice is a pure function of the descriptor, so that
+// goldy_linear_query can size the workspace without a device.
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cstring>
+#include <mutex>
+#include <string>
+
+#include "goldy_internal.h"
+#include "layer_internal.h"
+
+namespace goldy {
+
+const void* linear_kernel_forward(int pair, int out_f32);
+const void* linear_kernel_input_grad(int pair, int out_f32);
+const void* linear_kernel_weight_grad(int pair, int out_f32);
+
+const void* linear_kernel_fn(int pass, int pair, int out_f32) {
+  switch (pass) {
+    case kLinForward: return linear_kernel_forward(pair, out_f32);
+    case kLinInputGrad: return linear_kernel_input_grad(pair, out_f32);
+    default: return linear_kernel_weight_grad(pair, out_f32);
+  }
+}
+
+namespace {
+
+constexpr int64_t kMaxDim = (int64_t(1) << 31) - 1024;   // TMA coordinates are 32-bit
+constexpr int kModelSms = 152;                           // SMs the choice is made for
+constexpr int kMaxDevices = 64;
+
+bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+size_t type_bytes(int dtype) { return dtype == GOLDY_F32 ? 4 : 2; }
+
+struct LinShape {
+  int pass;
+  int64_t rows, size_c, size_r, red;   // size_r: rows, or input features (weight grad); red as in LinearParams
+  int groups;
+  int out_dtype;
+};
+
+LinShape shape_of(const goldy_linear_desc& d, int pass) {
+  LinShape s;
+  s.pass = pass;
+  s.rows = d.rows;
+  s.groups = std::max(1, d.groups);
+  s.size_c = pass == kLinInputGrad ? d.in : d.out;
+  s.size_r = pass == kLinWeightGrad ? d.in : d.rows;
+  s.red = pass == kLinForward ? d.in : pass == kLinInputGrad ? d.out : d.rows;
+  s.out_dtype = pass == kLinForward ? d.y_dtype : pass == kLinInputGrad ? d.dx_dtype : d.dw_dtype;
+  return s;
+}
+
+struct LinChoice {
+  int pair, tile_r, split;
+  int64_t max_tiles;       // upper bound over all group sizes
+  size_t part_bytes;       // workspace behind the counters
+};
+
+int part_chunks(int tile_r) { return int(ceil_div(ceil_div(tile_r, 32), 2)); }
+
+// Time model in SM cycles: a 64-deep stage of an nw-row tile costs the larger
+// of its tensor time (2 nw) and of its operand bytes at kLoadRate per SM; a
+// unit adds kUnitCost for filling the pipeline and draining the accumulator,
+// a split its partials' trip through L2.  Group sizes are on the device, so
+// groups are taken as equal.
+constexpr double kLoadRate = 70.0;       // bytes per cycle and SM from L2, all SMs loading
+constexpr double kUnitCost = 1200.0;
+constexpr double kSplitCost = 2500.0;
+
+LinChoice choose(const LinShape& s) {
+  struct Candidate { int pair, tile_r; };
+  static const Candidate cand[] = {{1, 256}, {1, 192}, {1, 128}, {0, 256}, {0, 128}, {0, 64}, {0, 32}, {0, 16}};
+  const bool wgrad = s.pass == kLinWeightGrad;
+  const int64_t live = std::max<int64_t>(1, std::min<int64_t>(s.groups, wgrad ? s.groups : s.rows));
+  const int64_t r_rows = wgrad ? s.size_r : ceil_div(std::max<int64_t>(s.rows, 1), live);
+  const int64_t red = wgrad ? ceil_div(std::max<int64_t>(s.rows, 1), live) : s.red;
+  const int64_t kbs = std::max<int64_t>(1, ceil_div(red, kLinStageK));
+  LinChoice best{0, 16, 1, 0, 0};
+  double best_t = -1.0;
+  for (const Candidate& c : cand) {
+    const int gran = c.pair ? 32 : 16;
+    const int64_t n_r = ceil_div(r_rows, c.tile_r);
+    const int64_t w = ceil_div(ceil_div(r_rows, n_r), gran) * gran;
+    const int64_t tiles = live * ceil_div(r_rows, w) * ceil_div(s.size_c, c.pair ? 256 : 128);
+    const int64_t workers = c.pair ? kModelSms / 2 : kModelSms;
+    const double stage = std::max(2.0 * double(w), (16384.0 + double(w) * (c.pair ? 64 : 128)) / kLoadRate);
+    // tiles over all groups, at most: each group may end in a partial tile
+    const int64_t most = (wgrad || s.groups == 1 ? s.groups * ceil_div(s.size_r, c.tile_r)
+                                                 : s.rows / c.tile_r + std::min<int64_t>(s.groups, s.rows)) *
+                         ceil_div(s.size_c, c.pair ? 256 : 128);
+    for (int split = 1; split <= 16; split *= 2) {
+      if (split > 1 && (split > kbs || size_t(most) * (c.pair ? 2 : 1) * kLinEpiWarps * 4 > kLayerCounterBytes)) break;
+      const double waves = double(ceil_div(tiles * split, workers));
+      double t = waves * (double(ceil_div(kbs, split)) * stage) + kUnitCost;
+      if (split > 1) t += kSplitCost + double(w) * 128 * 4 * split / kLoadRate;
+      if (best_t < 0 || t < best_t) {
+        best_t = t;
+        best.pair = c.pair;
+        best.tile_r = c.tile_r;
+        best.split = split;
+        best.max_tiles = most;
+      }
+    }
+  }
+  best.part_bytes = best.split > 1 ? size_t(best.max_tiles) * best.split * (best.pair ? 2 : 1) * kLinEpiWarps *
+                                         part_chunks(best.tile_r) * 4096
+                                   : 0;
+  return best;
+}
+
+goldy_status bad(const std::string& why) { return fail(GOLDY_ERR_INVALID_ARG, why); }
+
+bool is_dtype(int t) { return t == GOLDY_BF16 || t == GOLDY_F32; }
+
+goldy_status check_operand(const void* ptr, int64_t ld, const char* name) {
+  if (!ptr || !aligned(ptr, 16)) return bad(std::string("linear layer: ") + name + " must be a 16-byte aligned device pointer");
+  if (ld % 8 != 0) return bad(std::string("linear layer: the row stride of ") + name + " must be a multiple of 8");
+  return GOLDY_OK;
+}
+
+// Tensor map of `batch` bf16 matrices (outer x inner), boxes of box_outer
+// rows x 64 elements, 128-byte swizzled.
+goldy_status encode(const LayerContext& ctx, CUtensorMap* m, const void* ptr, int64_t inner, int64_t outer,
+                    int64_t batch, int64_t ld, int64_t batch_stride, int box_outer) {
+  cuuint64_t dims[3] = {cuuint64_t(inner), cuuint64_t(outer), cuuint64_t(batch)};
+  cuuint64_t strides[2] = {cuuint64_t(ld) * 2, cuuint64_t(batch_stride) * 2};
+  cuuint32_t box[3] = {64, cuuint32_t(box_outer), 1};
+  cuuint32_t one[3] = {1, 1, 1};
+  const CUresult r = ctx.encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), dims, strides, box,
+                                one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(GOLDY_ERR_CUDA, "cuTensorMapEncodeTiled failed with code " + std::to_string(int(r)));
+  return GOLDY_OK;
+}
+
+goldy_status set_smem(const LayerContext& ctx, const void* fn, int pass, int pair, int f32) {
+  static std::mutex mu;
+  static bool done[kMaxDevices][3][2][2] = {};
+  std::lock_guard<std::mutex> lock(mu);
+  bool& d = done[ctx.device][pass][pair][f32];
+  if (!d) {
+    const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kLinSmemBudget);
+    if (e != cudaSuccess) return fail(GOLDY_ERR_CUDA, std::string("cudaFuncSetAttribute: ") + cudaGetErrorString(e));
+    d = true;
+  }
+  return GOLDY_OK;
+}
+
+struct LinCall {
+  LinShape s;
+  const goldy_linear_desc* d;
+  const void* p_ptr;       // operand along c: W, or dY
+  const void* q_ptr;       // operand along r: X, dY, or X
+  LinearParams prm;        // epilogue fields filled in by the entry point
+  void* workspace;
+  size_t workspace_bytes;
+  void* stream;
+};
+
+goldy_status launch_linear(const LayerContext& ctx, void* arg) {
+  LinCall& call = *static_cast<LinCall*>(arg);
+  const LinShape& s = call.s;
+  const goldy_linear_desc& d = *call.d;
+  LinearParams& p = call.prm;
+  const LinChoice c = choose(s);
+  if (c.split > 1) {
+    if (!call.workspace || !aligned(call.workspace, 256))
+      return bad("linear layer: the workspace must be a 256-byte aligned device pointer");
+    if (call.workspace_bytes < kLayerCounterBytes + c.part_bytes)
+      return fail(GOLDY_ERR_NOMEM, "linear layer: workspace of " + std::to_string(call.workspace_bytes) + " bytes, " +
+                                       std::to_string(kLayerCounterBytes + c.part_bytes) + " needed");
+    p.cnt = static_cast<unsigned*>(call.workspace);
+    p.part = reinterpret_cast<float*>(static_cast<char*>(call.workspace) + kLayerCounterBytes);
+  }
+  const bool wgrad = s.pass == kLinWeightGrad;
+  const int ctas = c.pair ? 2 : 1;
+  p.groups = s.groups;
+  p.rows = int32_t(s.rows);
+  p.size_c = int32_t(s.size_c);
+  p.size_r = int32_t(s.size_r);
+  p.red = int32_t(s.red);
+  p.tile_r = c.tile_r;
+  p.tiles_c = int32_t(ceil_div(s.size_c, 128 * ctas));
+  p.split = c.split;
+  p.part_box = std::min(32, c.tile_r / ctas);
+  p.part_chunks = part_chunks(c.tile_r);
+  p.loads = s.red > 0 ? 1 : 0;
+  const int b_rows = wgrad ? int(ceil_div(c.tile_r / ctas, 64)) * 64 : c.tile_r / ctas;
+  p.stage_bytes = 128 * kLinStageK * 2 + b_rows * kLinStageK * 2;
+  const int fixed = 1024 + kLinStagingBytes + 1024;
+  p.stages = std::min<int>(kLinMaxStages, (kLinSmemBudget - fixed) / p.stage_bytes);
+  p.err = ctx.err_word;
+  if (p.loads) {
+    goldy_status st;
+    if (wgrad) {
+      st = encode(ctx, &p.ta, call.p_ptr, d.out, d.rows, 1, d.ldy, d.rows * d.ldy, kLinStageK);
+      if (st == GOLDY_OK) st = encode(ctx, &p.tb, call.q_ptr, d.in, d.rows, 1, d.ldx, d.rows * d.ldx, kLinStageK);
+    } else {
+      const int64_t q_ld = s.pass == kLinForward ? d.ldx : d.ldy;
+      const int64_t w_stride = d.groups > 1 ? d.stride_w : d.in * d.ldw;
+      st = encode(ctx, &p.ta, call.p_ptr, d.out, d.in, s.groups, d.ldw, w_stride,
+                  s.pass == kLinForward ? kLinStageK : 128);
+      if (st == GOLDY_OK) st = encode(ctx, &p.tb, call.q_ptr, s.red, d.rows, 1, q_ld, d.rows * q_ld, c.tile_r / ctas);
+      if (st == GOLDY_OK) st = encode(ctx, &p.tb_part, call.q_ptr, s.red, d.rows, 1, q_ld, d.rows * q_ld, p.part_box);
+    }
+    if (st != GOLDY_OK) return st;
+  }
+  const int f32 = s.out_dtype == GOLDY_F32 ? 1 : 0;
+  const void* fn = linear_kernel_fn(s.pass, c.pair, f32);
+  goldy_status st = set_smem(ctx, fn, s.pass, c.pair, f32);
+  if (st != GOLDY_OK) return st;
+  const int64_t units = c.max_tiles * c.split;
+  const int64_t workers = std::max<int64_t>(1, std::min<int64_t>(units, ctx.sm_count / ctas));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(unsigned(workers * ctas));
+  cfg.blockDim = dim3(kLinThreads);
+  cfg.dynamicSmemBytes = size_t(fixed + p.stages * p.stage_bytes);
+  cfg.stream = static_cast<cudaStream_t>(call.stream);
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.numAttrs = 1;
+  if (c.pair) {
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 2;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.numAttrs = 2;
+  }
+  cfg.attrs = attr;
+  void* args[] = {&p};
+  const cudaError_t e = cudaLaunchKernelExC(&cfg, fn, args);
+  if (e != cudaSuccess) return fail(GOLDY_ERR_CUDA, std::string("linear layer launch: ") + cudaGetErrorString(e));
+  return GOLDY_OK;
+}
+
+// Fields of the result and what is added to it, common to the passes.
+goldy_status set_result(LinearParams& p, const LinShape& s, void* C, int64_t ldc, const void* R, int64_t ldr,
+                        const char* name) {
+  const size_t es = type_bytes(s.out_dtype);
+  if (!C || !aligned(C, es)) return bad(std::string("linear layer: ") + name + " null or misaligned");
+  if (ldr == 0) ldr = ldc;
+  if (R && (!aligned(R, es) || ldr < s.size_c)) return bad("linear layer: residual misaligned or its row stride too small");
+  p.c = C;
+  p.ldc = ldc;
+  p.res = R;
+  p.ldr = ldr;
+  p.vec_c = aligned(C, 16) && (size_t(ldc) * es) % 16 == 0;
+  p.vec_r = aligned(R, 16) && (size_t(ldr) * es) % 16 == 0;
+  return GOLDY_OK;
+}
+
+goldy_status set_saved(LinearParams& p, const LinShape& s, const void* Z, int64_t ldz) {
+  if (!aligned(Z, 2) || ldz < s.size_c) return bad("linear layer: Z misaligned or its row stride too small");
+  p.ldz = ldz;
+  p.vec_z = aligned(Z, 16) && ldz % 8 == 0;
+  return GOLDY_OK;
+}
+
+}  // namespace
+
+goldy_status check_linear(const goldy_linear_desc* d) {
+  if (!d) return bad("null descriptor");
+  if (d->rows < 0 || d->in < 0 || d->out < 0 || d->rows > kMaxDim || d->in > kMaxDim || d->out > kMaxDim)
+    return bad("linear layer: a size is negative or too large");
+  if (d->groups < 0 || d->groups > GOLDY_MAX_GROUPS) return bad("linear layer: groups out of range");
+  if (d->ldx < d->in || d->ldw < d->out || d->ldy < d->out || d->ldz < 0 || d->ldr < 0)
+    return bad("linear layer: a row stride is smaller than its row");
+  if (d->ldx > kMaxDim || d->ldw > kMaxDim || d->ldy > kMaxDim || d->ldz > kMaxDim || d->ldr > kMaxDim)
+    return bad("linear layer: a row stride is too large");
+  if (d->groups > 1 && (d->stride_w < d->in * d->ldw || d->stride_w % 8 != 0))
+    return bad("linear layer: stride_w must be a multiple of 8 and at least in * ldw");
+  if (d->act < GOLDY_ACT_NONE || d->act > GOLDY_ACT_SILU || d->act_x < GOLDY_ACT_NONE || d->act_x > GOLDY_ACT_SILU)
+    return bad("linear layer: unknown activation");
+  if (!is_dtype(d->y_dtype) || !is_dtype(d->dx_dtype) || !is_dtype(d->dw_dtype) || !is_dtype(d->bias_dtype))
+    return fail(GOLDY_ERR_UNSUPPORTED, "linear layer: types are GOLDY_BF16 or GOLDY_F32");
+  if (d->reserved != 0) return bad("linear layer: reserved must be 0");
+  return GOLDY_OK;
+}
+
+goldy_status check_offsets(const goldy_linear_desc& d, const int32_t* offsets) {
+  if (d.groups > 0 && (!offsets || !aligned(offsets, 4)))
+    return bad("linear layer: grouped rows need offsets (groups + 1 device integers)");
+  if (d.groups == 0 && offsets) return bad("linear layer: offsets given, but the descriptor has no groups");
+  return GOLDY_OK;
+}
+
+}  // namespace goldy
+
+using namespace goldy;
+
+extern "C" goldy_status goldy_linear_query(const goldy_linear_desc* desc, size_t* workspace_bytes) {
+  goldy_status st = check_linear(desc);
+  if (st != GOLDY_OK) return st;
+  if (!workspace_bytes) return bad("null argument");
+  size_t part = 0;
+  for (int pass = 0; pass < 3; ++pass) {
+    const LinShape s = shape_of(*desc, pass);
+    if (s.size_c > 0 && s.size_r > 0) part = std::max(part, choose(s).part_bytes);
+  }
+  part = std::max(part, bias_grad_part_bytes(*desc));
+  *workspace_bytes = part > 0 ? kLayerCounterBytes + part : 0;
+  return ok();
+}
+
+extern "C" goldy_status goldy_linear_forward(const goldy_linear_desc* desc, const int32_t* offsets, const void* X,
+                                             const void* W, const void* bias, const void* R, void* Z, void* Y,
+                                             void* workspace, size_t workspace_bytes, void* stream) {
+  goldy_status st = check_linear(desc);
+  if (st == GOLDY_OK) st = check_offsets(*desc, offsets);
+  if (st != GOLDY_OK) return st;
+  LinCall call{};
+  call.d = desc;
+  call.s = shape_of(*desc, kLinForward);
+  if (call.s.size_c == 0 || call.s.size_r == 0) return ok();
+  if (call.s.red > 0) {
+    st = check_operand(X, desc->ldx, "X");
+    if (st == GOLDY_OK) st = check_operand(W, desc->ldw, "W");
+    if (st != GOLDY_OK) return st;
+  }
+  LinearParams& p = call.prm;
+  st = set_result(p, call.s, Y, desc->ldy, R, desc->ldr, "Y");
+  if (st == GOLDY_OK && Z) st = set_saved(p, call.s, Z, desc->ldz ? desc->ldz : desc->ldy);
+  if (st != GOLDY_OK) return st;
+  if (bias && !aligned(bias, type_bytes(desc->bias_dtype))) return bad("linear layer: bias misaligned");
+  p.z_out = Z;
+  p.bias = bias;
+  p.bias_f32 = desc->bias_dtype == GOLDY_F32;
+  p.act = desc->act;
+  p.offsets = offsets;
+  call.p_ptr = W;
+  call.q_ptr = X;
+  call.workspace = workspace;
+  call.workspace_bytes = workspace_bytes;
+  call.stream = stream;
+  st = with_layer_context(stream, launch_linear, &call);
+  return st == GOLDY_OK ? ok() : st;
+}
+
+extern "C" goldy_status goldy_linear_input_grad(const goldy_linear_desc* desc, const int32_t* offsets, const void* dY,
+                                                const void* W, const void* Z, const void* R, void* dX, void* workspace,
+                                                size_t workspace_bytes, void* stream) {
+  goldy_status st = check_linear(desc);
+  if (st == GOLDY_OK) st = check_offsets(*desc, offsets);
+  if (st != GOLDY_OK) return st;
+  if (desc->act_x != GOLDY_ACT_NONE && !Z) return bad("linear layer: the activation's gradient needs Z");
+  if (desc->act_x == GOLDY_ACT_NONE && Z) return bad("linear layer: Z given, but act_x is GOLDY_ACT_NONE");
+  LinCall call{};
+  call.d = desc;
+  call.s = shape_of(*desc, kLinInputGrad);
+  if (call.s.size_c == 0 || call.s.size_r == 0) return ok();
+  if (call.s.red > 0) {
+    st = check_operand(dY, desc->ldy, "dY");
+    if (st == GOLDY_OK) st = check_operand(W, desc->ldw, "W");
+    if (st != GOLDY_OK) return st;
+  }
+  LinearParams& p = call.prm;
+  st = set_result(p, call.s, dX, desc->ldx, R, desc->ldr, "dX");
+  if (st == GOLDY_OK && Z) st = set_saved(p, call.s, Z, desc->ldz ? desc->ldz : desc->ldx);
+  if (st != GOLDY_OK) return st;
+  p.z_in = Z;
+  p.act = desc->act_x;
+  p.offsets = offsets;
+  call.p_ptr = W;
+  call.q_ptr = dY;
+  call.workspace = workspace;
+  call.workspace_bytes = workspace_bytes;
+  call.stream = stream;
+  st = with_layer_context(stream, launch_linear, &call);
+  return st == GOLDY_OK ? ok() : st;
+}
+
+extern "C" goldy_status goldy_linear_weight_grad(const goldy_linear_desc* desc, const int32_t* offsets, const void* X,
+                                                 const void* dY, void* dW, int accumulate, void* workspace,
+                                                 size_t workspace_bytes, void* stream) {
+  goldy_status st = check_linear(desc);
+  if (st == GOLDY_OK) st = check_offsets(*desc, offsets);
+  if (st != GOLDY_OK) return st;
+  if (accumulate != 0 && accumulate != 1) return bad("linear layer: accumulate must be 0 or 1");
+  LinCall call{};
+  call.d = desc;
+  call.s = shape_of(*desc, kLinWeightGrad);
+  if (call.s.size_c == 0 || call.s.size_r == 0) return ok();
+  if (call.s.red > 0) {
+    st = check_operand(X, desc->ldx, "X");
+    if (st == GOLDY_OK) st = check_operand(dY, desc->ldy, "dY");
+    if (st != GOLDY_OK) return st;
+  }
+  LinearParams& p = call.prm;
+  st = set_result(p, call.s, dW, desc->ldw, accumulate ? dW : nullptr, desc->ldw, "dW");
+  if (st != GOLDY_OK) return st;
+  p.c_group = p.r_group = desc->groups > 1 ? desc->stride_w : 0;
+  p.offsets = offsets;
+  call.p_ptr = dY;
+  call.q_ptr = X;
+  call.workspace = workspace;
+  call.workspace_bytes = workspace_bytes;
+  call.stream = stream;
+  st = with_layer_context(stream, launch_linear, &call);
+  return st == GOLDY_OK ? ok() : st;
+}

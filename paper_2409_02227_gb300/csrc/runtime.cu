@@ -28,6 +28,7 @@
 
 #include "go_kernel.cuh"
 #include "goldy_internal.h"
+#include "layer_internal.h"
 
 namespace goldy {
 
@@ -1424,6 +1425,26 @@ goldy_status launch_planned_gemm(const GemmPlan& gp, const void* A, const void* 
     if (e != cudaSuccess) return cuda_fail(e, "cudaMemsetAsync (split-K counters)");
   }
   return launch_gemm(*d, gp, A, B, C, ws, static_cast<cudaStream_t>(stream));
+}
+}  // namespace goldy
+
+namespace goldy {
+// What the layer operators (linear.cu, layernorm.cu) need to launch: per-device
+// set-up as above, inside the SM partition `stream` belongs to.
+goldy_status with_layer_context(void* stream, goldy_status (*body)(const LayerContext&, void*), void* arg) {
+  DeviceState* d = nullptr;
+  goldy_status st = device_state(&d);
+  if (st != GOLDY_OK) return st;
+  LayerContext ctx;
+  cudaError_t e = cudaGetDevice(&ctx.device);
+  if (e != cudaSuccess) return cuda_fail(e, "cudaGetDevice");
+  PartitionScope part;
+  st = part.enter(stream);
+  if (st != GOLDY_OK) return st;
+  ctx.sm_count = sms(*d);
+  ctx.err_word = d->err_word;
+  ctx.encode = g_encode;
+  return body(ctx, arg);
 }
 }  // namespace goldy
 

@@ -39,6 +39,13 @@ GOLDY_PLAN_FUSED = 0x10
 GOLDY_MAX_GEMMS = 64
 GOLDY_MAX_STREAMS = 16
 
+GOLDY_ACT_NONE = 0
+GOLDY_ACT_RELU = 1
+GOLDY_ACT_GELU = 2
+GOLDY_ACT_GELU_TANH = 3
+GOLDY_ACT_SILU = 4
+GOLDY_MAX_GROUPS = 4096
+
 
 def force_cd(cd: int) -> int:
     """Flags for GOLDY_PLAN_FORCE_CD with concurrency degree ``cd``."""
@@ -63,6 +70,18 @@ class goldy_gemm_desc(ctypes.Structure):
                 ("c_dtype", ctypes.c_int32), ("reserved", ctypes.c_int32),
                 ("batch", ctypes.c_int64), ("stride_a", ctypes.c_int64), ("stride_b", ctypes.c_int64),
                 ("stride_c", ctypes.c_int64)]
+
+
+class goldy_linear_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("rows", "in", "out", "ldx", "ldw", "ldy", "ldz", "ldr", "stride_w")] + \
+               [(n, ctypes.c_int32) for n in ("groups", "act", "act_x", "y_dtype", "dx_dtype", "dw_dtype", "bias_dtype",
+                                              "reserved")]
+
+
+class goldy_layernorm_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("rows", "n", "ldx", "ldy")] + \
+               [("dtype", ctypes.c_int32), ("param_dtype", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("reserved", ctypes.c_int32)]
 
 
 class goldy_run_opts(ctypes.Structure):
@@ -92,6 +111,8 @@ def _load():
     PP = ctypes.POINTER(ctypes.c_void_p)
     IP = ctypes.POINTER(ctypes.c_int)
     DP = ctypes.POINTER(goldy_gemm_desc)
+    LP = ctypes.POINTER(goldy_linear_desc)
+    NP = ctypes.POINTER(goldy_layernorm_desc)
     sig = {
         "goldy_abi_version": ([], I),
         "goldy_last_error": ([], ctypes.c_char_p),
@@ -134,6 +155,14 @@ def _load():
         "goldy_exec_free": ([P], None),
         "goldy_graph_free": ([P], None),
         "goldy_gemm_noalloc": ([DP, I, P, P, P, P], I),
+        "goldy_linear_query": ([LP, ctypes.POINTER(SZ)], I),
+        "goldy_linear_forward": ([LP, P, P, P, P, P, P, P, P, SZ, P], I),
+        "goldy_linear_input_grad": ([LP, P, P, P, P, P, P, P, SZ, P], I),
+        "goldy_linear_weight_grad": ([LP, P, P, P, P, I, P, SZ, P], I),
+        "goldy_linear_bias_grad": ([LP, P, P, P, P, P, I, P, SZ, P], I),
+        "goldy_layernorm_query": ([NP, ctypes.POINTER(SZ)], I),
+        "goldy_layernorm_forward": ([NP, P, P, P, P, P, P, P], I),
+        "goldy_layernorm_backward": ([NP, P, P, P, P, P, P, P, P, I, P, SZ, P], I),
         "goldy_device_error": ([IP, I], I),
         "goldy_device_info": ([I, IP, IP], I),
     }
@@ -496,6 +525,89 @@ def goldy_gemm_noalloc(d: goldy_gemm_desc, variant: int, A: int, B: int, C: int,
     allocation anywhere); see goldy.h for who needs it and its limits."""
     _check(_lib.goldy_gemm_noalloc(ctypes.byref(d), int(variant), int(A) or None, int(B) or None,
                                    int(C) or None, int(stream) or None), "goldy_gemm_noalloc")
+
+
+def linear_desc(rows: int, fan_in: int, fan_out: int, groups: int = 0, act: int = GOLDY_ACT_NONE,
+                act_x: int = GOLDY_ACT_NONE, y_dtype: int = GOLDY_BF16, dx_dtype: int = GOLDY_BF16,
+                dw_dtype: int = GOLDY_F32, bias_dtype: int = GOLDY_BF16, ldx: Optional[int] = None,
+                ldw: Optional[int] = None, ldy: Optional[int] = None, ldz: int = 0, ldr: int = 0,
+                stride_w: Optional[int] = None) -> goldy_linear_desc:
+    """Descriptor of a linear layer Y (rows x fan_out) = act(X (rows x fan_in)
+    W (fan_in x fan_out) + b) + R, or of `groups` experts over ragged row
+    ranges (default: packed rows, experts' weights back to back)."""
+    ldw = fan_out if ldw is None else ldw
+    return goldy_linear_desc(rows, fan_in, fan_out, fan_in if ldx is None else ldx, ldw,
+                             fan_out if ldy is None else ldy, ldz, ldr,
+                             fan_in * ldw if stride_w is None else stride_w, int(groups), int(act), int(act_x),
+                             int(y_dtype), int(dx_dtype), int(dw_dtype), int(bias_dtype), 0)
+
+
+def goldy_linear_query(d: goldy_linear_desc) -> int:
+    """Workspace bytes that cover every call with this descriptor."""
+    ws = ctypes.c_size_t()
+    _check(_lib.goldy_linear_query(d, ctypes.byref(ws)), "goldy_linear_query")
+    return int(ws.value)
+
+
+def goldy_linear_forward(d: goldy_linear_desc, X: int, W: int, Y: int, bias: int = 0, residual: int = 0, z: int = 0,
+                         offsets: int = 0, workspace: int = 0, workspace_bytes: int = 0, stream: int = 0) -> None:
+    """Y = act(X W + bias) + residual; z receives X W + bias."""
+    _check(_lib.goldy_linear_forward(d, offsets or None, X or None, W or None, bias or None, residual or None,
+                                     z or None, Y or None, workspace or None, workspace_bytes, stream or None),
+           "goldy_linear_forward")
+
+
+def goldy_linear_input_grad(d: goldy_linear_desc, dY: int, W: int, dX: int, z: int = 0, residual: int = 0,
+                            offsets: int = 0, workspace: int = 0, workspace_bytes: int = 0, stream: int = 0) -> None:
+    """dX = (dY W^T) * act_x'(z) + residual."""
+    _check(_lib.goldy_linear_input_grad(d, offsets or None, dY or None, W or None, z or None, residual or None,
+                                        dX or None, workspace or None, workspace_bytes, stream or None),
+           "goldy_linear_input_grad")
+
+
+def goldy_linear_weight_grad(d: goldy_linear_desc, X: int, dY: int, dW: int, accumulate: bool = False,
+                             offsets: int = 0, workspace: int = 0, workspace_bytes: int = 0, stream: int = 0) -> None:
+    """dW (+)= X^T dY, per expert."""
+    _check(_lib.goldy_linear_weight_grad(d, offsets or None, X or None, dY or None, dW or None, 1 if accumulate else 0,
+                                         workspace or None, workspace_bytes, stream or None),
+           "goldy_linear_weight_grad")
+
+
+def goldy_linear_bias_grad(d: goldy_linear_desc, dY: int, db: int, z: int = 0, dz: int = 0, accumulate: bool = False,
+                           offsets: int = 0, workspace: int = 0, workspace_bytes: int = 0, stream: int = 0) -> None:
+    """db (+)= sum over rows of dz, dz = dY * act'(z) (z = dz = 0: of dY)."""
+    _check(_lib.goldy_linear_bias_grad(d, offsets or None, dY or None, z or None, dz or None, db or None,
+                                       1 if accumulate else 0, workspace or None, workspace_bytes, stream or None),
+           "goldy_linear_bias_grad")
+
+
+def layernorm_desc(rows: int, n: int, dtype: int = GOLDY_BF16, param_dtype: int = GOLDY_BF16, eps: float = 1e-5,
+                   ldx: Optional[int] = None, ldy: Optional[int] = None) -> goldy_layernorm_desc:
+    """Descriptor of a layer norm over rows of n elements (default: packed)."""
+    return goldy_layernorm_desc(rows, n, n if ldx is None else ldx, n if ldy is None else ldy, int(dtype),
+                                int(param_dtype), float(eps), 0)
+
+
+def goldy_layernorm_query(d: goldy_layernorm_desc) -> int:
+    """Workspace bytes of the backward call."""
+    ws = ctypes.c_size_t()
+    _check(_lib.goldy_layernorm_query(d, ctypes.byref(ws)), "goldy_layernorm_query")
+    return int(ws.value)
+
+
+def goldy_layernorm_forward(d: goldy_layernorm_desc, X: int, gamma: int, beta: int, Y: int, mean: int = 0,
+                            rstd: int = 0, stream: int = 0) -> None:
+    _check(_lib.goldy_layernorm_forward(d, X or None, gamma or None, beta or None, Y or None, mean or None,
+                                        rstd or None, stream or None), "goldy_layernorm_forward")
+
+
+def goldy_layernorm_backward(d: goldy_layernorm_desc, dY: int, X: int, gamma: int, mean: int, rstd: int, dX: int,
+                             dgamma: int = 0, dbeta: int = 0, workspace: int = 0, workspace_bytes: int = 0,
+                             stream: int = 0, accumulate: bool = False) -> None:
+    _check(_lib.goldy_layernorm_backward(d, dY or None, X or None, gamma or None, mean or None, rstd or None,
+                                         dX or None, dgamma or None, dbeta or None, 1 if accumulate else 0,
+                                         workspace or None, workspace_bytes, stream or None),
+           "goldy_layernorm_backward")
 
 
 def goldy_device_error(clear: bool = True) -> int:
