@@ -494,13 +494,15 @@ goldy_status goldy_gemm_noalloc(const goldy_gemm_desc* desc, int variant, const 
  * where they decrease the rows concerned are assigned in an unspecified way
  * (nothing outside the arrays is touched).
  *
- * Row strides are in elements.  ldx: X and dX; ldw: W and dW; ldy: Y, dY and
- * dZ; ldz: Z (0: the stride of the call's result, ldy or ldx); ldr: R (0: the
- * same).  X, W and dY start on 16-byte boundaries and their strides are
- * multiples of 8 where a product reads them; results, R, Z and biases need
- * only their element's alignment, with faster accesses where base and row
- * stride are multiples of 16 bytes.  in, out and rows are arbitrary, 0
- * included (an empty sum is 0).
+ * Row strides are in elements; 0 stands for dense rows, which for bf16 are
+ * padded to a multiple of 8 elements (16 bytes) and for fp32 are packed.
+ * ldx: X; lddx: dX; ldw: W and dW; ldy: Y, dY and dZ; ldz: Z; ldr: R.  A
+ * product reads X, W and dY in place where their row strides (and stride_w)
+ * are multiples of 8, and they then start on 16-byte boundaries; other strides
+ * cost a padded copy in the workspace.  Results, R, Z and biases need their
+ * element's alignment only, with faster accesses where base and row stride are
+ * multiples of 16 bytes.  in, out and rows are arbitrary, 0 included (an empty
+ * sum is 0).
  *
  * Results must not overlap inputs, except that R may be the result itself
  * (Y += ..., same stride). */
@@ -516,9 +518,8 @@ typedef enum goldy_act {
 
 typedef struct goldy_linear_desc {
   int64_t rows, in, out;
-  int64_t ldx, ldw, ldy;
-  int64_t ldz, ldr;
-  int64_t stride_w;         /* elements between two experts' W (and dW): >= in * ldw, a multiple of 8 */
+  int64_t ldx, lddx, ldw, ldy, ldz, ldr;
+  int64_t stride_w;         /* elements between two experts' W (and dW); 0: in * ldw */
   int32_t groups;           /* 0, or experts 1 .. GOLDY_MAX_GROUPS */
   int32_t act;              /* goldy_act of this layer (forward, bias gradient) */
   int32_t act_x;            /* goldy_act that made X (input gradient) */

@@ -4,7 +4,7 @@ Plain nvcc/g++ invocations, one object per translation unit, compiled in
 parallel: ``planner.cpp`` (host C++), ``runtime.cu`` (launch manager),
 ``noalloc.cu`` (the entry point with a compiled-in scratch array),
 ``kernels.cu`` once per GO-Kernel kind (``-DGOLDY_KIND=k``), the layer
-operators (``linear.cu``, ``bias_grad.cu``, ``layernorm.cu``) and
+operators (``linear.cu``, ``repack.cu``, ``bias_grad.cu``, ``layernorm.cu``) and
 ``linear_kernels.cu`` once per pass (``-DGOLDY_LINEAR_PASS=k``).  Objects go to
 ``_build/`` next to this file and the library to
 ``paper_2409_02227_gb300/libgoldy.so``; both are git-ignored.  A rebuild is
@@ -56,7 +56,7 @@ def _jobs(ptxas_verbose: bool):
     jobs.append(("runtime", cu + ["-c", os.path.join(CSRC, "runtime.cu")]))
     jobs.append(("noalloc", cu + ["-c", os.path.join(CSRC, "noalloc.cu")]))
     jobs.append(("ewise", cu + ["-c", os.path.join(CSRC, "ewise.cu")]))
-    for name in ("linear", "bias_grad", "layernorm"):
+    for name in ("linear", "repack", "bias_grad", "layernorm"):
         jobs.append((name, cu + ["-c", os.path.join(CSRC, name + ".cu")]))
     for k in range(NUM_LINEAR_PASSES):
         jobs.append((f"linear_kernels_{k}",

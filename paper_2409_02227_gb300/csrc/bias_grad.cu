@@ -194,7 +194,8 @@ extern "C" goldy_status goldy_linear_bias_grad(const goldy_linear_desc* desc, co
   if (ceil_div(desc->out, kCols) > int64_t(kLayerCounterBytes / sizeof(unsigned)))
     return fail(GOLDY_ERR_UNSUPPORTED, "bias gradient: too many columns");
   if (!db || !aligned(db, 4)) return bad("linear layer: db null or misaligned");
-  const int64_t ldz = desc->ldz ? desc->ldz : desc->ldy;
+  const int64_t ldy = stride_or_dense(desc->ldy, desc->out, GOLDY_BF16);
+  const int64_t ldz = stride_or_dense(desc->ldz, desc->out, GOLDY_BF16);
   if (desc->rows > 0 && (!dY || !aligned(dY, 2) || !aligned(Z, 2) || !aligned(dZ, 2)))
     return bad("linear layer: dY null, or dY, Z or dZ misaligned");
   if (Z && ldz < desc->out) return bad("linear layer: the row stride of Z is smaller than its row");
@@ -212,15 +213,15 @@ extern "C" goldy_status goldy_linear_bias_grad(const goldy_linear_desc* desc, co
   p.offsets = offsets;
   p.cnt = static_cast<unsigned*>(workspace);
   p.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + kLayerCounterBytes);
-  p.lddy = desc->ldy;
+  p.lddy = ldy;
   p.ldz = ldz;
-  p.lddz = desc->ldy;
+  p.lddz = ldy;
   p.rows = int32_t(desc->rows);
   p.cols = int32_t(desc->out);
   p.groups = std::max(1, desc->groups);
   p.act = desc->act;
   p.slices = slices_for(desc->rows, desc->out);
-  p.vec = aligned(dY, 16) && desc->ldy % 8 == 0 && (!Z || (aligned(Z, 16) && ldz % 8 == 0 && aligned(dZ, 16)));
+  p.vec = aligned(dY, 16) && ldy % 8 == 0 && (!Z || (aligned(Z, 16) && ldz % 8 == 0 && aligned(dZ, 16)));
   p.accumulate = accumulate;
   call.stream = stream;
   st = with_layer_context(stream, launch_bias_grad, &call);

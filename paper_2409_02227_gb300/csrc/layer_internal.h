@@ -69,7 +69,7 @@ struct LinearParams {
   int32_t part_chunks;     // 32-row chunks per epilogue warp in a partial
   int32_t act;
   int32_t bias_f32;
-  int32_t vec_c, vec_r, vec_z;   // 16-byte accesses possible
+  int32_t vec;             // results, residual and Z allow 16-byte accesses
   int32_t loads;           // 0: empty reduction, no tensor maps
   void* c;
   int64_t ldc, c_group;    // row stride and group stride of C (group stride: weight gradient)
@@ -103,6 +103,12 @@ struct BiasGradParams {
 
 // Argument checks shared by the linear-layer entry points (linear.cu), and the
 // bias gradient's workspace behind the counters (bias_grad.cu).
+// A row stride of 0 stands for dense rows; bf16 rows are then padded to 16 bytes.
+inline int64_t dense_stride(int64_t width, int dtype) { return dtype == GOLDY_BF16 ? (width + 7) / 8 * 8 : width; }
+inline int64_t stride_or_dense(int64_t ld, int64_t width, int dtype) { return ld ? ld : dense_stride(width, dtype); }
+// `batch` bf16 matrices with any strides -> packed ones with rows of ceil(cols / 8) * 8 (repack.cu).
+goldy_status launch_repack(const LayerContext& ctx, const void* from, void* to, int64_t batch, int64_t rows,
+                           int64_t cols, int64_t ld, int64_t batch_stride, void* stream);
 goldy_status check_linear(const goldy_linear_desc* d);
 goldy_status check_offsets(const goldy_linear_desc& d, const int32_t* offsets);
 size_t bias_grad_part_bytes(const goldy_linear_desc& d);

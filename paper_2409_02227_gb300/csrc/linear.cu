@@ -71,6 +71,7 @@ int part_chunks(int tile_r) { return int(ceil_div(ceil_div(tile_r, 32), 2)); }
 constexpr double kLoadRate = 70.0;       // bytes per cycle and SM from L2, all SMs loading
 constexpr double kUnitCost = 1200.0;
 constexpr double kSplitCost = 2500.0;
+constexpr double kSplitRate = 16.0;      // bytes per cycle of partials published or summed by one CTA
 
 LinChoice choose(const LinShape& s) {
   struct Candidate { int pair, tile_r; };
@@ -94,10 +95,12 @@ LinChoice choose(const LinShape& s) {
                                                  : s.rows / c.tile_r + std::min<int64_t>(s.groups, s.rows)) *
                          ceil_div(s.size_c, c.pair ? 256 : 128);
     for (int split = 1; split <= 16; split *= 2) {
+      // a split pays where it fills idle SMs, not to even out the last wave
+      if (split > 1 && tiles * split > workers) break;
       if (split > 1 && (split > kbs || size_t(most) * (c.pair ? 2 : 1) * kLinEpiWarps * 4 > kLayerCounterBytes)) break;
       const double waves = double(ceil_div(tiles * split, workers));
       double t = waves * (double(ceil_div(kbs, split)) * stage) + kUnitCost;
-      if (split > 1) t += kSplitCost + double(w) * 128 * 4 * split / kLoadRate;
+      if (split > 1) t += kSplitCost + double(w) * 128 * 4 * (split + 1) / kSplitRate;
       if (best_t < 0 || t < best_t) {
         best_t = t;
         best.pair = c.pair;
@@ -117,21 +120,52 @@ goldy_status bad(const std::string& why) { return fail(GOLDY_ERR_INVALID_ARG, wh
 
 bool is_dtype(int t) { return t == GOLDY_BF16 || t == GOLDY_F32; }
 
-goldy_status check_operand(const void* ptr, int64_t ld, const char* name) {
-  if (!ptr || !aligned(ptr, 16)) return bad(std::string("linear layer: ") + name + " must be a 16-byte aligned device pointer");
-  if (ld % 8 != 0) return bad(std::string("linear layer: the row stride of ") + name + " must be a multiple of 8");
+// A bf16 operand of a product: `batch` matrices of rows x cols.  The tensor
+// memory accelerator reads it in place if its rows start on 16-byte
+// boundaries, else a padded copy in the workspace.
+struct Operand {
+  const void* ptr;
+  int64_t batch, rows, cols, ld, stride;
+  bool copied() const { return ld % 8 != 0 || (batch > 1 && stride % 8 != 0); }
+  size_t copy_bytes() const {
+    if (!copied()) return 0;
+    return (size_t(batch) * size_t(rows) * size_t(dense_stride(cols, GOLDY_BF16)) * 2 + 255) & ~size_t(255);
+  }
+};
+
+Operand operand_x(const goldy_linear_desc& d, const void* x) {
+  const int64_t ld = stride_or_dense(d.ldx, d.in, GOLDY_BF16);
+  return {x, 1, d.rows, d.in, ld, d.rows * ld};
+}
+Operand operand_dy(const goldy_linear_desc& d, const void* dy) {
+  const int64_t ld = stride_or_dense(d.ldy, d.out, GOLDY_BF16);
+  return {dy, 1, d.rows, d.out, ld, d.rows * ld};
+}
+int64_t weight_stride(const goldy_linear_desc& d, int64_t ldw) { return d.stride_w ? d.stride_w : d.in * ldw; }
+Operand operand_w(const goldy_linear_desc& d, const void* w) {
+  const int64_t ld = stride_or_dense(d.ldw, d.out, GOLDY_BF16);
+  return {w, std::max(1, d.groups), d.in, d.out, ld, d.groups > 1 ? weight_stride(d, ld) : d.in * ld};
+}
+// the operands along c and along r of a pass
+void operands_of(const goldy_linear_desc& d, int pass, const void* p_ptr, const void* q_ptr, Operand (&o)[2]) {
+  o[0] = pass == kLinWeightGrad ? operand_dy(d, p_ptr) : operand_w(d, p_ptr);
+  o[1] = pass == kLinInputGrad ? operand_dy(d, q_ptr) : operand_x(d, q_ptr);
+}
+
+goldy_status check_operand(const Operand& o, const char* name) {
+  if (!o.ptr || !aligned(o.ptr, o.copied() ? 2 : 16))
+    return bad(std::string("linear layer: ") + name + (o.copied() ? " null or misaligned" : " must be a 16-byte aligned device pointer"));
   return GOLDY_OK;
 }
 
-// Tensor map of `batch` bf16 matrices (outer x inner), boxes of box_outer
-// rows x 64 elements, 128-byte swizzled.
-goldy_status encode(const LayerContext& ctx, CUtensorMap* m, const void* ptr, int64_t inner, int64_t outer,
-                    int64_t batch, int64_t ld, int64_t batch_stride, int box_outer) {
-  cuuint64_t dims[3] = {cuuint64_t(inner), cuuint64_t(outer), cuuint64_t(batch)};
-  cuuint64_t strides[2] = {cuuint64_t(ld) * 2, cuuint64_t(batch_stride) * 2};
-  cuuint32_t box[3] = {64, cuuint32_t(box_outer), 1};
+// Tensor map of an operand, boxes of box_rows rows x 64 elements, 128-byte
+// swizzled.
+goldy_status encode(const LayerContext& ctx, CUtensorMap* m, const Operand& o, int box_rows) {
+  cuuint64_t dims[3] = {cuuint64_t(o.cols), cuuint64_t(o.rows), cuuint64_t(o.batch)};
+  cuuint64_t strides[2] = {cuuint64_t(o.ld) * 2, cuuint64_t(o.stride) * 2};
+  cuuint32_t box[3] = {64, cuuint32_t(box_rows), 1};
   cuuint32_t one[3] = {1, 1, 1};
-  const CUresult r = ctx.encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), dims, strides, box,
+  const CUresult r = ctx.encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(o.ptr), dims, strides, box,
                                 one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                                 CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) return fail(GOLDY_ERR_CUDA, "cuTensorMapEncodeTiled failed with code " + std::to_string(int(r)));
@@ -153,9 +187,7 @@ goldy_status set_smem(const LayerContext& ctx, const void* fn, int pass, int pai
 
 struct LinCall {
   LinShape s;
-  const goldy_linear_desc* d;
-  const void* p_ptr;       // operand along c: W, or dY
-  const void* q_ptr;       // operand along r: X, dY, or X
+  Operand o[2];            // along c: W, or dY; along r: X, dY, or X
   LinearParams prm;        // epilogue fields filled in by the entry point
   void* workspace;
   size_t workspace_bytes;
@@ -165,17 +197,31 @@ struct LinCall {
 goldy_status launch_linear(const LayerContext& ctx, void* arg) {
   LinCall& call = *static_cast<LinCall*>(arg);
   const LinShape& s = call.s;
-  const goldy_linear_desc& d = *call.d;
   LinearParams& p = call.prm;
   const LinChoice c = choose(s);
-  if (c.split > 1) {
+  Operand* const o = call.o;
+  const size_t copy_bytes = s.red > 0 ? o[0].copy_bytes() + o[1].copy_bytes() : 0;
+  if (c.split > 1 || copy_bytes > 0) {
     if (!call.workspace || !aligned(call.workspace, 256))
       return bad("linear layer: the workspace must be a 256-byte aligned device pointer");
-    if (call.workspace_bytes < kLayerCounterBytes + c.part_bytes)
+    const size_t need = kLayerCounterBytes + c.part_bytes + copy_bytes;
+    if (call.workspace_bytes < need)
       return fail(GOLDY_ERR_NOMEM, "linear layer: workspace of " + std::to_string(call.workspace_bytes) + " bytes, " +
-                                       std::to_string(kLayerCounterBytes + c.part_bytes) + " needed");
-    p.cnt = static_cast<unsigned*>(call.workspace);
-    p.part = reinterpret_cast<float*>(static_cast<char*>(call.workspace) + kLayerCounterBytes);
+                                       std::to_string(need) + " needed");
+    char* ws = static_cast<char*>(call.workspace);
+    p.cnt = reinterpret_cast<unsigned*>(ws);
+    p.part = reinterpret_cast<float*>(ws + kLayerCounterBytes);
+    ws += kLayerCounterBytes + c.part_bytes;
+    for (int i = 0; i < 2 && copy_bytes > 0; ++i) {
+      const size_t bytes = o[i].copy_bytes();
+      if (bytes == 0) continue;
+      goldy_status st = launch_repack(ctx, o[i].ptr, ws, o[i].batch, o[i].rows, o[i].cols, o[i].ld, o[i].stride, call.stream);
+      if (st != GOLDY_OK) return st;
+      o[i].ptr = ws;
+      o[i].ld = dense_stride(o[i].cols, GOLDY_BF16);
+      o[i].stride = o[i].rows * o[i].ld;
+      ws += bytes;
+    }
   }
   const bool wgrad = s.pass == kLinWeightGrad;
   const int ctas = c.pair ? 2 : 1;
@@ -197,17 +243,9 @@ goldy_status launch_linear(const LayerContext& ctx, void* arg) {
   p.err = ctx.err_word;
   if (p.loads) {
     goldy_status st;
-    if (wgrad) {
-      st = encode(ctx, &p.ta, call.p_ptr, d.out, d.rows, 1, d.ldy, d.rows * d.ldy, kLinStageK);
-      if (st == GOLDY_OK) st = encode(ctx, &p.tb, call.q_ptr, d.in, d.rows, 1, d.ldx, d.rows * d.ldx, kLinStageK);
-    } else {
-      const int64_t q_ld = s.pass == kLinForward ? d.ldx : d.ldy;
-      const int64_t w_stride = d.groups > 1 ? d.stride_w : d.in * d.ldw;
-      st = encode(ctx, &p.ta, call.p_ptr, d.out, d.in, s.groups, d.ldw, w_stride,
-                  s.pass == kLinForward ? kLinStageK : 128);
-      if (st == GOLDY_OK) st = encode(ctx, &p.tb, call.q_ptr, s.red, d.rows, 1, q_ld, d.rows * q_ld, c.tile_r / ctas);
-      if (st == GOLDY_OK) st = encode(ctx, &p.tb_part, call.q_ptr, s.red, d.rows, 1, q_ld, d.rows * q_ld, p.part_box);
-    }
+    st = encode(ctx, &p.ta, o[0], s.pass == kLinInputGrad ? 128 : kLinStageK);
+    if (st == GOLDY_OK) st = encode(ctx, &p.tb, o[1], wgrad ? kLinStageK : c.tile_r / ctas);
+    if (st == GOLDY_OK && !wgrad) st = encode(ctx, &p.tb_part, o[1], p.part_box);
     if (st != GOLDY_OK) return st;
   }
   const int f32 = s.out_dtype == GOLDY_F32 ? 1 : 0;
@@ -244,21 +282,21 @@ goldy_status set_result(LinearParams& p, const LinShape& s, void* C, int64_t ldc
                         const char* name) {
   const size_t es = type_bytes(s.out_dtype);
   if (!C || !aligned(C, es)) return bad(std::string("linear layer: ") + name + " null or misaligned");
-  if (ldr == 0) ldr = ldc;
+  ldr = stride_or_dense(ldr, s.size_c, s.out_dtype);
   if (R && (!aligned(R, es) || ldr < s.size_c)) return bad("linear layer: residual misaligned or its row stride too small");
   p.c = C;
   p.ldc = ldc;
   p.res = R;
   p.ldr = ldr;
-  p.vec_c = aligned(C, 16) && (size_t(ldc) * es) % 16 == 0;
-  p.vec_r = aligned(R, 16) && (size_t(ldr) * es) % 16 == 0;
+  p.vec = aligned(C, 16) && (size_t(ldc) * es) % 16 == 0 && (!R || (aligned(R, 16) && (size_t(ldr) * es) % 16 == 0));
   return GOLDY_OK;
 }
 
 goldy_status set_saved(LinearParams& p, const LinShape& s, const void* Z, int64_t ldz) {
+  ldz = stride_or_dense(ldz, s.size_c, GOLDY_BF16);
   if (!aligned(Z, 2) || ldz < s.size_c) return bad("linear layer: Z misaligned or its row stride too small");
   p.ldz = ldz;
-  p.vec_z = aligned(Z, 16) && ldz % 8 == 0;
+  p.vec = p.vec && aligned(Z, 16) && ldz % 8 == 0;
   return GOLDY_OK;
 }
 
@@ -269,12 +307,13 @@ goldy_status check_linear(const goldy_linear_desc* d) {
   if (d->rows < 0 || d->in < 0 || d->out < 0 || d->rows > kMaxDim || d->in > kMaxDim || d->out > kMaxDim)
     return bad("linear layer: a size is negative or too large");
   if (d->groups < 0 || d->groups > GOLDY_MAX_GROUPS) return bad("linear layer: groups out of range");
-  if (d->ldx < d->in || d->ldw < d->out || d->ldy < d->out || d->ldz < 0 || d->ldr < 0)
+  if ((d->ldx && d->ldx < d->in) || (d->lddx && d->lddx < d->in) || (d->ldw && d->ldw < d->out) ||
+      (d->ldy && d->ldy < d->out) || d->ldz < 0 || d->ldr < 0)
     return bad("linear layer: a row stride is smaller than its row");
-  if (d->ldx > kMaxDim || d->ldw > kMaxDim || d->ldy > kMaxDim || d->ldz > kMaxDim || d->ldr > kMaxDim)
+  if (d->ldx > kMaxDim || d->lddx > kMaxDim || d->ldw > kMaxDim || d->ldy > kMaxDim || d->ldz > kMaxDim || d->ldr > kMaxDim)
     return bad("linear layer: a row stride is too large");
-  if (d->groups > 1 && (d->stride_w < d->in * d->ldw || d->stride_w % 8 != 0))
-    return bad("linear layer: stride_w must be a multiple of 8 and at least in * ldw");
+  if (d->stride_w < 0 || (d->groups > 1 && d->stride_w && d->stride_w < d->in * stride_or_dense(d->ldw, d->out, GOLDY_BF16)))
+    return bad("linear layer: stride_w is smaller than in * ldw");
   if (d->act < GOLDY_ACT_NONE || d->act > GOLDY_ACT_SILU || d->act_x < GOLDY_ACT_NONE || d->act_x > GOLDY_ACT_SILU)
     return bad("linear layer: unknown activation");
   if (!is_dtype(d->y_dtype) || !is_dtype(d->dx_dtype) || !is_dtype(d->dw_dtype) || !is_dtype(d->bias_dtype))
@@ -301,7 +340,10 @@ extern "C" goldy_status goldy_linear_query(const goldy_linear_desc* desc, size_t
   size_t part = 0;
   for (int pass = 0; pass < 3; ++pass) {
     const LinShape s = shape_of(*desc, pass);
-    if (s.size_c > 0 && s.size_r > 0) part = std::max(part, choose(s).part_bytes);
+    if (s.size_c == 0 || s.size_r == 0) continue;
+    Operand o[2];
+    operands_of(*desc, pass, nullptr, nullptr, o);
+    part = std::max(part, choose(s).part_bytes + o[0].copy_bytes() + o[1].copy_bytes());
   }
   part = std::max(part, bias_grad_part_bytes(*desc));
   *workspace_bytes = part > 0 ? kLayerCounterBytes + part : 0;
@@ -315,17 +357,17 @@ extern "C" goldy_status goldy_linear_forward(const goldy_linear_desc* desc, cons
   if (st == GOLDY_OK) st = check_offsets(*desc, offsets);
   if (st != GOLDY_OK) return st;
   LinCall call{};
-  call.d = desc;
   call.s = shape_of(*desc, kLinForward);
+  operands_of(*desc, kLinForward, W, X, call.o);
   if (call.s.size_c == 0 || call.s.size_r == 0) return ok();
   if (call.s.red > 0) {
-    st = check_operand(X, desc->ldx, "X");
-    if (st == GOLDY_OK) st = check_operand(W, desc->ldw, "W");
+    st = check_operand(call.o[0], "W");
+    if (st == GOLDY_OK) st = check_operand(call.o[1], "X");
     if (st != GOLDY_OK) return st;
   }
   LinearParams& p = call.prm;
-  st = set_result(p, call.s, Y, desc->ldy, R, desc->ldr, "Y");
-  if (st == GOLDY_OK && Z) st = set_saved(p, call.s, Z, desc->ldz ? desc->ldz : desc->ldy);
+  st = set_result(p, call.s, Y, stride_or_dense(desc->ldy, desc->out, desc->y_dtype), R, desc->ldr, "Y");
+  if (st == GOLDY_OK && Z) st = set_saved(p, call.s, Z, desc->ldz);
   if (st != GOLDY_OK) return st;
   if (bias && !aligned(bias, type_bytes(desc->bias_dtype))) return bad("linear layer: bias misaligned");
   p.z_out = Z;
@@ -333,8 +375,6 @@ extern "C" goldy_status goldy_linear_forward(const goldy_linear_desc* desc, cons
   p.bias_f32 = desc->bias_dtype == GOLDY_F32;
   p.act = desc->act;
   p.offsets = offsets;
-  call.p_ptr = W;
-  call.q_ptr = X;
   call.workspace = workspace;
   call.workspace_bytes = workspace_bytes;
   call.stream = stream;
@@ -351,23 +391,21 @@ extern "C" goldy_status goldy_linear_input_grad(const goldy_linear_desc* desc, c
   if (desc->act_x != GOLDY_ACT_NONE && !Z) return bad("linear layer: the activation's gradient needs Z");
   if (desc->act_x == GOLDY_ACT_NONE && Z) return bad("linear layer: Z given, but act_x is GOLDY_ACT_NONE");
   LinCall call{};
-  call.d = desc;
   call.s = shape_of(*desc, kLinInputGrad);
+  operands_of(*desc, kLinInputGrad, W, dY, call.o);
   if (call.s.size_c == 0 || call.s.size_r == 0) return ok();
   if (call.s.red > 0) {
-    st = check_operand(dY, desc->ldy, "dY");
-    if (st == GOLDY_OK) st = check_operand(W, desc->ldw, "W");
+    st = check_operand(call.o[0], "W");
+    if (st == GOLDY_OK) st = check_operand(call.o[1], "dY");
     if (st != GOLDY_OK) return st;
   }
   LinearParams& p = call.prm;
-  st = set_result(p, call.s, dX, desc->ldx, R, desc->ldr, "dX");
-  if (st == GOLDY_OK && Z) st = set_saved(p, call.s, Z, desc->ldz ? desc->ldz : desc->ldx);
+  st = set_result(p, call.s, dX, stride_or_dense(desc->lddx, desc->in, desc->dx_dtype), R, desc->ldr, "dX");
+  if (st == GOLDY_OK && Z) st = set_saved(p, call.s, Z, desc->ldz);
   if (st != GOLDY_OK) return st;
   p.z_in = Z;
   p.act = desc->act_x;
   p.offsets = offsets;
-  call.p_ptr = W;
-  call.q_ptr = dY;
   call.workspace = workspace;
   call.workspace_bytes = workspace_bytes;
   call.stream = stream;
@@ -383,21 +421,21 @@ extern "C" goldy_status goldy_linear_weight_grad(const goldy_linear_desc* desc, 
   if (st != GOLDY_OK) return st;
   if (accumulate != 0 && accumulate != 1) return bad("linear layer: accumulate must be 0 or 1");
   LinCall call{};
-  call.d = desc;
   call.s = shape_of(*desc, kLinWeightGrad);
+  operands_of(*desc, kLinWeightGrad, dY, X, call.o);
   if (call.s.size_c == 0 || call.s.size_r == 0) return ok();
   if (call.s.red > 0) {
-    st = check_operand(X, desc->ldx, "X");
-    if (st == GOLDY_OK) st = check_operand(dY, desc->ldy, "dY");
+    st = check_operand(call.o[0], "dY");
+    if (st == GOLDY_OK) st = check_operand(call.o[1], "X");
     if (st != GOLDY_OK) return st;
   }
   LinearParams& p = call.prm;
-  st = set_result(p, call.s, dW, desc->ldw, accumulate ? dW : nullptr, desc->ldw, "dW");
+  const int64_t ldw = stride_or_dense(desc->ldw, desc->out, desc->dw_dtype);
+  st = set_result(p, call.s, dW, ldw, accumulate ? dW : nullptr, ldw, "dW");
   if (st != GOLDY_OK) return st;
-  p.c_group = p.r_group = desc->groups > 1 ? desc->stride_w : 0;
+  p.c_group = p.r_group = desc->groups > 1 ? weight_stride(*desc, ldw) : 0;
+  p.vec = p.vec && (size_t(p.c_group) * type_bytes(desc->dw_dtype)) % 16 == 0;
   p.offsets = offsets;
-  call.p_ptr = dY;
-  call.q_ptr = X;
   call.workspace = workspace;
   call.workspace_bytes = workspace_bytes;
   call.stream = stream;

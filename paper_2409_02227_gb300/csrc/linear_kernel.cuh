@@ -203,14 +203,23 @@ struct LinBias {
   float v[8];
 };
 
-// Epilogue of one 32-row chunk: v[j] is row j of this lane's column.
-template <bool OUT_F32>
-__device__ __forceinline__ void lin_finish_chunk(const LinearParams& p, const LinUnit& t, uint32_t buf, int lane,
-                                                 int row0, int col0, const LinBias& bias, const float (&v)[32]) {
-  const int sub = lane >> 2;                       // row within 8
-  const int col = col0 + (lane & 3) * 8;           // this lane's 8 columns
-  const int n_col = min(8, p.size_c - col);
-  const bool whole = n_col == 8;
+template <int PASS>
+__device__ __forceinline__ void lin_load_bias(const LinearParams& p, int e, int col, LinBias& b) {
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    b.v[k] = 0.0f;
+    if (PASS == kLinForward && p.bias && col + k < p.size_c) {
+      const int64_t i = int64_t(e) * p.size_c + col + k;
+      b.v[k] = p.bias_f32 ? static_cast<const float*>(p.bias)[i] : load_bf16(p.bias, i);
+    }
+  }
+}
+
+// Epilogue of one 32-row chunk: v[j] is row j of this lane's column.  After
+// the transposition a lane has 8 consecutive columns of 4 rows, 8 apart.  What
+// the rows need from memory (saved pre-activation, residual) is asked for
+// first, all 4 rows at once, so that its latency is paid once per chunk.
+__device__ __forceinline__ void lin_transpose(uint32_t buf, int lane, const float (&v)[32]) {
   __syncwarp();
 #pragma unroll
   for (int j = 0; j < 32; ++j) {
@@ -218,100 +227,157 @@ __device__ __forceinline__ void lin_finish_chunk(const LinearParams& p, const Li
     asm volatile("st.shared.f32 [%0], %1;" ::"r"(a), "f"(v[j]) : "memory");
   }
   __syncwarp();
+}
+__device__ __forceinline__ void lin_transposed(uint32_t buf, int lane, int row, const LinBias& bias, float (&f)[8]) {
+  const float4 a = ptx::ld_shared_v4(lin_stage_addr(buf, row, (lane & 3) * 2));
+  const float4 b = ptx::ld_shared_v4(lin_stage_addr(buf, row, (lane & 3) * 2 + 1));
+  f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) f[k] += bias.v[k];
+}
+
+// Whole 16-byte accesses: every tensor of the epilogue on 16-byte boundaries,
+// 32 whole columns.  bf16 results.
+template <int PASS, int ACT>
+__device__ __forceinline__ void lin_finish_fast(const LinearParams& p, const LinUnit& t, uint32_t buf, int lane,
+                                                int row0, int col, const LinBias& bias, const float (&v)[32]) {
+  const int sub = lane >> 2;
+  const int64_t r0 = int64_t(t.r0) + row0 + sub;
+  const int left = t.w - row0 - sub;               // row i * 8 of this lane exists if i * 8 < left
+  const int64_t c_at = int64_t(t.e) * p.c_group + r0 * p.ldc + col;
+  const int64_t q_at = int64_t(t.e) * p.r_group + r0 * p.ldr + col;
+  constexpr bool SLOPE = PASS == kLinInputGrad && ACT != GOLDY_ACT_NONE;
+  uint4 z[4], q[4];
+  if (SLOPE) {
+    const uint16_t* from = static_cast<const uint16_t*>(p.z_in) + r0 * p.ldz + col;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i * 8 < left) z[i] = __ldg(reinterpret_cast<const uint4*>(from + i * 8 * p.ldz));
+  }
+  if (p.res) {
+    const uint16_t* from = static_cast<const uint16_t*>(p.res) + q_at;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i * 8 < left) q[i] = *reinterpret_cast<const uint4*>(from + i * 8 * p.ldr);
+  }
+  lin_transpose(buf, lane, v);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (i * 8 >= left) break;
+    float f[8];
+    lin_transposed(buf, lane, i * 8 + sub, bias, f);
+    if (PASS == kLinForward && p.z_out)
+      *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.z_out) + (r0 + i * 8) * p.ldz + col) = pack8(f);
+    if (SLOPE) {
+      float zf[8];
+      unpack8(z[i], zf);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) f[k] *= act_slope(zf[k], ACT);
+    } else if (PASS == kLinForward) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) f[k] = act_value(f[k], ACT);
+    }
+    if (p.res) {
+      float qf[8];
+      unpack8(q[i], qf);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) f[k] += qf[k];
+    }
+    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.c) + c_at + i * 8 * p.ldc) = pack8(f);
+  }
+}
+
+// The same for fp32 results, rolled up: the sums of the chunks still to come
+// occupy the registers.
+template <int PASS>
+__device__ __forceinline__ void lin_finish_f32(const LinearParams& p, const LinUnit& t, uint32_t buf, int lane,
+                                               int row0, int col, const LinBias& bias) {
+  const int sub = lane >> 2;
 #pragma unroll 1
   for (int i = 0; i < 4; ++i) {
     const int row = i * 8 + sub;
-    if (row0 + i * 8 >= t.w) break;
-    if (row0 + row >= t.w || n_col <= 0) continue;
+    if (row0 + row >= t.w) break;
     const int64_t r = int64_t(t.r0) + row0 + row;
+    float4 q0 = make_float4(0.0f, 0.0f, 0.0f, 0.0f), q1 = q0;
+    if (PASS != kLinWeightGrad && p.res) {
+      const float* from = static_cast<const float*>(p.res) + r * p.ldr + col;
+      q0 = *reinterpret_cast<const float4*>(from);
+      q1 = *reinterpret_cast<const float4*>(from + 4);
+    }
     float f[8];
-    {
-      const float4 a = ptx::ld_shared_v4(lin_stage_addr(buf, row, (lane & 3) * 2));
-      const float4 b = ptx::ld_shared_v4(lin_stage_addr(buf, row, (lane & 3) * 2 + 1));
-      f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
-    }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) f[k] += bias.v[k];
-    if (p.z_out) {
-      uint16_t* z = static_cast<uint16_t*>(p.z_out) + r * p.ldz + col;
-      if (whole && p.vec_z) {
-        *reinterpret_cast<uint4*>(z) = pack8(f);
-      } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (k < n_col) store_bf16(z, k, f[k]);
-      }
-    }
-    if (p.z_in) {
-      const uint16_t* z = static_cast<const uint16_t*>(p.z_in) + r * p.ldz + col;
-      float zf[8];
-      if (whole && p.vec_z) {
-        unpack8(__ldg(reinterpret_cast<const uint4*>(z)), zf);
-      } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) zf[k] = k < n_col ? load_bf16(z, k) : 0.0f;
-      }
-#pragma unroll
-      for (int k = 0; k < 8; ++k) f[k] *= act_slope(zf[k], p.act);
-    } else if (p.act != GOLDY_ACT_NONE) {
+    lin_transposed(buf, lane, row, bias, f);
+    if (PASS == kLinForward) {
+      if (p.z_out) *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.z_out) + r * p.ldz + col) = pack8(f);
 #pragma unroll
       for (int k = 0; k < 8; ++k) f[k] = act_value(f[k], p.act);
     }
-    const int64_t c_at = int64_t(t.e) * p.c_group + r * p.ldc + col;
-    if (OUT_F32) {
-      float* c = static_cast<float*>(p.c) + c_at;
-      if (p.res) {
-        const float* q = static_cast<const float*>(p.res) + int64_t(t.e) * p.r_group + r * p.ldr + col;
-        if (whole && p.vec_r) {
-          const float4 a = *reinterpret_cast<const float4*>(q), b = *reinterpret_cast<const float4*>(q + 4);
-          f[0] += a.x, f[1] += a.y, f[2] += a.z, f[3] += a.w, f[4] += b.x, f[5] += b.y, f[6] += b.z, f[7] += b.w;
-        } else {
+    if (PASS == kLinInputGrad && p.z_in) {
+      float zf[8];
+      unpack8(__ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.z_in) + r * p.ldz + col)), zf);
 #pragma unroll
-          for (int k = 0; k < 8; ++k)
-            if (k < n_col) f[k] += q[k];
-        }
+      for (int k = 0; k < 8; ++k) f[k] *= act_slope(zf[k], p.act);
+    }
+    float* c = static_cast<float*>(p.c) + int64_t(t.e) * p.c_group + r * p.ldc + col;
+    *reinterpret_cast<float4*>(c) = make_float4(f[0] + q0.x, f[1] + q0.y, f[2] + q0.z, f[3] + q0.w);
+    *reinterpret_cast<float4*>(c + 4) = make_float4(f[4] + q1.x, f[5] + q1.y, f[6] + q1.z, f[7] + q1.w);
+  }
+}
+
+// Any alignment and the columns at C's edge, element by element.
+template <int PASS, bool OUT_F32>
+__device__ __noinline__ void lin_finish_slow(const LinearParams& p, int e, int first_row, int rows, uint32_t buf,
+                                             int lane, int col) {
+  const int sub = lane >> 2;
+  const int n_col = min(8, p.size_c - col);
+  LinBias bias;
+  lin_load_bias<PASS>(p, e, col, bias);
+#pragma unroll 1
+  for (int i = 0; i < 4; ++i) {
+    const int row = i * 8 + sub;
+    if (row >= rows) break;
+    const int64_t r = int64_t(first_row) + row;
+    float f[8];
+    lin_transposed(buf, lane, row, bias, f);
+    const int64_t c_at = int64_t(e) * p.c_group + r * p.ldc + col;
+    const int64_t q_at = int64_t(e) * p.r_group + r * p.ldr + col;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (k >= n_col) break;
+      float v = f[k];
+      if (PASS == kLinForward) {
+        if (p.z_out) store_bf16(p.z_out, r * p.ldz + col + k, v);
+        v = act_value(v, p.act);
+      } else if (PASS == kLinInputGrad && p.z_in) {
+        v *= act_slope(load_bf16(p.z_in, r * p.ldz + col + k), p.act);
       }
-      if (whole && p.vec_c) {
-        *reinterpret_cast<float4*>(c) = make_float4(f[0], f[1], f[2], f[3]);
-        *reinterpret_cast<float4*>(c + 4) = make_float4(f[4], f[5], f[6], f[7]);
-      } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (k < n_col) c[k] = f[k];
-      }
-    } else {
-      uint16_t* c = static_cast<uint16_t*>(p.c) + c_at;
-      if (p.res) {
-        const uint16_t* q = static_cast<const uint16_t*>(p.res) + int64_t(t.e) * p.r_group + r * p.ldr + col;
-        float qf[8];
-        if (whole && p.vec_r) {
-          unpack8(*reinterpret_cast<const uint4*>(q), qf);
-        } else {
-#pragma unroll
-          for (int k = 0; k < 8; ++k) qf[k] = k < n_col ? load_bf16(q, k) : 0.0f;
-        }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) f[k] += qf[k];
-      }
-      if (whole && p.vec_c) {
-        *reinterpret_cast<uint4*>(c) = pack8(f);
-      } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (k < n_col) store_bf16(c, k, f[k]);
-      }
+      if (p.res && !(OUT_F32 && PASS == kLinWeightGrad))
+        v += OUT_F32 ? static_cast<const float*>(p.res)[q_at + k] : load_bf16(p.res, q_at + k);
+      if (OUT_F32) static_cast<float*>(p.c)[c_at + k] = v;
+      else store_bf16(p.c, c_at + k, v);
     }
   }
 }
 
-__device__ __forceinline__ void lin_load_bias(const LinearParams& p, int e, int col, LinBias& b) {
-#pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    b.v[k] = 0.0f;
-    if (p.bias && col + k < p.size_c) {
-      const int64_t i = int64_t(e) * p.size_c + col + k;
-      b.v[k] = p.bias_f32 ? static_cast<const float*>(p.bias)[i] : load_bf16(p.bias, i);
-    }
+template <int PASS, bool OUT_F32>
+__device__ __forceinline__ void lin_finish_chunk(const LinearParams& p, const LinUnit& t, uint32_t buf, int lane,
+                                                 int row0, int col0, const LinBias& bias, const float (&v)[32]) {
+  const int col = col0 + (lane & 3) * 8;           // this lane's 8 columns
+  if (!p.vec || col0 + 32 > p.size_c) {
+    lin_transpose(buf, lane, v);
+    if (col < p.size_c) lin_finish_slow<PASS, OUT_F32>(p, t.e, t.r0 + row0, t.w - row0, buf, lane, col);
+    return;
+  }
+  if (OUT_F32) {
+    lin_transpose(buf, lane, v);
+    lin_finish_f32<PASS>(p, t, buf, lane, row0, col, bias);
+    return;
+  }
+  switch (PASS == kLinWeightGrad ? GOLDY_ACT_NONE : p.act) {
+    case GOLDY_ACT_RELU: lin_finish_fast<PASS, GOLDY_ACT_RELU>(p, t, buf, lane, row0, col, bias, v); break;
+    case GOLDY_ACT_GELU: lin_finish_fast<PASS, GOLDY_ACT_GELU>(p, t, buf, lane, row0, col, bias, v); break;
+    case GOLDY_ACT_GELU_TANH: lin_finish_fast<PASS, GOLDY_ACT_GELU_TANH>(p, t, buf, lane, row0, col, bias, v); break;
+    case GOLDY_ACT_SILU: lin_finish_fast<PASS, GOLDY_ACT_SILU>(p, t, buf, lane, row0, col, bias, v); break;
+    default: lin_finish_fast<PASS, GOLDY_ACT_NONE>(p, t, buf, lane, row0, col, bias, v);
   }
 }
 
@@ -586,7 +652,7 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
     for (int u = worker; ok && walk.find(u, t); u += n_workers) {
       const int col0 = t.c0 + int(rank) * 128 + q * 32;
       LinBias bias;
-      lin_load_bias(p, t.e, col0 + (lane & 3) * 8, bias);
+      lin_load_bias<PASS>(p, t.e, col0 + (lane & 3) * 8, bias);
       const uint32_t lanes = tmem_base + (uint32_t(q * 32) << 16);
       const bool split = p.split > 1;
       float* part = p.part + ((size_t(t.tile) * p.split * CTAS + rank) * kLinEpiWarps + ew) * (size_t(p.part_chunks) * 1024);
@@ -597,12 +663,21 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
         for (int j = 0; j < 32; ++j)
           if (chunk * 32 + j < t.w) __stcg(to + j * 32, v[j]);
       };
+      bool last = true;
       if (OUT_F32) {
         float sum[4][32];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int j = 0; j < 32; ++j) sum[i][j] = 0.0f;
+          for (int j = 0; j < 32; ++j) {
+            sum[i][j] = 0.0f;
+            // a gradient that is added to starts from it (split 0 does), read
+            // while the tensor cores work
+            const int row = (side + 2 * i) * 32 + j;
+            if (PASS == kLinWeightGrad && p.res && t.s == 0 && row < t.w && col0 + lane < p.size_c)
+              sum[i][j] = static_cast<const float*>(p.res)[int64_t(t.e) * p.r_group + (int64_t(t.r0) + row) * p.ldr +
+                                                           col0 + lane];
+          }
         for (int kb = t.kb0; kb < t.kb1; kb += kLinPromote) {
           ok = lin_wait(ptx::smem_u32(&tfull[acc]), acc_phase, abort_flag);
           if (!ok) break;
@@ -622,68 +697,80 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
           next_acc();
         }
         if (!ok) break;
+        if (!split) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int chunk = side + 2 * i;
-          if (chunk * 32 >= t.w) continue;
-          if (split) publish(i, chunk, sum[i]);
-          else lin_finish_chunk<OUT_F32>(p, t, buf, lane, chunk * 32, col0, bias, sum[i]);
-        }
-      } else {
-        const bool some = t.kb1 > t.kb0;
-        if (some) {
-          ok = lin_wait(ptx::smem_u32(&tfull[acc]), acc_phase, abort_flag);
-          if (!ok) break;
-          ptx::tc_fence_after();
-        }
-#pragma unroll 1
-        for (int i = 0; (side + 2 * i) * 32 < t.w; ++i) {
-          const int chunk = side + 2 * i;
-          float v[32];
-          if (some) {
-            uint32_t raw[32];
-            ptx::tmem_ld_32x32b_x32(lanes + uint32_t(acc * 256 + chunk * 32), raw);
-            ptx::tmem_ld_wait();
-#pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(raw[j]);
-          } else {
-#pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = 0.0f;
+          for (int i = 0; i < 4; ++i) {
+            const int chunk = side + 2 * i;
+            if (chunk * 32 < t.w) lin_finish_chunk<PASS, OUT_F32>(p, t, buf, lane, chunk * 32, col0, bias, sum[i]);
           }
-          if (split) publish(i, chunk, v);
-          else lin_finish_chunk<OUT_F32>(p, t, buf, lane, chunk * 32, col0, bias, v);
+          continue;
         }
-        if (some) {
-          release();
-          next_acc();
-        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if ((side + 2 * i) * 32 < t.w) publish(i, side + 2 * i, sum[i]);
       }
+      const bool some = !OUT_F32 && t.kb1 > t.kb0;     // the result is in accumulator `acc`
+      if (some) {
+        ok = lin_wait(ptx::smem_u32(&tfull[acc]), acc_phase, abort_flag);
+        if (!ok) break;
+        ptx::tc_fence_after();
+      }
+      auto read_acc = [&](int chunk, float (&v)[32]) {
+        if (some) {
+          uint32_t raw[32];
+          ptx::tmem_ld_32x32b_x32(lanes + uint32_t(acc * 256 + chunk * 32), raw);
+          ptx::tmem_ld_wait();
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(raw[j]);
+          // the accumulator is free once its last chunk is in registers
+          if ((chunk + 2) * 32 >= t.w) release();
+        } else {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = 0.0f;
+        }
+      };
+      unsigned* cnt = p.cnt + (size_t(t.tile) * CTAS + rank) * kLinEpiWarps + ew;
       if (split) {
-        // the last of the splits to arrive at this warp's part of the tile
-        // sums all of them in split order and leaves the counter at zero
-        unsigned* cnt = p.cnt + (size_t(t.tile) * CTAS + rank) * kLinEpiWarps + ew;
+        if (!OUT_F32) {
+#pragma unroll 1
+          for (int i = 0; (side + 2 * i) * 32 < t.w; ++i) {
+            float v[32];
+            read_acc(side + 2 * i, v);
+            publish(i, side + 2 * i, v);
+          }
+        }
         __threadfence();
         __syncwarp();
         unsigned old = 0;
         if (lane == 0) old = atomicAdd(cnt, 1u);
-        old = __shfl_sync(0xFFFFFFFFu, old, 0);
-        if (old == unsigned(p.split - 1)) {
-          __threadfence();
-          for (int i = 0; (side + 2 * i) * 32 < t.w; ++i) {
-            const int chunk = side + 2 * i;
-            float v[32];
+        last = __shfl_sync(0xFFFFFFFFu, old, 0) == unsigned(p.split - 1);
+        if (last) __threadfence();
+      }
+      // the last of the splits to arrive at this warp's part of the tile sums
+      // all of them in split order and leaves the counter at zero
+#pragma unroll 1
+      for (int i = 0; last && (side + 2 * i) * 32 < t.w; ++i) {
+        const int chunk = side + 2 * i;
+        float v[32];
+        if (split) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = 0.0f;
-            for (int s = 0; s < p.split; ++s) {
-              const float* from = part + s * split_stride + size_t(i) * 1024 + lane;
+          for (int j = 0; j < 32; ++j) v[j] = 0.0f;
+#pragma unroll 1
+          for (int s = 0; s < p.split; ++s) {
+            const float* from = part + s * split_stride + size_t(i) * 1024 + lane;
 #pragma unroll
-              for (int j = 0; j < 32; ++j)
-                if (chunk * 32 + j < t.w) v[j] += __ldcg(from + j * 32);
-            }
-            lin_finish_chunk<OUT_F32>(p, t, buf, lane, chunk * 32, col0, bias, v);
+            for (int j = 0; j < 32; ++j)
+              if (chunk * 32 + j < t.w) v[j] += __ldcg(from + j * 32);
           }
-          if (lane == 0) *cnt = 0u;
+        } else {
+          read_acc(chunk, v);
         }
+        lin_finish_chunk<PASS, OUT_F32>(p, t, buf, lane, chunk * 32, col0, bias, v);
+      }
+      if (split && last && lane == 0) *cnt = 0u;
+      if (some) {
+        if (side * 32 >= t.w) release();               // no chunk of this warp's
+        next_acc();
       }
     }
     if (!ok && lane == 0) raise_error(p.err, abort_flag, kErrEpilogueWait);

@@ -73,7 +73,7 @@ class goldy_gemm_desc(ctypes.Structure):
 
 
 class goldy_linear_desc(ctypes.Structure):
-    _fields_ = [(n, ctypes.c_int64) for n in ("rows", "in", "out", "ldx", "ldw", "ldy", "ldz", "ldr", "stride_w")] + \
+    _fields_ = [(n, ctypes.c_int64) for n in ("rows", "in", "out", "ldx", "lddx", "ldw", "ldy", "ldz", "ldr", "stride_w")] + \
                [(n, ctypes.c_int32) for n in ("groups", "act", "act_x", "y_dtype", "dx_dtype", "dw_dtype", "bias_dtype",
                                               "reserved")]
 
@@ -529,17 +529,14 @@ def goldy_gemm_noalloc(d: goldy_gemm_desc, variant: int, A: int, B: int, C: int,
 
 def linear_desc(rows: int, fan_in: int, fan_out: int, groups: int = 0, act: int = GOLDY_ACT_NONE,
                 act_x: int = GOLDY_ACT_NONE, y_dtype: int = GOLDY_BF16, dx_dtype: int = GOLDY_BF16,
-                dw_dtype: int = GOLDY_F32, bias_dtype: int = GOLDY_BF16, ldx: Optional[int] = None,
-                ldw: Optional[int] = None, ldy: Optional[int] = None, ldz: int = 0, ldr: int = 0,
-                stride_w: Optional[int] = None) -> goldy_linear_desc:
+                dw_dtype: int = GOLDY_F32, bias_dtype: int = GOLDY_BF16, ldx: int = 0, lddx: int = 0, ldw: int = 0,
+                ldy: int = 0, ldz: int = 0, ldr: int = 0, stride_w: int = 0) -> goldy_linear_desc:
     """Descriptor of a linear layer Y (rows x fan_out) = act(X (rows x fan_in)
     W (fan_in x fan_out) + b) + R, or of `groups` experts over ragged row
-    ranges (default: packed rows, experts' weights back to back)."""
-    ldw = fan_out if ldw is None else ldw
-    return goldy_linear_desc(rows, fan_in, fan_out, fan_in if ldx is None else ldx, ldw,
-                             fan_out if ldy is None else ldy, ldz, ldr,
-                             fan_in * ldw if stride_w is None else stride_w, int(groups), int(act), int(act_x),
-                             int(y_dtype), int(dx_dtype), int(dw_dtype), int(bias_dtype), 0)
+    ranges.  Row strides of 0 stand for dense rows: fp32 rows packed, bf16 rows
+    padded to a multiple of 8 elements."""
+    return goldy_linear_desc(rows, fan_in, fan_out, ldx, lddx, ldw, ldy, ldz, ldr, stride_w, int(groups), int(act),
+                             int(act_x), int(y_dtype), int(dx_dtype), int(dw_dtype), int(bias_dtype), 0)
 
 
 def goldy_linear_query(d: goldy_linear_desc) -> int:

@@ -236,7 +236,7 @@ def run_input_grad(rows, k, n, counts=None, first=0, act="none", residual=False,
     z = matrix(gen, rows, k, scale=1.5) if act != "none" else None
     r = torch.randn(rows, k, generator=gen, device="cuda").to(TORCH[dx_dtype]) if residual else None
     dx = out_matrix(rows, k, dx_dtype, ldx)
-    d = G.linear_desc(rows, k, n, groups=groups, act_x=ACTS[act], dx_dtype=dx_dtype, ldx=dx.stride(0), ldw=w.stride(-2),
+    d = G.linear_desc(rows, k, n, groups=groups, act_x=ACTS[act], dx_dtype=dx_dtype, lddx=dx.stride(0), ldw=w.stride(-2),
                       ldy=dy.stride(0), ldz=z.stride(0) if z is not None else 0, ldr=k if residual else 0)
     ws, off = workspace(d), offsets_of(counts, first)
     G.goldy_linear_input_grad(d, ptr(dy), ptr(w), ptr(dx), z=ptr(z), residual=ptr(r), offsets=ptr(off),
@@ -290,9 +290,7 @@ def run_weight_grad(rows, k, n, counts=None, first=0, dw_dtype=F32, accumulate=F
     if accumulate:
         dw[...] = torch.randn(*lead, k, n, generator=gen, device="cuda").to(TORCH[dw_dtype])
     before = dw.double().clone()
-    stride_w = (k * ldw + 7) // 8 * 8
-    if groups > 1 and stride_w != k * ldw:
-        pytest.skip("packed result needs in * ldw a multiple of 8")
+    stride_w = k * ldw
     d = G.linear_desc(rows, k, n, groups=groups, dw_dtype=dw_dtype, ldx=x.stride(0), ldw=ldw, ldy=dy.stride(0), stride_w=stride_w)
     ws, off = workspace(d), offsets_of(counts, first)
     G.goldy_linear_weight_grad(d, ptr(x), ptr(dy), ptr(dw), accumulate=accumulate, offsets=ptr(off), workspace=ptr(ws),
@@ -330,6 +328,34 @@ def test_weight_grad_large_groups(cuda_ok, size):
     counts = [1, 63, 64, 65, 190, 0, 7, 129, 300]
     run_weight_grad(sum(counts) + 9, size, 2 * size, counts=counts, first=4, dw_dtype=BF16)
     run_weight_grad(sum(counts) + 9, size, 2 * size, counts=counts, first=4, dw_dtype=F32)
+
+
+@pytest.mark.parametrize("rows,k,n,counts", [(50, 75, 130, None), (1, 1001, 77, None), (700, 333, 515, None),
+                                             (300, 131, 259, [100, 0, 37, 163])])
+def test_rows_off_16_byte_boundaries(cuda_ok, rows, k, n, counts):
+    """Packed rows of odd length, products in all directions."""
+    gen = gen_of(k)
+    groups = 0 if counts is None else len(counts)
+    lead = (groups,) if groups else ()
+    packed = lambda *s: torch.randn(*s, generator=gen, device="cuda").bfloat16()  # noqa: E731
+    x, w, dy = packed(rows, k), packed(*lead, k, n) * k ** -0.5, packed(rows, n)
+    # base one element off as well
+    x = torch.cat([x.new_full((1,), NAN), x.flatten()])[1:].view(rows, k)
+    y, dx = out_matrix(rows, n, BF16), out_matrix(rows, k, BF16)
+    dw = out_matrix(k, n, F32, lead=lead)
+    d = G.linear_desc(rows, k, n, groups=groups, ldx=k, lddx=k, ldw=n, ldy=n, dw_dtype=F32)
+    ws, off = workspace(d), offsets_of(counts)
+    kw = dict(offsets=ptr(off), workspace=ptr(ws), workspace_bytes=ws.numel(), stream=torch.cuda.current_stream().cuda_stream)
+    G.goldy_linear_forward(d, ptr(x), ptr(w), ptr(y), **kw)
+    G.goldy_linear_input_grad(d, ptr(dy), ptr(w), ptr(dx), **kw)
+    G.goldy_linear_weight_grad(d, ptr(x), ptr(dy), ptr(dw), **kw)
+    finish(ws)
+    for e, lo, hi in spans(rows, counts):
+        xe, ge, we = x[lo:hi].double(), dy[lo:hi].double(), (w[e] if groups else w).double()
+        for got, a, b, kk, dt in ((y[lo:hi], xe, we, k, BF16), (dx[lo:hi], ge, we.T, n, BF16),
+                                  (dw[e] if groups else dw, xe.T, ge, hi - lo, F32)):
+            ref = a @ b
+            check(got, ref, (steps(kk, dt) + 4) * 2.0 ** -22 * (a.abs() @ b.abs()) + round_tol(ref, dt) * 1.01, f"group {e}")
 
 
 @pytest.mark.parametrize("rows,n,counts,first", [(1, 8, None, 0), (70, 257, None, 0), (1000, 1024, None, 0), (4097, 96, None, 0)] +

@@ -25,7 +25,7 @@ def changed(d, **fields):
 
 @pytest.mark.parametrize("fields", [dict(rows=-1), {"in": -1}, dict(out=-5), dict(rows=1 << 31), dict(ldx=63), dict(ldw=127),
                                     dict(ldy=100), dict(ldz=-1), dict(ldr=-8), dict(groups=-1),
-                                    dict(groups=G.GOLDY_MAX_GROUPS + 1), dict(groups=2, stride_w=8), dict(groups=2, stride_w=64 * 128 + 4),
+                                    dict(groups=G.GOLDY_MAX_GROUPS + 1), dict(groups=2, stride_w=8), dict(stride_w=-8), dict(lddx=63),
                                     dict(act=5), dict(act=-1), dict(act_x=9), dict(reserved=1)])
 def test_linear_descriptor(fields):
     refused(BAD, G.goldy_linear_query, changed(G.linear_desc(32, 64, 128), **fields))
@@ -50,8 +50,10 @@ def test_linear_pointers():
     refused(BAD, G.goldy_linear_forward, d, A, A, A, z=A + 1)
     refused(BAD, G.goldy_linear_forward, changed(G.linear_desc(32, 64, 128), ldz=100), A, A, A, z=A)
     refused(BAD, G.goldy_linear_forward, changed(G.linear_desc(32, 64, 128), ldr=100), A, A, A, residual=A)
-    refused(BAD, G.goldy_linear_forward, G.linear_desc(32, 60, 128), A, A, A)          # rows of X off 16 bytes
-    refused(BAD, G.goldy_linear_forward, G.linear_desc(32, 64, 126), A, A, A)          # rows of W
+    odd = G.linear_desc(32, 60, 128, ldx=60)                     # rows of X off 16 bytes: a copy, so a workspace
+    assert G.goldy_linear_query(odd) >= 65536 + 32 * 64 * 2
+    assert G.goldy_linear_query(G.linear_desc(32, 64, 126, ldw=126)) >= 65536 + 64 * 128 * 2
+    refused(BAD, G.goldy_linear_forward, odd, A + 1, A, A)
     refused(BAD, G.goldy_linear_forward, G.linear_desc(32, 64, 128, groups=2), A, A, A)             # no offsets
     refused(BAD, G.goldy_linear_forward, G.linear_desc(32, 64, 128, groups=2), A, A, A, offsets=A + 2)
     refused(BAD, G.goldy_linear_forward, d, A, A, A, offsets=A)
@@ -63,7 +65,6 @@ def test_gradient_pointers():
     refused(BAD, G.goldy_linear_input_grad, d, A, A, 0)
     refused(BAD, G.goldy_linear_input_grad, d, A, A, A, z=A)                                        # no activation
     refused(BAD, G.goldy_linear_input_grad, G.linear_desc(32, 64, 128, act_x=G.GOLDY_ACT_GELU), A, A, A)
-    refused(BAD, G.goldy_linear_input_grad, G.linear_desc(32, 64, 100, ldw=104), A, A, A)           # rows of dY
     refused(BAD, G.goldy_linear_weight_grad, d, 0, A, A)
     refused(BAD, G.goldy_linear_weight_grad, d, A, 0, A)
     refused(BAD, G.goldy_linear_weight_grad, d, A, A, 0)
