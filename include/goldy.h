@@ -500,8 +500,8 @@ goldy_status goldy_gemm_noalloc(const goldy_gemm_desc* desc, int variant, const 
  * product reads X, W and dY in place where their row strides (and stride_w)
  * are multiples of 8, and they then start on 16-byte boundaries; other strides
  * cost a padded copy in the workspace.  Results, R, Z and biases need their
- * element's alignment only, with faster accesses where base and row stride are
- * multiples of 16 bytes.  in, out and rows are arbitrary, 0 included (an empty
+ * element's alignment only (bf16: faster accesses where base and row stride
+ * are multiples of 4 bytes).  in, out and rows are arbitrary, 0 included (an empty
  * sum is 0).
  *
  * Results must not overlap inputs, except that R may be the result itself

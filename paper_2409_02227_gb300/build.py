@@ -5,7 +5,7 @@ parallel: ``planner.cpp`` (host C++), ``runtime.cu`` (launch manager),
 ``noalloc.cu`` (the entry point with a compiled-in scratch array),
 ``kernels.cu`` once per GO-Kernel kind (``-DGOLDY_KIND=k``), the layer
 operators (``linear.cu``, ``repack.cu``, ``bias_grad.cu``, ``layernorm.cu``) and
-``linear_kernels.cu`` once per pass (``-DGOLDY_LINEAR_PASS=k``).  Objects go to
+``linear_kernels.cu`` once per pass and activation.  Objects go to
 ``_build/`` next to this file and the library to
 ``paper_2409_02227_gb300/libgoldy.so``; both are git-ignored.  A rebuild is
 skipped when the library is newer than every source and header.
@@ -26,7 +26,8 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libgoldy.so")
 NUM_KINDS = 11
-NUM_LINEAR_PASSES = 3
+# (pass, activation) of the linear-layer kernels; the weight gradient has none
+LINEAR_KERNELS = [(k, a) for k in range(2) for a in range(5)] + [(2, 0)]
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
@@ -58,9 +59,9 @@ def _jobs(ptxas_verbose: bool):
     jobs.append(("ewise", cu + ["-c", os.path.join(CSRC, "ewise.cu")]))
     for name in ("linear", "repack", "bias_grad", "layernorm"):
         jobs.append((name, cu + ["-c", os.path.join(CSRC, name + ".cu")]))
-    for k in range(NUM_LINEAR_PASSES):
-        jobs.append((f"linear_kernels_{k}",
-                     cu + [f"-DGOLDY_LINEAR_PASS={k}", "-c", os.path.join(CSRC, "linear_kernels.cu")]))
+    for k, a in LINEAR_KERNELS:
+        jobs.append((f"linear_kernels_p{k}_a{a}", cu + [f"-DGOLDY_LINEAR_PASS={k}", f"-DGOLDY_LINEAR_ACT={a}", "-c",
+                                                        os.path.join(CSRC, "linear_kernels.cu")]))
     for k in range(NUM_KINDS):
         jobs.append((f"kernels_k{k}", cu + [f"-DGOLDY_KIND={k}", "-c", os.path.join(CSRC, "kernels.cu")]))
     return jobs

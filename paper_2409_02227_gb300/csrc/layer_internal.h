@@ -41,14 +41,21 @@ constexpr size_t kLayerCounterBytes = 64 * 1024;
 constexpr int kLinForward = 0;
 constexpr int kLinInputGrad = 1;
 constexpr int kLinWeightGrad = 2;
-constexpr int kLinThreads = 320;          // load warp, MMA warp, 8 epilogue warps
-constexpr int kLinEpiWarps = 8;
+constexpr int kLinEpiWarps = 12;
+constexpr int kLinThreads = (2 + kLinEpiWarps) * 32;   // a load warp, an MMA warp, the epilogue's
 constexpr int kLinStageK = 64;            // reduction elements per pipeline stage
 constexpr int kLinMaxStages = 12;
 constexpr int kLinRowBand = 8;            // row tiles walked before the next column tile
 constexpr int kLinPromote = 8;            // stages accumulated in tensor memory for fp32 results
-constexpr int kLinStagingBytes = kLinEpiWarps * 4096;
 constexpr int kLinSmemBudget = 232448;    // 227 KB
+
+// n / d for 0 <= n < 2^31 as the high half of n * mul, mul = floor(2^64 / d) + 1.
+struct LinDivisor {
+  uint64_t mul;
+  int32_t one;             // d = 1
+  int32_t pad;
+};
+inline LinDivisor lin_divisor(uint32_t d) { return {d > 1 ? ~uint64_t(0) / d + 1 : 0, d == 1, 0}; }
 
 struct LinearParams {
   CUtensorMap ta;          // operand along c (weights, or dY of the weight gradient)
@@ -63,13 +70,13 @@ struct LinearParams {
   int32_t tile_r;          // rows of C per tile, at most
   int32_t tiles_c;         // column tiles
   int32_t split;           // reduction split over this many units
+  LinDivisor div_split, div_band;   // by split; by kLinRowBand * tiles_c
   int32_t stages;
   int32_t stage_bytes;
   int32_t part_box;        // rows per box of tb_part
-  int32_t part_chunks;     // 32-row chunks per epilogue warp in a partial
-  int32_t act;
+  int32_t part_chunks;     // 8-row chunks per epilogue warp in a partial
   int32_t bias_f32;
-  int32_t vec;             // results, residual and Z allow 16-byte accesses
+  int32_t vec;             // bf16 results, residual and Z allow 4-byte accesses
   int32_t loads;           // 0: empty reduction, no tensor maps
   void* c;
   int64_t ldc, c_group;    // row stride and group stride of C (group stride: weight gradient)
@@ -84,9 +91,6 @@ struct LinearParams {
   int* err;
 };
 static_assert(sizeof(LinearParams) <= 4096, "kernel parameter block");
-
-// Host stub of the kernel for a pass; pair: CTA-pair tiles of 256 columns, else 128.
-const void* linear_kernel_fn(int pass, int pair, int out_f32);
 
 // ---- bias gradient and layer norm -------------------------------------------
 struct BiasGradParams {

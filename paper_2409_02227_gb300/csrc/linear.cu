@@ -15,19 +15,28 @@
 
 namespace goldy {
 
-const void* linear_kernel_forward(int pair, int out_f32);
-const void* linear_kernel_input_grad(int pair, int out_f32);
-const void* linear_kernel_weight_grad(int pair, int out_f32);
-
-const void* linear_kernel_fn(int pass, int pair, int out_f32) {
-  switch (pass) {
-    case kLinForward: return linear_kernel_forward(pair, out_f32);
-    case kLinInputGrad: return linear_kernel_input_grad(pair, out_f32);
-    default: return linear_kernel_weight_grad(pair, out_f32);
-  }
-}
+// linear_kernels.cu, compiled once per pass and activation
+const void* linear_kernel_p0_a0(int pair, int out_f32);
+const void* linear_kernel_p0_a1(int pair, int out_f32);
+const void* linear_kernel_p0_a2(int pair, int out_f32);
+const void* linear_kernel_p0_a3(int pair, int out_f32);
+const void* linear_kernel_p0_a4(int pair, int out_f32);
+const void* linear_kernel_p1_a0(int pair, int out_f32);
+const void* linear_kernel_p1_a1(int pair, int out_f32);
+const void* linear_kernel_p1_a2(int pair, int out_f32);
+const void* linear_kernel_p1_a3(int pair, int out_f32);
+const void* linear_kernel_p1_a4(int pair, int out_f32);
+const void* linear_kernel_p2_a0(int pair, int out_f32);
 
 namespace {
+
+const void* linear_kernel_fn(int pass, int act, int pair, int out_f32) {
+  typedef const void* (*Pick)(int, int);
+  static const Pick picks[2][5] = {
+      {linear_kernel_p0_a0, linear_kernel_p0_a1, linear_kernel_p0_a2, linear_kernel_p0_a3, linear_kernel_p0_a4},
+      {linear_kernel_p1_a0, linear_kernel_p1_a1, linear_kernel_p1_a2, linear_kernel_p1_a3, linear_kernel_p1_a4}};
+  return (pass == kLinWeightGrad ? linear_kernel_p2_a0 : picks[pass][act])(pair, out_f32);
+}
 
 constexpr int64_t kMaxDim = (int64_t(1) << 31) - 1024;   // TMA coordinates are 32-bit
 constexpr int kModelSms = 152;                           // SMs the choice is made for
@@ -61,7 +70,7 @@ struct LinChoice {
   size_t part_bytes;       // workspace behind the counters
 };
 
-int part_chunks(int tile_r) { return int(ceil_div(ceil_div(tile_r, 32), 2)); }
+int part_chunks(int tile_r) { return int(ceil_div(ceil_div(tile_r, 8), kLinEpiWarps / 4)); }
 
 // Time model in SM cycles: a 64-deep stage of an nw-row tile costs the larger
 // of its tensor time (2 nw) and of its operand bytes at kLoadRate per SM; a
@@ -111,7 +120,7 @@ LinChoice choose(const LinShape& s) {
     }
   }
   best.part_bytes = best.split > 1 ? size_t(best.max_tiles) * best.split * (best.pair ? 2 : 1) * kLinEpiWarps *
-                                         part_chunks(best.tile_r) * 4096
+                                         part_chunks(best.tile_r) * 1024
                                    : 0;
   return best;
 }
@@ -172,11 +181,11 @@ goldy_status encode(const LayerContext& ctx, CUtensorMap* m, const Operand& o, i
   return GOLDY_OK;
 }
 
-goldy_status set_smem(const LayerContext& ctx, const void* fn, int pass, int pair, int f32) {
+goldy_status set_smem(const LayerContext& ctx, const void* fn, int pass, int act, int pair, int f32) {
   static std::mutex mu;
-  static bool done[kMaxDevices][3][2][2] = {};
+  static bool done[kMaxDevices][3][5][2][2] = {};
   std::lock_guard<std::mutex> lock(mu);
-  bool& d = done[ctx.device][pass][pair][f32];
+  bool& d = done[ctx.device][pass][act][pair][f32];
   if (!d) {
     const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kLinSmemBudget);
     if (e != cudaSuccess) return fail(GOLDY_ERR_CUDA, std::string("cudaFuncSetAttribute: ") + cudaGetErrorString(e));
@@ -189,6 +198,7 @@ struct LinCall {
   LinShape s;
   Operand o[2];            // along c: W, or dY; along r: X, dY, or X
   LinearParams prm;        // epilogue fields filled in by the entry point
+  int act;                 // of the result, or whose slope the result is multiplied by
   void* workspace;
   size_t workspace_bytes;
   void* stream;
@@ -233,12 +243,14 @@ goldy_status launch_linear(const LayerContext& ctx, void* arg) {
   p.tile_r = c.tile_r;
   p.tiles_c = int32_t(ceil_div(s.size_c, 128 * ctas));
   p.split = c.split;
+  p.div_split = lin_divisor(unsigned(c.split));
+  p.div_band = lin_divisor(unsigned(kLinRowBand) * unsigned(p.tiles_c));
   p.part_box = std::min(32, c.tile_r / ctas);
   p.part_chunks = part_chunks(c.tile_r);
   p.loads = s.red > 0 ? 1 : 0;
   const int b_rows = wgrad ? int(ceil_div(c.tile_r / ctas, 64)) * 64 : c.tile_r / ctas;
   p.stage_bytes = 128 * kLinStageK * 2 + b_rows * kLinStageK * 2;
-  const int fixed = 1024 + kLinStagingBytes + 1024;
+  const int fixed = 2048;      // alignment of the tiles; barriers
   p.stages = std::min<int>(kLinMaxStages, (kLinSmemBudget - fixed) / p.stage_bytes);
   p.err = ctx.err_word;
   if (p.loads) {
@@ -249,8 +261,8 @@ goldy_status launch_linear(const LayerContext& ctx, void* arg) {
     if (st != GOLDY_OK) return st;
   }
   const int f32 = s.out_dtype == GOLDY_F32 ? 1 : 0;
-  const void* fn = linear_kernel_fn(s.pass, c.pair, f32);
-  goldy_status st = set_smem(ctx, fn, s.pass, c.pair, f32);
+  const void* fn = linear_kernel_fn(s.pass, call.act, c.pair, f32);
+  goldy_status st = set_smem(ctx, fn, s.pass, call.act, c.pair, f32);
   if (st != GOLDY_OK) return st;
   const int64_t units = c.max_tiles * c.split;
   const int64_t workers = std::max<int64_t>(1, std::min<int64_t>(units, ctx.sm_count / ctas));
@@ -288,7 +300,7 @@ goldy_status set_result(LinearParams& p, const LinShape& s, void* C, int64_t ldc
   p.ldc = ldc;
   p.res = R;
   p.ldr = ldr;
-  p.vec = aligned(C, 16) && (size_t(ldc) * es) % 16 == 0 && (!R || (aligned(R, 16) && (size_t(ldr) * es) % 16 == 0));
+  p.vec = aligned(C, 4) && ldc % 2 == 0 && (!R || (aligned(R, 4) && ldr % 2 == 0));
   return GOLDY_OK;
 }
 
@@ -296,7 +308,7 @@ goldy_status set_saved(LinearParams& p, const LinShape& s, const void* Z, int64_
   ldz = stride_or_dense(ldz, s.size_c, GOLDY_BF16);
   if (!aligned(Z, 2) || ldz < s.size_c) return bad("linear layer: Z misaligned or its row stride too small");
   p.ldz = ldz;
-  p.vec = p.vec && aligned(Z, 16) && ldz % 8 == 0;
+  p.vec = p.vec && aligned(Z, 4) && ldz % 2 == 0;
   return GOLDY_OK;
 }
 
@@ -373,7 +385,7 @@ extern "C" goldy_status goldy_linear_forward(const goldy_linear_desc* desc, cons
   p.z_out = Z;
   p.bias = bias;
   p.bias_f32 = desc->bias_dtype == GOLDY_F32;
-  p.act = desc->act;
+  call.act = desc->act;
   p.offsets = offsets;
   call.workspace = workspace;
   call.workspace_bytes = workspace_bytes;
@@ -404,7 +416,7 @@ extern "C" goldy_status goldy_linear_input_grad(const goldy_linear_desc* desc, c
   if (st == GOLDY_OK && Z) st = set_saved(p, call.s, Z, desc->ldz);
   if (st != GOLDY_OK) return st;
   p.z_in = Z;
-  p.act = desc->act_x;
+  call.act = desc->act_x;
   p.offsets = offsets;
   call.workspace = workspace;
   call.workspace_bytes = workspace_bytes;
@@ -434,7 +446,7 @@ extern "C" goldy_status goldy_linear_weight_grad(const goldy_linear_desc* desc, 
   st = set_result(p, call.s, dW, ldw, accumulate ? dW : nullptr, ldw, "dW");
   if (st != GOLDY_OK) return st;
   p.c_group = p.r_group = desc->groups > 1 ? weight_stride(*desc, ldw) : 0;
-  p.vec = p.vec && (size_t(p.c_group) * type_bytes(desc->dw_dtype)) % 16 == 0;
+  p.vec = p.vec && p.c_group % 2 == 0;
   p.offsets = offsets;
   call.workspace = workspace;
   call.workspace_bytes = workspace_bytes;

@@ -24,12 +24,10 @@
 // in split order (workspace), so results do not depend on the order of
 // arrival.
 //
-// Roles (320 threads): warp 0 loads by TMA, warp 1 issues the MMAs, warps 2-9
-// drain the accumulator (double buffered in tensor memory): each takes every
-// second 32-row chunk of its 32 lanes through a 4 KB transposing buffer, so
-// that global accesses run along c (64-byte bf16 or 128-byte fp32 segments)
-// and bias, activation, its gradient, residual and the saved pre-activation
-// cost no further pass over C.
+// Roles: warp 0 loads by TMA, warp 1 issues the MMAs, the other warps drain
+// the accumulator (double buffered in tensor memory) straight from registers
+// to C, and bias, activation, its gradient, residual and the saved
+// pre-activation cost no further pass over C.
 //
 // OUT_F32: the tensor cores add into fp32 accumulators with truncation, a
 // relative error of about 1e-9 per reduction element (4.4e-6 at 4096,
@@ -49,12 +47,46 @@
 
 namespace goldy {
 
-// Arrive on an mbarrier of a CTA of the cluster and add `bytes` to what its
-// phase waits for.
-__device__ __forceinline__ void mbar_arrive_expect_tx_remote(uint32_t cluster_addr, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.release.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(cluster_addr),
-               "r"(bytes)
-               : "memory");
+// Arrive on an mbarrier of a CTA of the cluster, ordering no memory but this
+// CTA's: all a drained accumulator needs (tcgen05 fences order the reads of
+// tensor memory).  A release at cluster scope would wait for the warp's stores
+// to C, about a microsecond per tile.
+__device__ __forceinline__ void lin_arrive_remote(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+
+// True in one lane of a converged warp, always the same one.  The copies, MMAs
+// and commits stand under this predicate, not under lane == 0: they take their
+// operands from registers shared by the warp, and only here does the compiler
+// know that one lane runs them.  Under lane == 0 each one became a loop over
+// the lanes, some 70 cycles apiece, and no tile, however narrow, took less than
+// 290 ns per 64-deep stage.
+__device__ __forceinline__ bool lin_elect() {
+  uint32_t one;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+  return one != 0;
+}
+
+// Bounded wait for the phase with parity `parity`, false if it gave up (the
+// limit, or another role's abort flag).  The timer is read at every 64th poll.
+// (Arrivals over tensor memory are ordered by the tcgen05 fences; CLUSTER adds
+// acquire at cluster scope for the peer's shared memory.)
+template <bool CLUSTER = false>
+__device__ __forceinline__ bool lin_wait(uint32_t bar, uint32_t parity, const volatile int* abort_flag) {
+  uint64_t t0 = 0;
+  for (uint32_t n = 1;; ++n) {
+    if (CLUSTER ? ptx::mbar_try_wait_acq_cluster(bar, parity) : ptx::mbar_try_wait(bar, parity)) return true;
+    if ((n & 63) != 0) continue;
+    if (abort_flag != nullptr && *abort_flag) return false;
+    const uint64_t now = ptx::global_timer();
+    if (t0 == 0) t0 = now;
+    else if (now - t0 > ptx::kWaitLimitNs) return false;
+  }
+}
+// The same for a whole warp, with one answer for all lanes.
+template <bool CLUSTER = false>
+__device__ __forceinline__ bool lin_wait_warp(uint32_t bar, uint32_t parity, const volatile int* abort_flag) {
+  return __all_sync(0xFFFFFFFFu, lin_wait<CLUSTER>(bar, parity, abort_flag));
 }
 
 // One unit of work: a tile of C, or one split of its reduction.
@@ -69,37 +101,56 @@ struct LinUnit {
   int tile, s;     // index of the tile over all groups, split
 };
 
+__device__ __forceinline__ int lin_div(int n, const LinDivisor& d) {
+  return d.one ? n : int(__umul64hi(uint64_t(unsigned(n)), d.mul));
+}
+
 // Walks the units of a launch in increasing order.  All lanes of a warp call
 // it together; groups are looked up 32 at a time (offsets clamped to
 // [0, rows] and taken as non-decreasing, so that no offsets make a launch
-// leave its buffers).
+// leave its buffers).  Every warp of every role walks, so a step within a
+// group has no division.
 template <int PASS, bool PAIR>
 struct LinWalk {
   static constexpr int G = PAIR ? 32 : 16;     // granularity of N
   const LinearParams& p;
   const int lane;
-  int e0 = 0, begin = 0, prev = 0;             // window of 32 groups: first, units before it, row before it
-  int start = 0, cnt = 0, incl = 0;            // this lane's group: first row, rows, units up to its end
-  bool loaded = false;
+  // the current group: its units, rows, tile height, row tiles, and 2^32 over
+  // the tiles of its last band
+  int e = 0, first = 0, end = 0, start = 0, rows = 0, w = 0, n_r = 0;
+  unsigned last_inv = 0;
+  // forward and input gradient: a window of 32 groups, one per lane
+  int e0 = 0, begin = 0, prev = 0;             // its first group, units and rows before it
+  int my_start = 0, my_rows = 0, my_end = 0;   // this lane's group: first row, rows, end of its units
 
-  __device__ LinWalk(const LinearParams& params, int lane_id) : p(params), lane(lane_id) {}
+  __device__ LinWalk(const LinearParams& params, int lane_id) : p(params), lane(lane_id) {
+    if (PASS == kLinWeightGrad || !p.offsets) {
+      rows = PASS == kLinWeightGrad ? p.size_r : p.rows;
+      end = set_group();
+    } else {
+      load_window();
+    }
+  }
 
   __device__ static int width(int rows, int tile_r) {
     if (rows <= 0) return G;
-    const int n = (rows + tile_r - 1) / tile_r;      // equal tiles
-    return ((rows + n - 1) / n + G - 1) / G * G;
+    const int n = int((unsigned(rows) + tile_r - 1) / unsigned(tile_r));      // equal tiles
+    return int((unsigned(rows) + n - 1) / unsigned(n) + G - 1) / G * G;
   }
-  __device__ int group_units(int rows) const {
-    if (rows <= 0) return 0;
-    const int w = width(rows, p.tile_r);
-    return (rows + w - 1) / w * p.tiles_c * p.split;
+  // tile height and count of the current group from its rows; returns its units
+  __device__ int set_group() {
+    w = width(rows, p.tile_r);
+    n_r = int((unsigned(rows) + w - 1) / unsigned(w));
+    const int rest = n_r % kLinRowBand;
+    last_inv = rest > 1 ? 0xFFFFFFFFu / unsigned(rest) + 1u : 0u;
+    return n_r * p.tiles_c * p.split;
   }
   __device__ void load_window() {
-    const int e = e0 + lane;
+    const int g = e0 + lane;
     int o = 0, o1 = 0;
-    if (e < p.groups) {
-      o = min(max(__ldg(p.offsets + e), 0), p.rows);
-      o1 = min(max(__ldg(p.offsets + e + 1), 0), p.rows);
+    if (g < p.groups) {
+      o = min(max(__ldg(p.offsets + g), 0), p.rows);
+      o1 = min(max(__ldg(p.offsets + g + 1), 0), p.rows);
     }
     int m = max(o, prev);
 #pragma unroll
@@ -107,282 +158,247 @@ struct LinWalk {
       const int t = __shfl_up_sync(0xFFFFFFFFu, m, d);
       if (lane >= d) m = max(m, t);
     }
-    start = m;
-    cnt = e < p.groups ? max(o1 - m, 0) : 0;
-    int u = group_units(cnt);
+    my_start = m;
+    my_rows = g < p.groups ? max(o1 - m, 0) : 0;
+    const int mw = width(my_rows, p.tile_r);
+    int u = int((unsigned(my_rows) + mw - 1) / unsigned(mw)) * p.tiles_c * p.split;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
       const int t = __shfl_up_sync(0xFFFFFFFFu, u, d);
       if (lane >= d) u += t;
     }
-    incl = begin + u;
-    loaded = true;
+    my_end = begin + u;
   }
 
   // Unit u (not below the last one asked for); false past the end.
-  __device__ bool find(int u, LinUnit& t) {
-    int rows, local;
+  __device__ __forceinline__ bool find(int u, LinUnit& t) {
     if (PASS == kLinWeightGrad) {
-      const int per = group_units(p.size_r);
-      t.e = u / per;
-      if (t.e >= p.groups) return false;
-      local = u - t.e * per;
-      rows = p.size_r;
+      while (u >= end) {
+        if (++e >= p.groups) return false;
+        const int units = end - first;
+        first = end;
+        end += units;
+      }
       int a = 0, b = p.rows;
       if (p.offsets) {
-        a = min(max(__ldg(p.offsets + t.e), 0), p.rows);
-        b = min(max(__ldg(p.offsets + t.e + 1), a), p.rows);
+        a = min(max(__ldg(p.offsets + e), 0), p.rows);
+        b = min(max(__ldg(p.offsets + e + 1), a), p.rows);
       }
       t.k0 = a;
-      t.red = max(b - a, 0);
-      t.r0 = 0;
+      t.red = b - a;
     } else {
-      if (p.offsets) {
-        if (!loaded) load_window();
+      if (u >= end) {
+        if (!p.offsets) return false;
         int last;
-        while (u >= (last = __shfl_sync(0xFFFFFFFFu, incl, 31))) {
+        while (u >= (last = __shfl_sync(0xFFFFFFFFu, my_end, 31))) {
           if (e0 + 32 >= p.groups) return false;
-          prev = __shfl_sync(0xFFFFFFFFu, start + cnt, 31);
+          prev = __shfl_sync(0xFFFFFFFFu, my_start + my_rows, 31);
           begin = last;
           e0 += 32;
           load_window();
         }
-        const int j = __ffs(__ballot_sync(0xFFFFFFFFu, u < incl)) - 1;
-        rows = __shfl_sync(0xFFFFFFFFu, cnt, j);
-        t.r0 = __shfl_sync(0xFFFFFFFFu, start, j);
-        local = u - (__shfl_sync(0xFFFFFFFFu, incl, j) - group_units(rows));
-        t.e = e0 + j;
-      } else {
-        rows = p.rows;
-        t.r0 = 0;
-        t.e = 0;
-        local = u;
-        if (u >= group_units(rows)) return false;
+        const int j = __ffs(__ballot_sync(0xFFFFFFFFu, u < my_end)) - 1;
+        e = e0 + j;
+        start = __shfl_sync(0xFFFFFFFFu, my_start, j);
+        rows = __shfl_sync(0xFFFFFFFFu, my_rows, j);
+        end = __shfl_sync(0xFFFFFFFFu, my_end, j);
+        first = end - set_group();
       }
       t.k0 = 0;
       t.red = p.red;
     }
-    t.tile = u / p.split;
-    const int w = width(rows, p.tile_r);
-    const int n_r = (rows + w - 1) / w;
-    const int i = local / p.split;
+    t.e = e;
+    const int local = u - first;
+    const int i = lin_div(local, p.div_split);
     t.s = local - i * p.split;
-    const int band = i / (kLinRowBand * p.tiles_c);
+    t.tile = lin_div(u, p.div_split);
+    const int band = lin_div(i, p.div_band);
     const int rem = i - band * kLinRowBand * p.tiles_c;
     const int in_band = min(kLinRowBand, n_r - band * kLinRowBand);
-    const int tc = rem / in_band;
+    const int tc = in_band == kLinRowBand ? rem / kLinRowBand : in_band == 1 ? rem : int(__umulhi(unsigned(rem), last_inv));
     const int tr = band * kLinRowBand + rem - tc * in_band;
-    t.r0 += tr * w;
+    t.r0 = start + tr * w;
     t.w = min(w, rows - tr * w);
     t.nw = (t.w + G - 1) / G * G;
     t.c0 = tc * (PAIR ? 256 : 128);
     const int kbs = (t.red + kLinStageK - 1) / kLinStageK;
-    t.kb0 = int(int64_t(kbs) * t.s / p.split);
-    t.kb1 = int(int64_t(kbs) * (t.s + 1) / p.split);
+    t.kb0 = lin_div(kbs * t.s, p.div_split);
+    t.kb1 = lin_div(kbs * (t.s + 1), p.div_split);
     return true;
   }
 };
 
-// A 32 x 32 fp32 block in shared memory, 128 bytes per row of C, 16-byte
-// pieces permuted by row so that neither the column-wise writes nor the
-// row-wise reads collide in a bank.
-__device__ __forceinline__ uint32_t lin_stage_addr(uint32_t base, int row, int piece) {
-  return base + uint32_t(row * 128 + ((piece ^ (row & 7)) << 4));
+// 8 accumulator columns of this warp's 32 lanes: tensor memory -> registers,
+// and back.
+__device__ __forceinline__ void lin_tmem_load(uint32_t taddr, uint32_t (&r)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr)
+               : "memory");
+}
+__device__ __forceinline__ void lin_tmem_store(uint32_t taddr, const float (&v)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "f"(v[0]),
+               "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
+               : "memory");
+}
+__device__ __forceinline__ void lin_tmem_store_wait() {
+  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
 
-// Bounded wait of a whole warp, with one answer for all lanes.
-__device__ __forceinline__ bool lin_wait(uint32_t bar, uint32_t parity, const volatile int* abort_flag) {
-  return __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar, parity, abort_flag));
-}
-__device__ __forceinline__ bool lin_wait_cluster(uint32_t bar, uint32_t parity, const volatile int* abort_flag) {
-  return __all_sync(0xFFFFFFFFu, ptx::mbar_wait_cluster(bar, parity, abort_flag));
-}
-
-// What a warp adds to 8 consecutive columns; loaded once per unit.
-struct LinBias {
-  float v[8];
-};
-
-template <int PASS>
-__device__ __forceinline__ void lin_load_bias(const LinearParams& p, int e, int col, LinBias& b) {
-#pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    b.v[k] = 0.0f;
-    if (PASS == kLinForward && p.bias && col + k < p.size_c) {
-      const int64_t i = int64_t(e) * p.size_c + col + k;
-      b.v[k] = p.bias_f32 ? static_cast<const float*>(p.bias)[i] : load_bf16(p.bias, i);
-    }
-  }
+// Transposes the 2 x 2 block of bf16 values that an even lane and the odd lane
+// next to it hold: (rows j, j + 1 of one column) <-> (two columns of one row,
+// the even lane's row j, the odd lane's row j + 1).
+__device__ __forceinline__ uint32_t lin_trade(uint32_t x, int odd) {
+  const uint32_t y = __shfl_xor_sync(0xFFFFFFFFu, x, 1);
+  return __byte_perm(x, y, odd ? 0x3276 : 0x5410);
 }
 
-// Epilogue of one 32-row chunk: v[j] is row j of this lane's column.  After
-// the transposition a lane has 8 consecutive columns of 4 rows, 8 apart.  What
-// the rows need from memory (saved pre-activation, residual) is asked for
-// first, all 4 rows at once, so that its latency is paid once per chunk.
-__device__ __forceinline__ void lin_transpose(uint32_t buf, int lane, const float (&v)[32]) {
-  __syncwarp();
-#pragma unroll
-  for (int j = 0; j < 32; ++j) {
-    const uint32_t a = lin_stage_addr(buf, j, lane >> 2) + uint32_t((lane & 3) * 4);
-    asm volatile("st.shared.f32 [%0], %1;" ::"r"(a), "f"(v[j]) : "memory");
-  }
-  __syncwarp();
-}
-__device__ __forceinline__ void lin_transposed(uint32_t buf, int lane, int row, const LinBias& bias, float (&f)[8]) {
-  const float4 a = ptx::ld_shared_v4(lin_stage_addr(buf, row, (lane & 3) * 2));
-  const float4 b = ptx::ld_shared_v4(lin_stage_addr(buf, row, (lane & 3) * 2 + 1));
-  f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
-#pragma unroll
-  for (int k = 0; k < 8; ++k) f[k] += bias.v[k];
-}
+// Drains this warp's part of a tile: 32 columns, one per lane, in chunks of 8
+// rows (chunks side, side + SIDES, ...).  The arithmetic is per column; bf16
+// values meet memory two columns at a time (PAIRS: rows on 4-byte boundaries
+// and 32 whole columns), so that an access covers two 64-byte row segments;
+// fp32 rows are 128-byte segments as they are.  The next chunk's accumulator
+// columns, saved pre-activations and residuals are on their way while a chunk
+// is finished.  The loop body is kept short: unrolled over 32 rows, the same
+// work waited for instructions (5.5 us a tile instead of 2).
+constexpr int kLinSides = kLinEpiWarps / 4;
 
-// Whole 16-byte accesses: every tensor of the epilogue on 16-byte boundaries,
-// 32 whole columns.  bf16 results.
-template <int PASS, int ACT>
-__device__ __forceinline__ void lin_finish_fast(const LinearParams& p, const LinUnit& t, uint32_t buf, int lane,
-                                                int row0, int col, const LinBias& bias, const float (&v)[32]) {
-  const int sub = lane >> 2;
-  const int64_t r0 = int64_t(t.r0) + row0 + sub;
-  const int left = t.w - row0 - sub;               // row i * 8 of this lane exists if i * 8 < left
-  const int64_t c_at = int64_t(t.e) * p.c_group + r0 * p.ldc + col;
-  const int64_t q_at = int64_t(t.e) * p.r_group + r0 * p.ldr + col;
+template <int PASS, bool OUT_F32, int ACT, bool PAIRS, typename Release>
+__device__ __forceinline__ void lin_drain(const LinearParams& p, const LinUnit& t, int lane, int side, int col0,
+                                          float bias, bool some, uint32_t cols, const float* part,
+                                          size_t split_stride, Release release) {
   constexpr bool SLOPE = PASS == kLinInputGrad && ACT != GOLDY_ACT_NONE;
-  uint4 z[4], q[4];
-  if (SLOPE) {
-    const uint16_t* from = static_cast<const uint16_t*>(p.z_in) + r0 * p.ldz + col;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (i * 8 < left) z[i] = __ldg(reinterpret_cast<const uint4*>(from + i * 8 * p.ldz));
-  }
-  if (p.res) {
-    const uint16_t* from = static_cast<const uint16_t*>(p.res) + q_at;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (i * 8 < left) q[i] = *reinterpret_cast<const uint4*>(from + i * 8 * p.ldr);
-  }
-  lin_transpose(buf, lane, v);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (i * 8 >= left) break;
-    float f[8];
-    lin_transposed(buf, lane, i * 8 + sub, bias, f);
-    if (PASS == kLinForward && p.z_out)
-      *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.z_out) + (r0 + i * 8) * p.ldz + col) = pack8(f);
+  constexpr int N = PAIRS ? 4 : 8;                 // accesses per chunk and array
+  constexpr int DOWN = PAIRS ? 2 : 1;              // rows between them
+  const int odd = PAIRS ? (lane & 1) : 0;
+  const int col = col0 + lane - odd;
+  const bool in = col < p.size_c;
+  const int chunks = (t.w + 7) / 8;
+  const int64_t r = int64_t(t.r0) + side * 8 + odd;
+  const bool res = p.res != nullptr;
+  const bool save = PASS == kLinForward && p.z_out != nullptr;
+  const int64_t es = OUT_F32 ? 4 : 2;
+  char* c = static_cast<char*>(p.c) + (int64_t(t.e) * p.c_group + r * p.ldc + col) * es;
+  const char* q_at = static_cast<const char*>(p.res) + (int64_t(t.e) * p.r_group + r * p.ldr + col) * es;
+  const char* z_at = static_cast<const char*>(p.z_in) + (r * p.ldz + col) * 2;
+  char* z_to = static_cast<char*>(p.z_out) + (r * p.ldz + col) * 2;
+  const int64_t c_step = DOWN * p.ldc * es, q_step = DOWN * p.ldr * es, z_step = DOWN * p.ldz * 2;
+
+  uint32_t zn[N], qn[N], an[8];
+  auto fetch = [&](int chunk) {                    // what the chunk needs from memory
+    const int left = t.w - chunk * 8 - odd;
     if (SLOPE) {
-      float zf[8];
-      unpack8(z[i], zf);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) f[k] *= act_slope(zf[k], ACT);
+      for (int i = 0; i < N; ++i, z_at += z_step)
+        if (in && DOWN * i < left)
+          zn[i] = PAIRS ? __ldg(reinterpret_cast<const uint32_t*>(z_at)) : uint32_t(*reinterpret_cast<const uint16_t*>(z_at));
+      z_at += (kLinSides - 1) * N * z_step;
+    }
+    if (res) {
+#pragma unroll
+      for (int i = 0; i < N; ++i, q_at += q_step)
+        if (in && DOWN * i < left)
+          qn[i] = PAIRS || OUT_F32 ? *reinterpret_cast<const uint32_t*>(q_at)
+                                   : uint32_t(*reinterpret_cast<const uint16_t*>(q_at));
+      q_at += (kLinSides - 1) * N * q_step;
+    }
+  };
+  if (side < chunks) {
+    fetch(side);
+    if (some) lin_tmem_load(cols + uint32_t(side * 8), an);
+  }
+#pragma unroll 1
+  for (int chunk = side; chunk < chunks; chunk += kLinSides) {
+    const int left = t.w - chunk * 8 - odd;
+    float v[8];
+    uint32_t z[N], q[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      z[i] = SLOPE ? zn[i] : 0u;
+      q[i] = qn[i];
+    }
+    if (some) {
+      ptx::tmem_ld_wait();
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(an[j]) + bias;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = bias;
+      if (part) {                                  // the splits' partials, in order
+        const float* from = part + (chunk / kLinSides) * 256 + lane;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+#pragma unroll 4
+        for (int s = 0; s < p.split; ++s) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] += __ldcg(from + s * split_stride + j * 32);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += bias;
+      }
+    }
+    if (chunk + kLinSides < chunks) {
+      if (some) lin_tmem_load(cols + uint32_t((chunk + kLinSides) * 8), an);
+      fetch(chunk + kLinSides);
+    } else if (some) {
+      release();                                   // the accumulator's last chunk is in registers
+    }
+    if (save) {
+#pragma unroll
+      for (int i = 0; i < N; ++i, z_to += z_step) {
+        if (PAIRS) {
+          const uint32_t w = lin_trade(pack_bf16(v[2 * i], v[2 * i + 1]), odd);
+          if (2 * i < left) *reinterpret_cast<uint32_t*>(z_to) = w;
+        } else if (in && i < left) {
+          store_bf16(z_to, 0, v[i]);
+        }
+      }
+      z_to += (kLinSides - 1) * N * z_step;
+    }
+    if (SLOPE) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        if (PAIRS) {
+          const uint32_t w = lin_trade(z[i], odd);
+          v[2 * i] *= act_slope(bf16_lo(w), ACT);
+          v[2 * i + 1] *= act_slope(bf16_hi(w), ACT);
+        } else {
+          v[i] *= act_slope(bf16_lo(z[i]), ACT);
+        }
+      }
     } else if (PASS == kLinForward) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) f[k] = act_value(f[k], ACT);
+      for (int j = 0; j < 8; ++j) v[j] = act_value(v[j], ACT);
     }
-    if (p.res) {
-      float qf[8];
-      unpack8(q[i], qf);
+    if (res) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) f[k] += qf[k];
-    }
-    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.c) + c_at + i * 8 * p.ldc) = pack8(f);
-  }
-}
-
-// The same for fp32 results, rolled up: the sums of the chunks still to come
-// occupy the registers.
-template <int PASS>
-__device__ __forceinline__ void lin_finish_f32(const LinearParams& p, const LinUnit& t, uint32_t buf, int lane,
-                                               int row0, int col, const LinBias& bias) {
-  const int sub = lane >> 2;
-#pragma unroll 1
-  for (int i = 0; i < 4; ++i) {
-    const int row = i * 8 + sub;
-    if (row0 + row >= t.w) break;
-    const int64_t r = int64_t(t.r0) + row0 + row;
-    float4 q0 = make_float4(0.0f, 0.0f, 0.0f, 0.0f), q1 = q0;
-    if (PASS != kLinWeightGrad && p.res) {
-      const float* from = static_cast<const float*>(p.res) + r * p.ldr + col;
-      q0 = *reinterpret_cast<const float4*>(from);
-      q1 = *reinterpret_cast<const float4*>(from + 4);
-    }
-    float f[8];
-    lin_transposed(buf, lane, row, bias, f);
-    if (PASS == kLinForward) {
-      if (p.z_out) *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.z_out) + r * p.ldz + col) = pack8(f);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) f[k] = act_value(f[k], p.act);
-    }
-    if (PASS == kLinInputGrad && p.z_in) {
-      float zf[8];
-      unpack8(__ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.z_in) + r * p.ldz + col)), zf);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) f[k] *= act_slope(zf[k], p.act);
-    }
-    float* c = static_cast<float*>(p.c) + int64_t(t.e) * p.c_group + r * p.ldc + col;
-    *reinterpret_cast<float4*>(c) = make_float4(f[0] + q0.x, f[1] + q0.y, f[2] + q0.z, f[3] + q0.w);
-    *reinterpret_cast<float4*>(c + 4) = make_float4(f[4] + q1.x, f[5] + q1.y, f[6] + q1.z, f[7] + q1.w);
-  }
-}
-
-// Any alignment and the columns at C's edge, element by element.
-template <int PASS, bool OUT_F32>
-__device__ __noinline__ void lin_finish_slow(const LinearParams& p, int e, int first_row, int rows, uint32_t buf,
-                                             int lane, int col) {
-  const int sub = lane >> 2;
-  const int n_col = min(8, p.size_c - col);
-  LinBias bias;
-  lin_load_bias<PASS>(p, e, col, bias);
-#pragma unroll 1
-  for (int i = 0; i < 4; ++i) {
-    const int row = i * 8 + sub;
-    if (row >= rows) break;
-    const int64_t r = int64_t(first_row) + row;
-    float f[8];
-    lin_transposed(buf, lane, row, bias, f);
-    const int64_t c_at = int64_t(e) * p.c_group + r * p.ldc + col;
-    const int64_t q_at = int64_t(e) * p.r_group + r * p.ldr + col;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      if (k >= n_col) break;
-      float v = f[k];
-      if (PASS == kLinForward) {
-        if (p.z_out) store_bf16(p.z_out, r * p.ldz + col + k, v);
-        v = act_value(v, p.act);
-      } else if (PASS == kLinInputGrad && p.z_in) {
-        v *= act_slope(load_bf16(p.z_in, r * p.ldz + col + k), p.act);
+      for (int i = 0; i < N; ++i) {
+        if (PAIRS) {
+          const uint32_t w = lin_trade(q[i], odd);
+          v[2 * i] += bf16_lo(w);
+          v[2 * i + 1] += bf16_hi(w);
+        } else {
+          v[i] += OUT_F32 ? __uint_as_float(q[i]) : bf16_lo(q[i]);
+        }
       }
-      if (p.res && !(OUT_F32 && PASS == kLinWeightGrad))
-        v += OUT_F32 ? static_cast<const float*>(p.res)[q_at + k] : load_bf16(p.res, q_at + k);
-      if (OUT_F32) static_cast<float*>(p.c)[c_at + k] = v;
-      else store_bf16(p.c, c_at + k, v);
     }
+#pragma unroll
+    for (int i = 0; i < N; ++i, c += c_step) {
+      if (PAIRS) {
+        const uint32_t w = lin_trade(pack_bf16(v[2 * i], v[2 * i + 1]), odd);
+        if (2 * i < left) *reinterpret_cast<uint32_t*>(c) = w;
+      } else if (in && i < left) {
+        if (OUT_F32) *reinterpret_cast<float*>(c) = v[i];
+        else store_bf16(c, 0, v[i]);
+      }
+    }
+    c += (kLinSides - 1) * N * c_step;
   }
 }
 
-template <int PASS, bool OUT_F32>
-__device__ __forceinline__ void lin_finish_chunk(const LinearParams& p, const LinUnit& t, uint32_t buf, int lane,
-                                                 int row0, int col0, const LinBias& bias, const float (&v)[32]) {
-  const int col = col0 + (lane & 3) * 8;           // this lane's 8 columns
-  if (!p.vec || col0 + 32 > p.size_c) {
-    lin_transpose(buf, lane, v);
-    if (col < p.size_c) lin_finish_slow<PASS, OUT_F32>(p, t.e, t.r0 + row0, t.w - row0, buf, lane, col);
-    return;
-  }
-  if (OUT_F32) {
-    lin_transpose(buf, lane, v);
-    lin_finish_f32<PASS>(p, t, buf, lane, row0, col, bias);
-    return;
-  }
-  switch (PASS == kLinWeightGrad ? GOLDY_ACT_NONE : p.act) {
-    case GOLDY_ACT_RELU: lin_finish_fast<PASS, GOLDY_ACT_RELU>(p, t, buf, lane, row0, col, bias, v); break;
-    case GOLDY_ACT_GELU: lin_finish_fast<PASS, GOLDY_ACT_GELU>(p, t, buf, lane, row0, col, bias, v); break;
-    case GOLDY_ACT_GELU_TANH: lin_finish_fast<PASS, GOLDY_ACT_GELU_TANH>(p, t, buf, lane, row0, col, bias, v); break;
-    case GOLDY_ACT_SILU: lin_finish_fast<PASS, GOLDY_ACT_SILU>(p, t, buf, lane, row0, col, bias, v); break;
-    default: lin_finish_fast<PASS, GOLDY_ACT_NONE>(p, t, buf, lane, row0, col, bias, v);
-  }
-}
-
-template <int PASS, bool PAIR, bool OUT_F32>
+template <int PASS, int ACT, bool PAIR, bool OUT_F32>
 __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_constant__ LinearParams p) {
+  static_assert(kLinThreads == (2 + kLinEpiWarps) * 32, "roles");
   constexpr bool A_MN = PASS != kLinInputGrad;         // P contiguous along c
   constexpr bool B_MN = PASS == kLinWeightGrad;        // Q contiguous along r
   constexpr bool TAIL = PASS == kLinWeightGrad;        // ragged reduction
@@ -395,15 +411,15 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   const int stages = p.stages;
   const uint32_t stage_bytes = uint32_t(p.stage_bytes);
-  uint8_t* staging = smem + size_t(stages) * stage_bytes;
-  uint64_t* bars = reinterpret_cast<uint64_t*>(staging + kLinStagingBytes);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + size_t(stages) * stage_bytes);
   uint64_t* full = bars;                               // pair: used in the even CTA only
   uint64_t* empty = bars + kLinMaxStages;
   uint64_t* tfull = bars + 2 * kLinMaxStages;
   uint64_t* tempty = tfull + ACC;
   uint64_t* drain = tempty + ACC;
-  uint64_t* tail = drain + 1;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tail + 1);
+  uint64_t* tail = drain + 1;                          // this CTA's last, ragged stage has landed
+  uint64_t* peer = tail + 1;                           // even CTA: the odd CTA has zeroed its part
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(peer + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
   const uint32_t tiles = ptx::smem_u32(smem);
@@ -421,8 +437,7 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
       if (!B_MN) ptx::prefetch_tensormap(&p.tb_part);
     }
     for (int s = 0; s < stages; ++s) {
-      // the weight gradient's pair counts both CTAs' load warps in
-      ptx::mbar_init(ptx::smem_u32(&full[s]), (PAIR && TAIL) ? 2 : 1);
+      ptx::mbar_init(ptx::smem_u32(&full[s]), 1);
       ptx::mbar_init(ptx::smem_u32(&empty[s]), 1);
     }
     for (int a = 0; a < ACC; ++a) {
@@ -431,6 +446,7 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
     }
     ptx::mbar_init(ptx::smem_u32(drain), 1);
     ptx::mbar_init(ptx::smem_u32(tail), 1);
+    ptx::mbar_init(ptx::smem_u32(peer), 1);
     *abort_flag = 0;
     ptx::fence_barrier_init();
     ptx::fence_proxy_async_smem();
@@ -471,74 +487,85 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
       const int boxes = B_MN ? (half + 63) / 64 : full_box ? 1 : (half + p.part_box - 1) / p.part_box;
       const uint32_t box_bytes = B_MN ? 8192u : uint32_t(full_box ? half : p.part_box) * 128u;
       const uint32_t bytes = A_BYTES + boxes * box_bytes;
-      for (int kb = t.kb0; kb < t.kb1; ++kb) {
-        if ((issued >> stage & 1) && !lin_wait(ptx::smem_u32(&empty[stage]), phase ^ 1, abort_flag)) {
-          ok = false;
-          break;
-        }
-        const uint32_t fb_local = ptx::smem_u32(&full[stage]);
-        const uint32_t fb = PAIR ? ptx::map_to_rank(fb_local, 0) : fb_local;
+      const int e = PASS == kLinWeightGrad ? 0 : t.e;
+      // the unit's last stage holds rows of the next group behind this one's last
+      const bool fix = TAIL && t.kb1 > t.kb0 && t.red < t.kb1 * kLinStageK && t.k0 + t.red < p.rows;
+      // one lane: starts a stage's copies, which complete on `bar`
+      auto fill = [&](int kb, uint32_t bar) {
         const uint32_t as = tiles + stage * stage_bytes;
         const uint32_t bs = as + A_BYTES;
         const int k = t.k0 + kb * kLinStageK;
-        // rows of the next group behind this group's last one
-        const int valid = t.red - kb * kLinStageK;
-        const bool fix = TAIL && valid < kLinStageK && t.k0 + t.red < p.rows;
-        if (lane == 0) {
-          uint32_t bar = fb;
-          if (fix) {
-            bar = ptx::smem_u32(tail);
-            ptx::mbar_arrive_expect_tx(bar, bytes);
-            if (PAIR) bar = ptx::map_to_rank(bar, rank);
-          } else if (!PAIR) {
-            ptx::mbar_arrive_expect_tx(fb_local, bytes);
-          } else if (TAIL) {
-            mbar_arrive_expect_tx_remote(fb, bytes);
-          } else if (lead) {
-            ptx::mbar_arrive_expect_tx(fb_local, 2 * bytes);
-          }
-          auto load = [&](uint32_t dst, const void* map, int x, int y, int z) {
-            if (PAIR) ptx::tma_load_3d_pair(dst, map, bar, x, y, z);
-            else ptx::tma_load_3d(dst, map, bar, x, y, z);
-          };
-          const int e = PASS == kLinWeightGrad ? 0 : t.e;
-          if (A_MN) {
-            load(as, &p.ta, c0, k, e);
-            load(as + 8192, &p.ta, c0 + 64, k, e);
-          } else {
-            load(as, &p.ta, k, c0, e);
-          }
-          if (B_MN) {
-            for (int b = 0; b < boxes; ++b) load(bs + b * 8192, &p.tb, r0 + b * 64, k, 0);
-          } else if (full_box) {
-            load(bs, &p.tb, k, r0, 0);
-          } else {
-            for (int b = 0; b < boxes; ++b) load(bs + b * box_bytes, &p.tb_part, k, r0 + b * p.part_box, 0);
-          }
+        auto load = [&](uint32_t dst, const void* map, int x, int y, int z) {
+          if (PAIR) ptx::tma_load_3d_pair(dst, map, bar, x, y, z);
+          else ptx::tma_load_3d(dst, map, bar, x, y, z);
+        };
+        if (A_MN) {
+          load(as, &p.ta, c0, k, e);
+          load(as + 8192, &p.ta, c0 + 64, k, e);
+        } else {
+          load(as, &p.ta, k, c0, e);
         }
+        if (B_MN) {
+          for (int b = 0; b < boxes; ++b) load(bs + b * 8192, &p.tb, r0 + b * 64, k, 0);
+        } else if (full_box) {
+          load(bs, &p.tb, k, r0, 0);
+        } else {
+          for (int b = 0; b < boxes; ++b) load(bs + b * box_bytes, &p.tb_part, k, r0 + b * p.part_box, 0);
+        }
+      };
+      auto claim_stage = [&]() {                       // the whole warp
+        if (issued >> stage & 1) ok = lin_wait_warp(ptx::smem_u32(&empty[stage]), phase ^ 1, abort_flag);
         issued |= 1u << stage;
+        return ok;
+      };
+      auto next_stage = [&]() {
         last_phase = (last_phase & ~(1u << stage)) | (phase << stage);
-        if (TAIL && fix) {
-          ok = lin_wait(ptx::smem_u32(tail), tail_phase, nullptr);
-          tail_phase ^= 1;
-          // lines of 128 bytes, one per reduction row, in 8 KB blocks of 64 columns
-          const int lines = kLinStageK - valid;
-          for (int i = lane; i < (2 + boxes) * lines * 8; i += 32) {
-            const int blk = i / (lines * 8), o = i - blk * lines * 8;
-            ptx::st_shared_v4(as + blk * 8192 + valid * 128 + o * 16, 0, 0, 0, 0);
-          }
-          ptx::fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) {
-            if (PAIR) ptx::mbar_arrive_remote_release(fb);
-            else ptx::mbar_arrive(fb_local);
-          }
-          if (!ok) break;
-        }
         if (++stage == stages) {
           stage = 0;
           phase ^= 1;
         }
+      };
+      const int whole = fix ? t.kb1 - 1 : t.kb1;
+      for (int kb = t.kb0; kb < whole; ++kb) {
+        if (!claim_stage()) break;
+        const uint32_t fb = ptx::smem_u32(&full[stage]);
+        if (lin_elect()) {
+          if (lead) ptx::mbar_arrive_expect_tx(fb, CTAS * bytes);
+          fill(kb, PAIR ? ptx::map_to_rank(fb, 0) : fb);   // a pair's copies complete in the even CTA
+        }
+        __syncwarp();
+        next_stage();
+      }
+      if (TAIL && fix && ok) {
+        // the last stage lands on this CTA's own barrier; the warp zeroes what
+        // is not of the group before the MMAs may have it
+        if (!claim_stage()) break;
+        const uint32_t tb = ptx::smem_u32(tail);
+        if (lin_elect()) {
+          ptx::mbar_arrive_expect_tx(tb, bytes);
+          fill(t.kb1 - 1, PAIR ? ptx::map_to_rank(tb, rank) : tb);
+        }
+        __syncwarp();
+        ok = lin_wait_warp(tb, tail_phase, nullptr);
+        const uint32_t as = tiles + stage * stage_bytes;
+        const int valid = t.red - (t.kb1 - 1) * kLinStageK;
+        // lines of 128 bytes, one per reduction row, in 8 KB blocks of 64 columns
+        const int pieces = (kLinStageK - valid) * 8;
+        for (int i = lane; i < (2 + boxes) * pieces; i += 32) {
+          const int blk = i / pieces;
+          ptx::st_shared_v4(as + blk * 8192 + valid * 128 + (i - blk * pieces) * 16, 0, 0, 0, 0);
+        }
+        ptx::fence_proxy_async_smem();
+        __syncwarp();
+        const uint32_t fb = ptx::smem_u32(&full[stage]);
+        if (PAIR && lead) ok = lin_wait_warp<true>(ptx::smem_u32(peer), tail_phase, abort_flag) && ok;
+        if (lane == 0) {
+          if (lead) ptx::mbar_arrive(fb);
+          else ptx::mbar_arrive_remote_release(ptx::map_to_rank(ptx::smem_u32(peer), 0));
+        }
+        __syncwarp();
+        next_stage();
+        tail_phase ^= 1;
       }
     }
     if (!ok && lane == 0) raise_error(p.err, abort_flag, kErrProducerWait);
@@ -567,37 +594,34 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
         for (int kb = t.kb0; kb < t.kb1;) {
           const int stop = OUT_F32 ? min(kb + kLinPromote, t.kb1) : t.kb1;
           if (acc_used >> acc & 1) {
-            const uint32_t b = ptx::smem_u32(&tempty[acc]);
-            ok = PAIR ? lin_wait_cluster(b, acc_phase ^ 1, abort_flag) : lin_wait(b, acc_phase ^ 1, abort_flag);
+            ok = lin_wait_warp<PAIR>(ptx::smem_u32(&tempty[acc]), acc_phase ^ 1, abort_flag);
             if (!ok) break;
           }
           acc_used |= 1u << acc;
           ptx::tc_fence_after();
           const uint32_t d = tmem_base + uint32_t(acc * 256);
-          bool fresh = true;
+          uint32_t add = 0;
           for (; kb < stop; ++kb) {
-            const uint32_t b = ptx::smem_u32(&full[stage]);
-            ok = (PAIR && TAIL) ? lin_wait_cluster(b, phase, abort_flag) : lin_wait(b, phase, abort_flag);
+            ok = lin_wait_warp(ptx::smem_u32(&full[stage]), phase, abort_flag);
             if (!ok) break;
             ptx::tc_fence_after();
-            if (lane == 0) {
-              const uint32_t as = tiles + stage * stage_bytes;
-              const uint32_t bs = as + A_BYTES;
+            const uint32_t as = tiles + stage * stage_bytes;
+            const uint32_t bs = as + A_BYTES;
+            if (lin_elect()) {
 #pragma unroll
               for (int kk = 0; kk < 4; ++kk) {
                 const uint64_t ad = A_MN ? ptx::make_sdesc_sw128(as + kk * 2048, 8192, 1024)
                                          : ptx::make_sdesc_sw128(as + kk * 32, 16, 1024);
                 const uint64_t bd = B_MN ? ptx::make_sdesc_sw128(bs + kk * 2048, 8192, 1024)
                                          : ptx::make_sdesc_sw128(bs + kk * 32, 16, 1024);
-                const uint32_t add = (!fresh || kk > 0) ? 1u : 0u;
-                if (PAIR) ptx::mma_bf16_pair(d, ad, bd, idesc, add);
-                else ptx::mma_bf16(d, ad, bd, idesc, add);
+                if (PAIR) ptx::mma_bf16_pair(d, ad, bd, idesc, kk > 0 ? 1u : add);
+                else ptx::mma_bf16(d, ad, bd, idesc, kk > 0 ? 1u : add);
               }
               if (PAIR) ptx::mma_commit_pair_multicast(ptx::smem_u32(&empty[stage]), 0x3);
               else ptx::mma_commit(ptx::smem_u32(&empty[stage]));
             }
             __syncwarp();
-            fresh = false;
+            add = 1;
             any = true;
             if (++stage == stages) {
               stage = 0;
@@ -605,7 +629,7 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
             }
           }
           if (!ok) break;
-          if (lane == 0) {
+          if (lin_elect()) {
             if (PAIR) ptx::mma_commit_pair_multicast(ptx::smem_u32(&tfull[acc]), 0x3);
             else ptx::mma_commit(ptx::smem_u32(&tfull[acc]));
           }
@@ -616,21 +640,24 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
           }
         }
       }
-      if (!ok && lane == 0) {
-        raise_error(p.err, abort_flag, kErrMmaWait);
+      if (!ok) {
+        if (lane == 0) raise_error(p.err, abort_flag, kErrMmaWait);
         if (any) {
-          if (PAIR) ptx::mma_commit_pair_multicast(ptx::smem_u32(drain), 0x1);
-          else ptx::mma_commit(ptx::smem_u32(drain));
-          ptx::mbar_wait(ptx::smem_u32(drain), 0, nullptr);
+          if (lin_elect()) {
+            if (PAIR) ptx::mma_commit_pair_multicast(ptx::smem_u32(drain), 0x1);
+            else ptx::mma_commit(ptx::smem_u32(drain));
+          }
+          __syncwarp();
+          lin_wait_warp(ptx::smem_u32(drain), 0, nullptr);
         }
       }
     }
   } else {
     // ------------------------------------------------------------ epilogue
+    constexpr int MOST = (32 + kLinSides - 1) / kLinSides;   // 8-row chunks of a tile per warp, at most
     const int ew = warp - 2;
     const int q = warp & 3;                            // lanes of tensor memory this warp may read
-    const int side = ew >> 2;                          // takes chunks side, side + 2, ...
-    const uint32_t buf = ptx::smem_u32(staging) + uint32_t(ew * 4096);
+    const int side = ew >> 2;                          // takes chunks side, side + kLinSides, ...
     int acc = 0;
     uint32_t acc_phase = 0;
     bool ok = true;
@@ -645,131 +672,100 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
       __syncwarp();
       if (lane == 0) {
         const uint32_t b = ptx::smem_u32(&tempty[acc]);
-        if (PAIR) ptx::mbar_arrive_remote_release(ptx::map_to_rank(b, 0));
+        if (PAIR) lin_arrive_remote(ptx::map_to_rank(b, 0));
         else ptx::mbar_arrive(b);
       }
     };
     for (int u = worker; ok && walk.find(u, t); u += n_workers) {
       const int col0 = t.c0 + int(rank) * 128 + q * 32;
-      LinBias bias;
-      lin_load_bias<PASS>(p, t.e, col0 + (lane & 3) * 8, bias);
-      const uint32_t lanes = tmem_base + (uint32_t(q * 32) << 16);
+      float bias = 0.0f;
+      if (PASS == kLinForward && p.bias && col0 + lane < p.size_c) {
+        const int64_t at = int64_t(t.e) * p.size_c + col0 + lane;
+        bias = p.bias_f32 ? static_cast<const float*>(p.bias)[at] : load_bf16(p.bias, at);
+      }
+      const int chunks = (t.w + 7) / 8;
+      const bool some = t.kb1 > t.kb0;                 // else the sum is empty and no accumulator is used
       const bool split = p.split > 1;
-      float* part = p.part + ((size_t(t.tile) * p.split * CTAS + rank) * kLinEpiWarps + ew) * (size_t(p.part_chunks) * 1024);
-      const size_t split_stride = size_t(CTAS) * kLinEpiWarps * p.part_chunks * 1024;
-      auto publish = [&](int i, int chunk, const float (&v)[32]) {
-        float* to = part + t.s * split_stride + size_t(i) * 1024 + lane;
+      uint32_t cols = tmem_base + (uint32_t(q * 32) << 16) + uint32_t(acc * 256);
+      if (OUT_F32 && t.kb1 - t.kb0 > kLinPromote) {
+        // sum the accumulators of kLinPromote stages each; the total goes back
+        // into the last one's tensor memory, where the code below finds it
+        float sum[MOST][8];
 #pragma unroll
-        for (int j = 0; j < 32; ++j)
-          if (chunk * 32 + j < t.w) __stcg(to + j * 32, v[j]);
-      };
-      bool last = true;
-      if (OUT_F32) {
-        float sum[4][32];
+        for (int i = 0; i < MOST; ++i)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            sum[i][j] = 0.0f;
-            // a gradient that is added to starts from it (split 0 does), read
-            // while the tensor cores work
-            const int row = (side + 2 * i) * 32 + j;
-            if (PASS == kLinWeightGrad && p.res && t.s == 0 && row < t.w && col0 + lane < p.size_c)
-              sum[i][j] = static_cast<const float*>(p.res)[int64_t(t.e) * p.r_group + (int64_t(t.r0) + row) * p.ldr +
-                                                           col0 + lane];
-          }
+          for (int j = 0; j < 8; ++j) sum[i][j] = 0.0f;
         for (int kb = t.kb0; kb < t.kb1; kb += kLinPromote) {
-          ok = lin_wait(ptx::smem_u32(&tfull[acc]), acc_phase, abort_flag);
+          ok = lin_wait_warp(ptx::smem_u32(&tfull[acc]), acc_phase, abort_flag);
           if (!ok) break;
           ptx::tc_fence_after();
+          cols = tmem_base + (uint32_t(q * 32) << 16) + uint32_t(acc * 256);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int chunk = side + 2 * i;
-            if (chunk * 32 < t.nw) {
-              uint32_t raw[32];
-              ptx::tmem_ld_32x32b_x32(lanes + uint32_t(acc * 256 + chunk * 32), raw);
+          for (int i = 0; i < MOST; ++i) {
+            const int chunk = side + kLinSides * i;
+            if (chunk < chunks) {
+              uint32_t raw[8];
+              lin_tmem_load(cols + uint32_t(chunk * 8), raw);
               ptx::tmem_ld_wait();
 #pragma unroll
-              for (int j = 0; j < 32; ++j) sum[i][j] += __uint_as_float(raw[j]);
+              for (int j = 0; j < 8; ++j) sum[i][j] += __uint_as_float(raw[j]);
             }
           }
-          release();
-          next_acc();
+          if (kb + kLinPromote < t.kb1) {
+            release();
+            next_acc();
+          }
         }
         if (!ok) break;
-        if (!split) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int chunk = side + 2 * i;
-            if (chunk * 32 < t.w) lin_finish_chunk<PASS, OUT_F32>(p, t, buf, lane, chunk * 32, col0, bias, sum[i]);
-          }
-          continue;
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if ((side + 2 * i) * 32 < t.w) publish(i, side + 2 * i, sum[i]);
-      }
-      const bool some = !OUT_F32 && t.kb1 > t.kb0;     // the result is in accumulator `acc`
-      if (some) {
-        ok = lin_wait(ptx::smem_u32(&tfull[acc]), acc_phase, abort_flag);
+        for (int i = 0; i < MOST; ++i)
+          if (side + kLinSides * i < chunks) lin_tmem_store(cols + uint32_t((side + kLinSides * i) * 8), sum[i]);
+        lin_tmem_store_wait();
+      } else if (some) {
+        ok = lin_wait_warp(ptx::smem_u32(&tfull[acc]), acc_phase, abort_flag);
         if (!ok) break;
         ptx::tc_fence_after();
       }
-      auto read_acc = [&](int chunk, float (&v)[32]) {
-        if (some) {
-          uint32_t raw[32];
-          ptx::tmem_ld_32x32b_x32(lanes + uint32_t(acc * 256 + chunk * 32), raw);
-          ptx::tmem_ld_wait();
-#pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(raw[j]);
-          // the accumulator is free once its last chunk is in registers
-          if ((chunk + 2) * 32 >= t.w) release();
-        } else {
-#pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = 0.0f;
-        }
-      };
-      unsigned* cnt = p.cnt + (size_t(t.tile) * CTAS + rank) * kLinEpiWarps + ew;
+      // partials of this warp's part of the tile: [split][chunk][row][column]
+      float* part = p.part + ((size_t(t.tile) * p.split * CTAS + rank) * kLinEpiWarps + ew) * (size_t(p.part_chunks) * 256);
+      const size_t split_stride = size_t(CTAS) * kLinEpiWarps * p.part_chunks * 256;
       if (split) {
-        if (!OUT_F32) {
 #pragma unroll 1
-          for (int i = 0; (side + 2 * i) * 32 < t.w; ++i) {
-            float v[32];
-            read_acc(side + 2 * i, v);
-            publish(i, side + 2 * i, v);
+        for (int chunk = side; chunk < chunks; chunk += kLinSides) {
+          uint32_t raw[8];
+          if (some) {
+            lin_tmem_load(cols + uint32_t(chunk * 8), raw);
+            ptx::tmem_ld_wait();
           }
+          float* to = part + t.s * split_stride + (chunk / kLinSides) * 256 + lane;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) __stcg(to + j * 32, some ? __uint_as_float(raw[j]) : 0.0f);
         }
+        if (some) {
+          release();
+          next_acc();
+        }
+        // the last of the splits to arrive sums all of them in split order and
+        // leaves the counter at zero
+        unsigned* cnt = p.cnt + (size_t(t.tile) * CTAS + rank) * kLinEpiWarps + ew;
         __threadfence();
         __syncwarp();
         unsigned old = 0;
-        if (lane == 0) old = atomicAdd(cnt, 1u);
-        last = __shfl_sync(0xFFFFFFFFu, old, 0) == unsigned(p.split - 1);
-        if (last) __threadfence();
-      }
-      // the last of the splits to arrive at this warp's part of the tile sums
-      // all of them in split order and leaves the counter at zero
-#pragma unroll 1
-      for (int i = 0; last && (side + 2 * i) * 32 < t.w; ++i) {
-        const int chunk = side + 2 * i;
-        float v[32];
-        if (split) {
-#pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = 0.0f;
-#pragma unroll 1
-          for (int s = 0; s < p.split; ++s) {
-            const float* from = part + s * split_stride + size_t(i) * 1024 + lane;
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-              if (chunk * 32 + j < t.w) v[j] += __ldcg(from + j * 32);
-          }
-        } else {
-          read_acc(chunk, v);
+        if (lane == 0) {
+          old = atomicAdd(cnt, 1u);
+          if (old == unsigned(p.split - 1)) *cnt = 0u;
         }
-        lin_finish_chunk<PASS, OUT_F32>(p, t, buf, lane, chunk * 32, col0, bias, v);
+        if (__shfl_sync(0xFFFFFFFFu, old, 0) != unsigned(p.split - 1)) continue;
+        __threadfence();
       }
-      if (split && last && lane == 0) *cnt = 0u;
-      if (some) {
-        if (side * 32 >= t.w) release();               // no chunk of this warp's
+      const bool from_acc = some && !split;
+      const float* sums = split ? part : nullptr;
+      if (!OUT_F32 && p.vec && col0 + 32 <= p.size_c)
+        lin_drain<PASS, OUT_F32, ACT, !OUT_F32>(p, t, lane, side, col0, bias, from_acc, cols, sums, split_stride, release);
+      else
+        lin_drain<PASS, OUT_F32, ACT, false>(p, t, lane, side, col0, bias, from_acc, cols, sums, split_stride, release);
+      if (from_acc) {
+        if (side >= chunks) release();                 // no chunk of this warp's
         next_acc();
       }
     }

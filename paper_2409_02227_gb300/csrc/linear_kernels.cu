@@ -1,24 +1,20 @@
-// Instantiations of the linear-layer kernel, one translation unit per pass
-// (-DGOLDY_LINEAR_PASS=0, 1, 2).
+// Instantiations of the linear-layer kernel, one translation unit per pass and
+// activation (-DGOLDY_LINEAR_PASS=0, 1, 2 -DGOLDY_LINEAR_ACT=0 .. 4; the weight
+// gradient has no activation).
 #include "linear_kernel.cuh"
+
+#define LIN_CAT_(a, b, c, d) a##b##c##d
+#define LIN_CAT(a, b, c, d) LIN_CAT_(a, b, c, d)
 
 namespace goldy {
 
-template <int PASS>
-static const void* pick(int pair, int out_f32) {
+const void* LIN_CAT(linear_kernel_p, GOLDY_LINEAR_PASS, _a, GOLDY_LINEAR_ACT)(int pair, int out_f32) {
+  constexpr int P = GOLDY_LINEAR_PASS, A = GOLDY_LINEAR_ACT;
   if (pair)
-    return out_f32 ? reinterpret_cast<const void*>(&linear_kernel<PASS, true, true>)
-                   : reinterpret_cast<const void*>(&linear_kernel<PASS, true, false>);
-  return out_f32 ? reinterpret_cast<const void*>(&linear_kernel<PASS, false, true>)
-                 : reinterpret_cast<const void*>(&linear_kernel<PASS, false, false>);
+    return out_f32 ? reinterpret_cast<const void*>(&linear_kernel<P, A, true, true>)
+                   : reinterpret_cast<const void*>(&linear_kernel<P, A, true, false>);
+  return out_f32 ? reinterpret_cast<const void*>(&linear_kernel<P, A, false, true>)
+                 : reinterpret_cast<const void*>(&linear_kernel<P, A, false, false>);
 }
-
-#if GOLDY_LINEAR_PASS == 0
-const void* linear_kernel_forward(int pair, int out_f32) { return pick<kLinForward>(pair, out_f32); }
-#elif GOLDY_LINEAR_PASS == 1
-const void* linear_kernel_input_grad(int pair, int out_f32) { return pick<kLinInputGrad>(pair, out_f32); }
-#else
-const void* linear_kernel_weight_grad(int pair, int out_f32) { return pick<kLinWeightGrad>(pair, out_f32); }
-#endif
 
 }  // namespace goldy
