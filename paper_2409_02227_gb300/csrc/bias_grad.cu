@@ -2,13 +2,13 @@
 //   dZ = dY * act'(Z)  (bf16, when Z is given),  db[e] = sum of dZ (or dY) over the rows of group e.
 //
 // HBM-bound: dY (and Z) are read once, dZ is written once.  A CTA sums a slice
-// of the rows for 256 columns (8 warps, 8 columns per lane: 512-byte rows per
-// warp access, several rows in flight), warps taking every eighth row, and
-// writes one fp32 partial row per group its slice meets.  Slice s and group e
-// use partial row s + e: along increasing rows slice and group numbers only
+// of the rows for 64 columns: a warp covers 4 rows of 128 bytes per access (8
+// columns per lane), 8 warps 32 rows, kUnroll such accesses in flight.  Per
+// group that its slice meets it writes one fp32 partial row.  Slice s and group
+// e use partial row s + e: along increasing rows slice and group numbers only
 // grow, so the sums are distinct.  The last slice to arrive at a column block
-// adds the partials in slice order.  Sums are fp32 in a fixed order (rows of a
-// warp, warps, slices), taken before dZ is rounded.
+// adds the partials in slice order.  Sums are fp32 in a fixed order (a lane's
+// rows, lanes, warps, slices), taken before dZ is rounded.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -22,10 +22,11 @@
 namespace goldy {
 namespace {
 
-constexpr int kCols = 256;         // columns per CTA
+constexpr int kCols = 64;          // columns per CTA
 constexpr int kWarps = 8;
-constexpr int kUnroll = 4;         // rows in flight per warp
-constexpr int kMinRows = 64;       // rows per slice, at least
+constexpr int kLines = kWarps * 4; // rows per pass of a CTA
+constexpr int kUnroll = 4;         // passes in flight
+constexpr int kMinRows = 32;       // rows per slice, at least
 constexpr int kTargetCtas = 608;   // 4 per SM
 
 int slices_for(int64_t rows, int64_t cols) {
@@ -36,13 +37,13 @@ int slices_for(int64_t rows, int64_t cols) {
 
 template <bool ACT>
 __global__ void __launch_bounds__(kWarps * 32) bias_grad_kernel(const BiasGradParams p) {
-  __shared__ float part[kWarps][kCols];
+  __shared__ float part[kLines][kCols];
   __shared__ unsigned arrived;
   ptx::griddep_launch_dependents();
   ptx::griddep_wait();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int line = threadIdx.x >> 3;               // row of a pass
   const int c0 = blockIdx.x * kCols;
-  const int col = c0 + lane * 8;
+  const int col = c0 + (threadIdx.x & 7) * 8;
   const int n = max(0, min(8, p.cols - col));
   const bool vec = p.vec && n == 8;
   const int height = (p.rows + p.slices - 1) / p.slices;
@@ -92,27 +93,34 @@ __global__ void __launch_bounds__(kWarps * 32) bias_grad_kernel(const BiasGradPa
       for (int k = 0; k < 8; ++k)
         if (k < n) sum[k] += f[k];
     };
-    int r = a + warp;
-    for (; r + (kUnroll - 1) * kWarps < b; r += kUnroll * kWarps) {
+    int r = a + line;
+    for (; r + (kUnroll - 1) * kLines < b; r += kUnroll * kLines) {
       float f[kUnroll][8], z[kUnroll][8];
 #pragma unroll
       for (int i = 0; i < kUnroll; ++i) {
-        load(p.dy, p.lddy, r + i * kWarps, f[i]);
-        if (ACT) load(p.z, p.ldz, r + i * kWarps, z[i]);
+        load(p.dy, p.lddy, r + i * kLines, f[i]);
+        if (ACT) load(p.z, p.ldz, r + i * kLines, z[i]);
       }
 #pragma unroll
-      for (int i = 0; i < kUnroll; ++i) take(r + i * kWarps, f[i], z[i]);
+      for (int i = 0; i < kUnroll; ++i) take(r + i * kLines, f[i], z[i]);
     }
-    for (; r < b; r += kWarps) {
+    for (; r < b; r += kLines) {
       float f[8], z[8];
       load(p.dy, p.lddy, r, f);
       if (ACT) load(p.z, p.ldz, r, z);
       take(r, f, z);
     }
 #pragma unroll
-    for (int k = 0; k < 8; ++k) part[warp][lane * 8 + k] = sum[k];
+    for (int k = 0; k < 8; ++k) {                  // the warp's 4 lines
+      sum[k] += __shfl_xor_sync(0xFFFFFFFFu, sum[k], 8);
+      sum[k] += __shfl_xor_sync(0xFFFFFFFFu, sum[k], 16);
+    }
+    if ((threadIdx.x & 24) == 0) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) part[threadIdx.x >> 5][(threadIdx.x & 7) * 8 + k] = sum[k];
+    }
     __syncthreads();
-    if (c0 + int(threadIdx.x) < p.cols) {
+    if (threadIdx.x < kCols && c0 + int(threadIdx.x) < p.cols) {
       float s = 0.0f;
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) s += part[w][threadIdx.x];
@@ -127,19 +135,49 @@ __global__ void __launch_bounds__(kWarps * 32) bias_grad_kernel(const BiasGradPa
   if (arrived != unsigned(p.slices - 1)) return;
   __threadfence();
   if (threadIdx.x == 0) p.cnt[blockIdx.x] = 0u;
-  // one thread per column; groups in turn, slices of a group in order
-  const int c = c0 + threadIdx.x;
-  if (c >= p.cols) return;
-  for (int g = 0; g < p.groups; ++g) {
-    const int a = first_row(g), b = first_row(g + 1);
+  // Four threads per column share the groups, or the slices of a single one.
+  constexpr int kShare = kWarps * 32 / kCols;
+  const int mine = threadIdx.x / kCols, c = c0 + int(threadIdx.x) % kCols;
+  if (p.groups == 1) {
     float s = 0.0f;
-    if (a < b) {
-      const int last = (b - 1) / height;
+    if (c < p.cols && p.rows > 0) {
+      const int used = (p.rows + height - 1) / height;
 #pragma unroll 8
-      for (int i = a / height; i <= last; ++i) s += __ldcg(p.part + int64_t(i + g) * p.cols + c);
+      for (int i = mine; i < used; i += kShare) s += __ldcg(p.part + int64_t(i) * p.cols + c);
     }
-    float* to = p.db + int64_t(g) * p.cols + c;
-    *to = p.accumulate ? *to + s : s;
+    part[mine][threadIdx.x % kCols] = s;
+    __syncthreads();
+    if (mine == 0 && c < p.cols) {
+#pragma unroll
+      for (int i = 1; i < kShare; ++i) s += part[i][threadIdx.x];
+      p.db[c] = p.accumulate ? p.db[c] + s : s;
+    }
+    return;
+  }
+  if (c >= p.cols) return;
+  for (int g0 = mine; g0 < p.groups; g0 += 4 * kShare) {
+    // four groups at a time, their first partials in flight together
+    int i[4], last[4];
+    float s[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int g = g0 + k * kShare;
+      const int a = g < p.groups ? first_row(g) : 0, b = g < p.groups ? first_row(g + 1) : 0;
+      i[k] = a < b ? a / height : 0;
+      last[k] = a < b ? (b - 1) / height : -1;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      s[k] = i[k] <= last[k] ? __ldcg(p.part + int64_t(i[k] + g0 + k * kShare) * p.cols + c) : 0.0f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int g = g0 + k * kShare;
+      if (g >= p.groups) break;
+#pragma unroll 4
+      for (int j = i[k] + 1; j <= last[k]; ++j) s[k] += __ldcg(p.part + int64_t(j + g) * p.cols + c);
+      float* to = p.db + int64_t(g) * p.cols + c;
+      *to = p.accumulate ? *to + s[k] : s[k];
+    }
   }
 }
 

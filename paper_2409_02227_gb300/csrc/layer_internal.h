@@ -46,7 +46,7 @@ constexpr int kLinThreads = (2 + kLinEpiWarps) * 32;   // a load warp, an MMA wa
 constexpr int kLinStageK = 64;            // reduction elements per pipeline stage
 constexpr int kLinMaxStages = 12;
 constexpr int kLinRowBand = 8;            // row tiles walked before the next column tile
-constexpr int kLinPromote = 8;            // stages accumulated in tensor memory for fp32 results
+constexpr int kLinPromote = 12;           // stages accumulated in tensor memory for fp32 results
 constexpr int kLinSmemBudget = 232448;    // 227 KB
 
 // n / d for 0 <= n < 2^31 as the high half of n * mul, mul = floor(2^64 / d) + 1.

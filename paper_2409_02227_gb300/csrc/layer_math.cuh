@@ -36,17 +36,33 @@ __device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
   return make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
 }
 
+// 2^x and 1 / x by the special-function unit (a few units in the last place,
+// subnormals flushed to zero).
+__device__ __forceinline__ float fast_exp2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float fast_rcp(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+constexpr float kLog2E = 1.4426950408889634f;
+// 1 / (1 + exp(-x))
+__device__ __forceinline__ float fast_sigmoid(float x) { return fast_rcp(1.0f + fast_exp2(x * -kLog2E)); }
+
 // Standard normal upper tail q(|z|) = erfc(|z| / sqrt 2) / 2 and density
 // factor g = exp(-z^2 / 2).
 __device__ __forceinline__ float normal_tail(float z, float& g) {
-  const float x = fabsf(z) * 0.70710678118654752f;
-  const float t = __fdividef(1.0f, fmaf(0.3275911f, x, 1.0f));
-  g = __expf(-x * x);
-  float s = fmaf(1.061405429f, t, -1.453152027f);
-  s = fmaf(s, t, 1.421413741f);
-  s = fmaf(s, t, -0.284496736f);
-  s = fmaf(s, t, 0.254829592f);
-  return 0.5f * s * t * g;
+  // p / sqrt 2; the coefficients are halved
+  const float t = fast_rcp(fmaf(0.23164189f, fabsf(z), 1.0f));
+  g = fast_exp2(z * z * (-0.5f * kLog2E));
+  float s = fmaf(0.5307027145f, t, -0.7265760135f);
+  s = fmaf(s, t, 0.7107068705f);
+  s = fmaf(s, t, -0.142248368f);
+  s = fmaf(s, t, 0.127414796f);
+  return s * t * g;
 }
 
 __device__ __forceinline__ float act_value(float z, int act) {
@@ -60,9 +76,9 @@ __device__ __forceinline__ float act_value(float z, int act) {
     case GOLDY_ACT_GELU_TANH: {
       // (1 + tanh u) / 2 = 1 / (1 + exp(-2u)), u = sqrt(2/pi) (z + 0.044715 z^3)
       const float u2 = 1.5957691216057308f * fmaf(0.044715f * z * z, z, z);
-      return __fdividef(z, 1.0f + __expf(-u2));
+      return z * fast_sigmoid(u2);
     }
-    case GOLDY_ACT_SILU: return __fdividef(z, 1.0f + __expf(-z));
+    case GOLDY_ACT_SILU: return z * fast_sigmoid(z);
     default: return z;
   }
 }
@@ -78,11 +94,11 @@ __device__ __forceinline__ float act_slope(float z, int act) {
     case GOLDY_ACT_GELU_TANH: {
       const float zz = fminf(z * z, 1e30f);      // finite, so that a saturated slope stays 0 or 1
       const float u2 = 1.5957691216057308f * fmaf(0.044715f * zz, z, z);
-      const float s = __fdividef(1.0f, 1.0f + __expf(-u2));
+      const float s = fast_sigmoid(u2);
       return fmaf(z * s * (1.0f - s), 1.5957691216057308f * fmaf(3.0f * 0.044715f, zz, 1.0f), s);
     }
     case GOLDY_ACT_SILU: {
-      const float s = __fdividef(1.0f, 1.0f + __expf(-z));
+      const float s = fast_sigmoid(z);
       return s * fmaf(z, 1.0f - s, 1.0f);
     }
     default: return 1.0f;

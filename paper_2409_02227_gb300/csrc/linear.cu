@@ -84,7 +84,7 @@ constexpr double kSplitRate = 16.0;      // bytes per cycle of partials publishe
 
 LinChoice choose(const LinShape& s) {
   struct Candidate { int pair, tile_r; };
-  static const Candidate cand[] = {{1, 256}, {1, 192}, {1, 128}, {0, 256}, {0, 128}, {0, 64}, {0, 32}, {0, 16}};
+  static const Candidate cand[] = {{1, 256}, {1, 224}, {1, 192}, {1, 128}, {0, 256}, {0, 128}, {0, 64}, {0, 32}, {0, 16}};
   const bool wgrad = s.pass == kLinWeightGrad;
   const int64_t live = std::max<int64_t>(1, std::min<int64_t>(s.groups, wgrad ? s.groups : s.rows));
   const int64_t r_rows = wgrad ? s.size_r : ceil_div(std::max<int64_t>(s.rows, 1), live);

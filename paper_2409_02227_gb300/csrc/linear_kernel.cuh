@@ -32,8 +32,10 @@
 // OUT_F32: the tensor cores add into fp32 accumulators with truncation, a
 // relative error of about 1e-9 per reduction element (4.4e-6 at 4096,
 // measured against fp64).  fp32 results therefore leave tensor memory every
-// kLinPromote stages (512 elements) and are summed in registers with rounding
-// to nearest: 5e-7 at any length.  bf16 results (relative rounding 2^-8) keep
+// kLinPromote stages (768 elements) and are summed in registers with rounding
+// to nearest: 7e-7 at any length.  (Parts of 512 elements are good to 5e-7, but
+// the drain of a tile, 3.6 us, then holds its accumulator past the next tile's
+// first part: 58 against 53 us for a 2048 x 8192 gradient over 2048 rows.)  bf16 results (relative rounding 2^-8) keep
 // the whole sum in tensor memory.
 //
 // Every wait is bounded; a wait that runs out sets the error word and the
@@ -67,6 +69,9 @@ __device__ __forceinline__ bool lin_elect() {
   return one != 0;
 }
 
+// A value that all lanes share, in a form that the compiler knows to be shared.
+__device__ __forceinline__ int lin_shared(int x) { return __shfl_sync(0xFFFFFFFFu, x, 0); }
+
 // Bounded wait for the phase with parity `parity`, false if it gave up (the
 // limit, or another role's abort flag).  The timer is read at every 64th poll.
 // (Arrivals over tensor memory are ordered by the tcgen05 fences; CLUSTER adds
@@ -87,6 +92,12 @@ __device__ __forceinline__ bool lin_wait(uint32_t bar, uint32_t parity, const vo
 template <bool CLUSTER = false>
 __device__ __forceinline__ bool lin_wait_warp(uint32_t bar, uint32_t parity, const volatile int* abort_flag) {
   return __all_sync(0xFFFFFFFFu, lin_wait<CLUSTER>(bar, parity, abort_flag));
+}
+
+// Stages per accumulator of an fp32 result: equal parts of at most kLinPromote.
+__device__ __forceinline__ int lin_promote(int kbs) {
+  const int parts = (kbs + kLinPromote - 1) / kLinPromote;
+  return parts > 1 ? int(unsigned(kbs + parts - 1) / unsigned(parts)) : kbs;
 }
 
 // One unit of work: a tile of C, or one split of its reduction.
@@ -227,6 +238,10 @@ struct LinWalk {
     return true;
   }
 };
+
+__device__ __forceinline__ void lin_prefetch(const void* at) {
+  asm volatile("prefetch.global.L2 [%0];" ::"l"(at));
+}
 
 // 8 accumulator columns of this warp's 32 lanes: tensor memory -> registers,
 // and back.
@@ -423,7 +438,7 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
   const uint32_t tiles = ptx::smem_u32(smem);
-  const int warp = threadIdx.x >> 5;
+  const int warp = lin_shared(threadIdx.x >> 5);
   const int lane = threadIdx.x & 31;
   const uint32_t rank = PAIR ? (ptx::cluster_ctarank() & 1u) : 0u;
   const bool lead = rank == 0;
@@ -467,7 +482,7 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
     ptx::cluster_sync_all();                           // the peer's barriers and tensor memory are ready
     ptx::tc_fence_after();
   }
-  const uint32_t tmem_base = *tmem_slot;
+  const uint32_t tmem_base = uint32_t(lin_shared(int(*tmem_slot)));
   ptx::griddep_launch_dependents();
   ptx::griddep_wait();                                 // inputs and offsets may come from the previous kernel
 
@@ -480,6 +495,8 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
     uint32_t phase = 0, issued = 0, last_phase = 0, tail_phase = 0;
     bool ok = true;
     for (int u = worker; ok && walk.find(u, t); u += n_workers) {
+      t.e = lin_shared(t.e), t.r0 = lin_shared(t.r0), t.nw = lin_shared(t.nw), t.c0 = lin_shared(t.c0);
+      t.k0 = lin_shared(t.k0), t.red = lin_shared(t.red), t.kb0 = lin_shared(t.kb0), t.kb1 = lin_shared(t.kb1);
       const int half = t.nw / CTAS;                    // rows of Q this CTA stages
       const int r0 = t.r0 + int(rank) * half;
       const int c0 = t.c0 + int(rank) * 128;
@@ -590,9 +607,11 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
       uint32_t phase = 0, acc_phase = 0, acc_used = 0;
       bool ok = true, any = false;
       for (int u = worker; ok && walk.find(u, t); u += n_workers) {
-        const uint32_t idesc = ptx::make_idesc_bf16(128 * CTAS, 16, A_MN, B_MN) + (uint32_t((t.nw - 16) >> 3) << 17);
-        for (int kb = t.kb0; kb < t.kb1;) {
-          const int stop = OUT_F32 ? min(kb + kLinPromote, t.kb1) : t.kb1;
+        const int nw = lin_shared(t.nw), kb0 = lin_shared(t.kb0), kb1 = lin_shared(t.kb1);
+        const uint32_t idesc = ptx::make_idesc_bf16(128 * CTAS, 16, A_MN, B_MN) + (uint32_t((nw - 16) >> 3) << 17);
+        const int step = lin_promote(kb1 - kb0);
+        for (int kb = kb0; kb < kb1;) {
+          const int stop = OUT_F32 ? min(kb + step, kb1) : kb1;
           if (acc_used >> acc & 1) {
             ok = lin_wait_warp<PAIR>(ptx::smem_u32(&tempty[acc]), acc_phase ^ 1, abort_flag);
             if (!ok) break;
@@ -683,19 +702,39 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
         const int64_t at = int64_t(t.e) * p.size_c + col0 + lane;
         bias = p.bias_f32 ? static_cast<const float*>(p.bias)[at] : load_bf16(p.bias, at);
       }
+      // the tile's rows of Z and R come into L2 while its products are computed
+      // (a 32-column segment is one or two 128-byte lines)
+      if (col0 < p.size_c && (PASS == kLinInputGrad ? (p.z_in || p.res) : p.res != nullptr)) {
+        const int last_col = min(col0 + 31, p.size_c - 1);
+        for (int row = side * 32 + lane; row < t.w; row += kLinSides * 32) {
+          const int64_t r = int64_t(t.r0) + row;
+          if (PASS == kLinInputGrad && p.z_in) {
+            const char* z = static_cast<const char*>(p.z_in) + r * p.ldz * 2;
+            lin_prefetch(z + int64_t(col0) * 2);
+            lin_prefetch(z + int64_t(last_col) * 2);
+          }
+          if (p.res) {
+            constexpr int64_t ES = OUT_F32 ? 4 : 2;
+            const char* q = static_cast<const char*>(p.res) + (int64_t(t.e) * p.r_group + r * p.ldr) * ES;
+            lin_prefetch(q + col0 * ES);
+            lin_prefetch(q + last_col * ES);
+          }
+        }
+      }
       const int chunks = (t.w + 7) / 8;
       const bool some = t.kb1 > t.kb0;                 // else the sum is empty and no accumulator is used
       const bool split = p.split > 1;
       uint32_t cols = tmem_base + (uint32_t(q * 32) << 16) + uint32_t(acc * 256);
       if (OUT_F32 && t.kb1 - t.kb0 > kLinPromote) {
-        // sum the accumulators of kLinPromote stages each; the total goes back
-        // into the last one's tensor memory, where the code below finds it
+        // sum the accumulators of some kLinPromote stages each; the total goes
+        // back into the last one's tensor memory, where the code below finds it
+        const int step = lin_promote(t.kb1 - t.kb0);
         float sum[MOST][8];
 #pragma unroll
         for (int i = 0; i < MOST; ++i)
 #pragma unroll
           for (int j = 0; j < 8; ++j) sum[i][j] = 0.0f;
-        for (int kb = t.kb0; kb < t.kb1; kb += kLinPromote) {
+        for (int kb = t.kb0; kb < t.kb1; kb += step) {
           ok = lin_wait_warp(ptx::smem_u32(&tfull[acc]), acc_phase, abort_flag);
           if (!ok) break;
           ptx::tc_fence_after();
@@ -711,7 +750,7 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
               for (int j = 0; j < 8; ++j) sum[i][j] += __uint_as_float(raw[j]);
             }
           }
-          if (kb + kLinPromote < t.kb1) {
+          if (kb + step < t.kb1) {
             release();
             next_acc();
           }
