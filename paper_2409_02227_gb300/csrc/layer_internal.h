@@ -42,7 +42,8 @@ constexpr int kLinForward = 0;
 constexpr int kLinInputGrad = 1;
 constexpr int kLinWeightGrad = 2;
 constexpr int kLinEpiWarps = 12;
-constexpr int kLinThreads = (2 + kLinEpiWarps) * 32;   // a load warp, an MMA warp, the epilogue's
+// a load warp, an MMA warp, the epilogue's, and the weight gradient's mending warp
+constexpr int lin_threads(int pass) { return (2 + kLinEpiWarps + (pass == kLinWeightGrad ? 1 : 0)) * 32; }
 constexpr int kLinStageK = 64;            // reduction elements per pipeline stage
 constexpr int kLinMaxStages = 12;
 constexpr int kLinRowBand = 8;            // row tiles walked before the next column tile

@@ -268,7 +268,7 @@ goldy_status launch_linear(const LayerContext& ctx, void* arg) {
   const int64_t workers = std::max<int64_t>(1, std::min<int64_t>(units, ctx.sm_count / ctas));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(unsigned(workers * ctas));
-  cfg.blockDim = dim3(kLinThreads);
+  cfg.blockDim = dim3(unsigned(lin_threads(s.pass)));
   cfg.dynamicSmemBytes = size_t(fixed + p.stages * p.stage_bytes);
   cfg.stream = static_cast<cudaStream_t>(call.stream);
   cudaLaunchAttribute attr[2];

@@ -12,8 +12,8 @@
 // rows costs ceil(w / 16) * 16 columns of tensor work whatever the group
 // sizes, a single token included, and no row is padded or copied in memory.
 // In the weight gradient the ragged axis is the reduction: a group's last
-// stage may hold rows of the next group, which the load warp zeroes in shared
-// memory before handing the stage on (zero times whatever the neighbour holds
+// stage may hold rows of the next group, which a further warp zeroes in
+// shared memory before the stage is used (zero times whatever the neighbour holds
 // would not do: 0 * inf is NaN).
 //
 // PAIR: a cluster of two CTAs computes 256 columns x up to 256 rows with
@@ -57,15 +57,16 @@ __device__ __forceinline__ void lin_arrive_remote(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 
-// True in one lane of a converged warp, always the same one.  The copies, MMAs
-// and commits stand under this predicate, not under lane == 0: they take their
-// operands from registers shared by the warp, and only here does the compiler
-// know that one lane runs them.  Under lane == 0 each one became a loop over
-// the lanes, some 70 cycles apiece, and no tile, however narrow, took less than
-// 290 ns per 64-deep stage.
-__device__ __forceinline__ bool lin_elect() {
+// True in one lane of a converged warp; `leader` gets that lane's number.  The
+// copies, MMAs and commits stand under this predicate, not under lane == 0:
+// they take their operands from registers shared by the warp, and only here
+// does the compiler know that one lane runs them.  Under lane == 0 each became
+// a loop over the lanes, some 70 cycles apiece, and no tile, however narrow,
+// took less than 290 ns per 64-deep stage.
+__device__ __forceinline__ bool lin_elect(int& leader) {
   uint32_t one;
-  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync %0|p, 0xFFFFFFFF;\n\tselp.u32 %1, 1, 0, p;\n\t}"
+               : "=r"(leader), "=r"(one));
   return one != 0;
 }
 
@@ -412,8 +413,7 @@ __device__ __forceinline__ void lin_drain(const LinearParams& p, const LinUnit& 
 }
 
 template <int PASS, int ACT, bool PAIR, bool OUT_F32>
-__global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_constant__ LinearParams p) {
-  static_assert(kLinThreads == (2 + kLinEpiWarps) * 32, "roles");
+__global__ void __launch_bounds__(lin_threads(PASS), 1) linear_kernel(const __grid_constant__ LinearParams p) {
   constexpr bool A_MN = PASS != kLinInputGrad;         // P contiguous along c
   constexpr bool B_MN = PASS == kLinWeightGrad;        // Q contiguous along r
   constexpr bool TAIL = PASS == kLinWeightGrad;        // ragged reduction
@@ -432,9 +432,9 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
   uint64_t* tfull = bars + 2 * kLinMaxStages;
   uint64_t* tempty = tfull + ACC;
   uint64_t* drain = tempty + ACC;
-  uint64_t* tail = drain + 1;                          // this CTA's last, ragged stage has landed
-  uint64_t* peer = tail + 1;                           // even CTA: the odd CTA has zeroed its part
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(peer + 1);
+  uint64_t* tail = drain + 1;                          // a group's last, ragged stage has landed in this CTA
+  uint64_t* peer = tail + kLinMaxStages;               // even CTA: the odd CTA has zeroed its part of one
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(peer + kLinMaxStages);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
   const uint32_t tiles = ptx::smem_u32(smem);
@@ -454,14 +454,16 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
     for (int s = 0; s < stages; ++s) {
       ptx::mbar_init(ptx::smem_u32(&full[s]), 1);
       ptx::mbar_init(ptx::smem_u32(&empty[s]), 1);
+      if (TAIL) {
+        ptx::mbar_init(ptx::smem_u32(&tail[s]), 1);
+        ptx::mbar_init(ptx::smem_u32(&peer[s]), 1);
+      }
     }
     for (int a = 0; a < ACC; ++a) {
       ptx::mbar_init(ptx::smem_u32(&tfull[a]), 1);
       ptx::mbar_init(ptx::smem_u32(&tempty[a]), kLinEpiWarps * CTAS);
     }
     ptx::mbar_init(ptx::smem_u32(drain), 1);
-    ptx::mbar_init(ptx::smem_u32(tail), 1);
-    ptx::mbar_init(ptx::smem_u32(peer), 1);
     *abort_flag = 0;
     ptx::fence_barrier_init();
     ptx::fence_proxy_async_smem();
@@ -488,11 +490,16 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
 
   LinWalk<PASS, PAIR> walk(p, lane);
   LinUnit t;
+  // weight gradient: the unit's last stage holds rows of the next group behind
+  // this one's last
+  auto ragged = [&]() {
+    return TAIL && t.kb1 > t.kb0 && t.red < t.kb1 * kLinStageK && t.k0 + t.red < p.rows;
+  };
 
   if (warp == 0) {
     // -------------------------------------------------------------- loads
     int stage = 0;
-    uint32_t phase = 0, issued = 0, last_phase = 0, tail_phase = 0;
+    uint32_t phase = 0, issued = 0, last_phase = 0;
     bool ok = true;
     for (int u = worker; ok && walk.find(u, t); u += n_workers) {
       t.e = lin_shared(t.e), t.r0 = lin_shared(t.r0), t.nw = lin_shared(t.nw), t.c0 = lin_shared(t.c0);
@@ -505,8 +512,6 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
       const uint32_t box_bytes = B_MN ? 8192u : uint32_t(full_box ? half : p.part_box) * 128u;
       const uint32_t bytes = A_BYTES + boxes * box_bytes;
       const int e = PASS == kLinWeightGrad ? 0 : t.e;
-      // the unit's last stage holds rows of the next group behind this one's last
-      const bool fix = TAIL && t.kb1 > t.kb0 && t.red < t.kb1 * kLinStageK && t.k0 + t.red < p.rows;
       // one lane: starts a stage's copies, which complete on `bar`
       auto fill = [&](int kb, uint32_t bar) {
         const uint32_t as = tiles + stage * stage_bytes;
@@ -530,8 +535,8 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
           for (int b = 0; b < boxes; ++b) load(bs + b * box_bytes, &p.tb_part, k, r0 + b * p.part_box, 0);
         }
       };
-      auto claim_stage = [&]() {                       // the whole warp
-        if (issued >> stage & 1) ok = lin_wait_warp(ptx::smem_u32(&empty[stage]), phase ^ 1, abort_flag);
+      auto claim_stage = [&]() {
+        if (issued >> stage & 1) ok = lin_wait(ptx::smem_u32(&empty[stage]), phase ^ 1, abort_flag);
         issued |= 1u << stage;
         return ok;
       };
@@ -542,53 +547,31 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
           phase ^= 1;
         }
       };
-      const int whole = fix ? t.kb1 - 1 : t.kb1;
-      for (int kb = t.kb0; kb < whole; ++kb) {
-        if (!claim_stage()) break;
-        const uint32_t fb = ptx::smem_u32(&full[stage]);
-        if (lin_elect()) {
-          if (lead) ptx::mbar_arrive_expect_tx(fb, CTAS * bytes);
-          fill(kb, PAIR ? ptx::map_to_rank(fb, 0) : fb);   // a pair's copies complete in the even CTA
+      const int whole = ragged() ? t.kb1 - 1 : t.kb1;
+      int leader;
+      if (lin_elect(leader)) {
+        for (int kb = t.kb0; kb < t.kb1; ++kb) {
+          if (!claim_stage()) break;
+          if (TAIL && kb >= whole) {                   // lands on this CTA's own barrier, to be mended
+            const uint32_t tb = ptx::smem_u32(&tail[stage]);
+            ptx::mbar_arrive_expect_tx(tb, bytes);
+            fill(kb, PAIR ? ptx::map_to_rank(tb, rank) : tb);
+          } else {
+            const uint32_t fb = ptx::smem_u32(&full[stage]);
+            if (lead) ptx::mbar_arrive_expect_tx(fb, CTAS * bytes);
+            fill(kb, PAIR ? ptx::map_to_rank(fb, 0) : fb);   // a pair's copies complete in the even CTA
+          }
+          next_stage();
         }
-        __syncwarp();
-        next_stage();
       }
-      if (TAIL && fix && ok) {
-        // the last stage lands on this CTA's own barrier; the warp zeroes what
-        // is not of the group before the MMAs may have it
-        if (!claim_stage()) break;
-        const uint32_t tb = ptx::smem_u32(tail);
-        if (lin_elect()) {
-          ptx::mbar_arrive_expect_tx(tb, bytes);
-          fill(t.kb1 - 1, PAIR ? ptx::map_to_rank(tb, rank) : tb);
-        }
-        __syncwarp();
-        ok = lin_wait_warp(tb, tail_phase, nullptr);
-        const uint32_t as = tiles + stage * stage_bytes;
-        const int valid = t.red - (t.kb1 - 1) * kLinStageK;
-        // lines of 128 bytes, one per reduction row, in 8 KB blocks of 64 columns
-        const int pieces = (kLinStageK - valid) * 8;
-        for (int i = lane; i < (2 + boxes) * pieces; i += 32) {
-          const int blk = i / pieces;
-          ptx::st_shared_v4(as + blk * 8192 + valid * 128 + (i - blk * pieces) * 16, 0, 0, 0, 0);
-        }
-        ptx::fence_proxy_async_smem();
-        __syncwarp();
-        const uint32_t fb = ptx::smem_u32(&full[stage]);
-        if (PAIR && lead) ok = lin_wait_warp<true>(ptx::smem_u32(peer), tail_phase, abort_flag) && ok;
-        if (lane == 0) {
-          if (lead) ptx::mbar_arrive(fb);
-          else ptx::mbar_arrive_remote_release(ptx::map_to_rank(ptx::smem_u32(peer), 0));
-        }
-        __syncwarp();
-        next_stage();
-        tail_phase ^= 1;
-      }
+      __syncwarp();
+      ok = __shfl_sync(0xFFFFFFFFu, ok, leader);
     }
     if (!ok && lane == 0) raise_error(p.err, abort_flag, kErrProducerWait);
     // every stage filled must have been consumed (and, for a pair, both CTAs'
     // commits landed) before the CTA may leave
-    if (lane == 0) {
+    int leader;
+    if (lin_elect(leader)) {
       const uint64_t t0 = ptx::global_timer();
       for (int s = 0; s < stages; ++s) {
         if (!(issued >> s & 1)) continue;
@@ -603,30 +586,30 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
   } else if (warp == 1) {
     // ---------------------------------------------------------------- MMAs
     if (lead) {
-      int stage = 0, acc = 0;
+      int stage = 0, acc = 0, leader = 0;
       uint32_t phase = 0, acc_phase = 0, acc_used = 0;
-      bool ok = true, any = false;
+      bool ok = true, any = false;                     // `any` and the ring's state: the elected lane's
       for (int u = worker; ok && walk.find(u, t); u += n_workers) {
         const int nw = lin_shared(t.nw), kb0 = lin_shared(t.kb0), kb1 = lin_shared(t.kb1);
         const uint32_t idesc = ptx::make_idesc_bf16(128 * CTAS, 16, A_MN, B_MN) + (uint32_t((nw - 16) >> 3) << 17);
-        const int step = lin_promote(kb1 - kb0);
-        for (int kb = kb0; kb < kb1;) {
-          const int stop = OUT_F32 ? min(kb + step, kb1) : kb1;
-          if (acc_used >> acc & 1) {
-            ok = lin_wait_warp<PAIR>(ptx::smem_u32(&tempty[acc]), acc_phase ^ 1, abort_flag);
-            if (!ok) break;
-          }
-          acc_used |= 1u << acc;
-          ptx::tc_fence_after();
-          const uint32_t d = tmem_base + uint32_t(acc * 256);
-          uint32_t add = 0;
-          for (; kb < stop; ++kb) {
-            ok = lin_wait_warp(ptx::smem_u32(&full[stage]), phase, abort_flag);
-            if (!ok) break;
+        const int step = OUT_F32 ? lin_promote(kb1 - kb0) : kb1 - kb0;
+        if (lin_elect(leader)) {
+          for (int kb = kb0; kb < kb1;) {
+            const int stop = min(kb + step, kb1);
+            if (acc_used >> acc & 1) {
+              ok = lin_wait<PAIR>(ptx::smem_u32(&tempty[acc]), acc_phase ^ 1, abort_flag);
+              if (!ok) break;
+            }
+            acc_used |= 1u << acc;
             ptx::tc_fence_after();
-            const uint32_t as = tiles + stage * stage_bytes;
-            const uint32_t bs = as + A_BYTES;
-            if (lin_elect()) {
+            const uint32_t d = tmem_base + uint32_t(acc * 256);
+            uint32_t add = 0;
+            for (; kb < stop; ++kb) {
+              ok = lin_wait(ptx::smem_u32(&full[stage]), phase, abort_flag);
+              if (!ok) break;
+              ptx::tc_fence_after();
+              const uint32_t as = tiles + stage * stage_bytes;
+              const uint32_t bs = as + A_BYTES;
 #pragma unroll
               for (int kk = 0; kk < 4; ++kk) {
                 const uint64_t ad = A_MN ? ptx::make_sdesc_sw128(as + kk * 2048, 8192, 1024)
@@ -638,39 +621,70 @@ __global__ void __launch_bounds__(kLinThreads, 1) linear_kernel(const __grid_con
               }
               if (PAIR) ptx::mma_commit_pair_multicast(ptx::smem_u32(&empty[stage]), 0x3);
               else ptx::mma_commit(ptx::smem_u32(&empty[stage]));
+              add = 1;
+              any = true;
+              if (++stage == stages) {
+                stage = 0;
+                phase ^= 1;
+              }
             }
-            __syncwarp();
-            add = 1;
-            any = true;
-            if (++stage == stages) {
-              stage = 0;
-              phase ^= 1;
-            }
-          }
-          if (!ok) break;
-          if (lin_elect()) {
+            if (!ok) break;
             if (PAIR) ptx::mma_commit_pair_multicast(ptx::smem_u32(&tfull[acc]), 0x3);
             else ptx::mma_commit(ptx::smem_u32(&tfull[acc]));
-          }
-          __syncwarp();
-          if (++acc == ACC) {
-            acc = 0;
-            acc_phase ^= 1;
+            if (++acc == ACC) {
+              acc = 0;
+              acc_phase ^= 1;
+            }
           }
         }
+        __syncwarp();
+        ok = __shfl_sync(0xFFFFFFFFu, ok, leader);
       }
       if (!ok) {
         if (lane == 0) raise_error(p.err, abort_flag, kErrMmaWait);
-        if (any) {
-          if (lin_elect()) {
-            if (PAIR) ptx::mma_commit_pair_multicast(ptx::smem_u32(drain), 0x1);
-            else ptx::mma_commit(ptx::smem_u32(drain));
-          }
-          __syncwarp();
-          lin_wait_warp(ptx::smem_u32(drain), 0, nullptr);
+        if (lin_elect(leader) && any) {
+          if (PAIR) ptx::mma_commit_pair_multicast(ptx::smem_u32(drain), 0x1);
+          else ptx::mma_commit(ptx::smem_u32(drain));
+          lin_wait(ptx::smem_u32(drain), 0, nullptr);
         }
+        __syncwarp();
       }
     }
+  } else if (TAIL && warp == 2 + kLinEpiWarps) {
+    // -------------------------------------------------------------- mending
+    // A ragged stage lands on this CTA's own barrier.  The warp zeroes what is
+    // behind the group's last row (lines of 128 bytes, one per reduction row,
+    // in 8 KB blocks of 64 columns) and then hands the stage to the MMAs.
+    // A warp of its own: the load warp would stop loading meanwhile, and the
+    // MMA warp multiplying (43 against 38 us for 8 groups of about 1000 rows,
+    // 2048 x 1024 each).
+    int stage = 0;
+    uint32_t tail_phase = 0;
+    bool ok = true;
+    for (int u = worker; ok && walk.find(u, t); u += n_workers) {
+      const int kbs = t.kb1 - t.kb0;
+      if (ragged()) {
+        const int at = (stage + kbs - 1) % stages;
+        const uint32_t parity = tail_phase >> at & 1;
+        tail_phase ^= 1u << at;
+        ok = lin_wait_warp(ptx::smem_u32(&tail[at]), parity, abort_flag);
+        const uint32_t as = tiles + at * stage_bytes;
+        const int valid = t.red - (t.kb1 - 1) * kLinStageK;
+        const int pieces = (kLinStageK - valid) * 8;
+        const int blocks = 2 + (t.nw / CTAS + 63) / 64;
+        for (int b = 0; b < blocks; ++b)
+          for (int i = lane; i < pieces; i += 32) ptx::st_shared_v4(as + b * 8192 + valid * 128 + i * 16, 0, 0, 0, 0);
+        ptx::fence_proxy_async_smem();
+        __syncwarp();
+        if (PAIR && lead && ok) ok = lin_wait_warp<true>(ptx::smem_u32(&peer[at]), parity, abort_flag);
+        if (lane == 0) {
+          if (lead) ptx::mbar_arrive(ptx::smem_u32(&full[at]));
+          else ptx::mbar_arrive_remote_release(ptx::map_to_rank(ptx::smem_u32(&peer[at]), 0));
+        }
+      }
+      stage = (stage + kbs) % stages;
+    }
+    if (!ok && lane == 0) raise_error(p.err, abort_flag, kErrProducerWait);
   } else {
     // ------------------------------------------------------------ epilogue
     constexpr int MOST = (32 + kLinSides - 1) / kLinSides;   // 8-row chunks of a tile per warp, at most
