@@ -69,46 +69,40 @@ __global__ void __launch_bounds__(kWarps * 32) bias_grad_kernel(const BiasGradPa
     for (int k = 0; k < 8; ++k) sum[k] = 0.0f;
     auto load = [&](const void* base, int64_t ld, int r, float (&f)[8]) {
       const uint16_t* at = static_cast<const uint16_t*>(base) + int64_t(r) * ld + col;
-      if (vec) {
+      if (vec && r < b) {
         unpack8(*reinterpret_cast<const uint4*>(at), f);
       } else {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) f[k] = k < n ? load_bf16(at, k) : 0.0f;
+        for (int k = 0; k < 8; ++k) f[k] = r < b && k < n ? load_bf16(at, k) : 0.0f;
       }
     };
-    auto take = [&](int r, float (&f)[8], const float (&z)[8]) {
-      if (ACT) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) f[k] *= act_slope(z[k], p.act);
-        uint16_t* to = static_cast<uint16_t*>(p.dz) + int64_t(r) * p.lddz + col;
-        if (vec) {
-          *reinterpret_cast<uint4*>(to) = pack8(f);
-        } else {
-#pragma unroll
-          for (int k = 0; k < 8; ++k)
-            if (k < n) store_bf16(to, k, f[k]);
-        }
-      }
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (k < n) sum[k] += f[k];
-    };
-    int r = a + line;
-    for (; r + (kUnroll - 1) * kLines < b; r += kUnroll * kLines) {
+    for (int r0 = a + line; r0 < b; r0 += kUnroll * kLines) {
       float f[kUnroll][8], z[kUnroll][8];
 #pragma unroll
       for (int i = 0; i < kUnroll; ++i) {
-        load(p.dy, p.lddy, r + i * kLines, f[i]);
-        if (ACT) load(p.z, p.ldz, r + i * kLines, z[i]);
+        load(p.dy, p.lddy, r0 + i * kLines, f[i]);
+        if (ACT) load(p.z, p.ldz, r0 + i * kLines, z[i]);
       }
 #pragma unroll
-      for (int i = 0; i < kUnroll; ++i) take(r + i * kLines, f[i], z[i]);
-    }
-    for (; r < b; r += kLines) {
-      float f[8], z[8];
-      load(p.dy, p.lddy, r, f);
-      if (ACT) load(p.z, p.ldz, r, z);
-      take(r, f, z);
+      for (int i = 0; i < kUnroll; ++i) {
+        const int r = r0 + i * kLines;
+        if (r >= b) continue;
+        if (ACT) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) f[i][k] *= act_slope(z[i][k], p.act);
+          uint16_t* to = static_cast<uint16_t*>(p.dz) + int64_t(r) * p.lddz + col;
+          if (vec) {
+            *reinterpret_cast<uint4*>(to) = pack8(f[i]);
+          } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+              if (k < n) store_bf16(to, k, f[i][k]);
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (k < n) sum[k] += f[i][k];
+      }
     }
 #pragma unroll
     for (int k = 0; k < 8; ++k) {                  // the warp's 4 lines

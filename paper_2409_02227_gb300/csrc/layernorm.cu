@@ -4,24 +4,29 @@
 //   g = dy gamma, xhat = (x - mean) rstd:
 //   dx = rstd (g - sum(g) / n - xhat sum(g xhat) / n),  dgamma = sum over rows of dy xhat,  dbeta = sum over rows of dy
 //
-// HBM-bound: x (and dy) read once, y (or dx) written once.  A team of threads
-// holds a row in registers, 16 values per thread (team of 32 to 512 threads by
-// the row's length), so both statistics passes of the forward direction and
-// the two sums of the backward direction cost no second read; the next row's
-// loads are issued before the current row's sums meet.  gamma and beta stay in
-// registers over all rows of a team.  The variance is a sum of squared
-// differences from each warp's own mean, warps combined by
-// M2 = sum(M2_w + n_w (mean_w - mean)^2): no cancellation, one barrier.
-// Backward, each thread owns its columns for all rows of its team and keeps
-// dgamma and dbeta in registers; the teams of a CTA combine in shared memory,
-// one fp32 partial row per CTA goes to the workspace, and a second small kernel
-// sums the partial rows in CTA order.  Nothing depends on the order of arrival.
-// Rows over 8192 elements stream through three (two) reads of the row instead.
+// HBM-bound: x (and dy) read once, y (or dx) written once.  A team of 32 to 512
+// threads, by the row's length, holds a row in registers (64 bytes per thread
+// forwards, 16 values backwards), so both statistics passes of the forward
+// direction and the two sums of the backward direction cost no second read.
+// The next rows are on their way meanwhile: each thread copies its own pieces
+// into shared memory with cp.async and reads back only those, so that rows in
+// flight take no registers and need no barrier.  gamma and beta are read per
+// row, from L1.
+// The variance is a sum of squared differences from each warp's own mean,
+// warps combined by M2 = sum(M2_w + n_w (mean_w - mean)^2): no cancellation,
+// one barrier per row.  Backward, each thread owns its columns for all rows of
+// its team and keeps dgamma and dbeta in registers; the teams of a CTA combine
+// in shared memory, one fp32 partial row per CTA goes to the workspace, and a
+// second small kernel sums the partial rows in CTA order.  Nothing depends on
+// the order of arrival.  Rows too long for a team stream through three (two)
+// reads of the row instead.
 #include <cuda_runtime.h>
 
 #include <algorithm>
-#include <cstring>
+#include <mutex>
+#include <set>
 #include <string>
+#include <utility>
 
 #include "goldy_internal.h"
 #include "layer_internal.h"
@@ -31,11 +36,15 @@
 namespace goldy {
 namespace {
 
-constexpr int kVals = 16;           // values of a row per thread
 constexpr int kMaxTeam = 512;
 constexpr int kStreamThreads = 512;
 constexpr int kFwdThreads = 256;    // per CTA, at least the team
 constexpr int kBwdThreads = 512;
+// values of a row per thread, and rows in a thread's ring
+template <typename T> __host__ __device__ constexpr int fwd_vals() { return 64 / int(sizeof(T)); }
+constexpr int kBwdVals = 16;
+constexpr int kFwdDepth = 3;
+template <typename T> __host__ __device__ constexpr int bwd_depth() { return sizeof(T) == 2 ? 3 : 2; }
 
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
@@ -48,76 +57,106 @@ __device__ __forceinline__ float param_at(const void* p, int f32, int i, float a
   return f32 ? static_cast<const float*>(p)[i] : load_bf16(p, i);
 }
 
-// A team's row in registers.  VEC: 16-byte accesses, columns (i * TEAM + t) *
-// per + k for the thread's i-th vector of `per` elements; otherwise single
-// elements, columns i * TEAM + t.
-template <typename T, int TEAM, bool VEC>
+// Sum over groups of N consecutive lanes (N a power of two), to all of them.
+template <int N>
+__device__ __forceinline__ float lanes_sum(float v) {
+#pragma unroll
+  for (int d = N / 2; d > 0; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+  return v;
+}
+
+// PER parameters from index c on (c < n); the row's own accesses are vectors
+// exactly when these may be.
+template <int PER>
+__device__ __forceinline__ void load_params(const void* p, int f32, int c, float absent, float* f) {
+  if (!p) {
+#pragma unroll
+    for (int k = 0; k < PER; ++k) f[k] = absent;
+  } else if (PER == 1) {
+    f[0] = f32 ? __ldg(static_cast<const float*>(p) + c) : load_bf16(p, c);
+  } else if (f32) {
+#pragma unroll
+    for (int k = 0; k < PER; k += 4) {
+      const float4 v = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(p) + c + k));
+      f[k] = v.x, f[k + 1] = v.y, f[k + 2] = v.z, f[k + 3] = v.w;
+    }
+  } else if (PER == 8) {
+    const uint4 v = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + c));
+    f[0] = bf16_lo(v.x), f[1] = bf16_hi(v.x), f[2] = bf16_lo(v.y), f[3] = bf16_hi(v.y);
+    f[4] = bf16_lo(v.z), f[5] = bf16_hi(v.z), f[6] = bf16_lo(v.w), f[7] = bf16_hi(v.w);
+  } else {
+    const uint2 v = __ldg(reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + c));
+    f[0] = bf16_lo(v.x), f[1] = bf16_hi(v.x), f[2] = bf16_lo(v.y), f[3] = bf16_hi(v.y);
+  }
+}
+
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void* to, const void* from) {
+  const uint32_t at = ptx::smem_u32(to);
+  if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(from) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(at), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// A thread's share of a row, VALS values.  VEC: 16-byte pieces, piece i of
+// thread t at column (i * TEAM + t) * PER; otherwise single elements.  Pieces
+// are inside the row or outside as a whole.  bf16 rows off 16-byte boundaries
+// have no ring (no such copy exists) and are loaded where they are used.
+template <typename T, int VALS, int TEAM, int THREADS, bool VEC>
 struct Row {
   static constexpr int PER = VEC ? 16 / int(sizeof(T)) : 1;
-  static constexpr int SLOTS = kVals / PER;
+  static constexpr int SLOTS = VALS / PER;
+  static constexpr bool RING = VEC || sizeof(T) == 4;
+  static constexpr int PIECE = VEC ? 16 : 4;
+  static constexpr int RING_BYTES = RING ? SLOTS * THREADS * PIECE : 0;   // of one row
   static __device__ __forceinline__ int col(int slot, int t) { return (slot * TEAM + t) * PER; }
+  static __device__ __forceinline__ bool in(int slot, int t, int n) { return col(slot, t) < n; }
 
-  // raw bits as loaded; converted when the row is used, so that a row in
-  // flight takes as few registers as it can
-  static constexpr int WORDS = VEC ? SLOTS * 4 : SLOTS;
-  uint32_t raw[WORDS];
-
-  __device__ __forceinline__ void load(const void* base, int64_t row, int64_t ld, int n, int t) {
+  static __device__ __forceinline__ void fetch(uint8_t* ring, const void* base, int64_t row, int64_t ld, int n, int t) {
+    if (!RING) return;
     const T* at = static_cast<const T*>(base) + row * ld;
 #pragma unroll
+    for (int s = 0; s < SLOTS; ++s)
+      if (in(s, t, n)) copy_async<PIECE>(ring + (s * THREADS + threadIdx.x) * PIECE, at + col(s, t));
+  }
+  static __device__ __forceinline__ void values(const uint8_t* ring, const void* base, int64_t row, int64_t ld, int n,
+                                                int t, float (&f)[VALS]) {
+#pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
-      const int c = col(s, t);
-      if (VEC) {
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (c < n) v = __ldcs(reinterpret_cast<const uint4*>(at + c));
-        raw[s * 4] = v.x, raw[s * 4 + 1] = v.y, raw[s * 4 + 2] = v.z, raw[s * 4 + 3] = v.w;
+      if (!in(s, t, n)) {
+#pragma unroll
+        for (int k = 0; k < PER; ++k) f[s * PER + k] = 0.0f;
+      } else if (!RING) {
+        f[s] = load_bf16(static_cast<const T*>(base) + row * ld, col(s, t));
+      } else if (!VEC) {
+        f[s] = *reinterpret_cast<const float*>(ring + (s * THREADS + threadIdx.x) * 4);
       } else {
-        raw[s] = 0;
-        if (c < n) {
-          if (sizeof(T) == 2) raw[s] = uint32_t(reinterpret_cast<const uint16_t*>(at)[c]) << 16;
-          else raw[s] = reinterpret_cast<const uint32_t*>(at)[c];
+        const uint4 v = *reinterpret_cast<const uint4*>(ring + (s * THREADS + threadIdx.x) * 16);
+        float* o = f + s * PER;
+        if (sizeof(T) == 2) {
+          o[0] = bf16_lo(v.x), o[1] = bf16_hi(v.x), o[2] = bf16_lo(v.y), o[3] = bf16_hi(v.y);
+          o[4 % PER] = bf16_lo(v.z), o[5 % PER] = bf16_hi(v.z), o[6 % PER] = bf16_lo(v.w), o[7 % PER] = bf16_hi(v.w);
+        } else {
+          o[0] = __uint_as_float(v.x), o[1] = __uint_as_float(v.y), o[2] = __uint_as_float(v.z), o[3] = __uint_as_float(v.w);
         }
       }
     }
   }
-  __device__ __forceinline__ void values(float (&f)[kVals]) const {
-#pragma unroll
-    for (int s = 0; s < SLOTS; ++s) {
-      if (!VEC) {
-        f[s] = __uint_as_float(raw[s]);
-      } else if (sizeof(T) == 2) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          f[(s * 4 + k) * 2] = bf16_lo(raw[s * 4 + k]);
-          f[(s * 4 + k) * 2 + 1] = bf16_hi(raw[s * 4 + k]);
-        }
-      } else {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) f[s * 4 + k] = __uint_as_float(raw[s * 4 + k]);
-      }
+  // piece s of the result
+  static __device__ __forceinline__ void store(void* base, int64_t row, int64_t ld, int t, int s, const float* f) {
+    T* at = static_cast<T*>(base) + row * ld + col(s, t);
+    if (!VEC) {
+      if (sizeof(T) == 2) store_bf16(at, 0, f[0]);
+      else *reinterpret_cast<float*>(at) = f[0];
+    } else if (sizeof(T) == 2) {
+      __stcs(reinterpret_cast<uint4*>(at), make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]),
+                                                      pack_bf16(f[4 % PER], f[5 % PER]), pack_bf16(f[6 % PER], f[7 % PER])));
+    } else {
+      __stcs(reinterpret_cast<float4*>(at), make_float4(f[0], f[1], f[2], f[3]));
     }
   }
-  static __device__ __forceinline__ void store(void* base, int64_t row, int64_t ld, int n, int t,
-                                               const float (&f)[kVals]) {
-    T* at = static_cast<T*>(base) + row * ld;
-#pragma unroll
-    for (int s = 0; s < SLOTS; ++s) {
-      const int c = col(s, t);
-      if (c >= n) continue;
-      if (!VEC) {
-        if (sizeof(T) == 2) store_bf16(at, c, f[s]);
-        else reinterpret_cast<float*>(at)[c] = f[s];
-      } else if (sizeof(T) == 2) {
-        __stcs(reinterpret_cast<uint4*>(at + c),
-               make_uint4(pack_bf16(f[s * 8], f[s * 8 + 1]), pack_bf16(f[s * 8 + 2], f[s * 8 + 3]),
-                          pack_bf16(f[s * 8 + 4], f[s * 8 + 5]), pack_bf16(f[s * 8 + 6], f[s * 8 + 7])));
-      } else {
-        __stcs(reinterpret_cast<float4*>(at + c), make_float4(f[s * 4], f[s * 4 + 1], f[s * 4 + 2], f[s * 4 + 3]));
-      }
-    }
-  }
-  // columns of this thread inside the row, and of value j
-  static __device__ __forceinline__ bool inside(int j, int t, int n) { return col(j / PER, t) + j % PER < n; }
 };
 
 // Barrier of one team: a warp needs none, the whole CTA has barrier 0.
@@ -128,70 +167,84 @@ __device__ __forceinline__ void team_sync(int team) {
   else ptx::named_bar_sync(uint32_t(team + 1), TEAM);
 }
 
+template <typename T, int TEAM>
+struct FwdShape {
+  static constexpr int THREADS = TEAM > kFwdThreads ? TEAM : kFwdThreads;
+  static constexpr int TEAMS = THREADS / TEAM;
+};
+
 template <typename T, int TEAM, bool VEC>
-__global__ void __launch_bounds__(TEAM > kFwdThreads ? TEAM : kFwdThreads)
+__global__ void __launch_bounds__(FwdShape<T, TEAM>::THREADS, 1024 / FwdShape<T, TEAM>::THREADS)
 norm_forward_kernel(const NormParams p) {
-  constexpr int THREADS = TEAM > kFwdThreads ? TEAM : kFwdThreads;
-  constexpr int TEAMS = THREADS / TEAM;
-  constexpr int WARPS = TEAM / 32;
-  using R = Row<T, TEAM, VEC>;
+  constexpr int THREADS = FwdShape<T, TEAM>::THREADS, TEAMS = FwdShape<T, TEAM>::TEAMS;
+  constexpr int WARPS = TEAM / 32, VALS = fwd_vals<T>(), D = kFwdDepth;
+  using R = Row<T, VALS, TEAM, THREADS, VEC>;
   __shared__ float4 slot[2][TEAMS][WARPS];         // per warp: sum, M2, elements, mean
-  const int team = threadIdx.x / TEAM, t = threadIdx.x % TEAM, w = t >> 5;
+  extern __shared__ __align__(16) uint8_t ring[];
+  const int team = threadIdx.x / TEAM, t = threadIdx.x % TEAM, w = t >> 5, lane = t & 31;
   const int n = p.n;
   ptx::griddep_launch_dependents();
   ptx::griddep_wait();
   const int64_t step = int64_t(gridDim.x) * TEAMS;
   int64_t row = int64_t(blockIdx.x) * TEAMS + team;
   if (row >= p.rows) return;                       // whole teams only
-  R next;
-  next.load(p.x, row, p.ldx, n, t);
-  float gamma[kVals], beta[kVals];
+#pragma unroll
+  for (int d = 0; d < D - 1; ++d) {
+    if (row + d * step < p.rows) R::fetch(ring + d * R::RING_BYTES, p.x, row + d * step, p.ldx, n, t);
+    copy_commit();
+  }
   int mine = 0;                                    // values this thread has
 #pragma unroll
-  for (int j = 0; j < kVals; ++j) {
-    const bool in = R::inside(j, t, n);
-    gamma[j] = in ? param_at(p.gamma, p.param_f32, R::col(j / R::PER, t) + j % R::PER, 1.0f) : 0.0f;
-    beta[j] = in ? param_at(p.beta, p.param_f32, R::col(j / R::PER, t) + j % R::PER, 0.0f) : 0.0f;
-    mine += in;
-  }
+  for (int i = 0; i < R::SLOTS; ++i) mine += R::in(i, t, n) ? R::PER : 0;
   const float warp_n = warp_sum(float(mine));
   const float warp_inv = warp_n > 0.0f ? 1.0f / warp_n : 0.0f;
+  int at = 0, ahead = D - 1;                       // ring places of this row and of the one fetched now
   for (int flip = 0; row < p.rows; row += step, flip ^= 1) {
-    float x[kVals];
-    next.values(x);
-    if (row + step < p.rows) next.load(p.x, row + step, p.ldx, n, t);
+    if (row + (D - 1) * step < p.rows) R::fetch(ring + ahead * R::RING_BYTES, p.x, row + (D - 1) * step, p.ldx, n, t);
+    copy_commit();
+    copy_wait<D - 1>();
+    float x[VALS];
+    R::values(ring + at * R::RING_BYTES, p.x, row, p.ldx, n, t, x);
+    at = at + 1 == D ? 0 : at + 1;
+    ahead = ahead + 1 == D ? 0 : ahead + 1;
     float s = 0.0f;
 #pragma unroll
-    for (int j = 0; j < kVals; ++j) s += x[j];     // zeros outside the row
+    for (int j = 0; j < VALS; ++j) s += x[j];      // zeros outside the row
     s = warp_sum(s);
     const float wm = s * warp_inv;
     float m2 = 0.0f;
 #pragma unroll
-    for (int j = 0; j < kVals; ++j) {
-      const float d = R::inside(j, t, n) ? x[j] - wm : 0.0f;
-      m2 = fmaf(d, d, m2);
+    for (int i = 0; i < R::SLOTS; ++i) {
+      if (!R::in(i, t, n)) continue;
+#pragma unroll
+      for (int k = 0; k < R::PER; ++k) {
+        x[i * R::PER + k] -= wm;                   // differences from the warp's mean from here on
+        m2 = fmaf(x[i * R::PER + k], x[i * R::PER + k], m2);
+      }
     }
     m2 = warp_sum(m2);
     float mean = wm;
     if (WARPS > 1) {
-      if ((t & 31) == 0) slot[flip][team][w] = make_float4(s, m2, warp_n, wm);
+      if (lane == 0) slot[flip][team][w] = make_float4(s, m2, warp_n, wm);
       team_sync<TEAM, THREADS>(team);
-      float total = 0.0f;
-#pragma unroll
-      for (int i = 0; i < WARPS; ++i) total += slot[flip][team][i].x;
-      mean = total * p.inv_n;
-      m2 = 0.0f;
-#pragma unroll
-      for (int i = 0; i < WARPS; ++i) {
-        const float4 o = slot[flip][team][i];
-        const float d = o.w - mean;
-        m2 += fmaf(o.z * d, d, o.y);
-      }
+      const float4 o = slot[flip][team][lane & (WARPS - 1)];
+      mean = lanes_sum<WARPS>(o.x) * p.inv_n;
+      const float d = o.w - mean;
+      m2 = lanes_sum<WARPS>(fmaf(o.z * d, d, o.y));
     }
     const float rstd = rsqrtf(fmaf(m2, p.inv_n, p.eps));
+    const float shift = (wm - mean) * rstd;
 #pragma unroll
-    for (int j = 0; j < kVals; ++j) x[j] = fmaf((x[j] - mean) * rstd, gamma[j], beta[j]);
-    R::store(p.out, row, p.ldy, n, t, x);
+    for (int i = 0; i < R::SLOTS; ++i) {
+      if (!R::in(i, t, n)) continue;
+      float gamma[R::PER], beta[R::PER];
+      load_params<R::PER>(p.gamma, p.param_f32, R::col(i, t), 1.0f, gamma);
+      load_params<R::PER>(p.beta, p.param_f32, R::col(i, t), 0.0f, beta);
+#pragma unroll
+      for (int k = 0; k < R::PER; ++k)
+        x[i * R::PER + k] = fmaf(fmaf(x[i * R::PER + k], rstd, shift), gamma[k], beta[k]);
+      R::store(p.out, row, p.ldy, t, i, x + i * R::PER);
+    }
     if (t == 0) {
       if (p.mean) p.mean[row] = mean;
       if (p.rstd) p.rstd[row] = rstd;
@@ -201,87 +254,109 @@ norm_forward_kernel(const NormParams p) {
 
 template <typename T, int TEAM, bool VEC>
 __global__ void __launch_bounds__(kBwdThreads) norm_backward_kernel(const NormParams p) {
-  constexpr int TEAMS = kBwdThreads / TEAM;
-  constexpr int WARPS = TEAM / 32;
-  using R = Row<T, TEAM, VEC>;
+  constexpr int TEAMS = kBwdThreads / TEAM, WARPS = TEAM / 32, VALS = kBwdVals, D = bwd_depth<T>();
+  using R = Row<T, VALS, TEAM, kBwdThreads, VEC>;
   __shared__ float2 slot[2][TEAMS][WARPS];
-  extern __shared__ float sums[];                  // [2][TEAM * kVals]
-  const int team = threadIdx.x / TEAM, t = threadIdx.x % TEAM, w = t >> 5;
+  extern __shared__ __align__(16) uint8_t ring[];  // D rows of x, D of dy; at the end the CTA's sums
+  const int team = threadIdx.x / TEAM, t = threadIdx.x % TEAM, w = t >> 5, lane = t & 31;
   const int n = p.n;
   ptx::griddep_launch_dependents();
   ptx::griddep_wait();
   const int64_t step = int64_t(gridDim.x) * TEAMS;
   int64_t row = int64_t(blockIdx.x) * TEAMS + team;
-  R nx, ny;
-  float mean = 0.0f, rstd = 0.0f;
-  auto fetch = [&](int64_t r) {
-    nx.load(p.x, r, p.ldx, n, t);
-    ny.load(p.dy, r, p.ldy, n, t);
-    mean = __ldg(p.mean + r);
-    rstd = __ldg(p.rstd + r);
+  auto fetch = [&](int d, int64_t r) {
+    if (r < p.rows) {
+      R::fetch(ring + 2 * d * R::RING_BYTES, p.x, r, p.ldx, n, t);
+      R::fetch(ring + (2 * d + 1) * R::RING_BYTES, p.dy, r, p.ldy, n, t);
+    }
+    copy_commit();
   };
-  if (row < p.rows) fetch(row);
-  float gamma[kVals], dg[kVals], db[kVals];
 #pragma unroll
-  for (int j = 0; j < kVals; ++j) {
-    gamma[j] = R::inside(j, t, n) ? param_at(p.gamma, p.param_f32, R::col(j / R::PER, t) + j % R::PER, 1.0f) : 0.0f;
-    dg[j] = db[j] = 0.0f;
+  for (int d = 0; d < D - 1; ++d) fetch(d, row + d * step);
+  float mean = 0.0f, rstd = 0.0f;
+  if (row < p.rows) {
+    mean = __ldg(p.mean + row);
+    rstd = __ldg(p.rstd + row);
   }
+  float dg[VALS], db[VALS];
+#pragma unroll
+  for (int j = 0; j < VALS; ++j) dg[j] = db[j] = 0.0f;
+  int at = 0, ahead = D - 1;
   for (int flip = 0; row < p.rows; row += step, flip ^= 1) {
-    float x[kVals], y[kVals];
-    nx.values(x);
-    ny.values(y);
+    fetch(ahead, row + (D - 1) * step);
     const float m = mean, rs = rstd;
-    if (row + step < p.rows) fetch(row + step);
+    if (row + step < p.rows) {
+      mean = __ldg(p.mean + row + step);
+      rstd = __ldg(p.rstd + row + step);
+    }
+    copy_wait<D - 1>();
+    float x[VALS], y[VALS];
+    R::values(ring + 2 * at * R::RING_BYTES, p.x, row, p.ldx, n, t, x);
+    R::values(ring + (2 * at + 1) * R::RING_BYTES, p.dy, row, p.ldy, n, t, y);
+    at = at + 1 == D ? 0 : at + 1;
+    ahead = ahead + 1 == D ? 0 : ahead + 1;
     float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
-    for (int j = 0; j < kVals; ++j) {
-      x[j] = R::inside(j, t, n) ? (x[j] - m) * rs : 0.0f;      // xhat
-      dg[j] = fmaf(y[j], x[j], dg[j]);
-      db[j] += y[j];
-      y[j] *= gamma[j];
-      s1 += y[j];
-      s2 = fmaf(y[j], x[j], s2);
+    for (int i = 0; i < R::SLOTS; ++i) {
+      if (!R::in(i, t, n)) continue;
+      float gamma[R::PER];
+      load_params<R::PER>(p.gamma, p.param_f32, R::col(i, t), 1.0f, gamma);
+#pragma unroll
+      for (int k = 0; k < R::PER; ++k) {
+        const int j = i * R::PER + k;
+        x[j] = (x[j] - m) * rs;                    // xhat
+        dg[j] = fmaf(y[j], x[j], dg[j]);
+        db[j] += y[j];
+        y[j] *= gamma[k];
+        s1 += y[j];
+        s2 = fmaf(y[j], x[j], s2);
+      }
     }
     s1 = warp_sum(s1);
     s2 = warp_sum(s2);
     if (WARPS > 1) {
-      if ((t & 31) == 0) slot[flip][team][w] = make_float2(s1, s2);
+      if (lane == 0) slot[flip][team][w] = make_float2(s1, s2);
       team_sync<TEAM, kBwdThreads>(team);
-      s1 = s2 = 0.0f;
-#pragma unroll
-      for (int i = 0; i < WARPS; ++i) {
-        const float2 o = slot[flip][team][i];
-        s1 += o.x;
-        s2 += o.y;
-      }
+      const float2 o = slot[flip][team][lane & (WARPS - 1)];
+      s1 = lanes_sum<WARPS>(o.x);
+      s2 = lanes_sum<WARPS>(o.y);
     }
     s1 *= p.inv_n;
     s2 *= p.inv_n;
 #pragma unroll
-    for (int j = 0; j < kVals; ++j) x[j] = rs * (y[j] - s1 - x[j] * s2);
-    R::store(p.out, row, p.ldx, n, t, x);
+    for (int i = 0; i < R::SLOTS; ++i) {
+      if (!R::in(i, t, n)) continue;
+#pragma unroll
+      for (int k = 0; k < R::PER; ++k) {
+        const int j = i * R::PER + k;
+        x[j] = rs * fmaf(-x[j], s2, y[j] - s1);
+      }
+      R::store(p.out, row, p.ldx, t, i, x + i * R::PER);
+    }
   }
   if (!p.part) return;
   // teams of the CTA, in order
+  float* sums = reinterpret_cast<float*>(ring);    // [2][TEAM * VALS]
+  copy_wait<0>();
+  __syncthreads();
   for (int k = 0; k < TEAMS; ++k) {
     if (team == k) {
 #pragma unroll
-      for (int j = 0; j < kVals; ++j) {
+      for (int j = 0; j < VALS; ++j) {
         float* a = sums + j * TEAM + t;
         a[0] = k == 0 ? dg[j] : a[0] + dg[j];
-        a[TEAM * kVals] = k == 0 ? db[j] : a[TEAM * kVals] + db[j];
+        a[TEAM * VALS] = k == 0 ? db[j] : a[TEAM * VALS] + db[j];
       }
     }
     __syncthreads();
   }
   float* to = p.part + int64_t(blockIdx.x) * 2 * n;
-  for (int i = threadIdx.x; i < TEAM * kVals; i += kBwdThreads) {
+  for (int i = threadIdx.x; i < TEAM * VALS; i += kBwdThreads) {
     const int j = i / TEAM, tt = i % TEAM;
     const int c = R::col(j / R::PER, tt) + j % R::PER;
     if (c < n) {
       __stcg(to + c, sums[i]);
-      __stcg(to + n + c, sums[TEAM * kVals + i]);
+      __stcg(to + n + c, sums[TEAM * VALS + i]);
     }
   }
 }
@@ -407,10 +482,12 @@ norm_reduce_kernel(const float* part, float* dgamma, float* dbeta, int n, int ro
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 goldy_status bad(const std::string& why) { return fail(GOLDY_ERR_INVALID_ARG, why); }
 
-int team_for(int64_t n) {
+// Threads per row; 0: the row streams.
+int team_for(const goldy_layernorm_desc& d, bool backward) {
+  const int64_t vals = backward ? kBwdVals : d.dtype == GOLDY_F32 ? fwd_vals<float>() : fwd_vals<uint16_t>();
   int team = 32;
-  while (team < kMaxTeam && int64_t(team) * kVals < n) team *= 2;
-  return int64_t(team) * kVals >= n ? team : 0;    // 0: the row streams
+  while (team < kMaxTeam && team * vals < d.n) team *= 2;
+  return team * vals >= d.n ? team : 0;
 }
 
 struct Kernel {
@@ -421,11 +498,14 @@ struct Kernel {
 
 template <typename T, int TEAM, bool VEC>
 Kernel pick(bool backward) {
-  if (backward)
+  if (backward) {
+    using R = Row<T, kBwdVals, TEAM, kBwdThreads, VEC>;
     return {reinterpret_cast<const void*>(&norm_backward_kernel<T, TEAM, VEC>), kBwdThreads, kBwdThreads / TEAM,
-            size_t(2) * TEAM * kVals * sizeof(float)};
-  const int threads = std::max(TEAM, kFwdThreads);
-  return {reinterpret_cast<const void*>(&norm_forward_kernel<T, TEAM, VEC>), threads, threads / TEAM, 0};
+            std::max(size_t(2) * bwd_depth<T>() * R::RING_BYTES, size_t(2) * TEAM * kBwdVals * sizeof(float))};
+  }
+  using R = Row<T, fwd_vals<T>(), TEAM, FwdShape<T, TEAM>::THREADS, VEC>;
+  return {reinterpret_cast<const void*>(&norm_forward_kernel<T, TEAM, VEC>), FwdShape<T, TEAM>::THREADS,
+          FwdShape<T, TEAM>::TEAMS, size_t(kFwdDepth) * R::RING_BYTES};
 }
 
 template <typename T, bool VEC>
@@ -444,7 +524,7 @@ Kernel pick_team(int team, bool backward) {
 }
 
 Kernel kernel_for(const goldy_layernorm_desc& d, bool vec, bool backward) {
-  const int team = team_for(d.n);
+  const int team = team_for(d, backward);
   if (d.dtype == GOLDY_F32) return vec ? pick_team<float, true>(team, backward) : pick_team<float, false>(team, backward);
   return vec ? pick_team<uint16_t, true>(team, backward) : pick_team<uint16_t, false>(team, backward);
 }
@@ -452,7 +532,7 @@ Kernel kernel_for(const goldy_layernorm_desc& d, bool vec, bool backward) {
 // CTAs of a backward launch: one partial row each
 constexpr int kBwdCtas = 152;      // one per SM
 int backward_ctas(const goldy_layernorm_desc& d) {
-  const int team = team_for(d.n);
+  const int team = team_for(d, true);
   const int64_t teams = team ? kBwdThreads / team : 1;
   return int(std::max<int64_t>(1, std::min<int64_t>(kBwdCtas, ceil_div(d.rows, teams))));
 }
@@ -491,11 +571,22 @@ cudaError_t launch(const void* fn, unsigned grid, unsigned threads, size_t smem,
   return cudaLaunchKernelExC(&cfg, fn, args);
 }
 
+// Opts a kernel into more than 48 KB of shared memory, once per device.
+cudaError_t allow_smem(int device, const Kernel& k) {
+  if (k.smem <= 40 * 1024) return cudaSuccess;     // with the kernel's static part below 48 KB
+  static std::mutex mu;
+  static std::set<std::pair<int, const void*>> done;
+  std::lock_guard<std::mutex> lock(mu);
+  if (done.count({device, k.fn})) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(k.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, int(k.smem));
+  if (e == cudaSuccess) done.insert({device, k.fn});
+  return e;
+}
+
 goldy_status launch_norm(const LayerContext& ctx, void* arg) {
   NormCall& call = *static_cast<NormCall*>(arg);
   const Kernel k = kernel_for(*call.d, call.vec, call.backward);
-  cudaError_t e = cudaSuccess;
-  if (k.smem > 48 * 1024) e = cudaFuncSetAttribute(k.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, int(k.smem));
+  cudaError_t e = allow_smem(ctx.device, k);
   if (e != cudaSuccess) return fail(GOLDY_ERR_CUDA, std::string("cudaFuncSetAttribute: ") + cudaGetErrorString(e));
   unsigned grid;
   if (call.backward) {
@@ -522,9 +613,11 @@ goldy_status launch_norm(const LayerContext& ctx, void* arg) {
 
 // 16-byte accesses: whole vectors in every row (a team's last vector may not
 // reach past the row), rows and bases on vector boundaries
-bool vectors(const goldy_layernorm_desc& d, const void* a, const void* b, const void* c) {
+bool vectors(const goldy_layernorm_desc& d, const void* a, const void* b, const void* c, const void* gamma,
+             const void* beta) {
   const int64_t per = d.dtype == GOLDY_F32 ? 4 : 8;
-  return d.n % per == 0 && d.ldx % per == 0 && d.ldy % per == 0 && aligned(a, 16) && aligned(b, 16) && aligned(c, 16);
+  return d.n % per == 0 && d.ldx % per == 0 && d.ldy % per == 0 && aligned(a, 16) && aligned(b, 16) && aligned(c, 16) &&
+         aligned(gamma, 16) && aligned(beta, 16);
 }
 
 size_t backward_bytes(const goldy_layernorm_desc& d) {
@@ -565,7 +658,7 @@ extern "C" goldy_status goldy_layernorm_forward(const goldy_layernorm_desc* desc
     return bad("layer norm: gamma, beta, mean or rstd misaligned");
   NormCall call{};
   call.d = desc;
-  call.vec = vectors(*desc, X, Y, nullptr);
+  call.vec = vectors(*desc, X, Y, nullptr, gamma, beta);
   call.stream = stream;
   common_params(call.p, *desc);
   call.p.x = X;
@@ -603,7 +696,7 @@ extern "C" goldy_status goldy_layernorm_backward(const goldy_layernorm_desc* des
   }
   NormCall call{};
   call.d = desc;
-  call.vec = vectors(*desc, X, dY, dX);
+  call.vec = vectors(*desc, X, dY, dX, gamma, nullptr);
   call.backward = true;
   call.dgamma = dgamma;
   call.dbeta = dbeta;

@@ -72,44 +72,52 @@ struct LinChoice {
 
 int part_chunks(int tile_r) { return int(ceil_div(ceil_div(tile_r, 8), kLinEpiWarps / 4)); }
 
-// Time model in SM cycles: a 64-deep stage of an nw-row tile costs the larger
-// of its tensor time (2 nw) and of its operand bytes at kLoadRate per SM; a
-// unit adds kUnitCost for filling the pipeline and draining the accumulator,
-// a split its partials' trip through L2.  Group sizes are on the device, so
-// groups are taken as equal.
-constexpr double kLoadRate = 70.0;       // bytes per cycle and SM from L2, all SMs loading
-constexpr double kUnitCost = 1200.0;
-constexpr double kSplitCost = 2500.0;
-constexpr double kSplitRate = 16.0;      // bytes per cycle of partials published or summed by one CTA
+// Time model of a launch in ns, fitted to the times of 46 shapes (1 to 8192
+// rows, 64 to 8192 features, 0 to 64 groups, all passes) under every tile and
+// split: the choice is 2% slower than the best measured one on average, 23% at
+// worst (9 rows per group on average, where sizes spread past one tile).
+//   A 64-deep stage of an nw-row tile costs the largest of its tensor time, the
+//   issue of its copies and products, and its operands' trip from L2.
+//   A unit costs its stages or, if longer, draining its accumulator; the last
+//   drain is not hidden.
+//   A split adds its partials' trip through L2.
+// Group sizes are on the device, so groups are taken as equal.
+constexpr double kTensorNs = 1.04;       // per row of a stage
+constexpr double kIssueNs = 110.0, kIssuePairNs = 258.0;
+constexpr double kSmRate = 237.0, kL2Rate = 21226.0;   // bytes per ns into one SM, into all
+constexpr double kDrainNs = 5.6, kUnitNs = 404.0;      // per row of a tile; per unit
+constexpr double kSplitNs = 418.0, kSplitEachNs = 99.0, kSplitRowNs = 3.9;
 
 LinChoice choose(const LinShape& s) {
   struct Candidate { int pair, tile_r; };
-  static const Candidate cand[] = {{1, 256}, {1, 224}, {1, 192}, {1, 128}, {0, 256}, {0, 128}, {0, 64}, {0, 32}, {0, 16}};
+  static const Candidate cand[] = {{1, 256}, {1, 224}, {1, 192}, {1, 128}, {1, 64}, {0, 256}, {0, 128}, {0, 64}, {0, 32}, {0, 16}};
   const bool wgrad = s.pass == kLinWeightGrad;
-  const int64_t live = std::max<int64_t>(1, std::min<int64_t>(s.groups, wgrad ? s.groups : s.rows));
+  const int64_t live = std::max<int64_t>(1, wgrad ? s.groups : std::min<int64_t>(s.groups, s.rows));
   const int64_t r_rows = wgrad ? s.size_r : ceil_div(std::max<int64_t>(s.rows, 1), live);
   const int64_t red = wgrad ? ceil_div(std::max<int64_t>(s.rows, 1), live) : s.red;
   const int64_t kbs = std::max<int64_t>(1, ceil_div(red, kLinStageK));
   LinChoice best{0, 16, 1, 0, 0};
   double best_t = -1.0;
   for (const Candidate& c : cand) {
-    const int gran = c.pair ? 32 : 16;
-    const int64_t n_r = ceil_div(r_rows, c.tile_r);
-    const int64_t w = ceil_div(ceil_div(r_rows, n_r), gran) * gran;
-    const int64_t tiles = live * ceil_div(r_rows, w) * ceil_div(s.size_c, c.pair ? 256 : 128);
-    const int64_t workers = c.pair ? kModelSms / 2 : kModelSms;
-    const double stage = std::max(2.0 * double(w), (16384.0 + double(w) * (c.pair ? 64 : 128)) / kLoadRate);
+    const int gran = c.pair ? 32 : 16, ctas = c.pair ? 2 : 1;
+    const int64_t w = ceil_div(ceil_div(r_rows, ceil_div(r_rows, c.tile_r)), gran) * gran;
+    const int64_t tiles_c = ceil_div(s.size_c, 128 * ctas);
+    const int64_t tiles = live * ceil_div(r_rows, w) * tiles_c;
+    const int64_t workers = kModelSms / ctas;
     // tiles over all groups, at most: each group may end in a partial tile
     const int64_t most = (wgrad || s.groups == 1 ? s.groups * ceil_div(s.size_r, c.tile_r)
-                                                 : s.rows / c.tile_r + std::min<int64_t>(s.groups, s.rows)) *
-                         ceil_div(s.size_c, c.pair ? 256 : 128);
-    for (int split = 1; split <= 16; split *= 2) {
-      // a split pays where it fills idle SMs, not to even out the last wave
-      if (split > 1 && tiles * split > workers) break;
-      if (split > 1 && (split > kbs || size_t(most) * (c.pair ? 2 : 1) * kLinEpiWarps * 4 > kLayerCounterBytes)) break;
-      const double waves = double(ceil_div(tiles * split, workers));
-      double t = waves * (double(ceil_div(kbs, split)) * stage) + kUnitCost;
-      if (split > 1) t += kSplitCost + double(w) * 128 * 4 * (split + 1) / kSplitRate;
+                                                 : s.rows / c.tile_r + std::min<int64_t>(s.groups, s.rows)) * tiles_c;
+    for (int split = 1; split <= 8; split *= 2) {
+      // splits fill idle SMs; their counters have a fixed place in the workspace
+      if (split > 1 && (tiles * split > 2 * workers || split > kbs ||
+                        size_t(most) * ctas * kLinEpiWarps * sizeof(unsigned) > kLayerCounterBytes))
+        break;
+      const double rows = double(w), waves = double(ceil_div(tiles * split, workers));
+      const double rate = std::min(kSmRate, kL2Rate / double(std::min<int64_t>(tiles * split, workers) * ctas));
+      const double stage = std::max({rows * kTensorNs, c.pair ? kIssuePairNs : kIssueNs,
+                                     (16384.0 + rows * 128 / ctas) / rate});
+      double t = waves * std::max(double(ceil_div(kbs, split)) * stage, rows * kDrainNs + kUnitNs) + rows * kDrainNs;
+      if (split > 1) t += kSplitNs + kSplitEachNs * split + kSplitRowNs * rows * (split + 1);
       if (best_t < 0 || t < best_t) {
         best_t = t;
         best.pair = c.pair;
