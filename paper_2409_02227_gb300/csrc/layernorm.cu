@@ -174,7 +174,7 @@ struct FwdShape {
 };
 
 template <typename T, int TEAM, bool VEC>
-__global__ void __launch_bounds__(FwdShape<T, TEAM>::THREADS, 1024 / FwdShape<T, TEAM>::THREADS)
+__global__ void __launch_bounds__(FwdShape<T, TEAM>::THREADS, 512 / FwdShape<T, TEAM>::THREADS)
 norm_forward_kernel(const NormParams p) {
   constexpr int THREADS = FwdShape<T, TEAM>::THREADS, TEAMS = FwdShape<T, TEAM>::TEAMS;
   constexpr int WARPS = TEAM / 32, VALS = fwd_vals<T>(), D = kFwdDepth;
@@ -193,9 +193,15 @@ norm_forward_kernel(const NormParams p) {
     if (row + d * step < p.rows) R::fetch(ring + d * R::RING_BYTES, p.x, row + d * step, p.ldx, n, t);
     copy_commit();
   }
+  float gamma[VALS], beta[VALS];
   int mine = 0;                                    // values this thread has
 #pragma unroll
-  for (int i = 0; i < R::SLOTS; ++i) mine += R::in(i, t, n) ? R::PER : 0;
+  for (int i = 0; i < R::SLOTS; ++i) {
+    if (!R::in(i, t, n)) continue;
+    load_params<R::PER>(p.gamma, p.param_f32, R::col(i, t), 1.0f, gamma + i * R::PER);
+    load_params<R::PER>(p.beta, p.param_f32, R::col(i, t), 0.0f, beta + i * R::PER);
+    mine += R::PER;
+  }
   const float warp_n = warp_sum(float(mine));
   const float warp_inv = warp_n > 0.0f ? 1.0f / warp_n : 0.0f;
   int at = 0, ahead = D - 1;                       // ring places of this row and of the one fetched now
@@ -237,12 +243,8 @@ norm_forward_kernel(const NormParams p) {
 #pragma unroll
     for (int i = 0; i < R::SLOTS; ++i) {
       if (!R::in(i, t, n)) continue;
-      float gamma[R::PER], beta[R::PER];
-      load_params<R::PER>(p.gamma, p.param_f32, R::col(i, t), 1.0f, gamma);
-      load_params<R::PER>(p.beta, p.param_f32, R::col(i, t), 0.0f, beta);
 #pragma unroll
-      for (int k = 0; k < R::PER; ++k)
-        x[i * R::PER + k] = fmaf(fmaf(x[i * R::PER + k], rstd, shift), gamma[k], beta[k]);
+      for (int j = i * R::PER; j < (i + 1) * R::PER; ++j) x[j] = fmaf(fmaf(x[j], rstd, shift), gamma[j], beta[j]);
       R::store(p.out, row, p.ldy, t, i, x + i * R::PER);
     }
     if (t == 0) {
@@ -278,7 +280,10 @@ __global__ void __launch_bounds__(kBwdThreads) norm_backward_kernel(const NormPa
     mean = __ldg(p.mean + row);
     rstd = __ldg(p.rstd + row);
   }
-  float dg[VALS], db[VALS];
+  float gamma[VALS], dg[VALS], db[VALS];
+#pragma unroll
+  for (int i = 0; i < R::SLOTS; ++i)
+    if (R::in(i, t, n)) load_params<R::PER>(p.gamma, p.param_f32, R::col(i, t), 1.0f, gamma + i * R::PER);
 #pragma unroll
   for (int j = 0; j < VALS; ++j) dg[j] = db[j] = 0.0f;
   int at = 0, ahead = D - 1;
@@ -295,19 +300,17 @@ __global__ void __launch_bounds__(kBwdThreads) norm_backward_kernel(const NormPa
     R::values(ring + (2 * at + 1) * R::RING_BYTES, p.dy, row, p.ldy, n, t, y);
     at = at + 1 == D ? 0 : at + 1;
     ahead = ahead + 1 == D ? 0 : ahead + 1;
+    const float off = -m * rs;
     float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
     for (int i = 0; i < R::SLOTS; ++i) {
       if (!R::in(i, t, n)) continue;
-      float gamma[R::PER];
-      load_params<R::PER>(p.gamma, p.param_f32, R::col(i, t), 1.0f, gamma);
 #pragma unroll
-      for (int k = 0; k < R::PER; ++k) {
-        const int j = i * R::PER + k;
-        x[j] = (x[j] - m) * rs;                    // xhat
+      for (int j = i * R::PER; j < (i + 1) * R::PER; ++j) {
+        x[j] = fmaf(x[j], rs, off);                // xhat
         dg[j] = fmaf(y[j], x[j], dg[j]);
         db[j] += y[j];
-        y[j] *= gamma[k];
+        y[j] *= gamma[j];
         s1 += y[j];
         s2 = fmaf(y[j], x[j], s2);
       }
@@ -321,16 +324,13 @@ __global__ void __launch_bounds__(kBwdThreads) norm_backward_kernel(const NormPa
       s1 = lanes_sum<WARPS>(o.x);
       s2 = lanes_sum<WARPS>(o.y);
     }
-    s1 *= p.inv_n;
-    s2 *= p.inv_n;
+    s1 *= p.inv_n * rs;
+    s2 *= p.inv_n * rs;
 #pragma unroll
     for (int i = 0; i < R::SLOTS; ++i) {
       if (!R::in(i, t, n)) continue;
 #pragma unroll
-      for (int k = 0; k < R::PER; ++k) {
-        const int j = i * R::PER + k;
-        x[j] = rs * fmaf(-x[j], s2, y[j] - s1);
-      }
+      for (int j = i * R::PER; j < (i + 1) * R::PER; ++j) x[j] = fmaf(-x[j], s2, fmaf(y[j], rs, -s1));
       R::store(p.out, row, p.ldx, t, i, x + i * R::PER);
     }
   }
@@ -462,7 +462,7 @@ norm_reduce_kernel(const float* part, float* dgamma, float* dbeta, int n, int ro
   const int64_t c = int64_t(blockIdx.x) * 32 + lane;
   float v = 0.0f;
   if (c < 2 * int64_t(n)) {
-#pragma unroll 4
+#pragma unroll 10
     for (int r = w; r < rows; r += kReduceWarps) v += __ldcg(part + int64_t(r) * 2 * n + c);
   }
   s[w][lane] = v;
@@ -552,6 +552,7 @@ struct NormCall {
   NormParams p;
   const goldy_layernorm_desc* d;
   bool vec, backward;
+  int team;                // 0: the row streams
   float *dgamma, *dbeta;
   int accumulate;
   void* stream;
@@ -592,8 +593,8 @@ goldy_status launch_norm(const LayerContext& ctx, void* arg) {
   if (call.backward) {
     grid = unsigned(backward_ctas(*call.d));
   } else {
-    // 2048 threads per SM, every team with rows of its own
-    const int64_t cap = int64_t(ctx.sm_count) * (2048 / k.threads);
+    // all CTAs resident at once, every team with rows of its own
+    const int64_t cap = int64_t(ctx.sm_count) * (call.team ? 512 / k.threads : 4);
     grid = unsigned(std::max<int64_t>(1, std::min<int64_t>(cap, ceil_div(call.d->rows, k.teams))));
   }
   void* args[] = {&call.p};
@@ -659,6 +660,7 @@ extern "C" goldy_status goldy_layernorm_forward(const goldy_layernorm_desc* desc
   NormCall call{};
   call.d = desc;
   call.vec = vectors(*desc, X, Y, nullptr, gamma, beta);
+  call.team = team_for(*desc, false);
   call.stream = stream;
   common_params(call.p, *desc);
   call.p.x = X;
@@ -697,6 +699,7 @@ extern "C" goldy_status goldy_layernorm_backward(const goldy_layernorm_desc* des
   NormCall call{};
   call.d = desc;
   call.vec = vectors(*desc, X, dY, dX, gamma, nullptr);
+  call.team = team_for(*desc, true);
   call.backward = true;
   call.dgamma = dgamma;
   call.dbeta = dbeta;
