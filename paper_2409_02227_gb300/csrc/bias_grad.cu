@@ -3,7 +3,7 @@
 //
 // HBM-bound: dY (and Z) are read once, dZ is written once.  A CTA sums a slice
 // of the rows for 64 columns: a warp covers 4 rows of 128 bytes per access (8
-// columns per lane), 8 warps 32 rows, kUnroll such accesses in flight.  Per
+// columns per lane), 8 warps 32 rows, kPasses such accesses in flight.  Per
 // group that its slice meets it writes one fp32 partial row.  Slice s and group
 // e use partial row s + e: along increasing rows slice and group numbers only
 // grow, so the sums are distinct.  The last slice to arrive at a column block
@@ -25,7 +25,7 @@ namespace {
 constexpr int kCols = 64;          // columns per CTA
 constexpr int kWarps = 8;
 constexpr int kLines = kWarps * 4; // rows per pass of a CTA
-constexpr int kUnroll = 4;         // passes in flight
+constexpr int kPasses = 8;         // passes in flight (half with an activation)
 constexpr int kMinRows = 32;       // rows per slice, at least
 constexpr int kTargetCtas = 608;   // 4 per SM
 
@@ -36,7 +36,8 @@ int slices_for(int64_t rows, int64_t cols) {
 }
 
 template <bool ACT>
-__global__ void __launch_bounds__(kWarps * 32) bias_grad_kernel(const BiasGradParams p) {
+__global__ void __launch_bounds__(kWarps * 32, 4) bias_grad_kernel(const BiasGradParams p) {
+  constexpr int kUnroll = ACT ? kPasses / 2 : kPasses;
   __shared__ float part[kLines][kCols];
   __shared__ unsigned arrived;
   ptx::griddep_launch_dependents();
@@ -67,41 +68,47 @@ __global__ void __launch_bounds__(kWarps * 32) bias_grad_kernel(const BiasGradPa
     float sum[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) sum[k] = 0.0f;
-    auto load = [&](const void* base, int64_t ld, int r, float (&f)[8]) {
-      const uint16_t* at = static_cast<const uint16_t*>(base) + int64_t(r) * ld + col;
-      if (vec && r < b) {
-        unpack8(*reinterpret_cast<const uint4*>(at), f);
-      } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) f[k] = r < b && k < n ? load_bf16(at, k) : 0.0f;
-      }
+    auto row = [&](const void* base, int64_t ld, int r) {
+      return static_cast<const uint16_t*>(base) + int64_t(r) * ld + col;
     };
-    for (int r0 = a + line; r0 < b; r0 += kUnroll * kLines) {
-      float f[kUnroll][8], z[kUnroll][8];
+    if (vec) {
+      for (int r0 = a + line; r0 < b; r0 += kUnroll * kLines) {
+        uint4 y[kUnroll], z[kUnroll];
 #pragma unroll
-      for (int i = 0; i < kUnroll; ++i) {
-        load(p.dy, p.lddy, r0 + i * kLines, f[i]);
-        if (ACT) load(p.z, p.ldz, r0 + i * kLines, z[i]);
-      }
-#pragma unroll
-      for (int i = 0; i < kUnroll; ++i) {
-        const int r = r0 + i * kLines;
-        if (r >= b) continue;
-        if (ACT) {
-#pragma unroll
-          for (int k = 0; k < 8; ++k) f[i][k] *= act_slope(z[i][k], p.act);
-          uint16_t* to = static_cast<uint16_t*>(p.dz) + int64_t(r) * p.lddz + col;
-          if (vec) {
-            *reinterpret_cast<uint4*>(to) = pack8(f[i]);
-          } else {
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-              if (k < n) store_bf16(to, k, f[i][k]);
-          }
+        for (int i = 0; i < kUnroll; ++i) {
+          const int r = r0 + i * kLines;
+          y[i] = make_uint4(0, 0, 0, 0);
+          if (r < b) y[i] = *reinterpret_cast<const uint4*>(row(p.dy, p.lddy, r));
+          if (ACT && r < b) z[i] = *reinterpret_cast<const uint4*>(row(p.z, p.ldz, r));
         }
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (k < n) sum[k] += f[i][k];
+        for (int i = 0; i < kUnroll; ++i) {
+          const int r = r0 + i * kLines;
+          float f[8];
+          unpack8(y[i], f);
+          if (ACT && r < b) {
+            float g[8];
+            unpack8(z[i], g);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) f[k] *= act_slope(g[k], p.act);
+            *reinterpret_cast<uint4*>(const_cast<uint16_t*>(row(p.dz, p.lddz, r))) = pack8(f);
+          }
+#pragma unroll
+          for (int k = 0; k < 8; ++k) sum[k] += f[k];
+        }
+      }
+    } else {
+      for (int r = a + line; r < b; r += kLines) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          if (k >= n) break;
+          float f = load_bf16(row(p.dy, p.lddy, r), k);
+          if (ACT) {
+            f *= act_slope(load_bf16(row(p.z, p.ldz, r), k), p.act);
+            store_bf16(const_cast<uint16_t*>(row(p.dz, p.lddz, r)), k, f);
+          }
+          sum[k] += f;
+        }
       }
     }
 #pragma unroll

@@ -127,6 +127,9 @@ struct NormParams {
   float* mean;             // forward: written, may be null
   float* rstd;
   float* part;             // backward: [grid][2][n] partial dgamma, dbeta (null: not wanted)
+  float* dgamma;
+  float* dbeta;
+  int32_t accumulate;
   int64_t ldx, ldy;        // row strides: X and dX; Y and dY
   int64_t rows;
   int32_t n;

@@ -335,28 +335,34 @@ __global__ void __launch_bounds__(kBwdThreads) norm_backward_kernel(const NormPa
     }
   }
   if (!p.part) return;
-  // teams of the CTA, in order
-  float* sums = reinterpret_cast<float*>(ring);    // [2][TEAM * VALS]
+  // the teams' sums go through shared memory, to be added in team order
+  float* sums = reinterpret_cast<float*>(ring);    // [teams][dgamma, dbeta][value][thread]
+  constexpr int ALL = TEAM * VALS;
   copy_wait<0>();
   __syncthreads();
-  for (int k = 0; k < TEAMS; ++k) {
-    if (team == k) {
 #pragma unroll
-      for (int j = 0; j < VALS; ++j) {
-        float* a = sums + j * TEAM + t;
-        a[0] = k == 0 ? dg[j] : a[0] + dg[j];
-        a[TEAM * VALS] = k == 0 ? db[j] : a[TEAM * VALS] + db[j];
-      }
-    }
-    __syncthreads();
+  for (int j = 0; j < VALS; ++j) {
+    sums[team * 2 * ALL + j * TEAM + t] = dg[j];
+    sums[team * 2 * ALL + ALL + j * TEAM + t] = db[j];
   }
+  __syncthreads();
   float* to = p.part + int64_t(blockIdx.x) * 2 * n;
-  for (int i = threadIdx.x; i < TEAM * VALS; i += kBwdThreads) {
+  for (int i = threadIdx.x; i < ALL; i += kBwdThreads) {
     const int j = i / TEAM, tt = i % TEAM;
     const int c = R::col(j / R::PER, tt) + j % R::PER;
-    if (c < n) {
-      __stcg(to + c, sums[i]);
-      __stcg(to + n + c, sums[TEAM * VALS + i]);
+    if (c >= n) continue;
+    float g = 0.0f, b = 0.0f;
+#pragma unroll
+    for (int k = 0; k < TEAMS; ++k) {
+      g += sums[k * 2 * ALL + i];
+      b += sums[k * 2 * ALL + ALL + i];
+    }
+    if (gridDim.x > 1) {
+      __stcg(to + c, g);
+      __stcg(to + n + c, b);
+    } else {                                       // this CTA's sums are the result
+      if (p.dgamma) p.dgamma[c] = p.accumulate ? p.dgamma[c] + g : g;
+      if (p.dbeta) p.dbeta[c] = p.accumulate ? p.dbeta[c] + b : b;
     }
   }
 }
@@ -501,7 +507,7 @@ Kernel pick(bool backward) {
   if (backward) {
     using R = Row<T, kBwdVals, TEAM, kBwdThreads, VEC>;
     return {reinterpret_cast<const void*>(&norm_backward_kernel<T, TEAM, VEC>), kBwdThreads, kBwdThreads / TEAM,
-            std::max(size_t(2) * bwd_depth<T>() * R::RING_BYTES, size_t(2) * TEAM * kBwdVals * sizeof(float))};
+            std::max(size_t(2) * bwd_depth<T>() * R::RING_BYTES, size_t(2) * kBwdThreads * kBwdVals * sizeof(float))};
   }
   using R = Row<T, fwd_vals<T>(), TEAM, FwdShape<T, TEAM>::THREADS, VEC>;
   return {reinterpret_cast<const void*>(&norm_forward_kernel<T, TEAM, VEC>), FwdShape<T, TEAM>::THREADS,
@@ -531,10 +537,15 @@ Kernel kernel_for(const goldy_layernorm_desc& d, bool vec, bool backward) {
 
 // CTAs of a backward launch: one partial row each
 constexpr int kBwdCtas = 152;      // one per SM
+// Rows per team up to which one CTA does them all: a further kernel that sums
+// partial rows costs 3.4 us, a further row of a team about 1.
+constexpr int kAloneRows = 3;
 int backward_ctas(const goldy_layernorm_desc& d) {
   const int team = team_for(d, true);
-  const int64_t teams = team ? kBwdThreads / team : 1;
-  return int(std::max<int64_t>(1, std::min<int64_t>(kBwdCtas, ceil_div(d.rows, teams))));
+  if (team == 0) return int(std::max<int64_t>(1, std::min<int64_t>(kBwdCtas, d.rows)));
+  const int64_t teams = kBwdThreads / team;
+  if (d.rows <= kAloneRows * teams) return 1;      // no second kernel
+  return int(std::min<int64_t>(kBwdCtas, ceil_div(d.rows, teams)));
 }
 
 goldy_status check_norm(const goldy_layernorm_desc* d) {
@@ -553,8 +564,6 @@ struct NormCall {
   const goldy_layernorm_desc* d;
   bool vec, backward;
   int team;                // 0: the row streams
-  float *dgamma, *dbeta;
-  int accumulate;
   void* stream;
 };
 
@@ -602,9 +611,9 @@ goldy_status launch_norm(const LayerContext& ctx, void* arg) {
     e = launch(k.fn, grid, unsigned(k.threads), k.smem, call.stream, args);
     if (e != cudaSuccess) return fail(GOLDY_ERR_CUDA, std::string("layer norm launch: ") + cudaGetErrorString(e));
   }
-  if (call.backward && call.p.part) {
+  if (call.backward && call.p.part && (grid > 1 || call.team == 0)) {
     int n = int(call.d->n), rows = int(grid);
-    void* rargs[] = {&call.p.part, &call.dgamma, &call.dbeta, &n, &rows, &call.accumulate};
+    void* rargs[] = {&call.p.part, &call.p.dgamma, &call.p.dbeta, &n, &rows, &call.p.accumulate};
     e = launch(reinterpret_cast<const void*>(&norm_reduce_kernel), unsigned(ceil_div(2 * call.d->n, 32)),
                kReduceWarps * 32, 0, call.stream, rargs);
     if (e != cudaSuccess) return fail(GOLDY_ERR_CUDA, std::string("layer norm launch: ") + cudaGetErrorString(e));
@@ -701,9 +710,6 @@ extern "C" goldy_status goldy_layernorm_backward(const goldy_layernorm_desc* des
   call.vec = vectors(*desc, X, dY, dX, gamma, nullptr);
   call.team = team_for(*desc, true);
   call.backward = true;
-  call.dgamma = dgamma;
-  call.dbeta = dbeta;
-  call.accumulate = accumulate;
   call.stream = stream;
   common_params(call.p, *desc);
   call.p.x = X;
@@ -712,6 +718,9 @@ extern "C" goldy_status goldy_layernorm_backward(const goldy_layernorm_desc* des
   call.p.out = dX;
   call.p.mean = const_cast<float*>(mean);
   call.p.rstd = const_cast<float*>(rstd);
+  call.p.dgamma = dgamma;
+  call.p.dbeta = dbeta;
+  call.p.accumulate = accumulate;
   call.p.part = sums ? reinterpret_cast<float*>(static_cast<char*>(workspace) + kLayerCounterBytes) : nullptr;
   st = with_layer_context(stream, launch_norm, &call);
   return st == GOLDY_OK ? ok() : st;

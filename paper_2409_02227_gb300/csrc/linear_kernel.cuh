@@ -279,137 +279,174 @@ __device__ __forceinline__ uint32_t lin_trade(uint32_t x, int odd) {
 // work waited for instructions (5.5 us a tile instead of 2).
 constexpr int kLinSides = kLinEpiWarps / 4;
 
-template <int PASS, bool OUT_F32, int ACT, bool PAIRS, typename Release>
-__device__ __forceinline__ void lin_drain(const LinearParams& p, const LinUnit& t, int lane, int side, int col0,
-                                          float bias, bool some, uint32_t cols, const float* part,
-                                          size_t split_stride, Release release) {
+constexpr int kLinNo = 0, kLinYes = 1, kLinMaybe = 2;
+
+// What a drain needs.
+struct LinDrain {
+  char* c;                 // this lane's first element of C, of R, and of Z
+  const char* q;
+  char* z;
+  int64_t c_step, q_step, z_step;   // bytes between the rows that it takes in turn
+  const float* part;       // splits' partials (null: the accumulator)
+  int64_t split_stride;
+  int split;
+  uint32_t cols;           // the accumulator's first column
+  uint32_t release;        // barrier of the accumulator's drain
+  int rows, side, lane;
+  float bias;
+  bool some;               // the sum is in the accumulator
+  bool save, has_q;        // Z is written; there is an R
+  bool in;                 // this lane's column exists
+};
+
+template <int PASS, bool PAIR, bool OUT_F32, int ACT, bool PAIRS, int RES_IS>
+__device__ __forceinline__ void lin_drain(LinDrain d) {
   constexpr bool SLOPE = PASS == kLinInputGrad && ACT != GOLDY_ACT_NONE;
   constexpr int N = PAIRS ? 4 : 8;                 // accesses per chunk and array
   constexpr int DOWN = PAIRS ? 2 : 1;              // rows between them
-  const int odd = PAIRS ? (lane & 1) : 0;
-  const int col = col0 + lane - odd;
-  const bool in = col < p.size_c;
-  const int chunks = (t.w + 7) / 8;
-  const int64_t r = int64_t(t.r0) + side * 8 + odd;
-  const bool res = p.res != nullptr;
-  const bool save = PASS == kLinForward && p.z_out != nullptr;
-  const int64_t es = OUT_F32 ? 4 : 2;
-  char* c = static_cast<char*>(p.c) + (int64_t(t.e) * p.c_group + r * p.ldc + col) * es;
-  const char* q_at = static_cast<const char*>(p.res) + (int64_t(t.e) * p.r_group + r * p.ldr + col) * es;
-  const char* z_at = static_cast<const char*>(p.z_in) + (r * p.ldz + col) * 2;
-  char* z_to = static_cast<char*>(p.z_out) + (r * p.ldz + col) * 2;
-  const int64_t c_step = DOWN * p.ldc * es, q_step = DOWN * p.ldr * es, z_step = DOWN * p.ldz * 2;
+  constexpr bool AHEAD = PAIRS || OUT_F32;         // else loaded where they are used (edges, odd strides)
+  const bool RES = RES_IS == kLinMaybe ? d.has_q : RES_IS == kLinYes;
+  const bool SAVE = PASS == kLinForward && d.save;
+  const int odd = PAIRS ? (d.lane & 1) : 0;
+  const int rows = d.in ? d.rows - odd : 0;        // this lane stores chunk-relative row i while i < rows - chunk * 8
+  const int chunks = (d.rows + 7) / 8;
+  const char* z_at = d.z;
 
-  uint32_t zn[N], qn[N], an[8];
+  uint32_t z[N], q[N], an[8];
   auto fetch = [&](int chunk) {                    // what the chunk needs from memory
-    const int left = t.w - chunk * 8 - odd;
+    const int left = chunk < chunks ? rows - chunk * 8 : 0;
     if (SLOPE) {
 #pragma unroll
-      for (int i = 0; i < N; ++i, z_at += z_step)
-        if (in && DOWN * i < left)
-          zn[i] = PAIRS ? __ldg(reinterpret_cast<const uint32_t*>(z_at)) : uint32_t(*reinterpret_cast<const uint16_t*>(z_at));
-      z_at += (kLinSides - 1) * N * z_step;
+      for (int i = 0; i < N; ++i, z_at += d.z_step)
+        if (DOWN * i < left)
+          z[i] = PAIRS ? __ldg(reinterpret_cast<const uint32_t*>(z_at)) : uint32_t(*reinterpret_cast<const uint16_t*>(z_at));
+      z_at += (kLinSides - 1) * N * d.z_step;
     }
-    if (res) {
+    if (RES) {
 #pragma unroll
-      for (int i = 0; i < N; ++i, q_at += q_step)
-        if (in && DOWN * i < left)
-          qn[i] = PAIRS || OUT_F32 ? *reinterpret_cast<const uint32_t*>(q_at)
-                                   : uint32_t(*reinterpret_cast<const uint16_t*>(q_at));
-      q_at += (kLinSides - 1) * N * q_step;
+      for (int i = 0; i < N; ++i, d.q += d.q_step)
+        if (DOWN * i < left)
+          q[i] = PAIRS || OUT_F32 ? *reinterpret_cast<const uint32_t*>(d.q)
+                                  : uint32_t(*reinterpret_cast<const uint16_t*>(d.q));
+      d.q += (kLinSides - 1) * N * d.q_step;
     }
   };
-  if (side < chunks) {
-    fetch(side);
-    if (some) lin_tmem_load(cols + uint32_t(side * 8), an);
-  }
+  auto release = [&]() {                           // this warp has read the accumulator
+    ptx::tc_fence_before();
+    __syncwarp();
+    if (d.lane == 0) {
+      if (PAIR) lin_arrive_remote(d.release);
+      else ptx::mbar_arrive(d.release);
+    }
+  };
+  if (AHEAD) fetch(d.side);
+  if (d.some && d.side < chunks) lin_tmem_load(d.cols + uint32_t(d.side * 8), an);
 #pragma unroll 1
-  for (int chunk = side; chunk < chunks; chunk += kLinSides) {
-    const int left = t.w - chunk * 8 - odd;
-    float v[8];
-    uint32_t z[N], q[N];
+  for (int chunk = d.side; chunk < chunks; chunk += kLinSides) {
+    const int left = rows - chunk * 8;
+    if (!AHEAD) fetch(chunk);
+    float v[8], slope[8];
+    uint32_t r_now[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      z[i] = SLOPE ? zn[i] : 0u;
-      q[i] = qn[i];
-    }
-    if (some) {
-      ptx::tmem_ld_wait();
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(an[j]) + bias;
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = bias;
-      if (part) {                                  // the splits' partials, in order
-        const float* from = part + (chunk / kLinSides) * 256 + lane;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = 0.0f;
-#pragma unroll 4
-        for (int s = 0; s < p.split; ++s) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) v[j] += __ldcg(from + s * split_stride + j * 32);
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += bias;
-      }
-    }
-    if (chunk + kLinSides < chunks) {
-      if (some) lin_tmem_load(cols + uint32_t((chunk + kLinSides) * 8), an);
-      fetch(chunk + kLinSides);
-    } else if (some) {
-      release();                                   // the accumulator's last chunk is in registers
-    }
-    if (save) {
-#pragma unroll
-      for (int i = 0; i < N; ++i, z_to += z_step) {
-        if (PAIRS) {
-          const uint32_t w = lin_trade(pack_bf16(v[2 * i], v[2 * i + 1]), odd);
-          if (2 * i < left) *reinterpret_cast<uint32_t*>(z_to) = w;
-        } else if (in && i < left) {
-          store_bf16(z_to, 0, v[i]);
-        }
-      }
-      z_to += (kLinSides - 1) * N * z_step;
-    }
-    if (SLOPE) {
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
+      if (SLOPE) {
         if (PAIRS) {
           const uint32_t w = lin_trade(z[i], odd);
-          v[2 * i] *= act_slope(bf16_lo(w), ACT);
-          v[2 * i + 1] *= act_slope(bf16_hi(w), ACT);
+          slope[2 * i] = act_slope(bf16_lo(w), ACT);
+          slope[2 * i + 1] = act_slope(bf16_hi(w), ACT);
         } else {
-          v[i] *= act_slope(bf16_lo(z[i]), ACT);
+          slope[i] = act_slope(bf16_lo(z[i]), ACT);
         }
       }
-    } else if (PASS == kLinForward) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = act_value(v[j], ACT);
+      if (RES) r_now[i] = q[i];
     }
-    if (res) {
+    if (AHEAD) fetch(chunk + kLinSides);
+    if (d.some) {
+      ptx::tmem_ld_wait();
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(an[j]);
+      if (chunk + kLinSides < chunks) lin_tmem_load(d.cols + uint32_t((chunk + kLinSides) * 8), an);
+      else release();                              // the last chunk is in registers
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+      if (d.part) {                                // in the splits' order
+        const float* from = d.part + (chunk / kLinSides) * 256 + d.lane;
+#pragma unroll 4
+        for (int s = 0; s < d.split; ++s) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] += __ldcg(from + s * d.split_stride + j * 32);
+        }
+      }
+    }
+    if (PASS == kLinForward) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] += d.bias;
+    }
+    if (SAVE) {
+#pragma unroll
+      for (int i = 0; i < N; ++i, d.z += d.z_step) {
+        if (PAIRS) {
+          const uint32_t w = lin_trade(pack_bf16(v[2 * i], v[2 * i + 1]), odd);
+          if (2 * i < left) *reinterpret_cast<uint32_t*>(d.z) = w;
+        } else if (i < left) {
+          store_bf16(d.z, 0, v[i]);
+        }
+      }
+      d.z += (kLinSides - 1) * N * d.z_step;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (SLOPE) v[j] *= slope[j];
+      if (PASS == kLinForward) v[j] = act_value(v[j], ACT);
+    }
+    if (RES) {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         if (PAIRS) {
-          const uint32_t w = lin_trade(q[i], odd);
+          const uint32_t w = lin_trade(r_now[i], odd);
           v[2 * i] += bf16_lo(w);
           v[2 * i + 1] += bf16_hi(w);
         } else {
-          v[i] += OUT_F32 ? __uint_as_float(q[i]) : bf16_lo(q[i]);
+          v[i] += OUT_F32 ? __uint_as_float(r_now[i]) : bf16_lo(r_now[i]);
         }
       }
     }
 #pragma unroll
-    for (int i = 0; i < N; ++i, c += c_step) {
+    for (int i = 0; i < N; ++i, d.c += d.c_step) {
       if (PAIRS) {
         const uint32_t w = lin_trade(pack_bf16(v[2 * i], v[2 * i + 1]), odd);
-        if (2 * i < left) *reinterpret_cast<uint32_t*>(c) = w;
-      } else if (in && i < left) {
-        if (OUT_F32) *reinterpret_cast<float*>(c) = v[i];
-        else store_bf16(c, 0, v[i]);
+        if (2 * i < left) *reinterpret_cast<uint32_t*>(d.c) = w;
+      } else if (i < left) {
+        if (OUT_F32) *reinterpret_cast<float*>(d.c) = v[i];
+        else store_bf16(d.c, 0, v[i]);
       }
     }
-    c += (kLinSides - 1) * N * c_step;
+    d.c += (kLinSides - 1) * N * d.c_step;
   }
+}
+
+template <int PASS, bool PAIR, bool OUT_F32, int ACT, bool PAIRS>
+__device__ __forceinline__ void lin_drain_as(const LinearParams& p, const LinUnit& t, int col0, LinDrain d) {
+  constexpr int64_t ES = OUT_F32 ? 4 : 2;
+  const int odd = PAIRS ? (d.lane & 1) : 0;
+  const int col = col0 + d.lane - odd;
+  const int64_t r = int64_t(t.r0) + d.side * 8 + odd;
+  const int64_t down = PAIRS ? 2 : 1;
+  const void* z = PASS == kLinInputGrad ? p.z_in : p.z_out;
+  d.in = col < p.size_c;
+  d.c = static_cast<char*>(p.c) + (int64_t(t.e) * p.c_group + r * p.ldc + col) * ES;
+  d.q = static_cast<const char*>(p.res) + (int64_t(t.e) * p.r_group + r * p.ldr + col) * ES;
+  d.z = static_cast<char*>(const_cast<void*>(z)) + (r * p.ldz + col) * 2;
+  d.c_step = down * p.ldc * ES;
+  d.q_step = down * p.ldr * ES;
+  d.z_step = down * p.ldz * 2;
+  d.save = p.z_out != nullptr;
+  d.has_q = p.res != nullptr;
+  // a drain of its own with a residual where that costs no registers
+  if (PASS == kLinInputGrad || !(PAIRS || OUT_F32)) lin_drain<PASS, PAIR, OUT_F32, ACT, PAIRS, kLinMaybe>(d);
+  else if (p.res) lin_drain<PASS, PAIR, OUT_F32, ACT, PAIRS, kLinYes>(d);
+  else lin_drain<PASS, PAIR, OUT_F32, ACT, PAIRS, kLinNo>(d);
 }
 
 template <int PASS, int ACT, bool PAIR, bool OUT_F32>
@@ -812,11 +849,21 @@ __global__ void __launch_bounds__(lin_threads(PASS), 1) linear_kernel(const __gr
         __threadfence();
       }
       const bool from_acc = some && !split;
-      const float* sums = split ? part : nullptr;
+      LinDrain d;
+      d.part = split ? part : nullptr;
+      d.split_stride = int64_t(split_stride);
+      d.split = p.split;
+      d.cols = cols;
+      d.release = PAIR ? ptx::map_to_rank(ptx::smem_u32(&tempty[acc]), 0) : ptx::smem_u32(&tempty[acc]);
+      d.rows = t.w;
+      d.side = side;
+      d.lane = lane;
+      d.bias = bias;
+      d.some = from_acc;
       if (!OUT_F32 && p.vec && col0 + 32 <= p.size_c)
-        lin_drain<PASS, OUT_F32, ACT, !OUT_F32>(p, t, lane, side, col0, bias, from_acc, cols, sums, split_stride, release);
+        lin_drain_as<PASS, PAIR, OUT_F32, ACT, !OUT_F32>(p, t, col0, d);
       else
-        lin_drain<PASS, OUT_F32, ACT, false>(p, t, lane, side, col0, bias, from_acc, cols, sums, split_stride, release);
+        lin_drain_as<PASS, PAIR, OUT_F32, ACT, false>(p, t, col0, d);
       if (from_acc) {
         if (side >= chunks) release();                 // no chunk of this warp's
         next_acc();
