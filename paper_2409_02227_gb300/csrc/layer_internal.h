@@ -47,6 +47,9 @@ constexpr int lin_threads(int pass) { return (2 + kLinEpiWarps + (pass == kLinWe
 constexpr int kLinStageK = 64;            // reduction elements per pipeline stage
 constexpr int kLinMaxStages = 12;
 constexpr int kLinRowBand = 8;            // row tiles walked before the next column tile
+// rows per tile of an fp32 result: its sums take registers, and 256 rows' did
+// not fit (spilled: 2048 x 8192 input gradient over 2048 columns 57 us, now 53)
+constexpr int kLinMaxTileF32 = 192;
 constexpr int kLinPromote = 12;           // stages accumulated in tensor memory for fp32 results
 constexpr int kLinSmemBudget = 232448;    // 227 KB
 

@@ -99,6 +99,7 @@ LinChoice choose(const LinShape& s) {
   LinChoice best{0, 16, 1, 0, 0};
   double best_t = -1.0;
   for (const Candidate& c : cand) {
+    if (s.out_dtype == GOLDY_F32 && c.tile_r > kLinMaxTileF32) continue;
     const int gran = c.pair ? 32 : 16, ctas = c.pair ? 2 : 1;
     const int64_t w = ceil_div(ceil_div(r_rows, ceil_div(r_rows, c.tile_r)), gran) * gran;
     const int64_t tiles_c = ceil_div(s.size_c, 128 * ctas);

@@ -70,6 +70,39 @@ __device__ __forceinline__ bool lin_elect(int& leader) {
   return one != 0;
 }
 
+// One K = 16 step of a product, operands by the low words of their shared-memory
+// descriptors (the address in 16-byte units and the leading offset); the high
+// words are constant, which leaves an addition per step to the issuing lane.
+template <bool PAIR>
+__device__ __forceinline__ void lin_mma(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t add) {
+  constexpr uint32_t HI = (1024u >> 4) | (1u << 14) | (2u << 29);   // 8-row groups 1024 bytes apart, version 1, 128-byte swizzle
+  if (PAIR)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\t"
+        "mov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %3, p;\n\t}" ::"r"(d),
+        "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(add), "r"(HI)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\t"
+        "mov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}" ::"r"(d),
+        "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(add), "r"(HI)
+        : "memory");
+}
+
+// Whether the phase with parity `parity` has completed, without waiting.
+__device__ __forceinline__ bool lin_test(uint32_t bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(done)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return done != 0;
+}
+
 // A value that all lanes share, in a form that the compiler knows to be shared.
 __device__ __forceinline__ int lin_shared(int x) { return __shfl_sync(0xFFFFFFFFu, x, 0); }
 
@@ -313,7 +346,9 @@ __device__ __forceinline__ void lin_drain(LinDrain d) {
   const char* z_at = d.z;
 
   uint32_t z[N], q[N], an[8];
-  auto fetch = [&](int chunk) {                    // what the chunk needs from memory
+  // what a chunk needs from memory, asked for as soon as the last chunk's has
+  // been used: nothing is copied, for a copy would wait for the load
+  auto fetch_z = [&](int chunk) {
     const int left = chunk < chunks ? rows - chunk * 8 : 0;
     if (SLOPE) {
 #pragma unroll
@@ -322,6 +357,9 @@ __device__ __forceinline__ void lin_drain(LinDrain d) {
           z[i] = PAIRS ? __ldg(reinterpret_cast<const uint32_t*>(z_at)) : uint32_t(*reinterpret_cast<const uint16_t*>(z_at));
       z_at += (kLinSides - 1) * N * d.z_step;
     }
+  };
+  auto fetch_q = [&](int chunk) {
+    const int left = chunk < chunks ? rows - chunk * 8 : 0;
     if (RES) {
 #pragma unroll
       for (int i = 0; i < N; ++i, d.q += d.q_step)
@@ -339,14 +377,16 @@ __device__ __forceinline__ void lin_drain(LinDrain d) {
       else ptx::mbar_arrive(d.release);
     }
   };
-  if (AHEAD) fetch(d.side);
+  if (AHEAD) {
+    fetch_z(d.side);
+    fetch_q(d.side);
+  }
   if (d.some && d.side < chunks) lin_tmem_load(d.cols + uint32_t(d.side * 8), an);
 #pragma unroll 1
   for (int chunk = d.side; chunk < chunks; chunk += kLinSides) {
     const int left = rows - chunk * 8;
-    if (!AHEAD) fetch(chunk);
+    if (!AHEAD) fetch_z(chunk);
     float v[8], slope[8];
-    uint32_t r_now[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       if (SLOPE) {
@@ -358,9 +398,8 @@ __device__ __forceinline__ void lin_drain(LinDrain d) {
           slope[i] = act_slope(bf16_lo(z[i]), ACT);
         }
       }
-      if (RES) r_now[i] = q[i];
     }
-    if (AHEAD) fetch(chunk + kLinSides);
+    if (AHEAD) fetch_z(chunk + kLinSides);
     if (d.some) {
       ptx::tmem_ld_wait();
 #pragma unroll
@@ -400,18 +439,20 @@ __device__ __forceinline__ void lin_drain(LinDrain d) {
       if (SLOPE) v[j] *= slope[j];
       if (PASS == kLinForward) v[j] = act_value(v[j], ACT);
     }
+    if (!AHEAD) fetch_q(chunk);
     if (RES) {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         if (PAIRS) {
-          const uint32_t w = lin_trade(r_now[i], odd);
+          const uint32_t w = lin_trade(q[i], odd);
           v[2 * i] += bf16_lo(w);
           v[2 * i + 1] += bf16_hi(w);
         } else {
-          v[i] += OUT_F32 ? __uint_as_float(r_now[i]) : bf16_lo(r_now[i]);
+          v[i] += OUT_F32 ? __uint_as_float(q[i]) : bf16_lo(q[i]);
         }
       }
     }
+    if (AHEAD) fetch_q(chunk + kLinSides);
 #pragma unroll
     for (int i = 0; i < N; ++i, d.c += d.c_step) {
       if (PAIRS) {
@@ -444,7 +485,7 @@ __device__ __forceinline__ void lin_drain_as(const LinearParams& p, const LinUni
   d.save = p.z_out != nullptr;
   d.has_q = p.res != nullptr;
   // a drain of its own with a residual where that costs no registers
-  if (PASS == kLinInputGrad || !(PAIRS || OUT_F32)) lin_drain<PASS, PAIR, OUT_F32, ACT, PAIRS, kLinMaybe>(d);
+  if (PASS == kLinInputGrad || !PAIRS) lin_drain<PASS, PAIR, OUT_F32, ACT, PAIRS, kLinMaybe>(d);
   else if (p.res) lin_drain<PASS, PAIR, OUT_F32, ACT, PAIRS, kLinYes>(d);
   else lin_drain<PASS, PAIR, OUT_F32, ACT, PAIRS, kLinNo>(d);
 }
@@ -625,12 +666,16 @@ __global__ void __launch_bounds__(lin_threads(PASS), 1) linear_kernel(const __gr
     if (lead) {
       int stage = 0, acc = 0, leader = 0;
       uint32_t phase = 0, acc_phase = 0, acc_used = 0;
-      bool ok = true, any = false;                     // `any` and the ring's state: the elected lane's
+      bool ok = true, any = false, ready = false;      // `any` and the ring's state: the elected lane's
+      const uint32_t full_at = ptx::smem_u32(full), words = stage_bytes >> 4;
+      const uint32_t a_base = (tiles >> 4) | (uint32_t((A_MN ? 8192 : 16) >> 4) << 16);
+      const uint32_t b_base = ((tiles + A_BYTES) >> 4) | (uint32_t((B_MN ? 8192 : 16) >> 4) << 16);
       for (int u = worker; ok && walk.find(u, t); u += n_workers) {
         const int nw = lin_shared(t.nw), kb0 = lin_shared(t.kb0), kb1 = lin_shared(t.kb1);
         const uint32_t idesc = ptx::make_idesc_bf16(128 * CTAS, 16, A_MN, B_MN) + (uint32_t((nw - 16) >> 3) << 17);
         const int step = OUT_F32 ? lin_promote(kb1 - kb0) : kb1 - kb0;
         if (lin_elect(leader)) {
+          ready = false;
           for (int kb = kb0; kb < kb1;) {
             const int stop = min(kb + step, kb1);
             if (acc_used >> acc & 1) {
@@ -642,20 +687,14 @@ __global__ void __launch_bounds__(lin_threads(PASS), 1) linear_kernel(const __gr
             const uint32_t d = tmem_base + uint32_t(acc * 256);
             uint32_t add = 0;
             for (; kb < stop; ++kb) {
-              ok = lin_wait(ptx::smem_u32(&full[stage]), phase, abort_flag);
+              if (!ready) ok = lin_wait(full_at + stage * 8, phase, abort_flag);
               if (!ok) break;
               ptx::tc_fence_after();
-              const uint32_t as = tiles + stage * stage_bytes;
-              const uint32_t bs = as + A_BYTES;
+              const uint32_t a_lo = a_base + stage * words, b_lo = b_base + stage * words;
 #pragma unroll
-              for (int kk = 0; kk < 4; ++kk) {
-                const uint64_t ad = A_MN ? ptx::make_sdesc_sw128(as + kk * 2048, 8192, 1024)
-                                         : ptx::make_sdesc_sw128(as + kk * 32, 16, 1024);
-                const uint64_t bd = B_MN ? ptx::make_sdesc_sw128(bs + kk * 2048, 8192, 1024)
-                                         : ptx::make_sdesc_sw128(bs + kk * 32, 16, 1024);
-                if (PAIR) ptx::mma_bf16_pair(d, ad, bd, idesc, kk > 0 ? 1u : add);
-                else ptx::mma_bf16(d, ad, bd, idesc, kk > 0 ? 1u : add);
-              }
+              for (int kk = 0; kk < 4; ++kk)
+                lin_mma<PAIR>(d, a_lo + kk * (A_MN ? 2048 : 32) / 16, b_lo + kk * (B_MN ? 2048 : 32) / 16, idesc,
+                              kk > 0 ? 1u : add);
               if (PAIR) ptx::mma_commit_pair_multicast(ptx::smem_u32(&empty[stage]), 0x3);
               else ptx::mma_commit(ptx::smem_u32(&empty[stage]));
               add = 1;
@@ -664,6 +703,7 @@ __global__ void __launch_bounds__(lin_threads(PASS), 1) linear_kernel(const __gr
                 stage = 0;
                 phase ^= 1;
               }
+              ready = lin_test(full_at + stage * 8, phase);   // the answer arrives behind the loop's end
             }
             if (!ok) break;
             if (PAIR) ptx::mma_commit_pair_multicast(ptx::smem_u32(&tfull[acc]), 0x3);
@@ -724,7 +764,7 @@ __global__ void __launch_bounds__(lin_threads(PASS), 1) linear_kernel(const __gr
     if (!ok && lane == 0) raise_error(p.err, abort_flag, kErrProducerWait);
   } else {
     // ------------------------------------------------------------ epilogue
-    constexpr int MOST = (32 + kLinSides - 1) / kLinSides;   // 8-row chunks of a tile per warp, at most
+    constexpr int MOST = (kLinMaxTileF32 / 8 + kLinSides - 1) / kLinSides;   // 8-row chunks of an fp32 tile per warp
     const int ew = warp - 2;
     const int q = warp & 3;                            // lanes of tensor memory this warp may read
     const int side = ew >> 2;                          // takes chunks side, side + kLinSides, ...
