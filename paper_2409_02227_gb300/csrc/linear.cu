@@ -74,7 +74,7 @@ int part_chunks(int tile_r) { return int(ceil_div(ceil_div(tile_r, 8), kLinEpiWa
 
 // Time model of a launch in ns, fitted to the times of 46 shapes (1 to 8192
 // rows, 64 to 8192 features, 0 to 64 groups, all passes) under every tile and
-// split: the choice is 2% slower than the best measured one on average, 23% at
+// split: the choice is 2% slower than the best measured one on average, 24% at
 // worst (9 rows per group on average, where sizes spread past one tile).
 //   A 64-deep stage of an nw-row tile costs the largest of its tensor time, the
 //   issue of its copies and products, and its operands' trip from L2.
@@ -83,10 +83,10 @@ int part_chunks(int tile_r) { return int(ceil_div(ceil_div(tile_r, 8), kLinEpiWa
 //   A split adds its partials' trip through L2.
 // Group sizes are on the device, so groups are taken as equal.
 constexpr double kTensorNs = 1.04;       // per row of a stage
-constexpr double kIssueNs = 110.0, kIssuePairNs = 258.0;
-constexpr double kSmRate = 237.0, kL2Rate = 21226.0;   // bytes per ns into one SM, into all
-constexpr double kDrainNs = 5.6, kUnitNs = 404.0;      // per row of a tile; per unit
-constexpr double kSplitNs = 418.0, kSplitEachNs = 99.0, kSplitRowNs = 3.9;
+constexpr double kIssueNs = 93.0, kIssuePairNs = 333.0;
+constexpr double kSmRate = 102.0, kL2Rate = 15655.0;   // bytes per ns into one SM, into all
+constexpr double kDrainNs = 8.7, kUnitNs = 654.0;      // per row of a tile; per unit
+constexpr double kSplitNs = 771.0, kSplitEachNs = 195.0, kSplitRowNs = 2.0;
 
 LinChoice choose(const LinShape& s) {
   struct Candidate { int pair, tile_r; };
