@@ -273,8 +273,10 @@ struct LinWalk {
   }
 };
 
-__device__ __forceinline__ void lin_prefetch(const void* at) {
-  asm volatile("prefetch.global.L2 [%0];" ::"l"(at));
+// Brings `bytes` from `at` on into L2.
+__device__ __forceinline__ void lin_prefetch(const char* at, int bytes) {
+  for (int i = 0; i < bytes; i += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(at + i));
+  asm volatile("prefetch.global.L2 [%0];" ::"l"(at + bytes - 1));
 }
 
 // 8 accumulator columns of this warp's 32 lanes: tensor memory -> registers,
@@ -644,6 +646,22 @@ __global__ void __launch_bounds__(lin_threads(PASS), 1) linear_kernel(const __gr
       }
       __syncwarp();
       ok = __shfl_sync(0xFFFFFFFFu, ok, leader);
+      // the tile's rows of Z and R come into L2 while its products, and the
+      // drain of the tile before, are under way (a warp's 32 columns and its
+      // neighbours' fill whole lines)
+      if (PASS == kLinInputGrad ? (p.z_in || p.res) : p.res != nullptr) {
+        const int first = t.c0 + int(rank) * 128, last = min(first + 128, p.size_c) - 1;
+        for (int row = lane; row < t.w && last >= first; row += 32) {
+          const int64_t r = int64_t(t.r0) + row;
+          if (PASS == kLinInputGrad && p.z_in)
+            lin_prefetch(static_cast<const char*>(p.z_in) + (r * p.ldz + first) * 2, (last - first + 1) * 2);
+          if (p.res) {
+            constexpr int ES = OUT_F32 ? 4 : 2;
+            lin_prefetch(static_cast<const char*>(p.res) + (int64_t(t.e) * p.r_group + r * p.ldr + first) * ES,
+                         (last - first + 1) * ES);
+          }
+        }
+      }
     }
     if (!ok && lane == 0) raise_error(p.err, abort_flag, kErrProducerWait);
     // every stage filled must have been consumed (and, for a pair, both CTAs'
@@ -793,38 +811,33 @@ __global__ void __launch_bounds__(lin_threads(PASS), 1) linear_kernel(const __gr
         const int64_t at = int64_t(t.e) * p.size_c + col0 + lane;
         bias = p.bias_f32 ? static_cast<const float*>(p.bias)[at] : load_bf16(p.bias, at);
       }
-      // the tile's rows of Z and R come into L2 while its products are computed
-      // (a 32-column segment is one or two 128-byte lines)
-      if (col0 < p.size_c && (PASS == kLinInputGrad ? (p.z_in || p.res) : p.res != nullptr)) {
-        const int last_col = min(col0 + 31, p.size_c - 1);
-        for (int row = side * 32 + lane; row < t.w; row += kLinSides * 32) {
-          const int64_t r = int64_t(t.r0) + row;
-          if (PASS == kLinInputGrad && p.z_in) {
-            const char* z = static_cast<const char*>(p.z_in) + r * p.ldz * 2;
-            lin_prefetch(z + int64_t(col0) * 2);
-            lin_prefetch(z + int64_t(last_col) * 2);
-          }
-          if (p.res) {
-            constexpr int64_t ES = OUT_F32 ? 4 : 2;
-            const char* q = static_cast<const char*>(p.res) + (int64_t(t.e) * p.r_group + r * p.ldr) * ES;
-            lin_prefetch(q + col0 * ES);
-            lin_prefetch(q + last_col * ES);
-          }
-        }
-      }
       const int chunks = (t.w + 7) / 8;
       const bool some = t.kb1 > t.kb0;                 // else the sum is empty and no accumulator is used
       const bool split = p.split > 1;
       uint32_t cols = tmem_base + (uint32_t(q * 32) << 16) + uint32_t(acc * 256);
       if (OUT_F32 && t.kb1 - t.kb0 > kLinPromote) {
-        // sum the accumulators of some kLinPromote stages each; the total goes
-        // back into the last one's tensor memory, where the code below finds it
+        // sum the accumulators of some kLinPromote stages each.  A weight
+        // gradient is stored from here, starting from what it is added to, so
+        // that the last accumulator is free at once; other totals go back into
+        // the last one's tensor memory, where the code below finds them.
         const int step = lin_promote(t.kb1 - t.kb0);
+        const bool direct = PASS == kLinWeightGrad && !split;
+        const int64_t c_step = p.ldc * 4;
+        char* c_out = static_cast<char*>(p.c) + (int64_t(t.e) * p.c_group + (int64_t(t.r0) + side * 8) * p.ldc + col0 + lane) * 4;
+        const int c_rows = col0 + lane < p.size_c ? t.w - side * 8 : 0;
         float sum[MOST][8];
 #pragma unroll
         for (int i = 0; i < MOST; ++i)
 #pragma unroll
           for (int j = 0; j < 8; ++j) sum[i][j] = 0.0f;
+        if (direct && p.res) {
+          const char* from = c_out;
+#pragma unroll
+          for (int i = 0; i < MOST; ++i, from += (kLinSides - 1) * 8 * c_step)
+#pragma unroll
+            for (int j = 0; j < 8; ++j, from += c_step)
+              if (i * kLinSides * 8 + j < c_rows) sum[i][j] = *reinterpret_cast<const float*>(from);
+        }
         for (int kb = t.kb0; kb < t.kb1; kb += step) {
           ok = lin_wait_warp(ptx::smem_u32(&tfull[acc]), acc_phase, abort_flag);
           if (!ok) break;
@@ -841,12 +854,20 @@ __global__ void __launch_bounds__(lin_threads(PASS), 1) linear_kernel(const __gr
               for (int j = 0; j < 8; ++j) sum[i][j] += __uint_as_float(raw[j]);
             }
           }
-          if (kb + step < t.kb1) {
+          if (direct || kb + step < t.kb1) {
             release();
             next_acc();
           }
         }
         if (!ok) break;
+        if (direct) {
+#pragma unroll
+          for (int i = 0; i < MOST; ++i, c_out += (kLinSides - 1) * 8 * c_step)
+#pragma unroll
+            for (int j = 0; j < 8; ++j, c_out += c_step)
+              if (i * kLinSides * 8 + j < c_rows) *reinterpret_cast<float*>(c_out) = sum[i][j];
+          continue;
+        }
 #pragma unroll
         for (int i = 0; i < MOST; ++i)
           if (side + kLinSides * i < chunks) lin_tmem_store(cols + uint32_t((side + kLinSides * i) * 8), sum[i]);
