@@ -136,6 +136,17 @@ __global__ void __launch_bounds__(kWarps * 32, 4) bias_grad_kernel(const BiasGra
   if (arrived != unsigned(p.slices - 1)) return;
   __threadfence();
   if (threadIdx.x == 0) p.cnt[blockIdx.x] = 0u;
+  // the sum of 12 partial rows i, i + step, ... below `end`, in flight together
+  auto partials = [&](int i, int step, int end, int g) {
+    const int col_at = c0 + int(threadIdx.x) % kCols;
+    float t[12], s = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 12; ++k)
+      t[k] = i + k * step < end ? __ldcg(p.part + int64_t(i + k * step + g) * p.cols + col_at) : 0.0f;
+#pragma unroll
+    for (int k = 0; k < 12; ++k) s += t[k];
+    return s;
+  };
   // Four threads per column share the groups, or the slices of a single one.
   constexpr int kShare = kWarps * 32 / kCols;
   const int mine = threadIdx.x / kCols, c = c0 + int(threadIdx.x) % kCols;
@@ -143,8 +154,7 @@ __global__ void __launch_bounds__(kWarps * 32, 4) bias_grad_kernel(const BiasGra
     float s = 0.0f;
     if (c < p.cols && p.rows > 0) {
       const int used = (p.rows + height - 1) / height;
-#pragma unroll 8
-      for (int i = mine; i < used; i += kShare) s += __ldcg(p.part + int64_t(i) * p.cols + c);
+      for (int i0 = mine; i0 < used; i0 += 12 * kShare) s += partials(i0, kShare, used, 0);
     }
     part[mine][threadIdx.x % kCols] = s;
     __syncthreads();
@@ -174,8 +184,7 @@ __global__ void __launch_bounds__(kWarps * 32, 4) bias_grad_kernel(const BiasGra
     for (int k = 0; k < 4; ++k) {
       const int g = g0 + k * kShare;
       if (g >= p.groups) break;
-#pragma unroll 4
-      for (int j = i[k] + 1; j <= last[k]; ++j) s[k] += __ldcg(p.part + int64_t(j + g) * p.cols + c);
+      for (int j = i[k] + 1; j <= last[k]; j += 12) s[k] += partials(j, 1, last[k] + 1, g);
       float* to = p.db + int64_t(g) * p.cols + c;
       *to = p.accumulate ? *to + s[k] : s[k];
     }
