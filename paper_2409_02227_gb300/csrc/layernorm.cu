@@ -5,8 +5,8 @@
 //   dx = rstd (g - sum(g) / n - xhat sum(g xhat) / n),  dgamma = sum over rows of dy xhat,  dbeta = sum over rows of dy
 //
 // HBM-bound: x (and dy) read once, y (or dx) written once.  A team of 32 to 512
-// threads, by the row's length, holds a row in registers (64 bytes per thread
-// forwards, 16 values backwards), so both statistics passes of the forward
+// threads, by the row's length, holds a row in registers (16 or 32 values per
+// thread), so both statistics passes of the forward
 // direction and the two sums of the backward direction cost no second read.
 // The next rows are on their way meanwhile: each thread copies its own pieces
 // into shared memory with cp.async and reads back only those, so that rows in
@@ -41,7 +41,11 @@ constexpr int kStreamThreads = 512;
 constexpr int kFwdThreads = 256;    // per CTA, at least the team
 constexpr int kBwdThreads = 512;
 // values of a row per thread, and rows in a thread's ring
-template <typename T> __host__ __device__ constexpr int fwd_vals() { return 64 / int(sizeof(T)); }
+// Values of a row per thread: 16 up to 256 threads (4096 values; 16384 rows of
+// 4096 take 44 us, with 32 values 50), then 32 (8192 rows of 8192: 45 us, with
+// 16 values and 512 threads 55).
+constexpr int kFwdVals = 16, kFwdMoreVals = 32;
+constexpr int kFwdTeam = 256;
 constexpr int kBwdVals = 16;
 constexpr int kFwdDepth = 3;
 // CTAs of a backward launch: one partial row each
@@ -169,17 +173,18 @@ __device__ __forceinline__ void team_sync(int team) {
   else ptx::named_bar_sync(uint32_t(team + 1), TEAM);
 }
 
-template <typename T, int TEAM>
+template <int TEAM, int VALS, bool VEC>
 struct FwdShape {
   static constexpr int THREADS = TEAM > kFwdThreads ? TEAM : kFwdThreads;
   static constexpr int TEAMS = THREADS / TEAM;
+  static constexpr int CTAS = VALS > 16 || !VEC ? 512 / THREADS : 3;   // per SM, by registers
 };
 
-template <typename T, int TEAM, bool VEC>
-__global__ void __launch_bounds__(FwdShape<T, TEAM>::THREADS, 512 / FwdShape<T, TEAM>::THREADS)
+template <typename T, int TEAM, int VALS, bool VEC>
+__global__ void __launch_bounds__(FwdShape<TEAM, VALS, VEC>::THREADS, FwdShape<TEAM, VALS, VEC>::CTAS)
 norm_forward_kernel(const NormParams p) {
-  constexpr int THREADS = FwdShape<T, TEAM>::THREADS, TEAMS = FwdShape<T, TEAM>::TEAMS;
-  constexpr int WARPS = TEAM / 32, VALS = fwd_vals<T>(), D = kFwdDepth;
+  constexpr int THREADS = FwdShape<TEAM, VALS, VEC>::THREADS, TEAMS = FwdShape<TEAM, VALS, VEC>::TEAMS;
+  constexpr int WARPS = TEAM / 32, D = kFwdDepth;
   using R = Row<T, VALS, TEAM, THREADS, VEC>;
   __shared__ float4 slot[2][TEAMS][WARPS];         // per warp: sum, M2, elements, mean
   extern __shared__ __align__(16) uint8_t ring[];
@@ -510,30 +515,39 @@ norm_reduce_kernel(const float* part, float* dgamma, float* dbeta, int n, int ro
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 goldy_status bad(const std::string& why) { return fail(GOLDY_ERR_INVALID_ARG, why); }
 
-// Threads per row; 0: the row streams.
+// Threads per row at 16 values each (forwards, more than kFwdTeam stand for half
+// as many with 32); 0: the row streams.
 int team_for(const goldy_layernorm_desc& d, bool backward) {
-  const int64_t vals = backward ? kBwdVals : d.dtype == GOLDY_F32 ? fwd_vals<float>() : fwd_vals<uint16_t>();
+  const int most = backward ? kMaxTeam : 2 * kMaxTeam;
+  const int64_t vals = backward ? kBwdVals : kFwdVals;
   int team = 32;
-  while (team < kMaxTeam && team * vals < d.n) team *= 2;
+  while (team < most && team * vals < d.n) team *= 2;
   return team * vals >= d.n ? team : 0;
 }
 
 struct Kernel {
   const void* fn;
-  int threads, teams;
+  int threads, teams, per_sm;      // per_sm: CTAs resident
   size_t smem;
 };
+
+template <typename T, int TEAM, int VALS, bool VEC>
+Kernel pick_forward() {
+  using S = FwdShape<TEAM, VALS, VEC>;
+  using R = Row<T, VALS, TEAM, S::THREADS, VEC>;
+  return {reinterpret_cast<const void*>(&norm_forward_kernel<T, TEAM, VALS, VEC>), S::THREADS, S::TEAMS, S::CTAS,
+          size_t(kFwdDepth) * R::RING_BYTES};
+}
 
 template <typename T, int TEAM, bool VEC>
 Kernel pick(bool backward) {
   if (backward) {
     using R = Row<T, kBwdVals, TEAM, kBwdThreads, VEC>;
-    return {reinterpret_cast<const void*>(&norm_backward_kernel<T, TEAM, VEC>), kBwdThreads, kBwdThreads / TEAM,
+    return {reinterpret_cast<const void*>(&norm_backward_kernel<T, TEAM, VEC>), kBwdThreads, kBwdThreads / TEAM, 1,
             std::max(size_t(2) * bwd_depth<T>() * R::RING_BYTES, size_t(2) * kBwdThreads * kBwdVals * sizeof(float))};
   }
-  using R = Row<T, fwd_vals<T>(), TEAM, FwdShape<T, TEAM>::THREADS, VEC>;
-  return {reinterpret_cast<const void*>(&norm_forward_kernel<T, TEAM, VEC>), FwdShape<T, TEAM>::THREADS,
-          FwdShape<T, TEAM>::TEAMS, size_t(kFwdDepth) * R::RING_BYTES};
+  if constexpr (TEAM > kFwdTeam) return pick_forward<T, TEAM / 2, kFwdMoreVals, VEC>();
+  else return pick_forward<T, TEAM, kFwdVals, VEC>();
 }
 
 template <typename T, bool VEC>
@@ -544,10 +558,11 @@ Kernel pick_team(int team, bool backward) {
     case 128: return pick<T, 128, VEC>(backward);
     case 256: return pick<T, 256, VEC>(backward);
     case 512: return pick<T, 512, VEC>(backward);
+    case 2 * kMaxTeam: return pick_forward<T, kMaxTeam, kFwdMoreVals, VEC>();
     default:
       return {backward ? reinterpret_cast<const void*>(&norm_backward_stream_kernel<T>)
                        : reinterpret_cast<const void*>(&norm_forward_stream_kernel<T>),
-              kStreamThreads, 1, 0};
+              kStreamThreads, 1, 4, 0};
   }
 }
 
@@ -623,7 +638,7 @@ goldy_status launch_norm(const LayerContext& ctx, void* arg) {
     grid = unsigned(backward_ctas(*call.d));
   } else {
     // all CTAs resident at once, every team with rows of its own
-    const int64_t cap = int64_t(ctx.sm_count) * (call.team ? 512 / k.threads : 4);
+    const int64_t cap = int64_t(ctx.sm_count) * k.per_sm;
     grid = unsigned(std::max<int64_t>(1, std::min<int64_t>(cap, ceil_div(call.d->rows, k.teams))));
   }
   void* args[] = {&call.p};

@@ -21,7 +21,7 @@ NAN = float("nan")
 
 
 def depth_of(n):
-    return (16 if n <= 8192 else -(-n // 512)) + 5 + 16
+    return (16 if n <= 4096 else 32 if n <= 16384 else -(-n // 512)) + 5 + 16
 
 
 def padded(t, ld, dtype):
@@ -90,7 +90,7 @@ def check_forward(x64, y, mean, rstd, gamma, beta, dtype, eps=1e-5):
 
 SIZES = [(1, 1), (3, 2), (2, 7), (5, 16), (150, 31), (33, 33), (1, 500), (1000, 512), (4, 513), (77, 1000), (300, 1023),
          (2000, 1024), (9, 1025), (129, 2048), (310, 2500), (1, 4096), (700, 4096), (20, 5000), (40, 8192), (3, 8193),
-         (160, 10001)]
+         (160, 10001), (30, 16384), (5, 16390)]
 
 
 @pytest.mark.parametrize("rows,n", SIZES)
