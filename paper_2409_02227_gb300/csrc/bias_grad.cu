@@ -231,7 +231,7 @@ using namespace goldy;
 
 extern "C" goldy_status goldy_linear_bias_grad(const goldy_linear_desc* desc, const int32_t* offsets, const void* dY,
                                                const void* Z, void* dZ, float* db, int accumulate, void* workspace,
-                                               size_t workspace_bytes, void* stream) {
+                                               size_t workspace_bytes, void* stream) try {
   goldy_status st = check_linear(desc);
   if (st == GOLDY_OK) st = check_offsets(*desc, offsets);
   if (st != GOLDY_OK) return st;
@@ -274,4 +274,6 @@ extern "C" goldy_status goldy_linear_bias_grad(const goldy_linear_desc* desc, co
   call.stream = stream;
   st = with_layer_context(stream, launch_bias_grad, &call);
   return st == GOLDY_OK ? ok() : st;
+} catch (...) {
+  return layer_exception();
 }

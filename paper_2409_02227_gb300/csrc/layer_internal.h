@@ -28,6 +28,10 @@ struct LayerContext {
 // current on this thread.
 goldy_status with_layer_context(void* stream, goldy_status (*body)(const LayerContext&, void*), void* arg);
 
+// What an entry point answers when C++ raised an exception inside it (host
+// memory for an error text or a table): nothing is thrown across the ABI.
+goldy_status layer_exception();
+
 // One workspace serves every layer operator: a fixed counter area in front
 // (zero between calls), fp32 partial results behind it.
 constexpr size_t kLayerCounterBytes = 64 * 1024;

@@ -684,16 +684,18 @@ void common_params(NormParams& p, const goldy_layernorm_desc& d) {
 
 using namespace goldy;
 
-extern "C" goldy_status goldy_layernorm_query(const goldy_layernorm_desc* desc, size_t* workspace_bytes) {
+extern "C" goldy_status goldy_layernorm_query(const goldy_layernorm_desc* desc, size_t* workspace_bytes) try {
   goldy_status st = check_norm(desc);
   if (st != GOLDY_OK) return st;
   if (!workspace_bytes) return bad("null argument");
   *workspace_bytes = desc->n > 0 ? backward_bytes(*desc) : 0;
   return ok();
+} catch (...) {
+  return layer_exception();
 }
 
 extern "C" goldy_status goldy_layernorm_forward(const goldy_layernorm_desc* desc, const void* X, const void* gamma,
-                                                const void* beta, void* Y, float* mean, float* rstd, void* stream) {
+                                                const void* beta, void* Y, float* mean, float* rstd, void* stream) try {
   goldy_status st = check_norm(desc);
   if (st != GOLDY_OK) return st;
   if (desc->rows == 0 || desc->n == 0) return ok();
@@ -715,12 +717,14 @@ extern "C" goldy_status goldy_layernorm_forward(const goldy_layernorm_desc* desc
   call.p.rstd = rstd;
   st = with_layer_context(stream, launch_norm, &call);
   return st == GOLDY_OK ? ok() : st;
+} catch (...) {
+  return layer_exception();
 }
 
 extern "C" goldy_status goldy_layernorm_backward(const goldy_layernorm_desc* desc, const void* dY, const void* X,
                                                  const void* gamma, const float* mean, const float* rstd, void* dX,
                                                  float* dgamma, float* dbeta, int accumulate, void* workspace,
-                                                 size_t workspace_bytes, void* stream) {
+                                                 size_t workspace_bytes, void* stream) try {
   goldy_status st = check_norm(desc);
   if (st != GOLDY_OK) return st;
   if (accumulate != 0 && accumulate != 1) return bad("layer norm: accumulate must be 0 or 1");
@@ -759,4 +763,6 @@ extern "C" goldy_status goldy_layernorm_backward(const goldy_layernorm_desc* des
   call.p.part = sums ? reinterpret_cast<float*>(static_cast<char*>(workspace) + kLayerCounterBytes) : nullptr;
   st = with_layer_context(stream, launch_norm, &call);
   return st == GOLDY_OK ? ok() : st;
+} catch (...) {
+  return layer_exception();
 }

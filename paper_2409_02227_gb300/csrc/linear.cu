@@ -242,6 +242,7 @@ goldy_status launch_linear(const LayerContext& ctx, void* arg) {
       ws += bytes;
     }
   }
+  if (c.max_tiles * c.split > kMaxDim) return fail(GOLDY_ERR_UNSUPPORTED, "linear layer: too many output tiles");
   const bool wgrad = s.pass == kLinWeightGrad;
   const int ctas = c.pair ? 2 : 1;
   p.groups = s.groups;
@@ -323,6 +324,14 @@ goldy_status set_saved(LinearParams& p, const LinShape& s, const void* Z, int64_
 
 }  // namespace
 
+goldy_status layer_exception() {
+  try {
+    return fail(GOLDY_ERR_NOMEM, "out of host memory");
+  } catch (...) {
+    return GOLDY_ERR_NOMEM;
+  }
+}
+
 goldy_status check_linear(const goldy_linear_desc* d) {
   if (!d) return bad("null descriptor");
   if (d->rows < 0 || d->in < 0 || d->out < 0 || d->rows > kMaxDim || d->in > kMaxDim || d->out > kMaxDim)
@@ -354,7 +363,7 @@ goldy_status check_offsets(const goldy_linear_desc& d, const int32_t* offsets) {
 
 using namespace goldy;
 
-extern "C" goldy_status goldy_linear_query(const goldy_linear_desc* desc, size_t* workspace_bytes) {
+extern "C" goldy_status goldy_linear_query(const goldy_linear_desc* desc, size_t* workspace_bytes) try {
   goldy_status st = check_linear(desc);
   if (st != GOLDY_OK) return st;
   if (!workspace_bytes) return bad("null argument");
@@ -369,11 +378,13 @@ extern "C" goldy_status goldy_linear_query(const goldy_linear_desc* desc, size_t
   part = std::max(part, bias_grad_part_bytes(*desc));
   *workspace_bytes = part > 0 ? kLayerCounterBytes + part : 0;
   return ok();
+} catch (...) {
+  return layer_exception();
 }
 
 extern "C" goldy_status goldy_linear_forward(const goldy_linear_desc* desc, const int32_t* offsets, const void* X,
                                              const void* W, const void* bias, const void* R, void* Z, void* Y,
-                                             void* workspace, size_t workspace_bytes, void* stream) {
+                                             void* workspace, size_t workspace_bytes, void* stream) try {
   goldy_status st = check_linear(desc);
   if (st == GOLDY_OK) st = check_offsets(*desc, offsets);
   if (st != GOLDY_OK) return st;
@@ -401,11 +412,13 @@ extern "C" goldy_status goldy_linear_forward(const goldy_linear_desc* desc, cons
   call.stream = stream;
   st = with_layer_context(stream, launch_linear, &call);
   return st == GOLDY_OK ? ok() : st;
+} catch (...) {
+  return layer_exception();
 }
 
 extern "C" goldy_status goldy_linear_input_grad(const goldy_linear_desc* desc, const int32_t* offsets, const void* dY,
                                                 const void* W, const void* Z, const void* R, void* dX, void* workspace,
-                                                size_t workspace_bytes, void* stream) {
+                                                size_t workspace_bytes, void* stream) try {
   goldy_status st = check_linear(desc);
   if (st == GOLDY_OK) st = check_offsets(*desc, offsets);
   if (st != GOLDY_OK) return st;
@@ -432,11 +445,13 @@ extern "C" goldy_status goldy_linear_input_grad(const goldy_linear_desc* desc, c
   call.stream = stream;
   st = with_layer_context(stream, launch_linear, &call);
   return st == GOLDY_OK ? ok() : st;
+} catch (...) {
+  return layer_exception();
 }
 
 extern "C" goldy_status goldy_linear_weight_grad(const goldy_linear_desc* desc, const int32_t* offsets, const void* X,
                                                  const void* dY, void* dW, int accumulate, void* workspace,
-                                                 size_t workspace_bytes, void* stream) {
+                                                 size_t workspace_bytes, void* stream) try {
   goldy_status st = check_linear(desc);
   if (st == GOLDY_OK) st = check_offsets(*desc, offsets);
   if (st != GOLDY_OK) return st;
@@ -462,4 +477,6 @@ extern "C" goldy_status goldy_linear_weight_grad(const goldy_linear_desc* desc, 
   call.stream = stream;
   st = with_layer_context(stream, launch_linear, &call);
   return st == GOLDY_OK ? ok() : st;
+} catch (...) {
+  return layer_exception();
 }

@@ -533,3 +533,29 @@ def test_offsets_that_are_not_ordered(cuda_ok):
     G.goldy_linear_bias_grad(d, ptr(y), ptr(db), **kw)
     finish(ws)
     assert (y[rows:] == 7.0).all()
+
+
+def test_in_an_sm_partition(cuda_ok):
+    """On a partition's stream the calls run inside it, with the same results."""
+    rows, k, n, counts = 300, 512, 640, [100, 0, 37, 163]
+    gen = gen_of(12)
+    x, w, dy = matrix(gen, rows, k), matrix(gen, k, n, None, k ** -0.5, (4,)), matrix(gen, rows, n)
+    off = offsets_of(counts)
+    d = G.linear_desc(rows, k, n, groups=4, dw_dtype=F32)
+    ws = workspace(d)
+    part = G.goldy_partition_create(16, 1)
+    sms, streams = G.goldy_partition_query(part, 1)
+    assert 16 <= sms < 152
+    results = []
+    for stream in (torch.cuda.current_stream().cuda_stream, streams[0]):
+        y, dw, db = out_matrix(rows, n, BF16), out_matrix(k, n, F32, lead=(4,)), torch.empty(4, n, device="cuda")
+        torch.cuda.synchronize()
+        kw = dict(offsets=ptr(off), workspace=ptr(ws), workspace_bytes=ws.numel(), stream=stream)
+        G.goldy_linear_forward(d, ptr(x), ptr(w), ptr(y), **kw)
+        G.goldy_linear_weight_grad(d, ptr(x), ptr(dy), ptr(dw), **kw)
+        G.goldy_linear_bias_grad(d, ptr(dy), ptr(db), **kw)
+        finish(ws)
+        results.append((y, dw, db))
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+    part.close()
