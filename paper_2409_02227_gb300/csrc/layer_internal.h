@@ -21,6 +21,7 @@ typedef CUresult (*TensorMapEncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint3
 struct LayerContext {
   int device;             // current device
   int sm_count;           // SMs the stream may use (its partition's, or the device's)
+  bool whole;             // that is all of the device's
   int* err_word;          // the kernels' error word (goldy_device_error)
   TensorMapEncodeFn encode;
 };
@@ -133,7 +134,7 @@ struct NormParams {
   void* out;               // Y, or dX
   float* mean;             // forward: written, may be null
   float* rstd;
-  float* part;             // backward: [grid][2][n] partial dgamma, dbeta (null: not wanted)
+  float* part;             // backward: [CTA or cluster][2][n] partial dgamma, dbeta (null: not wanted)
   float* dgamma;
   float* dbeta;
   int32_t accumulate;
@@ -143,6 +144,8 @@ struct NormParams {
   int32_t param_f32;
   float eps;
   float inv_n;
+  int32_t cluster;         // CTAs that share a row, each with `seg` of its columns (the last with the rest)
+  int32_t seg;
 };
 
 }  // namespace goldy

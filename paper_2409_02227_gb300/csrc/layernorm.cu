@@ -18,14 +18,20 @@
 // its team and keeps dgamma and dbeta in registers; the teams of a CTA combine
 // in shared memory, one fp32 partial row per CTA goes to the workspace, and a
 // second small kernel sums the partial rows in CTA order.  Nothing depends on
-// the order of arrival.  Rows too long for a team stream through three (two)
-// reads of the row instead.
+// the order of arrival.  Rows too long for a team are shared by a cluster of 2 to
+// 8 CTAs, which exchange their statistics through distributed shared memory,
+// one cluster barrier per row (8192 rows of 12288, bf16: backwards 186 us, and
+// 1176 when such rows streamed; 2048 rows of 65536 forwards 149 and 471 us);
+// rows too long for 8 CTAs (131072 elements, backwards 65536), and those of
+// clusters inside an SM partition, stream through three (two) reads instead.
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <map>
 #include <mutex>
 #include <set>
 #include <string>
+#include <tuple>
 #include <utility>
 
 #include "goldy_internal.h"
@@ -37,6 +43,7 @@ namespace goldy {
 namespace {
 
 constexpr int kMaxTeam = 512;
+constexpr int kMaxCluster = 8;      // CTAs that may share a row
 constexpr int kStreamThreads = 512;
 constexpr int kFwdThreads = 256;    // per CTA, at least the team
 constexpr int kBwdThreads = 512;
@@ -55,6 +62,47 @@ template <typename T> __host__ __device__ constexpr int bwd_depth() { return siz
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+  return v;
+}
+
+// Two fp32 values in one register pair: this hardware multiplies and adds both
+// with one instruction, rounding each as ever (the backward pass of 8192 rows of
+// 8192 took 89 us with single values, 75 with pairs: it issues 24 instructions
+// per element otherwise).
+__device__ __forceinline__ uint64_t two(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ uint64_t two(float v) { return two(v, v); }
+__device__ __forceinline__ float2 apart(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
+// Sums of a and of b over the warp, in lanes 0 to 15 that of a, in the others
+// that of b: half the exchanges of two sums.
+__device__ __forceinline__ float warp_sum2(float a, float b, int lane) {
+  const bool upper = lane & 16;
+  float v = (upper ? b : a) + __shfl_xor_sync(0xFFFFFFFFu, upper ? a : b, 16);
+#pragma unroll
+  for (int d = 8; d > 0; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
   return v;
 }
 
@@ -165,6 +213,17 @@ struct Row {
   }
 };
 
+// What a cluster's CTAs tell one another about a row: each writes its value
+// into every CTA's place `rank`, in this CTA's shared memory at `to`.
+__device__ __forceinline__ void tell_cluster(float4* to, int rank, int cluster, float4 v) {
+  if (threadIdx.x < unsigned(cluster))
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(
+                     ptx::map_to_rank(ptx::smem_u32(to + rank), threadIdx.x)),
+                 "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w)
+                 : "memory");
+  ptx::cluster_sync_all();
+}
+
 // Barrier of one team: a warp needs none, the whole CTA has barrier 0.
 template <int TEAM, int THREADS>
 __device__ __forceinline__ void team_sync(int team) {
@@ -180,24 +239,32 @@ struct FwdShape {
   static constexpr int CTAS = VALS > 16 || !VEC ? 512 / THREADS : 3;   // per SM, by registers
 };
 
-template <typename T, int TEAM, int VALS, bool VEC>
+template <typename T, int TEAM, int VALS, bool VEC, bool WIDE>
 __global__ void __launch_bounds__(FwdShape<TEAM, VALS, VEC>::THREADS, FwdShape<TEAM, VALS, VEC>::CTAS)
 norm_forward_kernel(const NormParams p) {
   constexpr int THREADS = FwdShape<TEAM, VALS, VEC>::THREADS, TEAMS = FwdShape<TEAM, VALS, VEC>::TEAMS;
   constexpr int WARPS = TEAM / 32, D = kFwdDepth;
   using R = Row<T, VALS, TEAM, THREADS, VEC>;
   __shared__ float4 slot[2][TEAMS][WARPS];         // per warp: sum, M2, elements, mean
+  __shared__ float4 part[2][WIDE ? kMaxCluster : 1];   // per CTA of the cluster: the same
   extern __shared__ __align__(16) uint8_t ring[];
   const int team = threadIdx.x / TEAM, t = threadIdx.x % TEAM, w = t >> 5, lane = t & 31;
-  const int n = p.n;
+  // WIDE: this CTA's n columns from c0 on, of rows that a cluster shares
+  const int rank = WIDE ? int(ptx::cluster_ctarank()) : 0, c0 = WIDE ? rank * p.seg : 0;
+  const int n = WIDE ? min(p.seg, p.n - c0) : p.n;
+  const int group = WIDE ? int(blockIdx.x) / p.cluster : int(blockIdx.x);
+  const int groups = WIDE ? int(gridDim.x) / p.cluster : int(gridDim.x);
+  const T* const in = static_cast<const T*>(p.x) + c0;
+  T* const out = static_cast<T*>(p.out) + c0;
+  if (WIDE) ptx::cluster_sync_all();               // the others have started
   ptx::griddep_launch_dependents();
   ptx::griddep_wait();
-  const int64_t step = int64_t(gridDim.x) * TEAMS;
-  int64_t row = int64_t(blockIdx.x) * TEAMS + team;
+  const int64_t step = int64_t(groups) * TEAMS;
+  int64_t row = int64_t(group) * TEAMS + team;
   if (row >= p.rows) return;                       // whole teams only
 #pragma unroll
   for (int d = 0; d < D - 1; ++d) {
-    if (row + d * step < p.rows) R::fetch(ring + d * R::RING_BYTES, p.x, row + d * step, p.ldx, n, t);
+    if (row + d * step < p.rows) R::fetch(ring + d * R::RING_BYTES, in, row + d * step, p.ldx, n, t);
     copy_commit();
   }
   float gamma[VALS], beta[VALS];
@@ -205,19 +272,19 @@ norm_forward_kernel(const NormParams p) {
 #pragma unroll
   for (int i = 0; i < R::SLOTS; ++i) {
     if (!R::in(i, t, n)) continue;
-    load_params<R::PER>(p.gamma, p.param_f32, R::col(i, t), 1.0f, gamma + i * R::PER);
-    load_params<R::PER>(p.beta, p.param_f32, R::col(i, t), 0.0f, beta + i * R::PER);
+    load_params<R::PER>(p.gamma, p.param_f32, c0 + R::col(i, t), 1.0f, gamma + i * R::PER);
+    load_params<R::PER>(p.beta, p.param_f32, c0 + R::col(i, t), 0.0f, beta + i * R::PER);
     mine += R::PER;
   }
   const float warp_n = warp_sum(float(mine));
   const float warp_inv = warp_n > 0.0f ? 1.0f / warp_n : 0.0f;
   int at = 0, ahead = D - 1;                       // ring places of this row and of the one fetched now
   for (int flip = 0; row < p.rows; row += step, flip ^= 1) {
-    if (row + (D - 1) * step < p.rows) R::fetch(ring + ahead * R::RING_BYTES, p.x, row + (D - 1) * step, p.ldx, n, t);
+    if (row + (D - 1) * step < p.rows) R::fetch(ring + ahead * R::RING_BYTES, in, row + (D - 1) * step, p.ldx, n, t);
     copy_commit();
     copy_wait<D - 1>();
     float x[VALS];
-    R::values(ring + at * R::RING_BYTES, p.x, row, p.ldx, n, t, x);
+    R::values(ring + at * R::RING_BYTES, in, row, p.ldx, n, t, x);
     at = at + 1 == D ? 0 : at + 1;
     ahead = ahead + 1 == D ? 0 : ahead + 1;
     float s = 0.0f;
@@ -241,9 +308,22 @@ norm_forward_kernel(const NormParams p) {
       if (lane == 0) slot[flip][team][w] = make_float4(s, m2, warp_n, wm);
       team_sync<TEAM, THREADS>(team);
       const float4 o = slot[flip][team][lane & (WARPS - 1)];
-      mean = lanes_sum<WARPS>(o.x) * p.inv_n;
+      const float total = lanes_sum<WARPS>(o.x);
+      mean = total * (WIDE ? 1.0f / float(n) : p.inv_n);
       const float d = o.w - mean;
       m2 = lanes_sum<WARPS>(fmaf(o.z * d, d, o.y));
+      if (WIDE) {                                  // the same once more, over the cluster's CTAs in order
+        tell_cluster(part[flip], rank, p.cluster, make_float4(total, m2, float(n), mean));
+        float all = 0.0f;
+        for (int k = 0; k < p.cluster; ++k) all += part[flip][k].x;
+        mean = all * p.inv_n;
+        m2 = 0.0f;
+        for (int k = 0; k < p.cluster; ++k) {
+          const float4 o = part[flip][k];
+          const float d = o.w - mean;
+          m2 += fmaf(o.z * d, d, o.y);
+        }
+      }
     }
     const float rstd = rsqrtf(fmaf(m2, p.inv_n, p.eps));
     const float shift = (wm - mean) * rstd;
@@ -252,31 +332,39 @@ norm_forward_kernel(const NormParams p) {
       if (!R::in(i, t, n)) continue;
 #pragma unroll
       for (int j = i * R::PER; j < (i + 1) * R::PER; ++j) x[j] = fmaf(fmaf(x[j], rstd, shift), gamma[j], beta[j]);
-      R::store(p.out, row, p.ldy, t, i, x + i * R::PER);
+      R::store(out, row, p.ldy, t, i, x + i * R::PER);
     }
-    if (t == 0) {
+    if (t == 0 && rank == 0) {
       if (p.mean) p.mean[row] = mean;
       if (p.rstd) p.rstd[row] = rstd;
     }
   }
 }
 
-template <typename T, int TEAM, bool VEC>
+template <typename T, int TEAM, bool VEC, bool WIDE>
 __global__ void __launch_bounds__(kBwdThreads) norm_backward_kernel(const NormParams p) {
   constexpr int TEAMS = kBwdThreads / TEAM, WARPS = TEAM / 32, VALS = kBwdVals, D = bwd_depth<T>();
   using R = Row<T, VALS, TEAM, kBwdThreads, VEC>;
   __shared__ float2 slot[2][TEAMS][WARPS];
+  __shared__ float4 part[2][WIDE ? kMaxCluster : 1];
   extern __shared__ __align__(16) uint8_t ring[];  // D rows of x, D of dy; at the end the CTA's sums
   const int team = threadIdx.x / TEAM, t = threadIdx.x % TEAM, w = t >> 5, lane = t & 31;
-  const int n = p.n;
+  const int rank = WIDE ? int(ptx::cluster_ctarank()) : 0, c0 = WIDE ? rank * p.seg : 0;
+  const int n = WIDE ? min(p.seg, p.n - c0) : p.n;
+  const int group = WIDE ? int(blockIdx.x) / p.cluster : int(blockIdx.x);
+  const int groups = WIDE ? int(gridDim.x) / p.cluster : int(gridDim.x);
+  const T* const in = static_cast<const T*>(p.x) + c0;
+  const T* const dy = static_cast<const T*>(p.dy) + c0;
+  T* const out = static_cast<T*>(p.out) + c0;
+  if (WIDE) ptx::cluster_sync_all();               // the others have started
   ptx::griddep_launch_dependents();
   ptx::griddep_wait();
-  const int64_t step = int64_t(gridDim.x) * TEAMS;
-  int64_t row = int64_t(blockIdx.x) * TEAMS + team;
+  const int64_t step = int64_t(groups) * TEAMS;
+  int64_t row = int64_t(group) * TEAMS + team;
   auto fetch = [&](int d, int64_t r) {
     if (r < p.rows) {
-      R::fetch(ring + 2 * d * R::RING_BYTES, p.x, r, p.ldx, n, t);
-      R::fetch(ring + (2 * d + 1) * R::RING_BYTES, p.dy, r, p.ldy, n, t);
+      R::fetch(ring + 2 * d * R::RING_BYTES, in, r, p.ldx, n, t);
+      R::fetch(ring + (2 * d + 1) * R::RING_BYTES, dy, r, p.ldy, n, t);
     }
     copy_commit();
   };
@@ -287,12 +375,25 @@ __global__ void __launch_bounds__(kBwdThreads) norm_backward_kernel(const NormPa
     mean = __ldg(p.mean + row);
     rstd = __ldg(p.rstd + row);
   }
-  float gamma[VALS], dg[VALS], db[VALS];
+  // in pairs; columns outside the row have dy = gamma = 0 and add nothing
+  uint64_t gamma[VALS / 2], dg2[VALS / 2], db2[VALS / 2];
+  {
+    float f[VALS];
 #pragma unroll
-  for (int i = 0; i < R::SLOTS; ++i)
-    if (R::in(i, t, n)) load_params<R::PER>(p.gamma, p.param_f32, R::col(i, t), 1.0f, gamma + i * R::PER);
+    for (int i = 0; i < R::SLOTS; ++i) {
+      if (R::in(i, t, n)) {
+        load_params<R::PER>(p.gamma, p.param_f32, c0 + R::col(i, t), 1.0f, f + i * R::PER);
+      } else {
 #pragma unroll
-  for (int j = 0; j < VALS; ++j) dg[j] = db[j] = 0.0f;
+        for (int k = 0; k < R::PER; ++k) f[i * R::PER + k] = 0.0f;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < VALS / 2; ++j) {
+      gamma[j] = two(f[2 * j], f[2 * j + 1]);
+      dg2[j] = db2[j] = two(0.0f);
+    }
+  }
   int at = 0, ahead = D - 1;
   for (int flip = 0; row < p.rows; row += step, flip ^= 1) {
     fetch(ahead, row + (D - 1) * step);
@@ -303,43 +404,62 @@ __global__ void __launch_bounds__(kBwdThreads) norm_backward_kernel(const NormPa
     }
     copy_wait<D - 1>();
     float x[VALS], y[VALS];
-    R::values(ring + 2 * at * R::RING_BYTES, p.x, row, p.ldx, n, t, x);
-    R::values(ring + (2 * at + 1) * R::RING_BYTES, p.dy, row, p.ldy, n, t, y);
+    R::values(ring + 2 * at * R::RING_BYTES, in, row, p.ldx, n, t, x);
+    R::values(ring + (2 * at + 1) * R::RING_BYTES, dy, row, p.ldy, n, t, y);
     at = at + 1 == D ? 0 : at + 1;
     ahead = ahead + 1 == D ? 0 : ahead + 1;
-    const float off = -m * rs;
-    float s1 = 0.0f, s2 = 0.0f;
+    const uint64_t scale = two(rs), off = two(-m * rs);
+    uint64_t xhat[VALS / 2], g[VALS / 2], sum1 = two(0.0f), sum2 = sum1;
 #pragma unroll
-    for (int i = 0; i < R::SLOTS; ++i) {
-      if (!R::in(i, t, n)) continue;
+    for (int j = 0; j < VALS / 2; ++j) {
+      xhat[j] = fma2(two(x[2 * j], x[2 * j + 1]), scale, off);
+      const uint64_t d = two(y[2 * j], y[2 * j + 1]);
+      dg2[j] = fma2(d, xhat[j], dg2[j]);
+      db2[j] = add2(db2[j], d);
+      g[j] = mul2(d, gamma[j]);
+      sum1 = add2(sum1, g[j]);
+      sum2 = fma2(g[j], xhat[j], sum2);
+    }
+    const float2 a1 = apart(sum1), a2 = apart(sum2);
+    const float both = warp_sum2(a1.x + a1.y, a2.x + a2.y, lane);
+    float s1, s2;
+    if (WARPS == 1) {
+      s1 = __shfl_sync(0xFFFFFFFFu, both, 0);
+      s2 = __shfl_sync(0xFFFFFFFFu, both, 16);
+    } else {
+      if ((lane & 15) == 0) reinterpret_cast<float*>(&slot[flip][team][w])[lane >> 4] = both;
+      team_sync<TEAM, kBwdThreads>(team);
+      if (WARPS <= 4) {
+        s1 = s2 = 0.0f;
 #pragma unroll
-      for (int j = i * R::PER; j < (i + 1) * R::PER; ++j) {
-        x[j] = fmaf(x[j], rs, off);                // xhat
-        dg[j] = fmaf(y[j], x[j], dg[j]);
-        db[j] += y[j];
-        y[j] *= gamma[j];
-        s1 += y[j];
-        s2 = fmaf(y[j], x[j], s2);
+        for (int k = 0; k < WARPS; ++k) {
+          s1 += slot[flip][team][k].x;
+          s2 += slot[flip][team][k].y;
+        }
+      } else {
+        const float2 o = slot[flip][team][lane & (WARPS - 1)];
+        s1 = lanes_sum<WARPS>(o.x);
+        s2 = lanes_sum<WARPS>(o.y);
+      }
+      if (WIDE) {
+        tell_cluster(part[flip], rank, p.cluster, make_float4(s1, s2, 0.0f, 0.0f));
+        s1 = s2 = 0.0f;
+        for (int k = 0; k < p.cluster; ++k) {
+          s1 += part[flip][k].x;
+          s2 += part[flip][k].y;
+        }
       }
     }
-    s1 = warp_sum(s1);
-    s2 = warp_sum(s2);
-    if (WARPS > 1) {
-      if (lane == 0) slot[flip][team][w] = make_float2(s1, s2);
-      team_sync<TEAM, kBwdThreads>(team);
-      const float2 o = slot[flip][team][lane & (WARPS - 1)];
-      s1 = lanes_sum<WARPS>(o.x);
-      s2 = lanes_sum<WARPS>(o.y);
-    }
-    s1 *= p.inv_n * rs;
-    s2 *= p.inv_n * rs;
+    const uint64_t less = two(-s1 * p.inv_n * rs), slope = two(-s2 * p.inv_n * rs);
 #pragma unroll
-    for (int i = 0; i < R::SLOTS; ++i) {
-      if (!R::in(i, t, n)) continue;
-#pragma unroll
-      for (int j = i * R::PER; j < (i + 1) * R::PER; ++j) x[j] = fmaf(-x[j], s2, fmaf(y[j], rs, -s1));
-      R::store(p.out, row, p.ldx, t, i, x + i * R::PER);
+    for (int j = 0; j < VALS / 2; ++j) {
+      const float2 v = apart(fma2(xhat[j], slope, fma2(g[j], scale, less)));
+      x[2 * j] = v.x;
+      x[2 * j + 1] = v.y;
     }
+#pragma unroll
+    for (int i = 0; i < R::SLOTS; ++i)
+      if (R::in(i, t, n)) R::store(out, row, p.ldx, t, i, x + i * R::PER);
   }
   if (!p.part) return;
   // the teams' sums go through shared memory, in column order, to be added in
@@ -348,6 +468,12 @@ __global__ void __launch_bounds__(kBwdThreads) norm_backward_kernel(const NormPa
   constexpr int ALL = TEAM * VALS;
   copy_wait<0>();
   __syncthreads();
+  float dg[VALS], db[VALS];
+#pragma unroll
+  for (int j = 0; j < VALS / 2; ++j) {
+    const float2 a = apart(dg2[j]), b = apart(db2[j]);
+    dg[2 * j] = a.x, dg[2 * j + 1] = a.y, db[2 * j] = b.x, db[2 * j + 1] = b.y;
+  }
 #pragma unroll
   for (int i = 0; i < R::SLOTS; ++i) {
     float* at = sums + team * 2 * ALL + R::col(i, t);
@@ -364,7 +490,7 @@ __global__ void __launch_bounds__(kBwdThreads) norm_backward_kernel(const NormPa
     }
   }
   __syncthreads();
-  float* to = p.part + int64_t(blockIdx.x) * 2 * n;
+  float* to = p.part + int64_t(group) * 2 * p.n + c0;
 #pragma unroll 4
   for (int c = threadIdx.x; c < n; c += kBwdThreads) {
     float g = 0.0f, b = 0.0f;
@@ -373,12 +499,12 @@ __global__ void __launch_bounds__(kBwdThreads) norm_backward_kernel(const NormPa
       g += sums[k * 2 * ALL + c];
       b += sums[k * 2 * ALL + ALL + c];
     }
-    if (gridDim.x > 1) {
+    if (groups > 1) {
       __stcg(to + c, g);
-      __stcg(to + n + c, b);
+      __stcg(to + p.n + c, b);
     } else {                                       // this CTA's sums are the result
-      if (p.dgamma) p.dgamma[c] = p.accumulate ? p.dgamma[c] + g : g;
-      if (p.dbeta) p.dbeta[c] = p.accumulate ? p.dbeta[c] + b : b;
+      if (p.dgamma) p.dgamma[c0 + c] = p.accumulate ? p.dgamma[c0 + c] + g : g;
+      if (p.dbeta) p.dbeta[c0 + c] = p.accumulate ? p.dbeta[c0 + c] + b : b;
     }
   }
 }
@@ -516,13 +642,21 @@ bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) %
 goldy_status bad(const std::string& why) { return fail(GOLDY_ERR_INVALID_ARG, why); }
 
 // Threads per row at 16 values each (forwards, more than kFwdTeam stand for half
-// as many with 32); 0: the row streams.
-int team_for(const goldy_layernorm_desc& d, bool backward) {
+// as many with 32); 0: the row streams.  `cluster` CTAs of kMaxTeam threads
+// share a row that is too long for one.
+struct NormShape {
+  int team, cluster, seg;
+};
+NormShape shape_for(const goldy_layernorm_desc& d, bool backward) {
   const int most = backward ? kMaxTeam : 2 * kMaxTeam;
   const int64_t vals = backward ? kBwdVals : kFwdVals;
   int team = 32;
   while (team < most && team * vals < d.n) team *= 2;
-  return team * vals >= d.n ? team : 0;
+  int cluster = 1;
+  while (cluster < kMaxCluster && cluster * team * vals < d.n) cluster *= 2;
+  if (cluster * team * vals < d.n) return {0, 1, 0};
+  const int64_t seg = ceil_div(ceil_div(d.n, cluster), 8) * 8;     // whole pieces
+  return {team, cluster, int(seg)};
 }
 
 struct Kernel {
@@ -531,28 +665,32 @@ struct Kernel {
   size_t smem;
 };
 
-template <typename T, int TEAM, int VALS, bool VEC>
+template <typename T, int TEAM, int VALS, bool VEC, bool WIDE = false>
 Kernel pick_forward() {
   using S = FwdShape<TEAM, VALS, VEC>;
   using R = Row<T, VALS, TEAM, S::THREADS, VEC>;
-  return {reinterpret_cast<const void*>(&norm_forward_kernel<T, TEAM, VALS, VEC>), S::THREADS, S::TEAMS, S::CTAS,
+  return {reinterpret_cast<const void*>(&norm_forward_kernel<T, TEAM, VALS, VEC, WIDE>), S::THREADS, S::TEAMS, S::CTAS,
           size_t(kFwdDepth) * R::RING_BYTES};
+}
+template <typename T, int TEAM, bool VEC, bool WIDE = false>
+Kernel pick_backward() {
+  using R = Row<T, kBwdVals, TEAM, kBwdThreads, VEC>;
+  return {reinterpret_cast<const void*>(&norm_backward_kernel<T, TEAM, VEC, WIDE>), kBwdThreads, kBwdThreads / TEAM, 1,
+          std::max(size_t(2) * bwd_depth<T>() * R::RING_BYTES, size_t(2) * kBwdThreads * kBwdVals * sizeof(float))};
 }
 
 template <typename T, int TEAM, bool VEC>
 Kernel pick(bool backward) {
-  if (backward) {
-    using R = Row<T, kBwdVals, TEAM, kBwdThreads, VEC>;
-    return {reinterpret_cast<const void*>(&norm_backward_kernel<T, TEAM, VEC>), kBwdThreads, kBwdThreads / TEAM, 1,
-            std::max(size_t(2) * bwd_depth<T>() * R::RING_BYTES, size_t(2) * kBwdThreads * kBwdVals * sizeof(float))};
-  }
+  if (backward) return pick_backward<T, TEAM, VEC>();
   if constexpr (TEAM > kFwdTeam) return pick_forward<T, TEAM / 2, kFwdMoreVals, VEC>();
   else return pick_forward<T, TEAM, kFwdVals, VEC>();
 }
 
 template <typename T, bool VEC>
-Kernel pick_team(int team, bool backward) {
-  switch (team) {
+Kernel pick_shape(const NormShape& s, bool backward) {
+  if (s.cluster > 1)
+    return backward ? pick_backward<T, kMaxTeam, VEC, true>() : pick_forward<T, kMaxTeam, kFwdMoreVals, VEC, true>();
+  switch (s.team) {
     case 32: return pick<T, 32, VEC>(backward);
     case 64: return pick<T, 64, VEC>(backward);
     case 128: return pick<T, 128, VEC>(backward);
@@ -566,21 +704,21 @@ Kernel pick_team(int team, bool backward) {
   }
 }
 
-Kernel kernel_for(const goldy_layernorm_desc& d, bool vec, bool backward) {
-  const int team = team_for(d, backward);
-  if (d.dtype == GOLDY_F32) return vec ? pick_team<float, true>(team, backward) : pick_team<float, false>(team, backward);
-  return vec ? pick_team<uint16_t, true>(team, backward) : pick_team<uint16_t, false>(team, backward);
+Kernel kernel_for(const goldy_layernorm_desc& d, const NormShape& s, bool vec, bool backward) {
+  if (d.dtype == GOLDY_F32) return vec ? pick_shape<float, true>(s, backward) : pick_shape<float, false>(s, backward);
+  return vec ? pick_shape<uint16_t, true>(s, backward) : pick_shape<uint16_t, false>(s, backward);
 }
 
 // Rows per team up to which one CTA does them all: a further kernel that sums
 // partial rows costs 3.4 us, a further row of a team about 1.
 constexpr int kAloneRows = 3;
-int backward_ctas(const goldy_layernorm_desc& d) {
-  const int team = team_for(d, true);
-  if (team == 0) return int(std::max<int64_t>(1, std::min<int64_t>(kBwdCtas, d.rows)));
-  const int64_t teams = kBwdThreads / team;
+// CTAs, or clusters of them, of a backward launch
+int backward_groups(const goldy_layernorm_desc& d) {
+  const NormShape s = shape_for(d, true);
+  if (s.team == 0) return int(std::max<int64_t>(1, std::min<int64_t>(kBwdCtas, d.rows)));
+  const int64_t teams = s.cluster > 1 ? 1 : kBwdThreads / s.team;
   if (d.rows <= kAloneRows * teams) return 1;      // no second kernel
-  return int(std::min<int64_t>(kBwdCtas, ceil_div(d.rows, teams)));
+  return int(std::min<int64_t>(kBwdCtas / s.cluster, ceil_div(d.rows, teams)));
 }
 
 goldy_status check_norm(const goldy_layernorm_desc* d) {
@@ -598,22 +736,47 @@ struct NormCall {
   NormParams p;
   const goldy_layernorm_desc* d;
   bool vec, backward;
-  int team;                // 0: the row streams
+  NormShape shape;
   void* stream;
 };
 
-cudaError_t launch(const void* fn, unsigned grid, unsigned threads, size_t smem, void* stream, void** args) {
+struct Launch {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = static_cast<cudaStream_t>(stream);
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelExC(&cfg, fn, args);
+  cudaLaunchAttribute attr[2];
+
+  Launch(unsigned grid, unsigned threads, size_t smem, void* stream, unsigned cluster = 1) {
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = static_cast<cudaStream_t>(stream);
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+  }
+  Launch(const Launch&) = delete;
+  cudaError_t run(const void* fn, void** args) { return cudaLaunchKernelExC(&cfg, fn, args); }
+};
+
+// Clusters of a kernel that the device holds at once (a GPC's SMs need not make
+// whole clusters), asked for once.
+cudaError_t resident_clusters(int device, const Kernel& k, int cluster, int* n) {
+  static std::mutex mu;
+  static std::map<std::tuple<int, const void*, int>, int> known;
+  std::lock_guard<std::mutex> lock(mu);
+  const auto key = std::make_tuple(device, k.fn, cluster);
+  const auto it = known.find(key);
+  if (it != known.end()) {
+    *n = it->second;
+    return cudaSuccess;
+  }
+  Launch l(unsigned(cluster), unsigned(k.threads), k.smem, nullptr, unsigned(cluster));
+  const cudaError_t e = cudaOccupancyMaxActiveClusters(n, k.fn, &l.cfg);
+  if (e == cudaSuccess) known[key] = *n;
+  return e;
 }
 
 // Opts a kernel into more than 48 KB of shared memory, once per device.
@@ -630,27 +793,35 @@ cudaError_t allow_smem(int device, const Kernel& k) {
 
 goldy_status launch_norm(const LayerContext& ctx, void* arg) {
   NormCall& call = *static_cast<NormCall*>(arg);
-  const Kernel k = kernel_for(*call.d, call.vec, call.backward);
+  // which SMs a partition has, and so whether a cluster fits into it, is not known
+  if (!ctx.whole && call.shape.cluster > 1) call.shape = {0, 1, 0};
+  const int cluster = call.shape.cluster;
+  const Kernel k = kernel_for(*call.d, call.shape, call.vec, call.backward);
   cudaError_t e = allow_smem(ctx.device, k);
   if (e != cudaSuccess) return fail(GOLDY_ERR_CUDA, std::string("cudaFuncSetAttribute: ") + cudaGetErrorString(e));
-  unsigned grid;
-  if (call.backward) {
-    grid = unsigned(backward_ctas(*call.d));
-  } else {
-    // all CTAs resident at once, every team with rows of its own
-    const int64_t cap = int64_t(ctx.sm_count) * k.per_sm;
-    grid = unsigned(std::max<int64_t>(1, std::min<int64_t>(cap, ceil_div(call.d->rows, k.teams))));
+  int64_t cap = int64_t(ctx.sm_count) * k.per_sm;              // CTAs, or clusters, resident at once
+  if (cluster > 1) {
+    int most = 0;
+    e = resident_clusters(ctx.device, k, cluster, &most);
+    if (e == cudaSuccess && most < 1) e = cudaErrorInvalidClusterSize;
+    if (e != cudaSuccess)
+      return fail(GOLDY_ERR_CUDA, std::string("layer norm, clusters: ") + cudaGetErrorString(e));
+    cap = std::min<int64_t>(cap / cluster, most);
   }
+  // all resident, every team with rows of its own
+  int64_t groups = call.backward ? backward_groups(*call.d) : std::min(cap, ceil_div(call.d->rows, int64_t(k.teams)));
+  if (cluster > 1) groups = std::min(groups, cap);
+  groups = std::max<int64_t>(1, groups);
   void* args[] = {&call.p};
   if (call.d->rows > 0 || call.backward) {
-    e = launch(k.fn, grid, unsigned(k.threads), k.smem, call.stream, args);
+    e = Launch(unsigned(groups * cluster), unsigned(k.threads), k.smem, call.stream, unsigned(cluster)).run(k.fn, args);
     if (e != cudaSuccess) return fail(GOLDY_ERR_CUDA, std::string("layer norm launch: ") + cudaGetErrorString(e));
   }
-  if (call.backward && call.p.part && (grid > 1 || call.team == 0)) {
-    int n = int(call.d->n), rows = int(grid);
+  if (call.backward && call.p.part && (groups > 1 || call.shape.team == 0)) {
+    int n = int(call.d->n), rows = int(groups);
     void* rargs[] = {&call.p.part, &call.p.dgamma, &call.p.dbeta, &n, &rows, &call.p.accumulate};
-    e = launch(reinterpret_cast<const void*>(&norm_reduce_kernel), unsigned(ceil_div(2 * call.d->n, 32)),
-               kReduceWarps * 32, 0, call.stream, rargs);
+    e = Launch(unsigned(ceil_div(2 * call.d->n, 32)), kReduceWarps * 32, 0, call.stream)
+            .run(reinterpret_cast<const void*>(&norm_reduce_kernel), rargs);
     if (e != cudaSuccess) return fail(GOLDY_ERR_CUDA, std::string("layer norm launch: ") + cudaGetErrorString(e));
   }
   return GOLDY_OK;
@@ -666,10 +837,12 @@ bool vectors(const goldy_layernorm_desc& d, const void* a, const void* b, const 
 }
 
 size_t backward_bytes(const goldy_layernorm_desc& d) {
-  return kLayerCounterBytes + size_t(backward_ctas(d)) * 2 * size_t(d.n) * sizeof(float);
+  return kLayerCounterBytes + size_t(backward_groups(d)) * 2 * size_t(d.n) * sizeof(float);
 }
 
-void common_params(NormParams& p, const goldy_layernorm_desc& d) {
+void common_params(NormParams& p, const goldy_layernorm_desc& d, const NormShape& s) {
+  p.cluster = s.cluster;
+  p.seg = s.seg;
   p.ldx = d.ldx;
   p.ldy = d.ldy;
   p.rows = d.rows;
@@ -706,9 +879,9 @@ extern "C" goldy_status goldy_layernorm_forward(const goldy_layernorm_desc* desc
   NormCall call{};
   call.d = desc;
   call.vec = vectors(*desc, X, Y, nullptr, gamma, beta);
-  call.team = team_for(*desc, false);
+  call.shape = shape_for(*desc, false);
   call.stream = stream;
-  common_params(call.p, *desc);
+  common_params(call.p, *desc, call.shape);
   call.p.x = X;
   call.p.gamma = gamma;
   call.p.beta = beta;
@@ -747,10 +920,10 @@ extern "C" goldy_status goldy_layernorm_backward(const goldy_layernorm_desc* des
   NormCall call{};
   call.d = desc;
   call.vec = vectors(*desc, X, dY, dX, gamma, nullptr);
-  call.team = team_for(*desc, true);
+  call.shape = shape_for(*desc, true);
   call.backward = true;
   call.stream = stream;
-  common_params(call.p, *desc);
+  common_params(call.p, *desc, call.shape);
   call.p.x = X;
   call.p.dy = dY;
   call.p.gamma = gamma;

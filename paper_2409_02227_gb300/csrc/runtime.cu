@@ -1442,6 +1442,7 @@ goldy_status with_layer_context(void* stream, goldy_status (*body)(const LayerCo
   st = part.enter(stream);
   if (st != GOLDY_OK) return st;
   ctx.sm_count = sms(*d);
+  ctx.whole = ctx.sm_count == d->sm_count;
   ctx.err_word = d->err_word;
   ctx.encode = g_encode;
   return body(ctx, arg);
