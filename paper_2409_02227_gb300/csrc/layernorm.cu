@@ -119,28 +119,30 @@ __device__ __forceinline__ float lanes_sum(float v) {
   return v;
 }
 
-// PER parameters from index c on (c < n); the row's own accesses are vectors
-// exactly when these may be.
-template <int PER>
-__device__ __forceinline__ void load_params(const void* p, int f32, int c, float absent, float* f) {
-  if (!p) {
+// PER parameters from index c on, 0 from n on; VEC: c + PER <= n, on a vector's
+// boundary.
+template <int PER, bool VEC>
+__device__ __forceinline__ void load_params(const void* p, int f32, int c, int n, float absent, float* f) {
+  if (!VEC || !p) {
 #pragma unroll
-    for (int k = 0; k < PER; ++k) f[k] = absent;
-  } else if (PER == 1) {
-    f[0] = f32 ? __ldg(static_cast<const float*>(p) + c) : load_bf16(p, c);
+    for (int k = 0; k < PER; ++k) {
+      if (!VEC && c + k >= n) f[k] = 0.0f;
+      else if (!p) f[k] = absent;
+      else f[k] = f32 ? __ldg(static_cast<const float*>(p) + c + k) : load_bf16(p, c + k);
+    }
   } else if (f32) {
 #pragma unroll
     for (int k = 0; k < PER; k += 4) {
       const float4 v = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(p) + c + k));
-      f[k] = v.x, f[k + 1] = v.y, f[k + 2] = v.z, f[k + 3] = v.w;
+      f[k] = v.x, f[(k + 1) % PER] = v.y, f[(k + 2) % PER] = v.z, f[(k + 3) % PER] = v.w;
     }
   } else if (PER == 8) {
     const uint4 v = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + c));
-    f[0] = bf16_lo(v.x), f[1] = bf16_hi(v.x), f[2] = bf16_lo(v.y), f[3] = bf16_hi(v.y);
-    f[4] = bf16_lo(v.z), f[5] = bf16_hi(v.z), f[6] = bf16_lo(v.w), f[7] = bf16_hi(v.w);
+    f[0] = bf16_lo(v.x), f[1 % PER] = bf16_hi(v.x), f[2 % PER] = bf16_lo(v.y), f[3 % PER] = bf16_hi(v.y);
+    f[4 % PER] = bf16_lo(v.z), f[5 % PER] = bf16_hi(v.z), f[6 % PER] = bf16_lo(v.w), f[7 % PER] = bf16_hi(v.w);
   } else {
     const uint2 v = __ldg(reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + c));
-    f[0] = bf16_lo(v.x), f[1] = bf16_hi(v.x), f[2] = bf16_lo(v.y), f[3] = bf16_hi(v.y);
+    f[0] = bf16_lo(v.x), f[1 % PER] = bf16_hi(v.x), f[2 % PER] = bf16_lo(v.y), f[3 % PER] = bf16_hi(v.y);
   }
 }
 
@@ -154,61 +156,161 @@ __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_gr
 template <int N>
 __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// A thread's share of a row, VALS values.  VEC: 16-byte pieces, piece i of
-// thread t at column (i * TEAM + t) * PER; otherwise single elements.  Pieces
-// are inside the row or outside as a whole.  bf16 rows off 16-byte boundaries
-// have no ring (no such copy exists) and are loaded where they are used.
-template <typename T, int VALS, int TEAM, int THREADS, bool VEC>
+// A thread's share of a row, VALS values, in pieces: piece i of thread t starts
+// at column (i * TEAM + t) * PER.  VEC: 16 bytes, inside the row or outside as a
+// whole.  fp32 otherwise: single elements.  bf16 otherwise (odd lengths or
+// strides, rows that start anywhere), SHIFT: 8 elements, maybe part of them
+// outside, that lie in two 16-byte blocks.  Whole blocks are copied, each by one
+// thread of the team, and a thread picks its elements from its block and the
+// next; a result's blocks are put together from a lane's and the lower lane's
+// elements and stored whole, but for those that two warps or two rows share
+// (16384 rows of 2047: 42 us, backwards 54; loading and storing single elements
+// took 62 and 69, aligned words traded between lanes 57 and 79).  What else a row's first and last block hold is read and ignored,
+// never written.
+// SURE: the first half of the pieces is inside whatever the row's length, as the
+// host takes the smallest team that holds the row: no tests for those.
+template <typename T, int VALS, int TEAM, int THREADS, bool VEC, bool WIDE>
 struct Row {
-  static constexpr int PER = VEC ? 16 / int(sizeof(T)) : 1;
+  static constexpr bool SHIFT = !VEC && sizeof(T) == 2;
+  static constexpr int PER = VEC ? 16 / int(sizeof(T)) : SHIFT ? 8 : 1;
   static constexpr int SLOTS = VALS / PER;
-  static constexpr bool RING = VEC || sizeof(T) == 4;
-  static constexpr int PIECE = VEC ? 16 : 4;
-  static constexpr int RING_BYTES = RING ? SLOTS * THREADS * PIECE : 0;   // of one row
+  static constexpr int PIECE = VEC || SHIFT ? 16 : 4;
+  static constexpr int BLOCKS = SLOTS * TEAM + 1;  // SHIFT: of one row
+  static constexpr int RING_BYTES = SHIFT ? THREADS / TEAM * BLOCKS * 16 : SLOTS * THREADS * PIECE;   // of one row per team
+  static constexpr int SURE = TEAM > 32 && !WIDE ? SLOTS / 2 : 0;
   static __device__ __forceinline__ int col(int slot, int t) { return (slot * TEAM + t) * PER; }
-  static __device__ __forceinline__ bool in(int slot, int t, int n) { return col(slot, t) < n; }
+  static __device__ __forceinline__ bool in(int slot, int t, int n) { return slot < SURE || col(slot, t) < n; }
+  static __device__ __forceinline__ bool whole(int slot, int t, int n) {
+    return !SHIFT || slot < SURE || col(slot, t) + PER <= n;
+  }
+  // SHIFT: elements by which a row starts behind a block's start
+  static __device__ __forceinline__ int shift(const T* at) { return int(reinterpret_cast<uintptr_t>(at) & 15) / 2; }
+  // place in the ring of a thread's piece, or block
+  static __device__ __forceinline__ int place(int slot, int t) {
+    return SHIFT ? (int(threadIdx.x) / TEAM * BLOCKS + slot * TEAM + t) * 16 : (slot * THREADS + int(threadIdx.x)) * PIECE;
+  }
 
   static __device__ __forceinline__ void fetch(uint8_t* ring, const void* base, int64_t row, int64_t ld, int n, int t) {
-    if (!RING) return;
     const T* at = static_cast<const T*>(base) + row * ld;
+    const int off = SHIFT ? shift(at) : 0;
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s)
-      if (in(s, t, n)) copy_async<PIECE>(ring + (s * THREADS + threadIdx.x) * PIECE, at + col(s, t));
+      if (in(s, t, n + off)) copy_async<PIECE>(ring + place(s, t), at + col(s, t) - off);
+    if (SHIFT && t == 0 && col(SLOTS, 0) < n + off) copy_async<PIECE>(ring + place(SLOTS, 0), at + col(SLOTS, 0) - off);
   }
-  static __device__ __forceinline__ void values(const uint8_t* ring, const void* base, int64_t row, int64_t ld, int n,
-                                                int t, float (&f)[VALS]) {
+
+  template <int OFF>
+  static __device__ __forceinline__ void pick(const uint8_t* ring, int n, int t, float (&f)[VALS]) {
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
-      if (!in(s, t, n)) {
+      const uint4 a = *reinterpret_cast<const uint4*>(ring + place(s, t));
+      const uint4 b = OFF > 0 ? *reinterpret_cast<const uint4*>(ring + place(s, t) + 16) : a;
+      const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
-        for (int k = 0; k < PER; ++k) f[s * PER + k] = 0.0f;
-      } else if (!RING) {
-        f[s] = load_bf16(static_cast<const T*>(base) + row * ld, col(s, t));
-      } else if (!VEC) {
-        f[s] = *reinterpret_cast<const float*>(ring + (s * THREADS + threadIdx.x) * 4);
-      } else {
-        const uint4 v = *reinterpret_cast<const uint4*>(ring + (s * THREADS + threadIdx.x) * 16);
-        float* o = f + s * PER;
-        if (sizeof(T) == 2) {
-          o[0] = bf16_lo(v.x), o[1] = bf16_hi(v.x), o[2] = bf16_lo(v.y), o[3] = bf16_hi(v.y);
-          o[4 % PER] = bf16_lo(v.z), o[5 % PER] = bf16_hi(v.z), o[6 % PER] = bf16_lo(v.w), o[7 % PER] = bf16_hi(v.w);
+      for (int k = 0; k < 8; ++k) f[(s * PER + k) % VALS] = (OFF + k) & 1 ? bf16_hi(w[(OFF + k) / 2]) : bf16_lo(w[(OFF + k) / 2]);
+      if (!whole(s, t, n)) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (col(s, t) + k >= n) f[(s * PER + k) % VALS] = 0.0f;
+      }
+    }
+  }
+  // the row's values, 0 outside it (SHIFT: behind the team's barrier)
+  static __device__ __forceinline__ void values(const uint8_t* ring, const void* base, int64_t row, int64_t ld, int n,
+                                                int t, float (&f)[VALS]) {
+    if constexpr (SHIFT) {
+      switch (shift(static_cast<const T*>(base) + row * ld)) {
+        case 0: pick<0>(ring, n, t, f); break;
+        case 1: pick<1>(ring, n, t, f); break;
+        case 2: pick<2>(ring, n, t, f); break;
+        case 3: pick<3>(ring, n, t, f); break;
+        case 4: pick<4>(ring, n, t, f); break;
+        case 5: pick<5>(ring, n, t, f); break;
+        case 6: pick<6>(ring, n, t, f); break;
+        default: pick<7>(ring, n, t, f); break;
+      }
+    } else {
+#pragma unroll
+      for (int s = 0; s < SLOTS; ++s) {
+        if (!in(s, t, n)) {
+#pragma unroll
+          for (int k = 0; k < PER; ++k) f[s * PER + k] = 0.0f;
+        } else if (!VEC) {
+          f[s] = *reinterpret_cast<const float*>(ring + place(s, t));
         } else {
-          o[0] = __uint_as_float(v.x), o[1] = __uint_as_float(v.y), o[2] = __uint_as_float(v.z), o[3] = __uint_as_float(v.w);
+          const uint4 v = *reinterpret_cast<const uint4*>(ring + place(s, t));
+          float* o = f + s * PER;
+          if (sizeof(T) == 2) {
+            o[0] = bf16_lo(v.x), o[1] = bf16_hi(v.x), o[2] = bf16_lo(v.y), o[3] = bf16_hi(v.y);
+            o[4 % PER] = bf16_lo(v.z), o[5 % PER] = bf16_hi(v.z), o[6 % PER] = bf16_lo(v.w), o[7 % PER] = bf16_hi(v.w);
+          } else {
+            o[0] = __uint_as_float(v.x), o[1] = __uint_as_float(v.y), o[2] = __uint_as_float(v.z), o[3] = __uint_as_float(v.w);
+          }
         }
       }
     }
   }
-  // piece s of the result
-  static __device__ __forceinline__ void store(void* base, int64_t row, int64_t ld, int t, int s, const float* f) {
-    T* at = static_cast<T*>(base) + row * ld + col(s, t);
-    if (!VEC) {
-      if (sizeof(T) == 2) store_bf16(at, 0, f[0]);
-      else *reinterpret_cast<float*>(at) = f[0];
-    } else if (sizeof(T) == 2) {
-      __stcs(reinterpret_cast<uint4*>(at), make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]),
-                                                      pack_bf16(f[4 % PER], f[5 % PER]), pack_bf16(f[6 % PER], f[7 % PER])));
+
+  // SHIFT: `at` is OFF elements behind a block's start
+  template <int OFF>
+  static __device__ __forceinline__ void put(T* at, int n, int t, const float (&f)[VALS]) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s) {
+      const int c = col(s, t);
+      uint32_t w[8];                               // the lower lane's elements, then this lane's
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        w[4 + k] = pack_bf16(f[(s * PER + 2 * k) % VALS], f[(s * PER + 2 * k + 1) % VALS]);
+        w[k] = 2 * k + 1 >= 8 - OFF ? __shfl_up_sync(0xFFFFFFFFu, w[4 + k], 1) : 0u;
+      }
+      uint32_t v[4];                               // elements 8 - OFF .. 15 - OFF of those
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int h = 8 - OFF + 2 * k;
+        v[k] = h & 1 ? __byte_perm(w[h / 2], w[(h / 2 + 1) % 8], 0x5432) : w[(h / 2) % 8];
+      }
+      // blocks that this lane, and the next, store whole
+      const bool own = (OFF == 0 || lane > 0) && (s < SURE || c + 8 - OFF <= n);
+      const bool next = lane < 31 && (s < SURE || c + 16 - OFF <= n);
+      if (own) __stcs(reinterpret_cast<uint4*>(at + c - OFF), make_uint4(v[0], v[1], v[2], v[3]));
+      if (!own || (OFF > 0 && !next)) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if ((k < 8 - OFF ? !own : !next) && (s < SURE || c + k < n))
+            reinterpret_cast<uint16_t*>(at)[c + k] = uint16_t(w[4 + k / 2] >> (k & 1) * 16);
+      }
+    }
+  }
+  // the row's results (all lanes of a warp)
+  static __device__ __forceinline__ void store(void* base, int64_t row, int64_t ld, int n, int t, const float (&f)[VALS]) {
+    T* at = static_cast<T*>(base) + row * ld;
+    if constexpr (SHIFT) {
+      switch (shift(at)) {
+        case 0: put<0>(at, n, t, f); break;
+        case 1: put<1>(at, n, t, f); break;
+        case 2: put<2>(at, n, t, f); break;
+        case 3: put<3>(at, n, t, f); break;
+        case 4: put<4>(at, n, t, f); break;
+        case 5: put<5>(at, n, t, f); break;
+        case 6: put<6>(at, n, t, f); break;
+        default: put<7>(at, n, t, f); break;
+      }
     } else {
-      __stcs(reinterpret_cast<float4*>(at), make_float4(f[0], f[1], f[2], f[3]));
+#pragma unroll
+      for (int s = 0; s < SLOTS; ++s) {
+        if (!in(s, t, n)) continue;
+        T* to = at + col(s, t);
+        const float* v = f + s * PER;
+        if (!VEC) {
+          *reinterpret_cast<float*>(to) = v[0];
+        } else if (sizeof(T) == 2) {
+          __stcs(reinterpret_cast<uint4*>(to), make_uint4(pack_bf16(v[0], v[1 % PER]), pack_bf16(v[2 % PER], v[3 % PER]),
+                                                          pack_bf16(v[4 % PER], v[5 % PER]), pack_bf16(v[6 % PER], v[7 % PER])));
+        } else {
+          __stcs(reinterpret_cast<float4*>(to), make_float4(v[0], v[1 % PER], v[2 % PER], v[3 % PER]));
+        }
+      }
     }
   }
 };
@@ -244,7 +346,7 @@ __global__ void __launch_bounds__(FwdShape<TEAM, VALS, VEC>::THREADS, FwdShape<T
 norm_forward_kernel(const NormParams p) {
   constexpr int THREADS = FwdShape<TEAM, VALS, VEC>::THREADS, TEAMS = FwdShape<TEAM, VALS, VEC>::TEAMS;
   constexpr int WARPS = TEAM / 32, D = kFwdDepth;
-  using R = Row<T, VALS, TEAM, THREADS, VEC>;
+  using R = Row<T, VALS, TEAM, THREADS, VEC, WIDE>;
   __shared__ float4 slot[2][TEAMS][WARPS];         // per warp: sum, M2, elements, mean
   __shared__ float4 part[2][WIDE ? kMaxCluster : 1];   // per CTA of the cluster: the same
   extern __shared__ __align__(16) uint8_t ring[];
@@ -272,9 +374,9 @@ norm_forward_kernel(const NormParams p) {
 #pragma unroll
   for (int i = 0; i < R::SLOTS; ++i) {
     if (!R::in(i, t, n)) continue;
-    load_params<R::PER>(p.gamma, p.param_f32, c0 + R::col(i, t), 1.0f, gamma + i * R::PER);
-    load_params<R::PER>(p.beta, p.param_f32, c0 + R::col(i, t), 0.0f, beta + i * R::PER);
-    mine += R::PER;
+    load_params<R::PER, VEC>(p.gamma, p.param_f32, c0 + R::col(i, t), c0 + n, 1.0f, gamma + i * R::PER);
+    load_params<R::PER, VEC>(p.beta, p.param_f32, c0 + R::col(i, t), c0 + n, 0.0f, beta + i * R::PER);
+    mine += R::whole(i, t, n) ? R::PER : n - R::col(i, t);
   }
   const float warp_n = warp_sum(float(mine));
   const float warp_inv = warp_n > 0.0f ? 1.0f / warp_n : 0.0f;
@@ -283,6 +385,7 @@ norm_forward_kernel(const NormParams p) {
     if (row + (D - 1) * step < p.rows) R::fetch(ring + ahead * R::RING_BYTES, in, row + (D - 1) * step, p.ldx, n, t);
     copy_commit();
     copy_wait<D - 1>();
+    if (R::SHIFT) team_sync<TEAM, THREADS>(team);
     float x[VALS];
     R::values(ring + at * R::RING_BYTES, in, row, p.ldx, n, t, x);
     at = at + 1 == D ? 0 : at + 1;
@@ -296,6 +399,11 @@ norm_forward_kernel(const NormParams p) {
 #pragma unroll
     for (int i = 0; i < R::SLOTS; ++i) {
       if (!R::in(i, t, n)) continue;
+      if (!R::whole(i, t, n)) {
+#pragma unroll
+        for (int k = 0; k < R::PER; ++k)
+          if (R::col(i, t) + k >= n) x[i * R::PER + k] = wm;
+      }
 #pragma unroll
       for (int k = 0; k < R::PER; ++k) {
         x[i * R::PER + k] -= wm;                   // differences from the warp's mean from here on
@@ -332,8 +440,8 @@ norm_forward_kernel(const NormParams p) {
       if (!R::in(i, t, n)) continue;
 #pragma unroll
       for (int j = i * R::PER; j < (i + 1) * R::PER; ++j) x[j] = fmaf(fmaf(x[j], rstd, shift), gamma[j], beta[j]);
-      R::store(out, row, p.ldy, t, i, x + i * R::PER);
     }
+    R::store(out, row, p.ldy, n, t, x);
     if (t == 0 && rank == 0) {
       if (p.mean) p.mean[row] = mean;
       if (p.rstd) p.rstd[row] = rstd;
@@ -344,7 +452,7 @@ norm_forward_kernel(const NormParams p) {
 template <typename T, int TEAM, bool VEC, bool WIDE>
 __global__ void __launch_bounds__(kBwdThreads) norm_backward_kernel(const NormParams p) {
   constexpr int TEAMS = kBwdThreads / TEAM, WARPS = TEAM / 32, VALS = kBwdVals, D = bwd_depth<T>();
-  using R = Row<T, VALS, TEAM, kBwdThreads, VEC>;
+  using R = Row<T, VALS, TEAM, kBwdThreads, VEC, WIDE>;
   __shared__ float2 slot[2][TEAMS][WARPS];
   __shared__ float4 part[2][WIDE ? kMaxCluster : 1];
   extern __shared__ __align__(16) uint8_t ring[];  // D rows of x, D of dy; at the end the CTA's sums
@@ -382,7 +490,7 @@ __global__ void __launch_bounds__(kBwdThreads) norm_backward_kernel(const NormPa
 #pragma unroll
     for (int i = 0; i < R::SLOTS; ++i) {
       if (R::in(i, t, n)) {
-        load_params<R::PER>(p.gamma, p.param_f32, c0 + R::col(i, t), 1.0f, f + i * R::PER);
+        load_params<R::PER, VEC>(p.gamma, p.param_f32, c0 + R::col(i, t), c0 + n, 1.0f, f + i * R::PER);
       } else {
 #pragma unroll
         for (int k = 0; k < R::PER; ++k) f[i * R::PER + k] = 0.0f;
@@ -403,6 +511,7 @@ __global__ void __launch_bounds__(kBwdThreads) norm_backward_kernel(const NormPa
       rstd = __ldg(p.rstd + row + step);
     }
     copy_wait<D - 1>();
+    if (R::SHIFT) team_sync<TEAM, kBwdThreads>(team);
     float x[VALS], y[VALS];
     R::values(ring + 2 * at * R::RING_BYTES, in, row, p.ldx, n, t, x);
     R::values(ring + (2 * at + 1) * R::RING_BYTES, dy, row, p.ldy, n, t, y);
@@ -457,9 +566,7 @@ __global__ void __launch_bounds__(kBwdThreads) norm_backward_kernel(const NormPa
       x[2 * j] = v.x;
       x[2 * j + 1] = v.y;
     }
-#pragma unroll
-    for (int i = 0; i < R::SLOTS; ++i)
-      if (R::in(i, t, n)) R::store(out, row, p.ldx, t, i, x + i * R::PER);
+    R::store(out, row, p.ldx, n, t, x);
   }
   if (!p.part) return;
   // the teams' sums go through shared memory, in column order, to be added in
@@ -668,13 +775,13 @@ struct Kernel {
 template <typename T, int TEAM, int VALS, bool VEC, bool WIDE = false>
 Kernel pick_forward() {
   using S = FwdShape<TEAM, VALS, VEC>;
-  using R = Row<T, VALS, TEAM, S::THREADS, VEC>;
+  using R = Row<T, VALS, TEAM, S::THREADS, VEC, WIDE>;
   return {reinterpret_cast<const void*>(&norm_forward_kernel<T, TEAM, VALS, VEC, WIDE>), S::THREADS, S::TEAMS, S::CTAS,
           size_t(kFwdDepth) * R::RING_BYTES};
 }
 template <typename T, int TEAM, bool VEC, bool WIDE = false>
 Kernel pick_backward() {
-  using R = Row<T, kBwdVals, TEAM, kBwdThreads, VEC>;
+  using R = Row<T, kBwdVals, TEAM, kBwdThreads, VEC, WIDE>;
   return {reinterpret_cast<const void*>(&norm_backward_kernel<T, TEAM, VEC, WIDE>), kBwdThreads, kBwdThreads / TEAM, 1,
           std::max(size_t(2) * bwd_depth<T>() * R::RING_BYTES, size_t(2) * kBwdThreads * kBwdVals * sizeof(float))};
 }
