@@ -158,17 +158,16 @@ __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group 
 
 // A thread's share of a row, VALS values, in pieces: piece i of thread t starts
 // at column (i * TEAM + t) * PER.  VEC: 16 bytes, inside the row or outside as a
-// whole.  fp32 otherwise: single elements
-// (4096 rows of 4095: 29 us, backwards 50; 30 and 55 in the bf16 rows' way).  bf16
-// otherwise (odd lengths or
-// strides, rows that start anywhere), SHIFT: 8 elements, maybe part of them
-// outside, that lie in two 16-byte blocks.  Whole blocks are copied, each by one
-// thread of the team, and a thread picks its elements from its block and the
-// next; a result's blocks are put together from a lane's and the lower lane's
-// elements and stored whole, but for those that two warps or two rows share
-// (16384 rows of 2047: 42 us, backwards 54; loading and storing single elements
-// took 62 and 69, aligned words traded between lanes 57 and 79).  What else a row's first and last block hold is read and ignored,
-// never written.
+// whole.  bf16 otherwise (odd lengths or strides, rows that start anywhere),
+// SHIFT: 8 elements, maybe part of them outside, that lie in two 16-byte blocks.
+// Whole blocks are copied, each by one thread of the team, and a thread picks its
+// elements from its block and the next; a result's blocks are put together from
+// a lane's and the lower lane's elements and stored whole, but for those that two
+// warps or two rows share (16384 rows of 2047: 42 us, backwards 54; loading and
+// storing single elements took 62 and 69, aligned words traded between lanes 57
+// and 79).  What else a row's first and last block hold is read and ignored,
+// never written.  fp32 otherwise: single elements (4096 rows of 4095: 29 us,
+// backwards 50; in blocks 30 and 55).
 // SURE: the first half of the pieces is inside whatever the row's length, as the
 // host takes the smallest team that holds the row: no tests for those.
 template <typename T, int VALS, int TEAM, int THREADS, bool VEC, bool WIDE>
