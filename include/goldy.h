@@ -575,7 +575,9 @@ goldy_status goldy_linear_bias_grad(const goldy_linear_desc* desc, const int32_t
  * y = (x - mean) * rstd * gamma + beta per row of n elements, mean = sum(x) /
  * n, rstd = 1 / sqrt(sum((x - mean)^2) / n + eps), in fp32.  X, Y, dX and dY
  * share `dtype` (any row strides >= n, element alignment; ldx: X and dX, ldy:
- * Y and dY); gamma and beta have param_dtype and may be null (1 and 0). */
+ * Y and dY); gamma and beta have param_dtype and may be null (1 and 0).  The
+ * aligned 16-byte blocks that a row begins and ends in may be read whole; only
+ * rows are written. */
 typedef struct goldy_layernorm_desc {
   int64_t rows, n;
   int64_t ldx, ldy;

@@ -6,12 +6,12 @@
 //
 // HBM-bound: x (and dy) read once, y (or dx) written once.  A team of 32 to 512
 // threads, by the row's length, holds a row in registers (16 or 32 values per
-// thread), so both statistics passes of the forward
-// direction and the two sums of the backward direction cost no second read.
-// The next rows are on their way meanwhile: each thread copies its own pieces
-// into shared memory with cp.async and reads back only those, so that rows in
-// flight take no registers and need no barrier.  gamma and beta are read per
-// row, from L1.
+// thread), so both statistics passes of the forward direction and the two sums of
+// the backward direction cost no second read.  The next rows are on their way
+// meanwhile: each thread copies its own pieces into shared memory with cp.async
+// and reads back only those, so that rows in flight take no registers and need no
+// barrier (but for bf16 rows off 16-byte boundaries, see Row).  gamma and beta
+// stay in registers.
 // The variance is a sum of squared differences from each warp's own mean,
 // warps combined by M2 = sum(M2_w + n_w (mean_w - mean)^2): no cancellation,
 // one barrier per row.  Backward, each thread owns its columns for all rows of
@@ -47,14 +47,13 @@ constexpr int kMaxCluster = 8;      // CTAs that may share a row
 constexpr int kStreamThreads = 512;
 constexpr int kFwdThreads = 256;    // per CTA, at least the team
 constexpr int kBwdThreads = 512;
-// values of a row per thread, and rows in a thread's ring
 // Values of a row per thread: 16 up to 256 threads (4096 values; 16384 rows of
-// 4096 take 44 us, with 32 values 50), then 32 (8192 rows of 8192: 45 us, with
+// 4096 take 44 us, with 32 values 50), then 32 (8192 rows of 8192: 44 us, with
 // 16 values and 512 threads 55).
 constexpr int kFwdVals = 16, kFwdMoreVals = 32;
 constexpr int kFwdTeam = 256;
 constexpr int kBwdVals = 16;
-constexpr int kFwdDepth = 3;
+constexpr int kFwdDepth = 3;        // rows in a thread's ring
 // CTAs of a backward launch: one partial row each
 constexpr int kBwdCtas = 152;      // one per SM
 template <typename T> __host__ __device__ constexpr int bwd_depth() { return sizeof(T) == 2 ? 3 : 2; }
