@@ -36,6 +36,35 @@ __device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
   return make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
 }
 
+// Two fp32 values in one register pair: this hardware multiplies and adds both
+// with one instruction, rounding each as ever.
+__device__ __forceinline__ uint64_t two(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ uint64_t two(float v) { return two(v, v); }
+__device__ __forceinline__ float2 apart(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
 // 2^x and 1 / x by the special-function unit (a few units in the last place,
 // subnormals flushed to zero).
 __device__ __forceinline__ float fast_exp2(float x) {
@@ -102,6 +131,74 @@ __device__ __forceinline__ float act_slope(float z, int act) {
       return s * fmaf(z, 1.0f - s, 1.0f);
     }
     default: return 1.0f;
+  }
+}
+
+// The same for two values (the layer kernels' epilogues: input gradient of 8192
+// rows, 512 -> 4096 features through gelu 52.1 -> 49.5 us, the others 0 to 2%).
+__device__ __forceinline__ uint64_t one_less(uint64_t v) { return fma2(v, two(-1.0f), two(1.0f)); }   // 1 - v
+__device__ __forceinline__ uint64_t fast_sigmoid2(uint64_t x) {
+  const float2 e = apart(mul2(x, two(-kLog2E)));
+  const float2 d = apart(add2(two(fast_exp2(e.x), fast_exp2(e.y)), two(1.0f)));
+  return two(fast_rcp(d.x), fast_rcp(d.y));
+}
+// P(Z <= z) of a standard normal Z, and the density factor
+__device__ __forceinline__ uint64_t normal_below2(uint64_t z2, uint64_t& g) {
+  const float2 z = apart(z2);
+  const float2 d = apart(fma2(two(0.23164189f), two(fabsf(z.x), fabsf(z.y)), two(1.0f)));
+  const uint64_t t = two(fast_rcp(d.x), fast_rcp(d.y));
+  const float2 e = apart(mul2(mul2(z2, z2), two(-0.5f * kLog2E)));
+  g = two(fast_exp2(e.x), fast_exp2(e.y));
+  uint64_t s = fma2(two(0.5307027145f), t, two(-0.7265760135f));
+  s = fma2(s, t, two(0.7107068705f));
+  s = fma2(s, t, two(-0.142248368f));
+  s = fma2(s, t, two(0.127414796f));
+  s = mul2(mul2(s, t), g);
+  const float2 q = apart(s), r = apart(one_less(s));
+  return two(z.x < 0.0f ? q.x : r.x, z.y < 0.0f ? q.y : r.y);
+}
+
+__device__ __forceinline__ uint64_t act_value2(uint64_t z, int act) {
+  switch (act) {
+    case GOLDY_ACT_GELU: {
+      uint64_t g;
+      return mul2(z, normal_below2(z, g));
+    }
+    case GOLDY_ACT_GELU_TANH: {
+      const uint64_t u2 = mul2(fma2(mul2(mul2(z, z), two(0.044715f)), z, z), two(1.5957691216057308f));
+      return mul2(z, fast_sigmoid2(u2));
+    }
+    case GOLDY_ACT_SILU: return mul2(z, fast_sigmoid2(z));
+    default: {
+      const float2 v = apart(z);
+      return two(act_value(v.x, act), act_value(v.y, act));
+    }
+  }
+}
+
+__device__ __forceinline__ uint64_t act_slope2(uint64_t z, int act) {
+  switch (act) {
+    case GOLDY_ACT_GELU: {
+      uint64_t g;
+      const uint64_t p = normal_below2(z, g);
+      return fma2(mul2(z, two(0.39894228040143268f)), g, p);
+    }
+    case GOLDY_ACT_GELU_TANH: {
+      const float2 sq = apart(mul2(z, z));
+      const uint64_t zz = two(fminf(sq.x, 1e30f), fminf(sq.y, 1e30f));
+      const uint64_t u2 = mul2(fma2(mul2(zz, two(0.044715f)), z, z), two(1.5957691216057308f));
+      const uint64_t s = fast_sigmoid2(u2);
+      const uint64_t inner = mul2(fma2(two(3.0f * 0.044715f), zz, two(1.0f)), two(1.5957691216057308f));
+      return fma2(mul2(mul2(z, s), one_less(s)), inner, s);
+    }
+    case GOLDY_ACT_SILU: {
+      const uint64_t s = fast_sigmoid2(z);
+      return mul2(s, fma2(z, one_less(s), two(1.0f)));
+    }
+    default: {
+      const float2 v = apart(z);
+      return two(act_slope(v.x, act), act_slope(v.y, act));
+    }
   }
 }
 

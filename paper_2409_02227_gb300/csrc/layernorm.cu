@@ -64,37 +64,6 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-// Two fp32 values in one register pair: this hardware multiplies and adds both
-// with one instruction, rounding each as ever (the backward pass of 8192 rows of
-// 8192 took 89 us with single values, 75 with pairs: it issues 24 instructions
-// per element otherwise).
-__device__ __forceinline__ uint64_t two(float lo, float hi) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-  return r;
-}
-__device__ __forceinline__ uint64_t two(float v) { return two(v, v); }
-__device__ __forceinline__ float2 apart(uint64_t v) {
-  float2 r;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-  return r;
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-
 // Sums of a and of b over the warp, in lanes 0 to 15 that of a, in the others
 // that of b: half the exchanges of two sums.
 __device__ __forceinline__ float warp_sum2(float a, float b, int lane) {
@@ -483,7 +452,8 @@ __global__ void __launch_bounds__(kBwdThreads) norm_backward_kernel(const NormPa
     mean = __ldg(p.mean + row);
     rstd = __ldg(p.rstd + row);
   }
-  // in pairs; columns outside the row have dy = gamma = 0 and add nothing
+  // in pairs (8192 rows of 8192: 75 us; one by one 89, at 24 instructions per
+  // element); columns outside the row have dy = gamma = 0 and add nothing
   uint64_t gamma[VALS / 2], dg2[VALS / 2], db2[VALS / 2];
   {
     float f[VALS];

@@ -388,17 +388,13 @@ __device__ __forceinline__ void lin_drain(LinDrain d) {
   for (int chunk = d.side; chunk < chunks; chunk += kLinSides) {
     const int left = rows - chunk * 8;
     if (!AHEAD) fetch_z(chunk);
-    float v[8], slope[8];
+    float v[8];
+    uint64_t slope[4];
+    if (SLOPE) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      if (SLOPE) {
-        if (PAIRS) {
-          const uint32_t w = lin_trade(z[i], odd);
-          slope[2 * i] = act_slope(bf16_lo(w), ACT);
-          slope[2 * i + 1] = act_slope(bf16_hi(w), ACT);
-        } else {
-          slope[i] = act_slope(bf16_lo(z[i]), ACT);
-        }
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t w = PAIRS ? lin_trade(z[i], odd) : (z[(2 * i) % N] & 0xFFFFu) | (z[(2 * i + 1) % N] << 16);
+        slope[i] = act_slope2(two(bf16_lo(w), bf16_hi(w)), ACT);
       }
     }
     if (AHEAD) fetch_z(chunk + kLinSides);
@@ -436,10 +432,15 @@ __device__ __forceinline__ void lin_drain(LinDrain d) {
       }
       d.z += (kLinSides - 1) * N * d.z_step;
     }
+    if (SLOPE || (PASS == kLinForward && ACT != GOLDY_ACT_NONE)) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if (SLOPE) v[j] *= slope[j];
-      if (PASS == kLinForward) v[j] = act_value(v[j], ACT);
+      for (int i = 0; i < 4; ++i) {
+        uint64_t pair = two(v[2 * i], v[2 * i + 1]);
+        pair = SLOPE ? mul2(pair, slope[i]) : act_value2(pair, ACT);
+        const float2 r = apart(pair);
+        v[2 * i] = r.x;
+        v[2 * i + 1] = r.y;
+      }
     }
     if (!AHEAD) fetch_q(chunk);
     if (RES) {
