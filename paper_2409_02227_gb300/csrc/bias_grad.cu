@@ -151,9 +151,11 @@ __global__ void __launch_bounds__(kWarps * 32, 4) bias_grad_kernel(const BiasGra
   const int mine = threadIdx.x / kCols, c = c0 + int(threadIdx.x) % kCols;
   if (p.groups == 1) {
     float s = 0.0f;
-    if (c < p.cols && p.rows > 0) {
-      const int used = (p.rows + height - 1) / height;
-      for (int i0 = mine; i0 < used; i0 += 12 * kShare) s += partials(i0, kShare, used, 0);
+    // only the slices that the group's rows lie in have written a partial row
+    const int a = first_row(0), b = first_row(1);
+    if (c < p.cols && a < b) {
+      const int used = (b - 1) / height + 1;
+      for (int i0 = a / height + mine; i0 < used; i0 += 12 * kShare) s += partials(i0, kShare, used, 0);
     }
     part[mine][threadIdx.x % kCols] = s;
     __syncthreads();
