@@ -8,7 +8,8 @@ activation and residual in their epilogues, and in the backward pass the
 input gradient through the activation, weight gradients, bias gradients and
 the norm's gradient.  With experts, token r goes through the weights of expert
 ids[r]: rows are ordered by expert once, and the products take the experts'
-row ranges from an offsets array on the device.
+row ranges from an offsets array on the device.  A token whose id is no
+expert's goes through none: its y is x, and it adds to no gradient but dx.
 
 ``python -m paper_2409_02227_gb300.ffn_block [--experts 8]`` trains one block
 on a fixed synthetic batch for a few steps and prints the loss.
@@ -53,6 +54,9 @@ class FeedForward:
         self.master: Optional[Dict[str, torch.Tensor]] = None
         self.order: Optional[torch.Tensor] = None
         self.offsets: Optional[torch.Tensor] = None
+        self.lost: Optional[torch.Tensor] = None         # rows without an expert, in the experts' order
+        self.bounds = torch.arange(experts + 1, device=device)
+        self.zero = torch.zeros((), device=device, dtype=torch.bfloat16)
 
     def _kw(self):
         return dict(offsets=0 if self.offsets is None else self.offsets.data_ptr(), workspace=self.work.data_ptr(),
@@ -63,16 +67,21 @@ class FeedForward:
             raise ValueError("expert ids come with experts")
         if ids is None:
             return
-        self.order = torch.argsort(ids, stable=True)
-        bounds = torch.arange(self.experts + 1, device=ids.device, dtype=ids.dtype)
-        self.offsets = torch.searchsorted(ids[self.order], bounds).int()
+        ids, self.order = ids.long().sort(stable=True)
+        self.offsets = torch.searchsorted(ids, self.bounds, out_int32=True)
+        self.lost = (ids.clamp(0, self.experts - 1) != ids)[:, None]
 
     def forward(self, x: torch.Tensor, ids: Optional[torch.Tensor] = None) -> torch.Tensor:
         """x: rows x width, bf16; ids: the expert of each row."""
         self._route(ids)
         p, kw = self.p, self._kw()
-        self.x = x if ids is None else x[self.order]
-        y = torch.empty_like(self.x)
+        if ids is None:
+            self.x, y = x, torch.empty_like(x)
+        else:
+            # rows without an expert: y keeps x, which the products leave as it is,
+            # and the norm sees zeros
+            y = x[self.order]
+            self.x = torch.where(self.lost, self.zero, y)
         G.goldy_layernorm_forward(self.norm, self.x.data_ptr(), p["gamma"].data_ptr(), p["beta"].data_ptr(),
                                   self.normed.data_ptr(), self.mean.data_ptr(), self.rstd.data_ptr(), kw["stream"])
         G.goldy_linear_forward(self.up, self.normed.data_ptr(), p["w1"].data_ptr(), self.h.data_ptr(),
@@ -85,7 +94,8 @@ class FeedForward:
         """The gradient of x; those of the parameters are in ``grads``."""
         p, g, kw = self.p, self.grads, self._kw()
         dy = dy if self.order is None else dy[self.order]
-        dz, dnormed, dx = torch.empty_like(self.z), torch.empty_like(self.normed), torch.empty_like(self.x)
+        dz, dx = torch.empty_like(self.z), torch.empty_like(self.x)
+        dnormed = torch.empty_like(self.normed) if self.order is None else torch.zeros_like(self.normed)
         # down projection; its input gradient is the up projection's dZ
         G.goldy_linear_bias_grad(self.down, dy.data_ptr(), g["b2"].data_ptr(), **kw)
         G.goldy_linear_weight_grad(self.down, self.h.data_ptr(), dy.data_ptr(), g["w2"].data_ptr(), **kw)
