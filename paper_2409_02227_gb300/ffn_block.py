@@ -36,7 +36,7 @@ class FeedForward:
         gen.manual_seed(seed)
         lead = (experts,) if experts else ()
         rnd = lambda *s: torch.randn(*s, generator=gen, device=device)  # noqa: E731
-        self.experts, self.rows = experts, rows
+        self.experts, self.rows, self.width = experts, rows, width
         self.p: Dict[str, torch.Tensor] = {
             "gamma": torch.ones(width, device=device), "beta": torch.zeros(width, device=device),
             "w1": (rnd(*lead, width, hidden) * width ** -0.5).bfloat16(), "b1": torch.zeros(*lead, hidden, device=device),
@@ -52,6 +52,7 @@ class FeedForward:
         need = max(G.goldy_linear_query(self.up), G.goldy_linear_query(self.down), G.goldy_layernorm_query(self.norm))
         self.work = torch.zeros(max(need, 256), dtype=torch.uint8, device=device)
         self.master: Optional[Dict[str, torch.Tensor]] = None
+        self.x: Optional[torch.Tensor] = None            # the forward pass's rows
         self.order: Optional[torch.Tensor] = None
         self.offsets: Optional[torch.Tensor] = None
         self.lost: Optional[torch.Tensor] = None         # rows without an expert, in the experts' order
@@ -59,20 +60,37 @@ class FeedForward:
         self.zero = torch.zeros((), device=device, dtype=torch.bfloat16)
 
     def _kw(self):
+        if not self.work.is_cuda:
+            raise RuntimeError(f"the block is on {self.work.device}: its kernels need a GPU")
         return dict(offsets=0 if self.offsets is None else self.offsets.data_ptr(), workspace=self.work.data_ptr(),
                     workspace_bytes=self.work.numel(), stream=torch.cuda.current_stream().cuda_stream)
+
+    def _check(self, t: torch.Tensor, name: str) -> torch.Tensor:
+        """A tensor for the kernels, which take an address: rows packed and on a
+        16-byte boundary, copied if they are not."""
+        shape = (self.rows, self.width)
+        if t.shape != shape or t.dtype != torch.bfloat16 or t.device != self.work.device:
+            raise ValueError(f"{name} must be a bf16 tensor of {shape[0]} x {shape[1]} on {self.work.device}, "
+                             f"not {t.dtype} of {' x '.join(map(str, t.shape))} on {t.device}")
+        t = t.contiguous()
+        return t.clone() if t.data_ptr() % 16 else t
 
     def _route(self, ids: Optional[torch.Tensor]) -> None:
         if (ids is not None) != (self.experts > 0):
             raise ValueError("expert ids come with experts")
         if ids is None:
             return
+        whole = ids.dtype in (torch.uint8, torch.int8, torch.int16, torch.int32, torch.int64)
+        if ids.shape != (self.rows,) or not whole or ids.device != self.work.device:
+            raise ValueError(f"ids must be {self.rows} integers on {self.work.device}, "
+                             f"not {ids.dtype} of {' x '.join(map(str, ids.shape))} on {ids.device}")
         ids, self.order = ids.long().sort(stable=True)
         self.offsets = torch.searchsorted(ids, self.bounds, out_int32=True)
         self.lost = (ids.clamp(0, self.experts - 1) != ids)[:, None]
 
     def forward(self, x: torch.Tensor, ids: Optional[torch.Tensor] = None) -> torch.Tensor:
-        """x: rows x width, bf16; ids: the expert of each row."""
+        """x: rows x width, bf16, any strides; ids: the expert of each row."""
+        x = self._check(x, "x")
         self._route(ids)
         p, kw = self.p, self._kw()
         if ids is None:
@@ -92,6 +110,9 @@ class FeedForward:
 
     def backward(self, dy: torch.Tensor) -> torch.Tensor:
         """The gradient of x; those of the parameters are in ``grads``."""
+        if self.x is None:
+            raise RuntimeError("backward needs a forward pass before it")
+        dy = self._check(dy, "dy")
         p, g, kw = self.p, self.grads, self._kw()
         dy = dy if self.order is None else dy[self.order]
         dz, dx = torch.empty_like(self.z), torch.empty_like(self.x)
