@@ -120,7 +120,8 @@ class FeedForward:
         # down projection; its input gradient is the up projection's dZ
         G.goldy_linear_bias_grad(self.down, dy.data_ptr(), g["b2"].data_ptr(), **kw)
         G.goldy_linear_weight_grad(self.down, self.h.data_ptr(), dy.data_ptr(), g["w2"].data_ptr(), **kw)
-        G.goldy_linear_input_grad(self.down, dy.data_ptr(), p["w2"].data_ptr(), dz.data_ptr(), z=self.z.data_ptr(), **kw)
+        z = self.z.data_ptr() if self.down.act_x != G.GOLDY_ACT_NONE else 0
+        G.goldy_linear_input_grad(self.down, dy.data_ptr(), p["w2"].data_ptr(), dz.data_ptr(), z=z, **kw)
         # up projection
         G.goldy_linear_bias_grad(self.up, dz.data_ptr(), g["b1"].data_ptr(), **kw)
         G.goldy_linear_weight_grad(self.up, self.normed.data_ptr(), dz.data_ptr(), g["w1"].data_ptr(), **kw)
