@@ -657,7 +657,7 @@ __global__ void __launch_bounds__(kStreamThreads) norm_backward_stream_kernel(co
   bool first = true;
   for (int64_t row = blockIdx.x; row < p.rows || first; row += gridDim.x) {
     if (row >= p.rows) {                           // a CTA without rows has a zero partial
-      for (int c = threadIdx.x; part && c < 2 * p.n; c += kStreamThreads) part[c] = 0.0f;
+      for (int64_t c = threadIdx.x; part && c < 2 * int64_t(p.n); c += kStreamThreads) part[c] = 0.0f;
       break;
     }
     const float m = p.mean[row], rs = p.rstd[row];
