@@ -51,7 +51,9 @@ __global__ void __launch_bounds__(kWarps * 32, 4) bias_grad_kernel(const BiasGra
   const int height = (p.rows + p.slices - 1) / p.slices;
   const int row_lo = min(p.rows, int(blockIdx.y) * height), row_hi = min(p.rows, row_lo + height);
 
-  auto first_row = [&](int e) { return p.offsets ? min(max(__ldg(p.offsets + e), 0), p.rows) : (e == 0 ? 0 : p.rows); };
+  // (a plain load: the kernel before may have written the offsets after this one
+  // began, which the read-only data path does not allow)
+  auto first_row = [&](int e) { return p.offsets ? min(max(p.offsets[e], 0), p.rows) : (e == 0 ? 0 : p.rows); };
   // the first group that ends behind row_lo: all ends are read at once (a
   // search would wait for one after the other)
   int e = 0;

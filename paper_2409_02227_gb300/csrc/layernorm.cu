@@ -88,7 +88,8 @@ __device__ __forceinline__ float lanes_sum(float v) {
 }
 
 // PER parameters from index c on, 0 from n on; VEC: c + PER <= n, on a vector's
-// boundary.
+// boundary.  Plain loads, as of mean and rstd: the kernel before this one may have
+// written them after this one began, which the read-only data path does not allow.
 template <int PER, bool VEC>
 __device__ __forceinline__ void load_params(const void* p, int f32, int c, int n, float absent, float* f) {
   if (!VEC || !p) {
@@ -96,20 +97,20 @@ __device__ __forceinline__ void load_params(const void* p, int f32, int c, int n
     for (int k = 0; k < PER; ++k) {
       if (!VEC && c + k >= n) f[k] = 0.0f;
       else if (!p) f[k] = absent;
-      else f[k] = f32 ? __ldg(static_cast<const float*>(p) + c + k) : load_bf16(p, c + k);
+      else f[k] = f32 ? static_cast<const float*>(p)[c + k] : load_bf16(p, c + k);
     }
   } else if (f32) {
 #pragma unroll
     for (int k = 0; k < PER; k += 4) {
-      const float4 v = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(p) + c + k));
+      const float4 v = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + c + k);
       f[k] = v.x, f[(k + 1) % PER] = v.y, f[(k + 2) % PER] = v.z, f[(k + 3) % PER] = v.w;
     }
   } else if (PER == 8) {
-    const uint4 v = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + c));
+    const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + c);
     f[0] = bf16_lo(v.x), f[1 % PER] = bf16_hi(v.x), f[2 % PER] = bf16_lo(v.y), f[3 % PER] = bf16_hi(v.y);
     f[4 % PER] = bf16_lo(v.z), f[5 % PER] = bf16_hi(v.z), f[6 % PER] = bf16_lo(v.w), f[7 % PER] = bf16_hi(v.w);
   } else {
-    const uint2 v = __ldg(reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + c));
+    const uint2 v = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + c);
     f[0] = bf16_lo(v.x), f[1 % PER] = bf16_hi(v.x), f[2 % PER] = bf16_lo(v.y), f[3 % PER] = bf16_hi(v.y);
   }
 }
@@ -449,8 +450,8 @@ __global__ void __launch_bounds__(kBwdThreads) norm_backward_kernel(const NormPa
   for (int d = 0; d < D - 1; ++d) fetch(d, row + d * step);
   float mean = 0.0f, rstd = 0.0f;
   if (row < p.rows) {
-    mean = __ldg(p.mean + row);
-    rstd = __ldg(p.rstd + row);
+    mean = p.mean[row];
+    rstd = p.rstd[row];
   }
   // in pairs (8192 rows of 8192: 75 us; one by one 89, at 24 instructions per
   // element); columns outside the row have dy = gamma = 0 and add nothing
@@ -477,8 +478,8 @@ __global__ void __launch_bounds__(kBwdThreads) norm_backward_kernel(const NormPa
     fetch(ahead, row + (D - 1) * step);
     const float m = mean, rs = rstd;
     if (row + step < p.rows) {
-      mean = __ldg(p.mean + row + step);
-      rstd = __ldg(p.rstd + row + step);
+      mean = p.mean[row + step];
+      rstd = p.rstd[row + step];
     }
     copy_wait<D - 1>();
     if (R::SHIFT) team_sync<TEAM, kBwdThreads>(team);

@@ -38,6 +38,11 @@
 // first part: 58 against 53 us for a 2048 x 8192 gradient over 2048 rows.)  bf16 results (relative rounding 2^-8) keep
 // the whole sum in tensor memory.
 //
+// A launch begins while the kernel before it still runs, so nothing that one may
+// have written (offsets, Z, R) goes through the read-only data path, which
+// wants data that does not change while the kernel lives: plain loads behind
+// griddepcontrol.wait.
+//
 // Every wait is bounded; a wait that runs out sets the error word and the
 // kernel ends.
 #pragma once
@@ -194,8 +199,8 @@ struct LinWalk {
     const int g = e0 + lane;
     int o = 0, o1 = 0;
     if (g < p.groups) {
-      o = min(max(__ldg(p.offsets + g), 0), p.rows);
-      o1 = min(max(__ldg(p.offsets + g + 1), 0), p.rows);
+      o = min(max(p.offsets[g], 0), p.rows);
+      o1 = min(max(p.offsets[g + 1], 0), p.rows);
     }
     int m = max(o, prev);
 #pragma unroll
@@ -226,8 +231,8 @@ struct LinWalk {
       }
       int a = 0, b = p.rows;
       if (p.offsets) {
-        a = min(max(__ldg(p.offsets + e), 0), p.rows);
-        b = min(max(__ldg(p.offsets + e + 1), a), p.rows);
+        a = min(max(p.offsets[e], 0), p.rows);
+        b = min(max(p.offsets[e + 1], a), p.rows);
       }
       t.k0 = a;
       t.red = b - a;
@@ -356,7 +361,7 @@ __device__ __forceinline__ void lin_drain(LinDrain d) {
 #pragma unroll
       for (int i = 0; i < N; ++i, z_at += d.z_step)
         if (DOWN * i < left)
-          z[i] = PAIRS ? __ldg(reinterpret_cast<const uint32_t*>(z_at)) : uint32_t(*reinterpret_cast<const uint16_t*>(z_at));
+          z[i] = PAIRS ? *reinterpret_cast<const uint32_t*>(z_at) : uint32_t(*reinterpret_cast<const uint16_t*>(z_at));
       z_at += (kLinSides - 1) * N * d.z_step;
     }
   };
