@@ -483,6 +483,10 @@ goldy_status goldy_gemm_noalloc(const goldy_gemm_desc* desc, int variant, const 
  * kernel with the work around the product in its epilogue.  X is rows x in, W
  * is in x out, Y is rows x out, row-major; X, W and dY are bf16, products are
  * accumulated in fp32, and every result is rounded once, to nearest even.
+ * (The tensor cores' fp32 accumulators truncate: about 1e-9 of the sum per
+ * reduction element.  An accumulator takes at most 768 elements of an fp32
+ * result and 8192 rows of a bf16 weight gradient over more than 65536; other
+ * bf16 results keep the whole reduction in one.)
  *
  * groups = 0: one W for all rows.  groups = E >= 1: E experts with weights
  * W + e * stride_w and packed biases b + e * out; rows offsets[e] ..

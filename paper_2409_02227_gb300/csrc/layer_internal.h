@@ -46,6 +46,10 @@ constexpr size_t kLayerCounterBytes = 64 * 1024;
 constexpr int kLinForward = 0;
 constexpr int kLinInputGrad = 1;
 constexpr int kLinWeightGrad = 2;
+// results of the kernels
+constexpr int kLinBf16 = 0;
+constexpr int kLinF32 = 1;
+constexpr int kLinBf16Long = 2;           // weight gradient over more than kLinLongRows rows
 constexpr int kLinEpiWarps = 12;
 // a load warp, an MMA warp, the epilogue's, and the weight gradient's mending warp
 constexpr int lin_threads(int pass) { return (2 + kLinEpiWarps + (pass == kLinWeightGrad ? 1 : 0)) * 32; }
@@ -56,6 +60,11 @@ constexpr int kLinRowBand = 8;            // row tiles walked before the next co
 // not fit (spilled: 2048 x 8192 input gradient over 2048 columns 57 us, now 53)
 constexpr int kLinMaxTileF32 = 192;
 constexpr int kLinPromote = 12;           // stages accumulated in tensor memory for fp32 results
+constexpr int kLinPromoteLong = 128;      // and for long bf16 ones, whose sums may spill: rarely touched
+// rows from which a bf16 weight gradient is summed that way too: the accumulator's
+// truncation, 1e-9 per row, is then 6% of a rounding to bf16 (1024 x 1024 over 65537
+// rows: 95 us, in one accumulator 88; 192-row tiles without spills 124)
+constexpr int64_t kLinLongRows = 65536;
 constexpr int kLinSmemBudget = 232448;    // 227 KB
 
 // n / d for 0 <= n < 2^31 as the high half of n * mul, mul = floor(2^64 / d) + 1.

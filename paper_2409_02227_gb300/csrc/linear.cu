@@ -16,26 +16,26 @@
 namespace goldy {
 
 // linear_kernels.cu, compiled once per pass and activation
-const void* linear_kernel_p0_a0(int pair, int out_f32);
-const void* linear_kernel_p0_a1(int pair, int out_f32);
-const void* linear_kernel_p0_a2(int pair, int out_f32);
-const void* linear_kernel_p0_a3(int pair, int out_f32);
-const void* linear_kernel_p0_a4(int pair, int out_f32);
-const void* linear_kernel_p1_a0(int pair, int out_f32);
-const void* linear_kernel_p1_a1(int pair, int out_f32);
-const void* linear_kernel_p1_a2(int pair, int out_f32);
-const void* linear_kernel_p1_a3(int pair, int out_f32);
-const void* linear_kernel_p1_a4(int pair, int out_f32);
-const void* linear_kernel_p2_a0(int pair, int out_f32);
+const void* linear_kernel_p0_a0(int pair, int out);
+const void* linear_kernel_p0_a1(int pair, int out);
+const void* linear_kernel_p0_a2(int pair, int out);
+const void* linear_kernel_p0_a3(int pair, int out);
+const void* linear_kernel_p0_a4(int pair, int out);
+const void* linear_kernel_p1_a0(int pair, int out);
+const void* linear_kernel_p1_a1(int pair, int out);
+const void* linear_kernel_p1_a2(int pair, int out);
+const void* linear_kernel_p1_a3(int pair, int out);
+const void* linear_kernel_p1_a4(int pair, int out);
+const void* linear_kernel_p2_a0(int pair, int out);
 
 namespace {
 
-const void* linear_kernel_fn(int pass, int act, int pair, int out_f32) {
+const void* linear_kernel_fn(int pass, int act, int pair, int out) {
   typedef const void* (*Pick)(int, int);
   static const Pick picks[2][5] = {
       {linear_kernel_p0_a0, linear_kernel_p0_a1, linear_kernel_p0_a2, linear_kernel_p0_a3, linear_kernel_p0_a4},
       {linear_kernel_p1_a0, linear_kernel_p1_a1, linear_kernel_p1_a2, linear_kernel_p1_a3, linear_kernel_p1_a4}};
-  return (pass == kLinWeightGrad ? linear_kernel_p2_a0 : picks[pass][act])(pair, out_f32);
+  return (pass == kLinWeightGrad ? linear_kernel_p2_a0 : picks[pass][act])(pair, out);
 }
 
 constexpr int64_t kMaxDim = (int64_t(1) << 31) - 1024;   // TMA coordinates are 32-bit
@@ -62,6 +62,12 @@ LinShape shape_of(const goldy_linear_desc& d, int pass) {
   s.red = pass == kLinForward ? d.in : pass == kLinInputGrad ? d.out : d.rows;
   s.out_dtype = pass == kLinForward ? d.y_dtype : pass == kLinInputGrad ? d.dx_dtype : d.dw_dtype;
   return s;
+}
+
+// What the kernel makes of a shape's result.
+int result_of(const LinShape& s) {
+  if (s.out_dtype == GOLDY_F32) return kLinF32;
+  return s.pass == kLinWeightGrad && s.rows > kLinLongRows ? kLinBf16Long : kLinBf16;
 }
 
 struct LinChoice {
@@ -190,11 +196,11 @@ goldy_status encode(const LayerContext& ctx, CUtensorMap* m, const Operand& o, i
   return GOLDY_OK;
 }
 
-goldy_status set_smem(const LayerContext& ctx, const void* fn, int pass, int act, int pair, int f32) {
+goldy_status set_smem(const LayerContext& ctx, const void* fn, int pass, int act, int pair, int out) {
   static std::mutex mu;
-  static bool done[kMaxDevices][3][5][2][2] = {};
+  static bool done[kMaxDevices][3][5][2][3] = {};
   std::lock_guard<std::mutex> lock(mu);
-  bool& d = done[ctx.device][pass][act][pair][f32];
+  bool& d = done[ctx.device][pass][act][pair][out];
   if (!d) {
     const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kLinSmemBudget);
     if (e != cudaSuccess) return fail(GOLDY_ERR_CUDA, std::string("cudaFuncSetAttribute: ") + cudaGetErrorString(e));
@@ -270,9 +276,9 @@ goldy_status launch_linear(const LayerContext& ctx, void* arg) {
     if (st == GOLDY_OK && !wgrad) st = encode(ctx, &p.tb_part, o[1], p.part_box);
     if (st != GOLDY_OK) return st;
   }
-  const int f32 = s.out_dtype == GOLDY_F32 ? 1 : 0;
-  const void* fn = linear_kernel_fn(s.pass, call.act, c.pair, f32);
-  goldy_status st = set_smem(ctx, fn, s.pass, call.act, c.pair, f32);
+  const int out = result_of(s);
+  const void* fn = linear_kernel_fn(s.pass, call.act, c.pair, out);
+  goldy_status st = set_smem(ctx, fn, s.pass, call.act, c.pair, out);
   if (st != GOLDY_OK) return st;
   const int64_t units = c.max_tiles * c.split;
   const int64_t workers = std::max<int64_t>(1, std::min<int64_t>(units, ctx.sm_count / ctas));

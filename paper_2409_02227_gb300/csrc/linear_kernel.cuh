@@ -35,8 +35,10 @@
 // kLinPromote stages (768 elements) and are summed in registers with rounding
 // to nearest: 7e-7 at any length.  (Parts of 512 elements are good to 5e-7, but
 // the drain of a tile, 3.6 us, then holds its accumulator past the next tile's
-// first part: 58 against 53 us for a 2048 x 8192 gradient over 2048 rows.)  bf16 results (relative rounding 2^-8) keep
-// the whole sum in tensor memory.
+// first part: 58 against 53 us for a 2048 x 8192 gradient over 2048 rows.)  bf16
+// results (relative rounding 2^-8) keep the whole sum in tensor memory, but for weight
+// gradients over more than kLinLongRows rows, which are PROMOTEd like fp32 ones, in
+// parts of 8192 rows: a million rows would lose 1e-3 of their sum.
 //
 // A launch begins while the kernel before it still runs, so nothing that one may
 // have written (offsets, Z, R) goes through the read-only data path, which
@@ -133,9 +135,10 @@ __device__ __forceinline__ bool lin_wait_warp(uint32_t bar, uint32_t parity, con
   return __all_sync(0xFFFFFFFFu, lin_wait<CLUSTER>(bar, parity, abort_flag));
 }
 
-// Stages per accumulator of an fp32 result: equal parts of at most kLinPromote.
+// Stages per accumulator of a promoted result: equal parts of at most MOST.
+template <int MOST>
 __device__ __forceinline__ int lin_promote(int kbs) {
-  const int parts = (kbs + kLinPromote - 1) / kLinPromote;
+  const int parts = (kbs + MOST - 1) / MOST;
   return parts > 1 ? int(unsigned(kbs + parts - 1) / unsigned(parts)) : kbs;
 }
 
@@ -498,11 +501,12 @@ __device__ __forceinline__ void lin_drain_as(const LinearParams& p, const LinUni
   else lin_drain<PASS, PAIR, OUT_F32, ACT, PAIRS, kLinNo>(d);
 }
 
-template <int PASS, int ACT, bool PAIR, bool OUT_F32>
+template <int PASS, int ACT, bool PAIR, bool OUT_F32, bool PROMOTE>
 __global__ void __launch_bounds__(lin_threads(PASS), 1) linear_kernel(const __grid_constant__ LinearParams p) {
   constexpr bool A_MN = PASS != kLinInputGrad;         // P contiguous along c
   constexpr bool B_MN = PASS == kLinWeightGrad;        // Q contiguous along r
   constexpr bool TAIL = PASS == kLinWeightGrad;        // ragged reduction
+  constexpr int PART = OUT_F32 ? kLinPromote : kLinPromoteLong;   // PROMOTE: stages per accumulator, at most
   constexpr int ACC = 2;
   constexpr int A_BYTES = 128 * kLinStageK * 2;
   constexpr int CTAS = PAIR ? 2 : 1;
@@ -697,7 +701,7 @@ __global__ void __launch_bounds__(lin_threads(PASS), 1) linear_kernel(const __gr
       for (int u = worker; ok && walk.find(u, t); u += n_workers) {
         const int nw = lin_shared(t.nw), kb0 = lin_shared(t.kb0), kb1 = lin_shared(t.kb1);
         const uint32_t idesc = ptx::make_idesc_bf16(128 * CTAS, 16, A_MN, B_MN) + (uint32_t((nw - 16) >> 3) << 17);
-        const int step = OUT_F32 ? lin_promote(kb1 - kb0) : kb1 - kb0;
+        const int step = PROMOTE ? lin_promote<PART>(kb1 - kb0) : kb1 - kb0;
         if (lin_elect(leader)) {
           ready = false;
           for (int kb = kb0; kb < kb1;) {
@@ -788,7 +792,7 @@ __global__ void __launch_bounds__(lin_threads(PASS), 1) linear_kernel(const __gr
     if (!ok && lane == 0) raise_error(p.err, abort_flag, kErrProducerWait);
   } else {
     // ------------------------------------------------------------ epilogue
-    constexpr int MOST = (kLinMaxTileF32 / 8 + kLinSides - 1) / kLinSides;   // 8-row chunks of an fp32 tile per warp
+    constexpr int MOST = ((OUT_F32 ? kLinMaxTileF32 : 256) / 8 + kLinSides - 1) / kLinSides;   // 8-row chunks of a tile per warp
     const int ew = warp - 2;
     const int q = warp & 3;                            // lanes of tensor memory this warp may read
     const int side = ew >> 2;                          // takes chunks side, side + kLinSides, ...
@@ -821,13 +825,13 @@ __global__ void __launch_bounds__(lin_threads(PASS), 1) linear_kernel(const __gr
       const bool some = t.kb1 > t.kb0;                 // else the sum is empty and no accumulator is used
       const bool split = p.split > 1;
       uint32_t cols = tmem_base + (uint32_t(q * 32) << 16) + uint32_t(acc * 256);
-      if (OUT_F32 && t.kb1 - t.kb0 > kLinPromote) {
-        // sum the accumulators of some kLinPromote stages each.  A weight
+      if (PROMOTE && t.kb1 - t.kb0 > PART) {
+        // sum the accumulators of some PART stages each.  An fp32 weight
         // gradient is stored from here, starting from what it is added to, so
         // that the last accumulator is free at once; other totals go back into
         // the last one's tensor memory, where the code below finds them.
-        const int step = lin_promote(t.kb1 - t.kb0);
-        const bool direct = PASS == kLinWeightGrad && !split;
+        const int step = lin_promote<PART>(t.kb1 - t.kb0);
+        const bool direct = PASS == kLinWeightGrad && OUT_F32 && !split;
         const int64_t c_step = p.ldc * 4;
         char* c_out = static_cast<char*>(p.c) + (int64_t(t.e) * p.c_group + (int64_t(t.r0) + side * 8) * p.ldc + col0 + lane) * 4;
         const int c_rows = col0 + lane < p.size_c ? t.w - side * 8 : 0;

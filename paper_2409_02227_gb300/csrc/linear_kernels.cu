@@ -8,13 +8,19 @@
 
 namespace goldy {
 
-const void* LIN_CAT(linear_kernel_p, GOLDY_LINEAR_PASS, _a, GOLDY_LINEAR_ACT)(int pair, int out_f32) {
+// out: kLinBf16, kLinF32 or (weight gradient) kLinBf16Long
+const void* LIN_CAT(linear_kernel_p, GOLDY_LINEAR_PASS, _a, GOLDY_LINEAR_ACT)(int pair, int out) {
   constexpr int P = GOLDY_LINEAR_PASS, A = GOLDY_LINEAR_ACT;
+  if constexpr (P == kLinWeightGrad) {
+    if (out == kLinBf16Long)
+      return pair ? reinterpret_cast<const void*>(&linear_kernel<P, A, true, false, true>)
+                  : reinterpret_cast<const void*>(&linear_kernel<P, A, false, false, true>);
+  }
   if (pair)
-    return out_f32 ? reinterpret_cast<const void*>(&linear_kernel<P, A, true, true>)
-                   : reinterpret_cast<const void*>(&linear_kernel<P, A, true, false>);
-  return out_f32 ? reinterpret_cast<const void*>(&linear_kernel<P, A, false, true>)
-                 : reinterpret_cast<const void*>(&linear_kernel<P, A, false, false>);
+    return out == kLinF32 ? reinterpret_cast<const void*>(&linear_kernel<P, A, true, true, true>)
+                          : reinterpret_cast<const void*>(&linear_kernel<P, A, true, false, false>);
+  return out == kLinF32 ? reinterpret_cast<const void*>(&linear_kernel<P, A, false, true, true>)
+                        : reinterpret_cast<const void*>(&linear_kernel<P, A, false, false, false>);
 }
 
 }  // namespace goldy
