@@ -224,6 +224,7 @@ goldy_status launch_linear(const LayerContext& ctx, void* arg) {
   const LinShape& s = call.s;
   LinearParams& p = call.prm;
   const LinChoice c = choose(s);
+  if (c.max_tiles * c.split > kMaxDim) return fail(GOLDY_ERR_UNSUPPORTED, "linear layer: too many output tiles");
   Operand* const o = call.o;
   const size_t copy_bytes = s.red > 0 ? o[0].copy_bytes() + o[1].copy_bytes() : 0;
   if (c.split > 1 || copy_bytes > 0) {
@@ -248,7 +249,6 @@ goldy_status launch_linear(const LayerContext& ctx, void* arg) {
       ws += bytes;
     }
   }
-  if (c.max_tiles * c.split > kMaxDim) return fail(GOLDY_ERR_UNSUPPORTED, "linear layer: too many output tiles");
   const bool wgrad = s.pass == kLinWeightGrad;
   const int ctas = c.pair ? 2 : 1;
   p.groups = s.groups;
@@ -350,6 +350,13 @@ goldy_status check_linear(const goldy_linear_desc* d) {
     return bad("linear layer: a row stride is too large");
   if (d->stride_w < 0 || (d->groups > 1 && d->stride_w && d->stride_w < d->in * stride_or_dense(d->ldw, d->out, GOLDY_BF16)))
     return bad("linear layer: stride_w is smaller than in * ldw");
+  // no array has more elements than this; sums of sizes then stay far from 64 bits
+  const double most = double(int64_t(1) << 46), rows = double(d->rows);
+  const int64_t ldw = stride_or_dense(d->ldw, d->out, GOLDY_BF16);
+  const double weights = d->groups > 1 && d->stride_w ? double(d->stride_w) : double(d->in) * double(ldw);
+  if (weights * std::max(1, d->groups) > most || rows * double(std::max({d->in, d->ldx, d->lddx})) > most ||
+      rows * double(std::max({d->out, d->ldy, d->ldz, d->ldr})) > most)
+    return bad("linear layer: an array is too large");
   if (d->act < GOLDY_ACT_NONE || d->act > GOLDY_ACT_SILU || d->act_x < GOLDY_ACT_NONE || d->act_x > GOLDY_ACT_SILU)
     return bad("linear layer: unknown activation");
   if (!is_dtype(d->y_dtype) || !is_dtype(d->dx_dtype) || !is_dtype(d->dw_dtype) || !is_dtype(d->bias_dtype))
