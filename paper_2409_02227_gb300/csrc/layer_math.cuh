@@ -94,24 +94,6 @@ __device__ __forceinline__ float normal_tail(float z, float& g) {
   return s * t * g;
 }
 
-__device__ __forceinline__ float act_value(float z, int act) {
-  switch (act) {
-    case GOLDY_ACT_RELU: return z < 0.0f ? 0.0f : z;
-    case GOLDY_ACT_GELU: {
-      float g;
-      const float q = normal_tail(z, g);
-      return z * (z < 0.0f ? q : 1.0f - q);
-    }
-    case GOLDY_ACT_GELU_TANH: {
-      // (1 + tanh u) / 2 = 1 / (1 + exp(-2u)), u = sqrt(2/pi) (z + 0.044715 z^3)
-      const float u2 = 1.5957691216057308f * fmaf(0.044715f * z * z, z, z);
-      return z * fast_sigmoid(u2);
-    }
-    case GOLDY_ACT_SILU: return z * fast_sigmoid(z);
-    default: return z;
-  }
-}
-
 __device__ __forceinline__ float act_slope(float z, int act) {
   switch (act) {
     case GOLDY_ACT_RELU: return z > 0.0f ? 1.0f : 0.0f;
@@ -169,10 +151,11 @@ __device__ __forceinline__ uint64_t act_value2(uint64_t z, int act) {
       return mul2(z, fast_sigmoid2(u2));
     }
     case GOLDY_ACT_SILU: return mul2(z, fast_sigmoid2(z));
-    default: {
+    case GOLDY_ACT_RELU: {
       const float2 v = apart(z);
-      return two(act_value(v.x, act), act_value(v.y, act));
+      return two(v.x < 0.0f ? 0.0f : v.x, v.y < 0.0f ? 0.0f : v.y);
     }
+    default: return z;
   }
 }
 
