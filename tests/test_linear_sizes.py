@@ -27,3 +27,22 @@ def test_long_strides_of_few_rows_are_not():
     G.goldy_linear_query(G.linear_desc(5, 72, 72, ldx=LARGEST, ldy=LARGEST, ldz=LARGEST, ldr=LARGEST))
     G.goldy_linear_query(G.linear_desc(300, 8192, 8192, groups=512, stride_w=1 << 32))
     G.goldy_linear_query(G.linear_desc(1 << 24, 8192, 8192))
+
+
+@pytest.mark.parametrize("groups", [0, 1, 8, 64, 4096])
+@pytest.mark.parametrize("rows", [1, 37, 500, 100000])
+@pytest.mark.parametrize("k,n", [(4096, 1024), (75, 130), (64, 8), (1001, 77)])
+def test_workspace_holds_what_the_calls_keep_there(rows, k, n, groups):
+    """64 KiB of counters and, one call at a time, the bias gradient's partial rows
+    (a slice's or an expert's, one more than their number apart from each other) or
+    padded copies of both operands whose rows are off 16 bytes."""
+    pad = lambda cols: (cols + 7) // 8 * 8  # noqa: E731
+    experts = max(1, groups)
+    x, y, w = rows * pad(k) * 2, rows * pad(n) * 2, experts * k * pad(n) * 2
+    assert G.goldy_linear_query(G.linear_desc(rows, k, n, groups=groups)) >= 65536 + (1 + experts) * n * 4
+    packed = G.goldy_linear_query(G.linear_desc(rows, k, n, groups=groups, ldx=k, ldw=n, ldy=n))
+    x, y, w = x if k % 8 else 0, y if n % 8 else 0, w if n % 8 else 0
+    assert packed >= 65536 + max(x + w, y + w, x + y)
+    if rows > 1 and groups > 1 and n % 8:
+        apart = G.linear_desc(rows, k, n, groups=groups, ldw=pad(n), ldy=pad(n), ldx=pad(k), stride_w=k * pad(n) + 4)
+        assert G.goldy_linear_query(apart) >= 65536 + w       # experts off 16 bytes from one another
