@@ -39,7 +39,7 @@ const void* linear_kernel_fn(int pass, int act, int pair, int out) {
 }
 
 constexpr int64_t kMaxDim = (int64_t(1) << 31) - 1024;   // TMA coordinates are 32-bit
-constexpr int kModelSms = 152;                           // SMs the choice is made for
+constexpr int kModelSms = 152;                           // SMs the choice is made for (a partition's calls take it too)
 constexpr int kMaxDevices = 64;
 
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
@@ -80,8 +80,9 @@ int part_chunks(int tile_r) { return int(ceil_div(ceil_div(tile_r, 8), kLinEpiWa
 
 // Time model of a launch in ns, fitted to the times of 46 shapes (1 to 8192
 // rows, 64 to 8192 features, 0 to 64 groups, all passes) under every tile and
-// split: the choice is 2% slower than the best measured one on average, 24% at
-// worst (9 rows per group on average, where sizes spread past one tile).
+// split.  With the kernels as they are now the choice is 4% slower than the best
+// measured one on average over these and over 46 other shapes, 34% at worst (8 rows
+// of 16 groups, 328 -> 5440 features, where a split of 8 is best).
 //   A 64-deep stage of an nw-row tile costs the largest of its tensor time, the
 //   issue of its copies and products, and its operands' trip from L2.
 //   A unit costs its stages or, if longer, draining its accumulator; the last
