@@ -20,8 +20,8 @@
 // second small kernel sums the partial rows in CTA order.  Nothing depends on
 // the order of arrival.  Rows too long for a team are shared by a cluster of 2 to
 // 8 CTAs, which exchange their statistics through distributed shared memory,
-// one cluster barrier per row (8192 rows of 12288, bf16: backwards 186 us, and
-// 1176 when such rows streamed; 2048 rows of 65536 forwards 149 and 471 us);
+// one cluster barrier per row (8192 rows of 12288, bf16: backwards 187 us, and
+// 1176 when such rows streamed; 2048 rows of 65536 forwards 154 and 471 us);
 // rows too long for 8 CTAs (131072 elements, backwards 65536), and those of
 // clusters inside an SM partition, stream through three (two) reads instead.
 #include <cuda_runtime.h>
