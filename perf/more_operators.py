@@ -258,9 +258,9 @@ def _plan(s):
             need = G.goldy_residual_norm_query(d)
     elif op == "keep":
         n = case["n"]
-        s["desc"] = G.keep8_desc(rows, n, dtype=dtype, act=getattr(G, "GOLDY_ACT_" + case["act"].upper()))
-        s["q"] = torch.empty(rows, n, dtype=torch.uint8, device="cuda")
-        s["scales"] = torch.empty(rows, -(-n // BLOCK), dtype=torch.uint8, device="cuda")
+        s["desc"] = d = G.keep8_desc(rows, n, dtype=dtype, act=getattr(G, "GOLDY_ACT_" + case["act"].upper()))
+        q_bytes, scale_bytes = G.goldy_keep8_query(d)
+        s["q"], s["scales"] = (torch.empty(b, dtype=torch.uint8, device="cuda") for b in (q_bytes, scale_bytes))
         s["z8"], s["h"] = torch.empty_like(s["z"]), torch.empty_like(s["z"])
     else:
         k, width = case["k"], case["width"]
