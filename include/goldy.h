@@ -607,6 +607,188 @@ goldy_status goldy_layernorm_backward(const goldy_layernorm_desc* desc, const vo
                                       float* dgamma, float* dbeta, int accumulate, void* workspace,
                                       size_t workspace_bytes, void* stream);
 
+/* ---- a router: experts and weights of each token ---------------------------
+ * Of each row of `experts` logits the k largest are chosen, ties to the lowest
+ * index (NaN counts as larger than any number, as it does in sorts).  An expert
+ * whose logit is -infinity is closed to the row and never chosen; a slot for
+ * which no open expert is left has id -1 and weight 0.  The weight of a chosen
+ * expert e is
+ *   GOLDY_ROUTER_ALL     scale * exp(l_e) / sum of exp(l) over all experts
+ *   GOLDY_ROUTER_CHOSEN  scale * exp(l_e) / sum of exp(l) over the chosen ones
+ * computed in fp32 from the logits less their largest.  Logits and dlogits have
+ * `dtype`, any row strides >= experts, element alignment; ids (int32) and
+ * weights (fp32) are packed rows x k. */
+typedef enum goldy_router_over { GOLDY_ROUTER_ALL = 0, GOLDY_ROUTER_CHOSEN = 1 } goldy_router_over;
+
+#define GOLDY_MAX_SLOTS 32      /* experts per token */
+
+typedef struct goldy_router_desc {
+  int64_t rows;
+  int64_t ld, ldd;          /* row strides of the logits and of dlogits */
+  int32_t experts;          /* 1 .. GOLDY_MAX_GROUPS */
+  int32_t k;                /* 1 .. min(experts, GOLDY_MAX_SLOTS) */
+  int32_t dtype;            /* GOLDY_BF16 or GOLDY_F32 */
+  int32_t over;             /* goldy_router_over */
+  float scale;              /* finite */
+  int32_t reserved;         /* must be 0 */
+} goldy_router_desc;
+
+/* ids and weights of every row, in falling order of the logits. */
+goldy_status goldy_router_forward(const goldy_router_desc* desc, const void* logits, int32_t* ids, float* weights,
+                                  void* stream);
+
+/* dlogits (all of them; 0 for closed experts, and for all that were not chosen
+ * under GOLDY_ROUTER_CHOSEN) from the gradient of the weights.  ids: as the
+ * forward call gave them; a slot with an id out of range adds nothing, and an
+ * expert that a row names twice takes both slots' gradients.  dlogits may be
+ * the logits themselves (ldd = ld). */
+goldy_status goldy_router_backward(const goldy_router_desc* desc, const void* logits, const int32_t* ids,
+                                   const float* dweights, void* dlogits, void* stream);
+
+/* ---- tokens sorted by expert, and back --------------------------------------
+ * Token t has k slots, slot t * k + j with the expert ids[t * k + j].  Sorted by
+ * expert (a slot's order within its expert is that of the slots), a slot's row
+ * among the experts' rows is its place; the grouped products take the experts'
+ * row ranges from the same offsets (goldy_linear_desc with rows = rows * k).  A
+ * slot whose id is not in 0 .. groups - 1 belongs to no expert: its place is -1,
+ * nothing is copied for it and it adds nothing.  Experts' rows from
+ * offsets[groups] on are never read or written.
+ *
+ * Tokens' rows (X, Y, R, dY) and experts' rows (E, dE) have `dtype` and `width`
+ * elements, any row strides >= width, element alignment; the aligned 16-byte
+ * blocks that a row begins and ends in may be read whole, only rows are
+ * written.  rows * k < 2^31.  A place that is not in 0 .. rows * k - 1 counts as -1; places
+ * must otherwise differ.  Results must not overlap inputs unless stated. */
+typedef struct goldy_route_desc {
+  int64_t rows, width;
+  int64_t ldx, lde, ldr;    /* row strides of tokens' rows (X, Y, dY), of experts' rows (E, dE), of R */
+  int32_t k;                /* slots per token, 1 .. GOLDY_MAX_SLOTS */
+  int32_t groups;           /* experts, 1 .. GOLDY_MAX_GROUPS */
+  int32_t dtype;            /* GOLDY_BF16 or GOLDY_F32 */
+  int32_t reserved;         /* must be 0 */
+} goldy_route_desc;
+
+/* Device workspace of goldy_route_sort (see goldy_linear_query; the other calls
+ * need none). */
+goldy_status goldy_route_query(const goldy_route_desc* desc, size_t* workspace_bytes);
+
+/* offsets (groups + 1), place (rows * k) and, if not null, source (rows * k: the
+ * slot whose place this is, -1 from offsets[groups] on).  All int32. */
+goldy_status goldy_route_sort(const goldy_route_desc* desc, const int32_t* ids, int32_t* offsets, int32_t* place,
+                              int32_t* source, void* workspace, size_t workspace_bytes, void* stream);
+
+/* E[place of slot (t, j)] = X[t].  Its gradient is goldy_route_combine of dE
+ * without weights. */
+goldy_status goldy_route_dispatch(const goldy_route_desc* desc, const void* X, const int32_t* place, void* E,
+                                  void* stream);
+
+/* Y[t] = R[t] + sum over j of weights[t, j] * E[place of slot (t, j)], summed in
+ * fp32 in the slots' order, R last.  weights (fp32, packed) and R may be null (1
+ * and 0).  Y may be R (ldx = ldr). */
+goldy_status goldy_route_combine(const goldy_route_desc* desc, const void* E, const int32_t* place,
+                                 const float* weights, const void* R, void* Y, void* stream);
+
+/* dE[place of slot (t, j)] = weights[t, j] * dY[t], dweights[t, j] = the dot
+ * product of dY[t] and that row of E (0 for a slot without an expert).  dE may
+ * be E.  dweights may be null (E is then not read and may be null), weights too
+ * (1). */
+goldy_status goldy_route_combine_grad(const goldy_route_desc* desc, const void* dY, const void* E,
+                                      const int32_t* place, const float* weights, void* dE, float* dweights,
+                                      void* stream);
+
+/* ---- norms before and after a block ------------------------------------------
+ * A block's output F joins the residual stream X through a norm of its own, a
+ * gate and the stream's scale, and the next block's norm follows at once:
+ *   S = alpha * X + gate * N_f(F),   Y = N_y(S)
+ * with N(v) = (v - mean) * rstd * gamma + beta per row of n elements:
+ *   GOLDY_NORM_NONE   N(v) = v
+ *   GOLDY_NORM_LAYER  mean = sum(v) / n, rstd = 1 / sqrt(sum((v - mean)^2) / n + eps)
+ *   GOLDY_NORM_RMS    mean = 0, rstd = 1 / sqrt(sum(v^2) / n + eps)
+ * in fp32; Y is the norm of S before S is rounded.  X, F, S, Y and their
+ * gradients share `dtype`, any row strides >= n, element alignment (the aligned
+ * 16-byte blocks that a row begins and ends in may be read whole; only rows are
+ * written).  gate, gamma and beta (n elements each) have param_dtype and may be
+ * null (1, 1 and 0); those of a norm that is GOLDY_NORM_NONE must be. */
+typedef enum goldy_norm_kind { GOLDY_NORM_NONE = 0, GOLDY_NORM_LAYER = 1, GOLDY_NORM_RMS = 2 } goldy_norm_kind;
+
+typedef struct goldy_residual_norm_desc {
+  int64_t rows, n;
+  int64_t ldx, ldf, lds, ldy;   /* row strides: X and dX; F and dF; S and dS; Y and dY */
+  int32_t dtype;                /* GOLDY_BF16 or GOLDY_F32 */
+  int32_t param_dtype;
+  int32_t norm_f, norm_y;       /* goldy_norm_kind */
+  float eps;                    /* >= 0 */
+  float alpha;                  /* finite */
+  int32_t reserved;             /* must be 0 */
+} goldy_residual_norm_desc;
+
+/* Device pointers of the parameters (forward and backward), or of their
+ * gradients (fp32; null: not wanted). */
+typedef struct goldy_residual_norm_params {
+  void* gate;
+  void* gamma_f;
+  void* beta_f;
+  void* gamma_y;
+  void* beta_y;
+} goldy_residual_norm_params;
+
+/* Device workspace of the backward call (see goldy_linear_query; the forward
+ * call needs none). */
+goldy_status goldy_residual_norm_query(const goldy_residual_norm_desc* desc, size_t* workspace_bytes);
+
+/* params may be null (all absent).  Y is null exactly when norm_y is
+ * GOLDY_NORM_NONE.  stats (fp32, 4 x rows: mean and rstd of N_f, mean and rstd of
+ * N_y; those that a norm does not have are left as they are) may be null when no
+ * backward pass needs them.  S and Y may each be X or F (same stride). */
+goldy_status goldy_residual_norm_forward(const goldy_residual_norm_desc* desc, const goldy_residual_norm_params* params,
+                                         const void* X, const void* F, void* S, void* Y, float* stats, void* stream);
+
+/* dX and dF from dY (null exactly when norm_y is GOLDY_NORM_NONE) and dS, the
+ * gradient that reaches S past N_y (may be null unless dY is); S and F as the
+ * forward call read and left them.  grads (may be null): the parameters'
+ * gradients, fp32, added to what they hold when accumulate is 1; a parameter
+ * that is absent because it is 1 or 0 has one all the same.  dX and dF may each
+ * be any of the four inputs (same stride).  The workspace is needed for grads. */
+goldy_status goldy_residual_norm_backward(const goldy_residual_norm_desc* desc,
+                                          const goldy_residual_norm_params* params, const void* dY, const void* dS,
+                                          const void* F, const void* S, const float* stats, void* dX, void* dF,
+                                          const goldy_residual_norm_params* grads, int accumulate, void* workspace,
+                                          size_t workspace_bytes, void* stream);
+
+/* ---- pre-activations kept in 8 bits --------------------------------------------
+ * What a layer's backward pass needs of its pre-activation Z, in half the bytes
+ * of bf16: each block of GOLDY_KEEP8_BLOCK elements of a row (the last one of a
+ * row may be shorter) is held as e4m3 numbers q times a power of two 2^e, the
+ * smallest that keeps the block's largest finite |z| within 448 * 2^e, at least
+ * 2^-127; q = z / 2^e rounded to nearest even (relative error at most 2^-4 from
+ * |z| = 2^(e-6) on, absolute error at most 2^(e-10) below).  An infinity or NaN
+ * is held as NaN.  Q holds the blocks of a row one after another, each of
+ * GOLDY_KEEP8_BLOCK bytes (zeros behind the row's end), rows packed: rows * blocks *
+ * GOLDY_KEEP8_BLOCK bytes, 16-byte aligned; scales holds e + 127 per block, one
+ * byte each, packed. */
+#define GOLDY_KEEP8_BLOCK 32
+
+typedef struct goldy_keep8_desc {
+  int64_t rows, n;
+  int64_t ldz, ldh;         /* row strides of Z and H, >= n */
+  int32_t dtype;            /* of Z and H: GOLDY_BF16 or GOLDY_F32 (element alignment) */
+  int32_t act;              /* goldy_act of H */
+  int32_t reserved;         /* must be 0 */
+} goldy_keep8_desc;
+
+/* Bytes of Q and of scales (host only). */
+goldy_status goldy_keep8_query(const goldy_keep8_desc* desc, size_t* q_bytes, size_t* scale_bytes);
+
+/* Q and scales from Z. */
+goldy_status goldy_keep8_pack(const goldy_keep8_desc* desc, const void* Z, void* Q, void* scales, void* stream);
+
+/* Z = q * 2^e (exact but for a bf16 or fp32 underflow) and H = act(Z), of the
+ * value before any rounding; either may be null: the backward pass takes Z for
+ * the activation's gradient (goldy_linear_input_grad) and H for the weight
+ * gradient of the layer that read it. */
+goldy_status goldy_keep8_unpack(const goldy_keep8_desc* desc, const void* Q, const void* scales, void* Z, void* H,
+                                void* stream);
+
 /* Error word the kernels set when a bounded wait gives up (0 = none; the
  * first failure wins): 1 a load-role wait, 2 an MMA-thread wait, 3 an
  * epilogue wait, 4 a split-K cluster-exchange wait.  Reads it synchronously

@@ -4,7 +4,8 @@ Plain nvcc/g++ invocations, one object per translation unit, compiled in
 parallel: ``planner.cpp`` (host C++), ``runtime.cu`` (launch manager),
 ``noalloc.cu`` (the entry point with a compiled-in scratch array),
 ``kernels.cu`` once per GO-Kernel kind (``-DGOLDY_KIND=k``), the layer
-operators (``linear.cu``, ``repack.cu``, ``bias_grad.cu``, ``layernorm.cu``) and
+operators (``linear.cu``, ``repack.cu``, ``bias_grad.cu``, ``layernorm.cu``,
+``router.cu``, ``route.cu``, ``residual_norm.cu``, ``keep8.cu``) and
 ``linear_kernels.cu`` once per pass and activation.  Objects go to
 ``_build/`` next to this file and the library to
 ``paper_2409_02227_gb300/libgoldy.so``; both are git-ignored.  A rebuild is
@@ -57,7 +58,7 @@ def _jobs(ptxas_verbose: bool):
     jobs.append(("runtime", cu + ["-c", os.path.join(CSRC, "runtime.cu")]))
     jobs.append(("noalloc", cu + ["-c", os.path.join(CSRC, "noalloc.cu")]))
     jobs.append(("ewise", cu + ["-c", os.path.join(CSRC, "ewise.cu")]))
-    for name in ("linear", "repack", "bias_grad", "layernorm"):
+    for name in ("linear", "repack", "bias_grad", "layernorm", "router", "route", "residual_norm", "keep8"):
         jobs.append((name, cu + ["-c", os.path.join(CSRC, name + ".cu")]))
     for k, a in LINEAR_KERNELS:
         jobs.append((f"linear_kernels_p{k}_a{a}", cu + [f"-DGOLDY_LINEAR_PASS={k}", f"-DGOLDY_LINEAR_ACT={a}", "-c",

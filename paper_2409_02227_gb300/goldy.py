@@ -45,6 +45,13 @@ GOLDY_ACT_GELU = 2
 GOLDY_ACT_GELU_TANH = 3
 GOLDY_ACT_SILU = 4
 GOLDY_MAX_GROUPS = 4096
+GOLDY_ROUTER_ALL = 0
+GOLDY_ROUTER_CHOSEN = 1
+GOLDY_MAX_SLOTS = 32
+GOLDY_NORM_NONE = 0
+GOLDY_NORM_LAYER = 1
+GOLDY_NORM_RMS = 2
+GOLDY_KEEP8_BLOCK = 32
 
 
 def force_cd(cd: int) -> int:
@@ -84,6 +91,32 @@ class goldy_layernorm_desc(ctypes.Structure):
                 ("reserved", ctypes.c_int32)]
 
 
+class goldy_router_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("rows", "ld", "ldd")] + \
+               [(n, ctypes.c_int32) for n in ("experts", "k", "dtype", "over")] + \
+               [("scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class goldy_route_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("rows", "width", "ldx", "lde", "ldr")] + \
+               [(n, ctypes.c_int32) for n in ("k", "groups", "dtype", "reserved")]
+
+
+class goldy_residual_norm_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("rows", "n", "ldx", "ldf", "lds", "ldy")] + \
+               [(n, ctypes.c_int32) for n in ("dtype", "param_dtype", "norm_f", "norm_y")] + \
+               [("eps", ctypes.c_float), ("alpha", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class goldy_residual_norm_params(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("gate", "gamma_f", "beta_f", "gamma_y", "beta_y")]
+
+
+class goldy_keep8_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("rows", "n", "ldz", "ldh")] + \
+               [(n, ctypes.c_int32) for n in ("dtype", "act", "reserved")]
+
+
 class goldy_run_opts(ctypes.Structure):
     _fields_ = [("ev_begin", ctypes.POINTER(ctypes.c_void_p)), ("ev_end", ctypes.POINTER(ctypes.c_void_p)),
                 ("trace", ctypes.c_void_p), ("trace_ctas", ctypes.c_size_t), ("serial_launch", ctypes.c_int32),
@@ -113,6 +146,11 @@ def _load():
     DP = ctypes.POINTER(goldy_gemm_desc)
     LP = ctypes.POINTER(goldy_linear_desc)
     NP = ctypes.POINTER(goldy_layernorm_desc)
+    RP = ctypes.POINTER(goldy_router_desc)
+    TP = ctypes.POINTER(goldy_route_desc)
+    SP = ctypes.POINTER(goldy_residual_norm_desc)
+    SPP = ctypes.POINTER(goldy_residual_norm_params)
+    KP = ctypes.POINTER(goldy_keep8_desc)
     sig = {
         "goldy_abi_version": ([], I),
         "goldy_last_error": ([], ctypes.c_char_p),
@@ -163,6 +201,19 @@ def _load():
         "goldy_layernorm_query": ([NP, ctypes.POINTER(SZ)], I),
         "goldy_layernorm_forward": ([NP, P, P, P, P, P, P, P], I),
         "goldy_layernorm_backward": ([NP, P, P, P, P, P, P, P, P, I, P, SZ, P], I),
+        "goldy_router_forward": ([RP, P, P, P, P], I),
+        "goldy_router_backward": ([RP, P, P, P, P, P], I),
+        "goldy_route_query": ([TP, ctypes.POINTER(SZ)], I),
+        "goldy_route_sort": ([TP, P, P, P, P, P, SZ, P], I),
+        "goldy_route_dispatch": ([TP, P, P, P, P], I),
+        "goldy_route_combine": ([TP, P, P, P, P, P, P], I),
+        "goldy_route_combine_grad": ([TP, P, P, P, P, P, P, P], I),
+        "goldy_residual_norm_query": ([SP, ctypes.POINTER(SZ)], I),
+        "goldy_residual_norm_forward": ([SP, SPP, P, P, P, P, P, P], I),
+        "goldy_residual_norm_backward": ([SP, SPP, P, P, P, P, P, P, P, SPP, I, P, SZ, P], I),
+        "goldy_keep8_query": ([KP, ctypes.POINTER(SZ), ctypes.POINTER(SZ)], I),
+        "goldy_keep8_pack": ([KP, P, P, P, P], I),
+        "goldy_keep8_unpack": ([KP, P, P, P, P, P], I),
         "goldy_device_error": ([IP, I], I),
         "goldy_device_info": ([I, IP, IP], I),
     }
@@ -605,6 +656,127 @@ def goldy_layernorm_backward(d: goldy_layernorm_desc, dY: int, X: int, gamma: in
                                          dX or None, dgamma or None, dbeta or None, 1 if accumulate else 0,
                                          workspace or None, workspace_bytes, stream or None),
            "goldy_layernorm_backward")
+
+
+def router_desc(rows: int, experts: int, k: int, dtype: int = GOLDY_F32, over: int = GOLDY_ROUTER_ALL, scale: float = 1.0,
+                ld: Optional[int] = None, ldd: Optional[int] = None) -> goldy_router_desc:
+    """Descriptor of a router over rows of `experts` logits (default: packed)."""
+    return goldy_router_desc(rows, experts if ld is None else ld, experts if ldd is None else ldd, int(experts), int(k),
+                             int(dtype), int(over), float(scale), 0)
+
+
+def goldy_router_forward(d: goldy_router_desc, logits: int, ids: int, weights: int, stream: int = 0) -> None:
+    """The k largest logits' ids (int32) and softmax weights (fp32) of each row."""
+    _check(_lib.goldy_router_forward(d, logits or None, ids or None, weights or None, stream or None),
+           "goldy_router_forward")
+
+
+def goldy_router_backward(d: goldy_router_desc, logits: int, ids: int, dweights: int, dlogits: int,
+                          stream: int = 0) -> None:
+    _check(_lib.goldy_router_backward(d, logits or None, ids or None, dweights or None, dlogits or None, stream or None),
+           "goldy_router_backward")
+
+
+def route_desc(rows: int, k: int, groups: int, width: int = 0, dtype: int = GOLDY_BF16, ldx: Optional[int] = None,
+               lde: Optional[int] = None, ldr: Optional[int] = None) -> goldy_route_desc:
+    """Descriptor of `rows` tokens with k slots each over `groups` experts, and of
+    their rows of `width` elements (default: packed)."""
+    return goldy_route_desc(rows, width, width if ldx is None else ldx, width if lde is None else lde,
+                            width if ldr is None else ldr, int(k), int(groups), int(dtype), 0)
+
+
+def goldy_route_query(d: goldy_route_desc) -> int:
+    """Workspace bytes of the sort."""
+    ws = ctypes.c_size_t()
+    _check(_lib.goldy_route_query(d, ctypes.byref(ws)), "goldy_route_query")
+    return int(ws.value)
+
+
+def goldy_route_sort(d: goldy_route_desc, ids: int, offsets: int, place: int, source: int = 0, workspace: int = 0,
+                     workspace_bytes: int = 0, stream: int = 0) -> None:
+    """Slots by expert: offsets per expert, place of each slot, slot at each place."""
+    _check(_lib.goldy_route_sort(d, ids or None, offsets or None, place or None, source or None, workspace or None,
+                                 workspace_bytes, stream or None), "goldy_route_sort")
+
+
+def goldy_route_dispatch(d: goldy_route_desc, X: int, place: int, E: int, stream: int = 0) -> None:
+    """E[place] = X."""
+    _check(_lib.goldy_route_dispatch(d, X or None, place or None, E or None, stream or None), "goldy_route_dispatch")
+
+
+def goldy_route_combine(d: goldy_route_desc, E: int, place: int, Y: int, weights: int = 0, residual: int = 0,
+                        stream: int = 0) -> None:
+    """Y = residual + sum over slots of weights * E[place]."""
+    _check(_lib.goldy_route_combine(d, E or None, place or None, weights or None, residual or None, Y or None,
+                                    stream or None), "goldy_route_combine")
+
+
+def goldy_route_combine_grad(d: goldy_route_desc, dY: int, E: int, place: int, weights: int, dE: int,
+                             dweights: int = 0, stream: int = 0) -> None:
+    """dE[place] = weights * dY, dweights = dY . E[place]."""
+    _check(_lib.goldy_route_combine_grad(d, dY or None, E or None, place or None, weights or None, dE or None,
+                                         dweights or None, stream or None), "goldy_route_combine_grad")
+
+
+def residual_norm_desc(rows: int, n: int, norm_f: int = GOLDY_NORM_RMS, norm_y: int = GOLDY_NORM_RMS,
+                       dtype: int = GOLDY_BF16, param_dtype: int = GOLDY_F32, eps: float = 1e-5, alpha: float = 1.0,
+                       ldx: Optional[int] = None, ldf: Optional[int] = None, lds: Optional[int] = None,
+                       ldy: Optional[int] = None) -> goldy_residual_norm_desc:
+    """Descriptor of S = alpha X + gate * N_f(F), Y = N_y(S) over rows of n
+    elements (default: packed)."""
+    ld = [n if v is None else v for v in (ldx, ldf, lds, ldy)]
+    return goldy_residual_norm_desc(rows, n, *ld, int(dtype), int(param_dtype), int(norm_f), int(norm_y), float(eps),
+                                    float(alpha), 0)
+
+
+def residual_norm_params(gate: int = 0, gamma_f: int = 0, beta_f: int = 0, gamma_y: int = 0,
+                         beta_y: int = 0) -> goldy_residual_norm_params:
+    """Device pointers of the parameters, or of their fp32 gradients (0: absent)."""
+    return goldy_residual_norm_params(gate or None, gamma_f or None, beta_f or None, gamma_y or None, beta_y or None)
+
+
+def goldy_residual_norm_query(d: goldy_residual_norm_desc) -> int:
+    """Workspace bytes of the backward call."""
+    ws = ctypes.c_size_t()
+    _check(_lib.goldy_residual_norm_query(d, ctypes.byref(ws)), "goldy_residual_norm_query")
+    return int(ws.value)
+
+
+def goldy_residual_norm_forward(d: goldy_residual_norm_desc, params: Optional[goldy_residual_norm_params], X: int, F: int,
+                                S: int, Y: int = 0, stats: int = 0, stream: int = 0) -> None:
+    _check(_lib.goldy_residual_norm_forward(d, params, X or None, F or None, S or None, Y or None, stats or None,
+                                            stream or None), "goldy_residual_norm_forward")
+
+
+def goldy_residual_norm_backward(d: goldy_residual_norm_desc, params: Optional[goldy_residual_norm_params], dY: int, dS: int,
+                                 F: int, S: int, stats: int, dX: int, dF: int,
+                                 grads: Optional[goldy_residual_norm_params] = None, workspace: int = 0,
+                                 workspace_bytes: int = 0, stream: int = 0, accumulate: bool = False) -> None:
+    _check(_lib.goldy_residual_norm_backward(d, params, dY or None, dS or None, F or None, S or None, stats or None,
+                                             dX or None, dF or None, grads, 1 if accumulate else 0, workspace or None,
+                                             workspace_bytes, stream or None), "goldy_residual_norm_backward")
+
+
+def keep8_desc(rows: int, n: int, dtype: int = GOLDY_BF16, act: int = GOLDY_ACT_NONE, ldz: Optional[int] = None,
+               ldh: Optional[int] = None) -> goldy_keep8_desc:
+    """Descriptor of rows of n pre-activations kept in 8 bits (default: packed)."""
+    return goldy_keep8_desc(rows, n, n if ldz is None else ldz, n if ldh is None else ldh, int(dtype), int(act), 0)
+
+
+def goldy_keep8_query(d: goldy_keep8_desc) -> Tuple[int, int]:
+    """(bytes of Q, bytes of scales)."""
+    q, s = ctypes.c_size_t(), ctypes.c_size_t()
+    _check(_lib.goldy_keep8_query(d, ctypes.byref(q), ctypes.byref(s)), "goldy_keep8_query")
+    return int(q.value), int(s.value)
+
+
+def goldy_keep8_pack(d: goldy_keep8_desc, Z: int, Q: int, scales: int, stream: int = 0) -> None:
+    _check(_lib.goldy_keep8_pack(d, Z or None, Q or None, scales or None, stream or None), "goldy_keep8_pack")
+
+
+def goldy_keep8_unpack(d: goldy_keep8_desc, Q: int, scales: int, Z: int = 0, H: int = 0, stream: int = 0) -> None:
+    """Z as it was kept, H = act(Z); either may be 0."""
+    _check(_lib.goldy_keep8_unpack(d, Q or None, scales or None, Z or None, H or None, stream or None), "goldy_keep8_unpack")
 
 
 def goldy_device_error(clear: bool = True) -> int:
