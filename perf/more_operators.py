@@ -251,6 +251,7 @@ def _plan(s):
         s["params"] = G.residual_norm_params(**{p: _ptr(s, p) for p in names})
         if op == "norms":
             s["s"], s["y"], s["stats"] = torch.empty_like(s["x"]), torch.empty_like(s["x"]), f32(4, rows)
+            s["out"] = dict(_stats(case, s["stats"]), s=s["s"], y=s["y"])
         else:
             s["dx"], s["df"] = torch.empty_like(s["s"]), torch.empty_like(s["s"])
             s["grads"] = {p: f32(n) for p in names if s[p] is not None}
@@ -295,7 +296,7 @@ def _run_own(s):
     if op == "norms":
         G.goldy_residual_norm_forward(d, s["params"], _ptr(s, "x"), _ptr(s, "f"), _ptr(s, "s"), _ptr(s, "y"),
                                       stats=_ptr(s, "stats"), stream=stream)
-        return dict(_stats(case, s["stats"]), s=s["s"], y=s["y"])
+        return s["out"]
     if op == "norms_grad":
         G.goldy_residual_norm_backward(d, s["params"], _ptr(s, "dy"), _ptr(s, "ds"), _ptr(s, "f"), _ptr(s, "s"),
                                        _ptr(s, "stats"), _ptr(s, "dx"), _ptr(s, "df"), s["grad_ptrs"],
