@@ -10,7 +10,7 @@
 // the backward direction cost no second read.  The next rows are on their way
 // meanwhile: each thread copies its own pieces into shared memory with cp.async
 // and reads back only those, so that rows in flight take no registers and need no
-// barrier (but for bf16 rows off 16-byte boundaries, see Row).  gamma and beta
+// barrier (but for bf16 rows off 16-byte boundaries, see NormRow).  gamma and beta
 // stay in registers.
 // The variance is a sum of squared differences from each warp's own mean,
 // warps combined by M2 = sum(M2_w + n_w (mean_w - mean)^2): no cancellation,
@@ -27,23 +27,19 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
-#include <map>
-#include <mutex>
-#include <set>
 #include <string>
-#include <tuple>
-#include <utility>
 
 #include "goldy_internal.h"
 #include "layer_internal.h"
 #include "layer_math.cuh"
+#include "norm_launch.h"
+#include "norm_rows.cuh"
 #include "sm103_ptx.cuh"
 
 namespace goldy {
 namespace {
 
 constexpr int kMaxTeam = 512;
-constexpr int kMaxCluster = 8;      // CTAs that may share a row
 constexpr int kStreamThreads = 512;
 constexpr int kFwdThreads = 256;    // per CTA, at least the team
 constexpr int kBwdThreads = 512;
@@ -58,252 +54,6 @@ constexpr int kFwdDepth = 3;        // rows in a thread's ring
 constexpr int kBwdCtas = 152;      // one per SM
 template <typename T> __host__ __device__ constexpr int bwd_depth() { return sizeof(T) == 2 ? 3 : 2; }
 
-__device__ __forceinline__ float warp_sum(float v) {
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
-  return v;
-}
-
-// Sums of a and of b over the warp, in lanes 0 to 15 that of a, in the others
-// that of b: half the exchanges of two sums.
-__device__ __forceinline__ float warp_sum2(float a, float b, int lane) {
-  const bool upper = lane & 16;
-  float v = (upper ? b : a) + __shfl_xor_sync(0xFFFFFFFFu, upper ? a : b, 16);
-#pragma unroll
-  for (int d = 8; d > 0; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
-  return v;
-}
-
-__device__ __forceinline__ float param_at(const void* p, int f32, int i, float absent) {
-  if (!p) return absent;
-  return f32 ? static_cast<const float*>(p)[i] : load_bf16(p, i);
-}
-
-// Sum over groups of N consecutive lanes (N a power of two), to all of them.
-template <int N>
-__device__ __forceinline__ float lanes_sum(float v) {
-#pragma unroll
-  for (int d = N / 2; d > 0; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
-  return v;
-}
-
-// PER parameters from index c on, 0 from n on; VEC: c + PER <= n, on a vector's
-// boundary.  Plain loads, as of mean and rstd: the kernel before this one may have
-// written them after this one began, which the read-only data path does not allow.
-template <int PER, bool VEC>
-__device__ __forceinline__ void load_params(const void* p, int f32, int c, int n, float absent, float* f) {
-  if (!VEC || !p) {
-#pragma unroll
-    for (int k = 0; k < PER; ++k) {
-      if (!VEC && c + k >= n) f[k] = 0.0f;
-      else if (!p) f[k] = absent;
-      else f[k] = f32 ? static_cast<const float*>(p)[c + k] : load_bf16(p, c + k);
-    }
-  } else if (f32) {
-#pragma unroll
-    for (int k = 0; k < PER; k += 4) {
-      const float4 v = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + c + k);
-      f[k] = v.x, f[(k + 1) % PER] = v.y, f[(k + 2) % PER] = v.z, f[(k + 3) % PER] = v.w;
-    }
-  } else if (PER == 8) {
-    const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + c);
-    f[0] = bf16_lo(v.x), f[1 % PER] = bf16_hi(v.x), f[2 % PER] = bf16_lo(v.y), f[3 % PER] = bf16_hi(v.y);
-    f[4 % PER] = bf16_lo(v.z), f[5 % PER] = bf16_hi(v.z), f[6 % PER] = bf16_lo(v.w), f[7 % PER] = bf16_hi(v.w);
-  } else {
-    const uint2 v = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + c);
-    f[0] = bf16_lo(v.x), f[1 % PER] = bf16_hi(v.x), f[2 % PER] = bf16_lo(v.y), f[3 % PER] = bf16_hi(v.y);
-  }
-}
-
-template <int BYTES>
-__device__ __forceinline__ void copy_async(void* to, const void* from) {
-  const uint32_t at = ptx::smem_u32(to);
-  if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(from) : "memory");
-  else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(at), "l"(from) : "memory");
-}
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
-// A thread's share of a row, VALS values, in pieces: piece i of thread t starts
-// at column (i * TEAM + t) * PER.  VEC: 16 bytes, inside the row or outside as a
-// whole.  bf16 otherwise (odd lengths or strides, rows that start anywhere),
-// SHIFT: 8 elements, maybe part of them outside, that lie in two 16-byte blocks.
-// Whole blocks are copied, each by one thread of the team, and a thread picks its
-// elements from its block and the next; a result's blocks are put together from
-// a lane's and the lower lane's elements and stored whole, but for those that two
-// warps or two rows share (16384 rows of 2047: 42 us, backwards 54; loading and
-// storing single elements took 62 and 69, aligned words traded between lanes 57
-// and 79).  What else a row's first and last block hold is read and ignored,
-// never written.  fp32 otherwise: single elements (4096 rows of 4095: 29 us,
-// backwards 50; in blocks 30 and 55).
-// SURE: the first half of the pieces is inside whatever the row's length, as the
-// host takes the smallest team that holds the row: no tests for those.
-template <typename T, int VALS, int TEAM, int THREADS, bool VEC, bool WIDE>
-struct Row {
-  static constexpr bool SHIFT = !VEC && sizeof(T) == 2;
-  static constexpr int PER = VEC ? 16 / int(sizeof(T)) : SHIFT ? 8 : 1;
-  static constexpr int SLOTS = VALS / PER;
-  static constexpr int PIECE = VEC || SHIFT ? 16 : 4;
-  static constexpr int BLOCKS = SLOTS * TEAM + 1;  // SHIFT: of one row
-  static constexpr int RING_BYTES = SHIFT ? THREADS / TEAM * BLOCKS * 16 : SLOTS * THREADS * PIECE;   // of one row per team
-  static constexpr int SURE = TEAM > 32 && !WIDE ? SLOTS / 2 : 0;
-  static __device__ __forceinline__ int col(int slot, int t) { return (slot * TEAM + t) * PER; }
-  static __device__ __forceinline__ bool in(int slot, int t, int n) { return slot < SURE || col(slot, t) < n; }
-  static __device__ __forceinline__ bool whole(int slot, int t, int n) {
-    return !SHIFT || slot < SURE || col(slot, t) + PER <= n;
-  }
-  // SHIFT: elements by which a row starts behind a block's start
-  static __device__ __forceinline__ int shift(const T* at) { return int(reinterpret_cast<uintptr_t>(at) & 15) / 2; }
-  // place in the ring of a thread's piece, or block
-  static __device__ __forceinline__ int place(int slot, int t) {
-    return SHIFT ? (int(threadIdx.x) / TEAM * BLOCKS + slot * TEAM + t) * 16 : (slot * THREADS + int(threadIdx.x)) * PIECE;
-  }
-
-  static __device__ __forceinline__ void fetch(uint8_t* ring, const void* base, int64_t row, int64_t ld, int n, int t) {
-    const T* at = static_cast<const T*>(base) + row * ld;
-    const int off = SHIFT ? shift(at) : 0;
-#pragma unroll
-    for (int s = 0; s < SLOTS; ++s)
-      if (in(s, t, n + off)) copy_async<PIECE>(ring + place(s, t), at + col(s, t) - off);
-    if (SHIFT && t == 0 && col(SLOTS, 0) < n + off) copy_async<PIECE>(ring + place(SLOTS, 0), at + col(SLOTS, 0) - off);
-  }
-
-  template <int OFF>
-  static __device__ __forceinline__ void pick(const uint8_t* ring, int n, int t, float (&f)[VALS]) {
-#pragma unroll
-    for (int s = 0; s < SLOTS; ++s) {
-      const uint4 a = *reinterpret_cast<const uint4*>(ring + place(s, t));
-      const uint4 b = OFF > 0 ? *reinterpret_cast<const uint4*>(ring + place(s, t) + 16) : a;
-      const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-      for (int k = 0; k < 8; ++k) f[(s * PER + k) % VALS] = (OFF + k) & 1 ? bf16_hi(w[(OFF + k) / 2]) : bf16_lo(w[(OFF + k) / 2]);
-      if (!whole(s, t, n)) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (col(s, t) + k >= n) f[(s * PER + k) % VALS] = 0.0f;
-      }
-    }
-  }
-  // the row's values, 0 outside it (SHIFT: behind the team's barrier)
-  static __device__ __forceinline__ void values(const uint8_t* ring, const void* base, int64_t row, int64_t ld, int n,
-                                                int t, float (&f)[VALS]) {
-    if constexpr (SHIFT) {
-      switch (shift(static_cast<const T*>(base) + row * ld)) {
-        case 0: pick<0>(ring, n, t, f); break;
-        case 1: pick<1>(ring, n, t, f); break;
-        case 2: pick<2>(ring, n, t, f); break;
-        case 3: pick<3>(ring, n, t, f); break;
-        case 4: pick<4>(ring, n, t, f); break;
-        case 5: pick<5>(ring, n, t, f); break;
-        case 6: pick<6>(ring, n, t, f); break;
-        default: pick<7>(ring, n, t, f); break;
-      }
-    } else {
-#pragma unroll
-      for (int s = 0; s < SLOTS; ++s) {
-        if (!in(s, t, n)) {
-#pragma unroll
-          for (int k = 0; k < PER; ++k) f[s * PER + k] = 0.0f;
-        } else if (!VEC) {
-          f[s] = *reinterpret_cast<const float*>(ring + place(s, t));
-        } else {
-          const uint4 v = *reinterpret_cast<const uint4*>(ring + place(s, t));
-          float* o = f + s * PER;
-          if (sizeof(T) == 2) {
-            o[0] = bf16_lo(v.x), o[1] = bf16_hi(v.x), o[2] = bf16_lo(v.y), o[3] = bf16_hi(v.y);
-            o[4 % PER] = bf16_lo(v.z), o[5 % PER] = bf16_hi(v.z), o[6 % PER] = bf16_lo(v.w), o[7 % PER] = bf16_hi(v.w);
-          } else {
-            o[0] = __uint_as_float(v.x), o[1] = __uint_as_float(v.y), o[2] = __uint_as_float(v.z), o[3] = __uint_as_float(v.w);
-          }
-        }
-      }
-    }
-  }
-
-  // SHIFT: `at` is OFF elements behind a block's start
-  template <int OFF>
-  static __device__ __forceinline__ void put(T* at, int n, int t, const float (&f)[VALS]) {
-    const int lane = threadIdx.x & 31;
-#pragma unroll
-    for (int s = 0; s < SLOTS; ++s) {
-      const int c = col(s, t);
-      uint32_t w[8];                               // the lower lane's elements, then this lane's
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        w[4 + k] = pack_bf16(f[(s * PER + 2 * k) % VALS], f[(s * PER + 2 * k + 1) % VALS]);
-        w[k] = 2 * k + 1 >= 8 - OFF ? __shfl_up_sync(0xFFFFFFFFu, w[4 + k], 1) : 0u;
-      }
-      uint32_t v[4];                               // elements 8 - OFF .. 15 - OFF of those
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int h = 8 - OFF + 2 * k;
-        v[k] = h & 1 ? __byte_perm(w[h / 2], w[(h / 2 + 1) % 8], 0x5432) : w[(h / 2) % 8];
-      }
-      // blocks that this lane, and the next, store whole
-      const bool own = (OFF == 0 || lane > 0) && (s < SURE || c + 8 - OFF <= n);
-      const bool next = lane < 31 && (s < SURE || c + 16 - OFF <= n);
-      if (own) __stcs(reinterpret_cast<uint4*>(at + c - OFF), make_uint4(v[0], v[1], v[2], v[3]));
-      if (!own || (OFF > 0 && !next)) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if ((k < 8 - OFF ? !own : !next) && (s < SURE || c + k < n))
-            reinterpret_cast<uint16_t*>(at)[c + k] = uint16_t(w[4 + k / 2] >> (k & 1) * 16);
-      }
-    }
-  }
-  // the row's results (all lanes of a warp)
-  static __device__ __forceinline__ void store(void* base, int64_t row, int64_t ld, int n, int t, const float (&f)[VALS]) {
-    T* at = static_cast<T*>(base) + row * ld;
-    if constexpr (SHIFT) {
-      switch (shift(at)) {
-        case 0: put<0>(at, n, t, f); break;
-        case 1: put<1>(at, n, t, f); break;
-        case 2: put<2>(at, n, t, f); break;
-        case 3: put<3>(at, n, t, f); break;
-        case 4: put<4>(at, n, t, f); break;
-        case 5: put<5>(at, n, t, f); break;
-        case 6: put<6>(at, n, t, f); break;
-        default: put<7>(at, n, t, f); break;
-      }
-    } else {
-#pragma unroll
-      for (int s = 0; s < SLOTS; ++s) {
-        if (!in(s, t, n)) continue;
-        T* to = at + col(s, t);
-        const float* v = f + s * PER;
-        if (!VEC) {
-          *reinterpret_cast<float*>(to) = v[0];
-        } else if (sizeof(T) == 2) {
-          __stcs(reinterpret_cast<uint4*>(to), make_uint4(pack_bf16(v[0], v[1 % PER]), pack_bf16(v[2 % PER], v[3 % PER]),
-                                                          pack_bf16(v[4 % PER], v[5 % PER]), pack_bf16(v[6 % PER], v[7 % PER])));
-        } else {
-          __stcs(reinterpret_cast<float4*>(to), make_float4(v[0], v[1 % PER], v[2 % PER], v[3 % PER]));
-        }
-      }
-    }
-  }
-};
-
-// What a cluster's CTAs tell one another about a row: each writes its value
-// into every CTA's place `rank`, in this CTA's shared memory at `to`.
-__device__ __forceinline__ void tell_cluster(float4* to, int rank, int cluster, float4 v) {
-  if (threadIdx.x < unsigned(cluster))
-    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(
-                     ptx::map_to_rank(ptx::smem_u32(to + rank), threadIdx.x)),
-                 "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w)
-                 : "memory");
-  ptx::cluster_sync_all();
-}
-
-// Barrier of one team: a warp needs none, the whole CTA has barrier 0.
-template <int TEAM, int THREADS>
-__device__ __forceinline__ void team_sync(int team) {
-  if (TEAM == 32) __syncwarp();
-  else if (TEAM == THREADS) __syncthreads();
-  else ptx::named_bar_sync(uint32_t(team + 1), TEAM);
-}
-
 template <int TEAM, int VALS, bool VEC>
 struct FwdShape {
   static constexpr int THREADS = TEAM > kFwdThreads ? TEAM : kFwdThreads;
@@ -316,7 +66,7 @@ __global__ void __launch_bounds__(FwdShape<TEAM, VALS, VEC>::THREADS, FwdShape<T
 norm_forward_kernel(const NormParams p) {
   constexpr int THREADS = FwdShape<TEAM, VALS, VEC>::THREADS, TEAMS = FwdShape<TEAM, VALS, VEC>::TEAMS;
   constexpr int WARPS = TEAM / 32, D = kFwdDepth;
-  using R = Row<T, VALS, TEAM, THREADS, VEC, WIDE>;
+  using R = NormRow<T, VALS, TEAM, THREADS, VEC, WIDE>;
   __shared__ float4 slot[2][TEAMS][WARPS];         // per warp: sum, M2, elements, mean
   __shared__ float4 part[2][WIDE ? kMaxCluster : 1];   // per CTA of the cluster: the same
   extern __shared__ __align__(16) uint8_t ring[];
@@ -422,7 +172,7 @@ norm_forward_kernel(const NormParams p) {
 template <typename T, int TEAM, bool VEC, bool WIDE>
 __global__ void __launch_bounds__(kBwdThreads) norm_backward_kernel(const NormParams p) {
   constexpr int TEAMS = kBwdThreads / TEAM, WARPS = TEAM / 32, VALS = kBwdVals, D = bwd_depth<T>();
-  using R = Row<T, VALS, TEAM, kBwdThreads, VEC, WIDE>;
+  using R = NormRow<T, VALS, TEAM, kBwdThreads, VEC, WIDE>;
   __shared__ float2 slot[2][TEAMS][WARPS];
   __shared__ float4 part[2][WIDE ? kMaxCluster : 1];
   extern __shared__ __align__(16) uint8_t ring[];  // D rows of x, D of dy; at the end the CTA's sums
@@ -745,35 +495,29 @@ NormShape shape_for(const goldy_layernorm_desc& d, bool backward) {
   return {team, cluster, int(seg)};
 }
 
-struct Kernel {
-  const void* fn;
-  int threads, teams, per_sm;      // per_sm: CTAs resident
-  size_t smem;
-};
-
 template <typename T, int TEAM, int VALS, bool VEC, bool WIDE = false>
-Kernel pick_forward() {
+NormKernel pick_forward() {
   using S = FwdShape<TEAM, VALS, VEC>;
-  using R = Row<T, VALS, TEAM, S::THREADS, VEC, WIDE>;
+  using R = NormRow<T, VALS, TEAM, S::THREADS, VEC, WIDE>;
   return {reinterpret_cast<const void*>(&norm_forward_kernel<T, TEAM, VALS, VEC, WIDE>), S::THREADS, S::TEAMS, S::CTAS,
           size_t(kFwdDepth) * R::RING_BYTES};
 }
 template <typename T, int TEAM, bool VEC, bool WIDE = false>
-Kernel pick_backward() {
-  using R = Row<T, kBwdVals, TEAM, kBwdThreads, VEC, WIDE>;
+NormKernel pick_backward() {
+  using R = NormRow<T, kBwdVals, TEAM, kBwdThreads, VEC, WIDE>;
   return {reinterpret_cast<const void*>(&norm_backward_kernel<T, TEAM, VEC, WIDE>), kBwdThreads, kBwdThreads / TEAM, 1,
           std::max(size_t(2) * bwd_depth<T>() * R::RING_BYTES, size_t(2) * kBwdThreads * kBwdVals * sizeof(float))};
 }
 
 template <typename T, int TEAM, bool VEC>
-Kernel pick(bool backward) {
+NormKernel pick(bool backward) {
   if (backward) return pick_backward<T, TEAM, VEC>();
   if constexpr (TEAM > kFwdTeam) return pick_forward<T, TEAM / 2, kFwdMoreVals, VEC>();
   else return pick_forward<T, TEAM, kFwdVals, VEC>();
 }
 
 template <typename T, bool VEC>
-Kernel pick_shape(const NormShape& s, bool backward) {
+NormKernel pick_shape(const NormShape& s, bool backward) {
   if (s.cluster > 1)
     return backward ? pick_backward<T, kMaxTeam, VEC, true>() : pick_forward<T, kMaxTeam, kFwdMoreVals, VEC, true>();
   switch (s.team) {
@@ -790,7 +534,7 @@ Kernel pick_shape(const NormShape& s, bool backward) {
   }
 }
 
-Kernel kernel_for(const goldy_layernorm_desc& d, const NormShape& s, bool vec, bool backward) {
+NormKernel kernel_for(const goldy_layernorm_desc& d, const NormShape& s, bool vec, bool backward) {
   if (d.dtype == GOLDY_F32) return vec ? pick_shape<float, true>(s, backward) : pick_shape<float, false>(s, backward);
   return vec ? pick_shape<uint16_t, true>(s, backward) : pick_shape<uint16_t, false>(s, backward);
 }
@@ -826,63 +570,12 @@ struct NormCall {
   void* stream;
 };
 
-struct Launch {
-  cudaLaunchConfig_t cfg = {};
-  cudaLaunchAttribute attr[2];
-
-  Launch(unsigned grid, unsigned threads, size_t smem, void* stream, unsigned cluster = 1) {
-    cfg.gridDim = dim3(grid);
-    cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = static_cast<cudaStream_t>(stream);
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = cluster;
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = cluster > 1 ? 2 : 1;
-  }
-  Launch(const Launch&) = delete;
-  cudaError_t run(const void* fn, void** args) { return cudaLaunchKernelExC(&cfg, fn, args); }
-};
-
-// Clusters of a kernel that the device holds at once (a GPC's SMs need not make
-// whole clusters), asked for once.
-cudaError_t resident_clusters(int device, const Kernel& k, int cluster, int* n) {
-  static std::mutex mu;
-  static std::map<std::tuple<int, const void*, int>, int> known;
-  std::lock_guard<std::mutex> lock(mu);
-  const auto key = std::make_tuple(device, k.fn, cluster);
-  const auto it = known.find(key);
-  if (it != known.end()) {
-    *n = it->second;
-    return cudaSuccess;
-  }
-  Launch l(unsigned(cluster), unsigned(k.threads), k.smem, nullptr, unsigned(cluster));
-  const cudaError_t e = cudaOccupancyMaxActiveClusters(n, k.fn, &l.cfg);
-  if (e == cudaSuccess) known[key] = *n;
-  return e;
-}
-
-// Opts a kernel into more than 48 KB of shared memory, once per device.
-cudaError_t allow_smem(int device, const Kernel& k) {
-  if (k.smem <= 40 * 1024) return cudaSuccess;     // with the kernel's static part below 48 KB
-  static std::mutex mu;
-  static std::set<std::pair<int, const void*>> done;
-  std::lock_guard<std::mutex> lock(mu);
-  if (done.count({device, k.fn})) return cudaSuccess;
-  const cudaError_t e = cudaFuncSetAttribute(k.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, int(k.smem));
-  if (e == cudaSuccess) done.insert({device, k.fn});
-  return e;
-}
-
 goldy_status launch_norm(const LayerContext& ctx, void* arg) {
   NormCall& call = *static_cast<NormCall*>(arg);
   // which SMs a partition has, and so whether a cluster fits into it, is not known
   if (!ctx.whole && call.shape.cluster > 1) call.shape = {0, 1, 0};
   const int cluster = call.shape.cluster;
-  const Kernel k = kernel_for(*call.d, call.shape, call.vec, call.backward);
+  const NormKernel k = kernel_for(*call.d, call.shape, call.vec, call.backward);
   cudaError_t e = allow_smem(ctx.device, k);
   if (e != cudaSuccess) return fail(GOLDY_ERR_CUDA, std::string("cudaFuncSetAttribute: ") + cudaGetErrorString(e));
   int64_t cap = int64_t(ctx.sm_count) * k.per_sm;              // CTAs, or clusters, resident at once
@@ -900,13 +593,13 @@ goldy_status launch_norm(const LayerContext& ctx, void* arg) {
   groups = std::max<int64_t>(1, groups);
   void* args[] = {&call.p};
   if (call.d->rows > 0 || call.backward) {
-    e = Launch(unsigned(groups * cluster), unsigned(k.threads), k.smem, call.stream, unsigned(cluster)).run(k.fn, args);
+    e = NormLaunch(unsigned(groups * cluster), unsigned(k.threads), k.smem, call.stream, unsigned(cluster)).run(k.fn, args);
     if (e != cudaSuccess) return fail(GOLDY_ERR_CUDA, std::string("layer norm launch: ") + cudaGetErrorString(e));
   }
   if (call.backward && call.p.part && (groups > 1 || call.shape.team == 0)) {
     int n = int(call.d->n), rows = int(groups);
     void* rargs[] = {&call.p.part, &call.p.dgamma, &call.p.dbeta, &n, &rows, &call.p.accumulate};
-    e = Launch(unsigned(ceil_div(2 * call.d->n, 32)), kReduceWarps * 32, 0, call.stream)
+    e = NormLaunch(unsigned(ceil_div(2 * call.d->n, 32)), kReduceWarps * 32, 0, call.stream)
             .run(reinterpret_cast<const void*>(&norm_reduce_kernel), rargs);
     if (e != cudaSuccess) return fail(GOLDY_ERR_CUDA, std::string("layer norm launch: ") + cudaGetErrorString(e));
   }

@@ -10,9 +10,14 @@
 
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
+#include <string>
+#include <utility>
 
 #include "layer_launch.h"
 #include "layer_math.cuh"
+#include "norm_launch.h"
+#include "norm_rows.cuh"
 #include "sm103_ptx.cuh"
 
 namespace goldy {
@@ -40,25 +45,17 @@ struct ResidualNormParams {
   int64_t rows, ldx, ldf, lds, ldy;
   int32_t n, param_f32, norm_f, norm_y;
   float eps, alpha, inv_n;
-};
-
-struct ReduceParams {
-  const float* part;
-  const void* gate;
-  const void* gamma_f;
-  const void* beta_f;
+  int32_t cluster;           // CTAs that share a row, each with `seg` of its columns (the last with the rest)
+  int32_t seg;
+  // the parameters' gradients (backward)
   float* dgate;
   float* dgamma_f;
   float* dbeta_f;
   float* dgamma_y;
   float* dbeta_y;
-  int32_t n, parts, accumulate, param_f32;
+  int32_t accumulate, parts;
 };
 
-__device__ __forceinline__ float param_at(const void* p, int f32, int i, float absent) {
-  if (!p) return absent;
-  return f32 ? static_cast<const float*>(p)[i] : load_bf16(p, i);
-}
 template <typename T>
 __device__ __forceinline__ float elem(const void* base, int64_t i) {
   return sizeof(T) == 2 ? load_bf16(base, i) : static_cast<const float*>(base)[i];
@@ -202,48 +199,482 @@ __global__ void __launch_bounds__(kStreamThreads) residual_norm_backward_stream_
   }
 }
 
-// The parameters' gradients from the CTAs' partial rows, in CTA order: 8 warps
-// take every eighth row of 32 columns' four sums, then the warps in order.
-constexpr int kReduceWarps = 8;
-__global__ void __launch_bounds__(kReduceWarps * 32) residual_norm_reduce_kernel(const ReduceParams p) {
-  __shared__ float s[kReduceWarps][kSums][32];
-  ptx::griddep_launch_dependents();
-  ptx::griddep_wait();
-  const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t c = int64_t(blockIdx.x) * 32 + lane;
-  float v[kSums] = {0.0f, 0.0f, 0.0f, 0.0f};
-  if (c < p.n)
-    for (int r = w; r < p.parts; r += kReduceWarps)
-#pragma unroll
-      for (int i = 0; i < kSums; ++i) v[i] += __ldcg(p.part + (int64_t(r) * kSums + i) * p.n + c);
-#pragma unroll
-  for (int i = 0; i < kSums; ++i) s[w][i][lane] = v[i];
-  __syncthreads();
-  if (w != 0 || c >= p.n) return;
-#pragma unroll
-  for (int i = 0; i < kSums; ++i) {
-    v[i] = 0.0f;
-#pragma unroll
-    for (int k = 0; k < kReduceWarps; ++k) v[i] += s[k][i][lane];
-  }
+// ---- rows in registers ----------------------------------------------------------
+
+constexpr int kMaxTeam = 512;
+constexpr int kFwdThreads = 256;       // per CTA, at least the team
+constexpr int kBwdThreads = 512;
+constexpr int kFwdVals = 16;           // values of a row per thread
+constexpr int kBwdVals = 8;
+constexpr int kFwdDepth = 3;           // rows in a thread's ring
+// (backwards a row's F and dS stay until the row after it has come in)
+template <typename T> __host__ __device__ constexpr int bwd_depth() { return sizeof(T) == 2 ? 4 : 3; }
+
+// The parameters' gradients of column c from its four sums.
+__device__ __forceinline__ void give_gradients(const ResidualNormParams& p, int64_t c, float a, float b, float cc, float d) {
   const float gate = param_at(p.gate, p.param_f32, int(c), 1.0f);
   auto give = [&](float* to, float g) {
     if (to) to[c] = p.accumulate ? to[c] + g : g;
   };
-  give(p.dgate, fmaf(param_at(p.gamma_f, p.param_f32, int(c), 1.0f), v[0], param_at(p.beta_f, p.param_f32, int(c), 0.0f) * v[1]));
-  give(p.dgamma_f, gate * v[0]);
-  give(p.dbeta_f, gate * v[1]);
-  give(p.dgamma_y, v[2]);
-  give(p.dbeta_y, v[3]);
+  give(p.dgate, fmaf(param_at(p.gamma_f, p.param_f32, int(c), 1.0f), a, param_at(p.beta_f, p.param_f32, int(c), 0.0f) * b));
+  give(p.dgamma_f, gate * a);
+  give(p.dbeta_f, gate * b);
+  give(p.dgamma_y, cc);
+  give(p.dbeta_y, d);
+}
+
+template <typename T, int TEAM, bool VEC, bool WIDE>
+__global__ void __launch_bounds__(TEAM > kFwdThreads ? TEAM : kFwdThreads, TEAM > kFwdThreads ? 1 : 2)
+residual_norm_forward_kernel(const ResidualNormParams p) {
+  constexpr int THREADS = TEAM > kFwdThreads ? TEAM : kFwdThreads, TEAMS = THREADS / TEAM, VALS = kFwdVals;
+  constexpr int WARPS = TEAM / 32, D = kFwdDepth;
+  using R = NormRow<T, VALS, TEAM, THREADS, VEC, WIDE>;
+  __shared__ float4 slot[2][2][TEAMS][WARPS];      // per row, norm and warp: sum, M2, elements, mean
+  __shared__ float4 part[2][2][WIDE ? kMaxCluster : 1];
+  extern __shared__ __align__(16) uint8_t ring[];  // D rows of F, D of X
+  const int team = threadIdx.x / TEAM, t = threadIdx.x % TEAM, w = t >> 5, lane = t & 31;
+  // WIDE: this CTA's n columns from c0 on, of rows that a cluster shares
+  const int rank = WIDE ? int(ptx::cluster_ctarank()) : 0, c0 = WIDE ? rank * p.seg : 0;
+  const int n = WIDE ? min(p.seg, p.n - c0) : p.n;
+  const int group = WIDE ? int(blockIdx.x) / p.cluster : int(blockIdx.x);
+  const int groups = WIDE ? int(gridDim.x) / p.cluster : int(gridDim.x);
+  const T* const f_in = static_cast<const T*>(p.f) + c0;
+  const T* const x_in = static_cast<const T*>(p.x) + c0;
+  T* const s_out = static_cast<T*>(p.s) + c0;
+  T* const y_out = static_cast<T*>(p.y) + c0;
+  if (WIDE) ptx::cluster_sync_all();               // the others have started
+  ptx::griddep_launch_dependents();
+  ptx::griddep_wait();
+  const int64_t step = int64_t(groups) * TEAMS;
+  int64_t row = int64_t(group) * TEAMS + team;
+  if (row >= p.rows) return;                       // whole teams only
+  auto fetch = [&](int d, int64_t r) {
+    if (r < p.rows) {
+      R::fetch(ring + 2 * d * R::RING_BYTES, f_in, r, p.ldf, n, t);
+      R::fetch(ring + (2 * d + 1) * R::RING_BYTES, x_in, r, p.ldx, n, t);
+    }
+    copy_commit();
+  };
+#pragma unroll
+  for (int d = 0; d < D - 1; ++d) fetch(d, row + d * step);
+  // gate * N_f(v) = xhat * a + b: two parameters instead of three
+  float a[VALS], b[VALS], gamma[VALS], beta[VALS];
+  int mine = 0;                                    // values this thread has
+#pragma unroll
+  for (int i = 0; i < R::SLOTS; ++i) {
+    if (!R::in(i, t, n)) {
+#pragma unroll
+      for (int k = i * R::PER; k < (i + 1) * R::PER; ++k) a[k] = b[k] = gamma[k] = beta[k] = 0.0f;
+      continue;
+    }
+    const int c = c0 + R::col(i, t), k0 = i * R::PER;
+    load_params<R::PER, VEC>(p.gate, p.param_f32, c, c0 + n, 1.0f, gamma + k0);
+    load_params<R::PER, VEC>(p.gamma_f, p.param_f32, c, c0 + n, 1.0f, a + k0);
+    load_params<R::PER, VEC>(p.beta_f, p.param_f32, c, c0 + n, 0.0f, b + k0);
+#pragma unroll
+    for (int k = k0; k < k0 + R::PER; ++k) a[k] *= gamma[k], b[k] *= gamma[k];
+    load_params<R::PER, VEC>(p.gamma_y, p.param_f32, c, c0 + n, 1.0f, gamma + k0);
+    load_params<R::PER, VEC>(p.beta_y, p.param_f32, c, c0 + n, 0.0f, beta + k0);
+    mine += R::whole(i, t, n) ? R::PER : n - R::col(i, t);
+  }
+  const float warp_n = warp_sum(float(mine));
+  const float warp_inv = warp_n > 0.0f ? 1.0f / warp_n : 0.0f;
+  int at = 0, ahead = D - 1;                       // ring places of this row and of the one fetched now
+  for (int flip = 0; row < p.rows; row += step, flip ^= 1) {
+    // xhat of the values in v, which are 0 outside the row and stay 0 there
+    // (a layer norm's as differences from the warp's mean first)
+    auto normalise = [&](int kind, int which, float (&v)[VALS]) {
+      if (kind == GOLDY_NORM_NONE) return;
+      float s = 0.0f, wm = 0.0f;
+      if (kind == GOLDY_NORM_LAYER) {
+#pragma unroll
+        for (int j = 0; j < VALS; ++j) s += v[j];
+        s = warp_sum(s);
+        wm = s * warp_inv;
+#pragma unroll
+        for (int i = 0; i < R::SLOTS; ++i) {
+          if (!R::in(i, t, n)) continue;
+#pragma unroll
+          for (int k = 0; k < R::PER; ++k) {
+            float& e = v[i * R::PER + k];
+            e = R::whole(i, t, n) || R::col(i, t) + k < n ? e - wm : 0.0f;
+          }
+        }
+      }
+      float m2 = 0.0f;
+#pragma unroll
+      for (int j = 0; j < VALS; ++j) m2 = fmaf(v[j], v[j], m2);
+      m2 = warp_sum(m2);
+      float mean = wm;
+      if (WARPS > 1) {
+        if (lane == 0) slot[flip][which][team][w] = make_float4(s, m2, warp_n, wm);
+        team_sync<TEAM, THREADS>(team);
+        const float4 o = slot[flip][which][team][lane & (WARPS - 1)];
+        float total = 0.0f;
+        if (kind == GOLDY_NORM_LAYER) {
+          total = lanes_sum<WARPS>(o.x);
+          mean = total * (WIDE ? 1.0f / float(n) : p.inv_n);
+        }
+        const float d = o.w - mean;
+        m2 = lanes_sum<WARPS>(fmaf(o.z * d, d, o.y));
+        if (WIDE) {                                // the same once more, over the cluster's CTAs in order
+          tell_cluster(part[flip][which], rank, p.cluster, make_float4(total, m2, float(n), mean));
+          float all = 0.0f;
+          for (int k = 0; k < p.cluster; ++k) all += part[flip][which][k].x;
+          mean = all * p.inv_n;
+          m2 = 0.0f;
+          for (int k = 0; k < p.cluster; ++k) {
+            const float4 q = part[flip][which][k];
+            const float e = q.w - mean;
+            m2 += fmaf(q.z * e, e, q.y);
+          }
+        }
+      }
+      const float rstd = rsqrtf(fmaf(m2, p.inv_n, p.eps)), shift = (wm - mean) * rstd;
+#pragma unroll
+      for (int i = 0; i < R::SLOTS; ++i) {
+        if (!R::in(i, t, n)) continue;
+#pragma unroll
+        for (int j = i * R::PER; j < (i + 1) * R::PER; ++j) v[j] = fmaf(v[j], rstd, shift);
+      }
+      if (t == 0 && rank == 0 && p.stats) {
+        if (kind == GOLDY_NORM_LAYER) p.stats[2 * which * p.rows + row] = mean;
+        p.stats[(2 * which + 1) * p.rows + row] = rstd;
+      }
+    };
+    fetch(ahead, row + (D - 1) * step);
+    copy_wait<D - 1>();
+    if (R::SHIFT) team_sync<TEAM, THREADS>(team);
+    float v[VALS], x[VALS];
+    R::values(ring + 2 * at * R::RING_BYTES, f_in, row, p.ldf, n, t, v);
+    R::values(ring + (2 * at + 1) * R::RING_BYTES, x_in, row, p.ldx, n, t, x);
+    if (R::SHIFT) team_sync<TEAM, THREADS>(team);  // the ring's place is used again: every piece has been read
+    at = at + 1 == D ? 0 : at + 1;
+    ahead = ahead + 1 == D ? 0 : ahead + 1;
+    normalise(p.norm_f, 0, v);
+#pragma unroll
+    for (int j = 0; j < VALS; ++j) v[j] = fmaf(v[j], a[j], fmaf(p.alpha, x[j], b[j]));
+    R::store(s_out, row, p.lds, n, t, v);
+    if (p.norm_y == GOLDY_NORM_NONE) continue;
+    normalise(p.norm_y, 1, v);
+#pragma unroll
+    for (int j = 0; j < VALS; ++j) v[j] = fmaf(v[j], gamma[j], beta[j]);
+    R::store(y_out, row, p.ldy, n, t, v);
+  }
+}
+
+template <typename T, int TEAM, bool VEC, bool WIDE>
+__global__ void __launch_bounds__(kBwdThreads) residual_norm_backward_kernel(const ResidualNormParams p) {
+  constexpr int TEAMS = kBwdThreads / TEAM, WARPS = TEAM / 32, VALS = kBwdVals, D = bwd_depth<T>();
+  using R = NormRow<T, VALS, TEAM, kBwdThreads, VEC, WIDE>;
+  __shared__ float4 slot[2][TEAMS][WARPS];
+  __shared__ float4 part[2][WIDE ? kMaxCluster : 1];
+  extern __shared__ __align__(16) uint8_t ring[];  // D rows of F, S, dY and dS each; at the end the CTA's sums
+  const int team = threadIdx.x / TEAM, t = threadIdx.x % TEAM, w = t >> 5, lane = t & 31;
+  const int rank = WIDE ? int(ptx::cluster_ctarank()) : 0, c0 = WIDE ? rank * p.seg : 0;
+  const int n = WIDE ? min(p.seg, p.n - c0) : p.n;
+  const int group = WIDE ? int(blockIdx.x) / p.cluster : int(blockIdx.x);
+  const int groups = WIDE ? int(gridDim.x) / p.cluster : int(gridDim.x);
+  const T* const f_in = static_cast<const T*>(p.f) + c0;
+  const T* const s_in = static_cast<const T*>(p.s_in) + c0;
+  const T* const dy_in = static_cast<const T*>(p.dy) + c0;
+  const T* const ds_in = static_cast<const T*>(p.ds) + c0;
+  T* const dx_out = static_cast<T*>(p.s) + c0;
+  T* const df_out = static_cast<T*>(p.y) + c0;
+  const bool has_y = p.norm_y != GOLDY_NORM_NONE, has_f = p.norm_f != GOLDY_NORM_NONE, has_ds = p.ds != nullptr;
+  const float layer_f = p.norm_f == GOLDY_NORM_LAYER ? p.inv_n : 0.0f, layer_y = p.norm_y == GOLDY_NORM_LAYER ? p.inv_n : 0.0f;
+  if (WIDE) ptx::cluster_sync_all();               // the others have started
+  ptx::griddep_launch_dependents();
+  ptx::griddep_wait();
+  const int64_t step = int64_t(groups) * TEAMS;
+  int64_t row = int64_t(group) * TEAMS + team;
+  auto fetch = [&](int d, int64_t r) {
+    if (r < p.rows) {
+      uint8_t* to = ring + 4 * d * R::RING_BYTES;
+      R::fetch(to, f_in, r, p.ldf, n, t);
+      if (has_y) {
+        R::fetch(to + R::RING_BYTES, s_in, r, p.lds, n, t);
+        R::fetch(to + 2 * R::RING_BYTES, dy_in, r, p.ldy, n, t);
+      }
+      if (has_ds) R::fetch(to + 3 * R::RING_BYTES, ds_in, r, p.lds, n, t);
+    }
+    copy_commit();
+  };
+  struct Stats {
+    float mf, rf, my, ry;
+  };
+  auto stats_of = [&](int64_t r) {
+    Stats s = {0.0f, 1.0f, 0.0f, 1.0f};
+    if (r < p.rows) {
+      if (p.norm_f == GOLDY_NORM_LAYER) s.mf = p.stats[r];
+      if (has_f) s.rf = p.stats[p.rows + r];
+      if (p.norm_y == GOLDY_NORM_LAYER) s.my = p.stats[2 * p.rows + r];
+      if (has_y) s.ry = p.stats[3 * p.rows + r];
+    }
+    return s;
+  };
+#pragma unroll
+  for (int d = 0; d < D - 1; ++d) fetch(d, row + d * step);
+  Stats now = stats_of(row), next = stats_of(row + step);
+  float gf[VALS], gy[VALS];                        // gate * gamma_f, gamma_y; 0 outside the row
+  float sum[kSums][VALS];
+#pragma unroll
+  for (int i = 0; i < R::SLOTS; ++i) {
+    const int k0 = i * R::PER, c = c0 + R::col(i, t);
+    if (R::in(i, t, n)) {
+      load_params<R::PER, VEC>(p.gate, p.param_f32, c, c0 + n, 1.0f, gf + k0);
+      load_params<R::PER, VEC>(p.gamma_f, p.param_f32, c, c0 + n, 1.0f, gy + k0);
+#pragma unroll
+      for (int k = k0; k < k0 + R::PER; ++k) gf[k] *= gy[k];
+      load_params<R::PER, VEC>(p.gamma_y, p.param_f32, c, c0 + n, 1.0f, gy + k0);
+    } else {
+#pragma unroll
+      for (int k = k0; k < k0 + R::PER; ++k) gf[k] = gy[k] = 0.0f;
+    }
+#pragma unroll
+    for (int k = k0; k < k0 + R::PER; ++k)
+#pragma unroll
+      for (int q = 0; q < kSums; ++q) sum[q][k] = 0.0f;
+  }
+  // A row takes two sums one after the other: (1) of dY gamma_y and its product
+  // with xhat_y, which T needs, (2) of T gate gamma_f and its product with xhat_f,
+  // which dF needs.  The second ones of a row and the first ones of the next row
+  // are exchanged together: one barrier per row, and each phase has another row's
+  // arithmetic beside it.
+  float g[VALS], hy[VALS], u[VALS], h[VALS];
+  float s1x, s1y, s2x = 0.0f, s2y = 0.0f;          // partial sums, then the rows'
+  auto first = [&](const uint8_t* from, int64_t r, const Stats& st) {
+    s1x = s1y = 0.0f;
+    if (!has_y || r >= p.rows) return;
+    R::values(from + R::RING_BYTES, s_in, r, p.lds, n, t, hy);
+    R::values(from + 2 * R::RING_BYTES, dy_in, r, p.ldy, n, t, g);
+    // the mean is subtracted before the scale: rows far from zero keep their
+    // digits; columns outside the row have dY = gamma = 0 and add nothing
+#pragma unroll
+    for (int j = 0; j < VALS; ++j) {
+      hy[j] = (hy[j] - st.my) * st.ry;
+      sum[2][j] = fmaf(g[j], hy[j], sum[2][j]);
+      sum[3][j] += g[j];
+      g[j] *= gy[j];
+      s1x += g[j];
+      s1y = fmaf(g[j], hy[j], s1y);
+    }
+  };
+  auto exchange = [&](int flip) {
+    const float4 v = warp_sum4(s1x, s1y, s2x, s2y, lane, WARPS > 1 ? reinterpret_cast<float*>(&slot[flip][team][w]) : nullptr);
+    float4 r = v;
+    if (WARPS > 1) {
+      team_sync<TEAM, kBwdThreads>(team);
+      if (WARPS <= 4) {
+        r = slot[flip][team][0];
+#pragma unroll
+        for (int k = 1; k < WARPS; ++k) {
+          const float4 o = slot[flip][team][k];
+          r.x += o.x, r.y += o.y, r.z += o.z, r.w += o.w;
+        }
+      } else {
+        const float4 o = slot[flip][team][lane & (WARPS - 1)];
+        r = make_float4(lanes_sum<WARPS>(o.x), lanes_sum<WARPS>(o.y), lanes_sum<WARPS>(o.z), lanes_sum<WARPS>(o.w));
+      }
+      if (WIDE) {
+        tell_cluster(part[flip], rank, p.cluster, r);
+        r = part[flip][0];
+        for (int k = 1; k < p.cluster; ++k) {
+          const float4 o = part[flip][k];
+          r.x += o.x, r.y += o.y, r.z += o.z, r.w += o.w;
+        }
+      }
+    } else if (R::SHIFT) {
+      __syncwarp();
+    }
+    s1x = r.x, s1y = r.y, s2x = r.z, s2y = r.w;
+  };
+  float last_rf = 0.0f;                            // of the row whose dF is left
+  auto finish = [&](int64_t r) {
+    const float less = -s2x * layer_f * last_rf, slope = -s2y * p.inv_n * last_rf;
+    if (has_f) {
+#pragma unroll
+      for (int j = 0; j < VALS; ++j) u[j] = fmaf(h[j], slope, fmaf(u[j], last_rf, less));
+    }
+    R::store(df_out, r, p.ldf, n, t, u);
+  };
+  const int64_t row0 = row;
+  int at = 0, ahead = D - 1;
+  if (row < p.rows) {                              // whole teams, and whole clusters
+    copy_wait<D - 2>();
+    if (R::SHIFT) team_sync<TEAM, kBwdThreads>(team);
+    first(ring, row, now);
+    exchange(1);
+  }
+  for (int flip = 0; row < p.rows; row += step, flip ^= 1) {
+    fetch(ahead, row + (D - 1) * step);            // where the row before this one was
+    const Stats later = stats_of(row + 2 * step);
+    copy_wait<D - 2>();
+    if (R::SHIFT) team_sync<TEAM, kBwdThreads>(team);
+    if (row != row0) finish(row - step);
+    // T, dX, and what dF needs
+    const uint8_t* from = ring + 4 * at * R::RING_BYTES;
+    at = at + 1 == D ? 0 : at + 1;
+    ahead = ahead + 1 == D ? 0 : ahead + 1;
+    float tt[VALS];
+    if (has_ds) {
+      R::values(from + 3 * R::RING_BYTES, ds_in, row, p.lds, n, t, tt);
+    } else {
+#pragma unroll
+      for (int j = 0; j < VALS; ++j) tt[j] = 0.0f;
+    }
+    if (has_y) {
+      const float less = -s1x * layer_y * now.ry, slope = -s1y * p.inv_n * now.ry;
+#pragma unroll
+      for (int j = 0; j < VALS; ++j) tt[j] += fmaf(hy[j], slope, fmaf(g[j], now.ry, less));
+    }
+    R::values(from, f_in, row, p.ldf, n, t, h);
+    s2x = s2y = 0.0f;
+#pragma unroll
+    for (int j = 0; j < VALS; ++j) {
+      h[j] = (h[j] - now.mf) * now.rf;
+      sum[0][j] = fmaf(tt[j], h[j], sum[0][j]);
+      sum[1][j] += tt[j];
+      u[j] = tt[j] * gf[j];
+      s2x += u[j];
+      s2y = fmaf(u[j], h[j], s2y);
+      tt[j] *= p.alpha;
+    }
+    R::store(dx_out, row, p.ldx, n, t, tt);
+    last_rf = now.rf;
+    now = next;
+    next = later;
+    first(ring + 4 * at * R::RING_BYTES, row + step, now);
+    exchange(flip);
+  }
+  if (row != row0) finish(row - step);
+  if (!p.part) return;
+  // the teams' sums go through shared memory, in column order, to be added in
+  // team order
+  float* sums = reinterpret_cast<float*>(ring);    // [teams][kSums][column]
+  constexpr int ALL = TEAM * VALS;
+  copy_wait<0>();
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < R::SLOTS; ++i)
+#pragma unroll
+    for (int q = 0; q < kSums; ++q)
+#pragma unroll
+      for (int k = 0; k < R::PER; ++k) sums[(team * kSums + q) * ALL + R::col(i, t) + k] = sum[q][i * R::PER + k];
+  __syncthreads();
+  float* to = p.part + int64_t(group) * kSums * p.n + c0;
+  for (int c = threadIdx.x; c < n; c += kBwdThreads) {
+    float v[kSums];
+#pragma unroll
+    for (int q = 0; q < kSums; ++q) {
+      v[q] = 0.0f;
+#pragma unroll
+      for (int k = 0; k < TEAMS; ++k) v[q] += sums[(k * kSums + q) * ALL + c];
+    }
+    if (groups > 1) {
+#pragma unroll
+      for (int q = 0; q < kSums; ++q) __stcg(to + int64_t(q) * p.n + c, v[q]);
+    } else {                                       // this CTA's sums are the result
+      give_gradients(p, c0 + c, v[0], v[1], v[2], v[3]);
+    }
+  }
+}
+
+// The parameters' gradients from the CTAs' partial rows, in CTA order: of 32
+// columns, eight warps per sum take every eighth row, all in flight together, and
+// the warps are added in order.
+constexpr int kReduceWarps = 8;
+constexpr int kReduceRows = (kBwdCtas + kReduceWarps - 1) / kReduceWarps;
+__global__ void __launch_bounds__(kSums * kReduceWarps * 32) residual_norm_reduce_kernel(const ResidualNormParams p) {
+  __shared__ float s[kSums][kReduceWarps][32];
+  ptx::griddep_launch_dependents();
+  ptx::griddep_wait();
+  const int w = threadIdx.x >> 5, lane = threadIdx.x & 31, q = w / kReduceWarps, k = w % kReduceWarps;
+  const int64_t c = int64_t(blockIdx.x) * 32 + lane;
+  float v = 0.0f, t[kReduceRows];
+#pragma unroll
+  for (int i = 0; i < kReduceRows; ++i) {
+    const int r = k + i * kReduceWarps;
+    t[i] = r < p.parts && c < p.n ? __ldcg(p.part + (int64_t(r) * kSums + q) * p.n + c) : 0.0f;
+  }
+#pragma unroll
+  for (int i = 0; i < kReduceRows; ++i) v += t[i];
+  s[q][k][lane] = v;
+  __syncthreads();
+  if (w != 0 || c >= p.n) return;
+  float all[kSums];
+#pragma unroll
+  for (int i = 0; i < kSums; ++i) {
+    all[i] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < kReduceWarps; ++j) all[i] += s[i][j][lane];
+  }
+  give_gradients(p, c, all[0], all[1], all[2], all[3]);
 }
 
 // ---- host ---------------------------------------------------------------------
 
-int64_t backward_parts(const goldy_residual_norm_desc& d) {
+// Threads per row; 0: the row streams.  `cluster` CTAs of kMaxTeam threads share
+// a row that is too long for one.
+struct NormShape {
+  int team, cluster, seg;
+};
+NormShape shape_for(const goldy_residual_norm_desc& d, bool backward) {
+  const int64_t vals = backward ? kBwdVals : kFwdVals;
+  int team = 32;
+  while (team < kMaxTeam && team * vals < d.n) team *= 2;
+  int cluster = 1;
+  while (cluster < kMaxCluster && cluster * team * vals < d.n) cluster *= 2;
+  if (cluster * team * vals < d.n) return {0, 1, 0};
+  return {team, cluster, int(ceil_div(ceil_div(d.n, cluster), 8) * 8)};     // whole pieces
+}
+
+// Partial rows of a backward launch, at most: CTAs, or clusters of them.
+int64_t stream_parts(const goldy_residual_norm_desc& d) {
   return std::max<int64_t>(1, std::min<int64_t>(kBwdCtas, d.rows));
 }
+// Rows per team up to which one CTA does them all: a further kernel that sums
+// partial rows costs more.
+constexpr int kAloneRows = 2;
+int64_t team_parts(const goldy_residual_norm_desc& d, const NormShape& s) {
+  const int64_t teams = s.cluster > 1 ? 1 : kBwdThreads / s.team;
+  if (d.rows <= kAloneRows * teams) return 1;      // no second kernel
+  return std::min<int64_t>(kBwdCtas / s.cluster, ceil_div(d.rows, teams));
+}
 size_t backward_bytes(const goldy_residual_norm_desc& d) {
-  return kLayerCounterBytes + size_t(backward_parts(d)) * kSums * size_t(d.n) * sizeof(float);
+  const NormShape s = shape_for(d, true);
+  // (inside an SM partition rows stream where clusters would share them)
+  const int64_t parts = s.team == 0 || s.cluster > 1 ? stream_parts(d) : team_parts(d, s);
+  return kLayerCounterBytes + size_t(parts) * kSums * size_t(d.n) * sizeof(float);
+}
+
+template <typename T, int TEAM, bool VEC, bool WIDE = false>
+NormKernel pick(bool backward) {
+  if (backward) {
+    using R = NormRow<T, kBwdVals, TEAM, kBwdThreads, VEC, WIDE>;
+    return {reinterpret_cast<const void*>(&residual_norm_backward_kernel<T, TEAM, VEC, WIDE>), kBwdThreads,
+            kBwdThreads / TEAM, 1,
+            std::max(size_t(4) * bwd_depth<T>() * R::RING_BYTES, size_t(kSums) * kBwdThreads * kBwdVals * sizeof(float))};
+  }
+  constexpr int THREADS = TEAM > kFwdThreads ? TEAM : kFwdThreads;
+  using R = NormRow<T, kFwdVals, TEAM, THREADS, VEC, WIDE>;
+  return {reinterpret_cast<const void*>(&residual_norm_forward_kernel<T, TEAM, VEC, WIDE>), THREADS, THREADS / TEAM,
+          TEAM > kFwdThreads ? 1 : 2, size_t(2) * kFwdDepth * R::RING_BYTES};
+}
+template <typename T, bool VEC>
+NormKernel pick_shape(const NormShape& s, bool backward) {
+  if (s.cluster > 1) return pick<T, kMaxTeam, VEC, true>(backward);
+  switch (s.team) {
+    case 32: return pick<T, 32, VEC>(backward);
+    case 64: return pick<T, 64, VEC>(backward);
+    case 128: return pick<T, 128, VEC>(backward);
+    case 256: return pick<T, 256, VEC>(backward);
+    case 512: return pick<T, 512, VEC>(backward);
+    default:
+      return {backward ? reinterpret_cast<const void*>(&residual_norm_backward_stream_kernel<T>)
+                       : reinterpret_cast<const void*>(&residual_norm_forward_stream_kernel<T>),
+              kStreamThreads, 1, 4, 0};
+  }
 }
 
 bool is_kind(int k) { return k == GOLDY_NORM_NONE || k == GOLDY_NORM_LAYER || k == GOLDY_NORM_RMS; }
@@ -278,34 +709,59 @@ goldy_status check_params(const goldy_residual_norm_desc& d, const goldy_residua
 
 struct ResidualNormCall {
   ResidualNormParams p;
-  ReduceParams r;
   const goldy_residual_norm_desc* d;
-  bool backward;
+  bool backward, vec;
   void* stream;
 };
 
 goldy_status launch_residual_norm(const LayerContext& ctx, void* arg) {
   ResidualNormCall& call = *static_cast<ResidualNormCall*>(arg);
   const goldy_residual_norm_desc& d = *call.d;
-  const bool f32 = d.dtype == GOLDY_F32;
-  void* args[] = {&call.p};
-  const void* fn;
-  int64_t grid;
-  if (call.backward) {
-    fn = f32 ? reinterpret_cast<const void*>(&residual_norm_backward_stream_kernel<float>)
-             : reinterpret_cast<const void*>(&residual_norm_backward_stream_kernel<uint16_t>);
-    grid = backward_parts(d);
-  } else {
-    fn = f32 ? reinterpret_cast<const void*>(&residual_norm_forward_stream_kernel<float>)
-             : reinterpret_cast<const void*>(&residual_norm_forward_stream_kernel<uint16_t>);
-    grid = std::min<int64_t>(d.rows, int64_t(ctx.sm_count) * 4);
+  NormShape shape = shape_for(d, call.backward);
+  // which SMs a partition has, and so whether a cluster fits into it, is not known
+  if (!ctx.whole && shape.cluster > 1) shape = {0, 1, 0};
+  const int cluster = shape.cluster;
+  NormKernel k;
+  if (d.dtype == GOLDY_F32) k = call.vec ? pick_shape<float, true>(shape, call.backward) : pick_shape<float, false>(shape, call.backward);
+  else k = call.vec ? pick_shape<uint16_t, true>(shape, call.backward) : pick_shape<uint16_t, false>(shape, call.backward);
+  cudaError_t e = allow_smem(ctx.device, k);
+  if (e != cudaSuccess) return fail(GOLDY_ERR_CUDA, std::string("cudaFuncSetAttribute: ") + cudaGetErrorString(e));
+  int64_t cap = int64_t(ctx.sm_count) * k.per_sm;              // CTAs, or clusters, resident at once
+  if (cluster > 1) {
+    int most = 0;
+    e = resident_clusters(ctx.device, k, cluster, &most);
+    if (e == cudaSuccess && most < 1) e = cudaErrorInvalidClusterSize;
+    if (e != cudaSuccess) return fail(GOLDY_ERR_CUDA, std::string("residual norm, clusters: ") + cudaGetErrorString(e));
+    cap = std::min<int64_t>(cap / cluster, most);
   }
-  const goldy_status st = launch_layer("residual norm", fn, grid, kStreamThreads, 0, call.stream, args);
-  if (st != GOLDY_OK || !call.p.part) return st;
-  call.r.parts = int32_t(grid);
-  void* rargs[] = {&call.r};
-  return launch_layer("residual norm", reinterpret_cast<const void*>(&residual_norm_reduce_kernel), ceil_div(d.n, 32),
-                      kReduceWarps * 32, 0, call.stream, rargs);
+  // all resident, every team with rows of its own
+  int64_t groups = std::min(cap, ceil_div(d.rows, int64_t(k.teams)));
+  if (call.backward) groups = shape.team == 0 ? stream_parts(d) : team_parts(d, shape);
+  if (cluster > 1) groups = std::min(groups, cap);
+  groups = std::max<int64_t>(1, groups);
+  call.p.cluster = cluster;
+  call.p.seg = shape.seg;
+  call.p.parts = int32_t(groups);
+  void* args[] = {&call.p};
+  e = NormLaunch(unsigned(groups * cluster), unsigned(k.threads), k.smem, call.stream, unsigned(cluster)).run(k.fn, args);
+  if (e == cudaSuccess && call.p.part && (groups > 1 || shape.team == 0))
+    e = NormLaunch(unsigned(ceil_div(d.n, 32)), kSums * kReduceWarps * 32, 0, call.stream)
+            .run(reinterpret_cast<const void*>(&residual_norm_reduce_kernel), args);
+  if (e != cudaSuccess) return fail(GOLDY_ERR_CUDA, std::string("residual norm launch: ") + cudaGetErrorString(e));
+  return GOLDY_OK;
+}
+
+// 16-byte accesses: whole vectors in every row, rows, bases and parameters on
+// vector boundaries
+bool whole_vectors(const goldy_residual_norm_desc& d, const goldy_residual_norm_params& given,
+                   std::initializer_list<std::pair<const void*, int64_t>> arrays) {
+  const int64_t per = d.dtype == GOLDY_F32 ? 4 : 8;
+  if (d.n % per != 0) return false;
+  for (const auto& a : arrays)
+    if (a.first && (!on_boundary(a.first, 16) || a.second % per != 0)) return false;
+  for (const void* q : {given.gate, given.gamma_f, given.beta_f, given.gamma_y, given.beta_y})
+    if (!on_boundary(q, 16)) return false;
+  return true;
 }
 
 void common_params(ResidualNormCall& call, const goldy_residual_norm_desc& d, const goldy_residual_norm_params& given) {
@@ -371,6 +827,7 @@ extern "C" goldy_status goldy_residual_norm_forward(const goldy_residual_norm_de
   call.p.s = S;
   call.p.y = Y;
   call.p.stats = stats;
+  call.vec = whole_vectors(*desc, given, {{X, desc->ldx}, {F, desc->ldf}, {S, desc->lds}, {Y, desc->ldy}});
   call.stream = stream;
   st = with_layer_context(stream, launch_residual_norm, &call);
   return st == GOLDY_OK ? ok() : st;
@@ -427,19 +884,14 @@ extern "C" goldy_status goldy_residual_norm_backward(const goldy_residual_norm_d
   call.p.s = dX;
   call.p.y = dF;
   call.p.part = sums ? reinterpret_cast<float*>(static_cast<char*>(workspace) + kLayerCounterBytes) : nullptr;
-  ReduceParams& r = call.r;
-  r.part = call.p.part;
-  r.gate = given.gate;
-  r.gamma_f = given.gamma_f;
-  r.beta_f = given.beta_f;
-  r.dgate = static_cast<float*>(want.gate);
-  r.dgamma_f = static_cast<float*>(want.gamma_f);
-  r.dbeta_f = static_cast<float*>(want.beta_f);
-  r.dgamma_y = static_cast<float*>(want.gamma_y);
-  r.dbeta_y = static_cast<float*>(want.beta_y);
-  r.n = int32_t(desc->n);
-  r.accumulate = accumulate;
-  r.param_f32 = desc->param_dtype == GOLDY_F32;
+  call.p.dgate = static_cast<float*>(want.gate);
+  call.p.dgamma_f = static_cast<float*>(want.gamma_f);
+  call.p.dbeta_f = static_cast<float*>(want.beta_f);
+  call.p.dgamma_y = static_cast<float*>(want.gamma_y);
+  call.p.dbeta_y = static_cast<float*>(want.beta_y);
+  call.p.accumulate = accumulate;
+  call.vec = whole_vectors(*desc, given, {{dY, desc->ldy}, {dS, desc->lds}, {F, desc->ldf}, {dY ? S : nullptr, desc->lds},
+                                          {dX, desc->ldx}, {dF, desc->ldf}});
   call.stream = stream;
   st = with_layer_context(stream, launch_residual_norm, &call);
   return st == GOLDY_OK ? ok() : st;
