@@ -416,49 +416,64 @@ __global__ void __launch_bounds__(kBwdThreads) residual_norm_backward_kernel(con
 #pragma unroll
   for (int d = 0; d < D - 1; ++d) fetch(d, row + d * step);
   Stats now = stats_of(row), next = stats_of(row + step);
-  float gf[VALS], gy[VALS];                        // gate * gamma_f, gamma_y; 0 outside the row
-  float sum[kSums][VALS];
+  // values in pairs: half the instructions
+  constexpr int PAIRS = VALS / 2;
+  uint64_t gf[PAIRS], gy[PAIRS], sum[kSums][PAIRS];      // gate * gamma_f, gamma_y; 0 outside the row
+  {
+    float a[VALS], b[VALS], c[VALS];
 #pragma unroll
-  for (int i = 0; i < R::SLOTS; ++i) {
-    const int k0 = i * R::PER, c = c0 + R::col(i, t);
-    if (R::in(i, t, n)) {
-      load_params<R::PER, VEC>(p.gate, p.param_f32, c, c0 + n, 1.0f, gf + k0);
-      load_params<R::PER, VEC>(p.gamma_f, p.param_f32, c, c0 + n, 1.0f, gy + k0);
+    for (int i = 0; i < R::SLOTS; ++i) {
+      const int k0 = i * R::PER, at = c0 + R::col(i, t);
+      if (R::in(i, t, n)) {
+        load_params<R::PER, VEC>(p.gate, p.param_f32, at, c0 + n, 1.0f, a + k0);
+        load_params<R::PER, VEC>(p.gamma_f, p.param_f32, at, c0 + n, 1.0f, b + k0);
+        load_params<R::PER, VEC>(p.gamma_y, p.param_f32, at, c0 + n, 1.0f, c + k0);
+      } else {
 #pragma unroll
-      for (int k = k0; k < k0 + R::PER; ++k) gf[k] *= gy[k];
-      load_params<R::PER, VEC>(p.gamma_y, p.param_f32, c, c0 + n, 1.0f, gy + k0);
-    } else {
-#pragma unroll
-      for (int k = k0; k < k0 + R::PER; ++k) gf[k] = gy[k] = 0.0f;
+        for (int k = k0; k < k0 + R::PER; ++k) a[k] = b[k] = c[k] = 0.0f;
+      }
     }
 #pragma unroll
-    for (int k = k0; k < k0 + R::PER; ++k)
+    for (int j = 0; j < PAIRS; ++j) {
+      gf[j] = mul2(two(a[2 * j], a[2 * j + 1]), two(b[2 * j], b[2 * j + 1]));
+      gy[j] = two(c[2 * j], c[2 * j + 1]);
 #pragma unroll
-      for (int q = 0; q < kSums; ++q) sum[q][k] = 0.0f;
+      for (int q = 0; q < kSums; ++q) sum[q][j] = two(0.0f);
+    }
   }
   // A row takes two sums one after the other: (1) of dY gamma_y and its product
   // with xhat_y, which T needs, (2) of T gate gamma_f and its product with xhat_f,
   // which dF needs.  The second ones of a row and the first ones of the next row
   // are exchanged together: one barrier per row, and each phase has another row's
   // arithmetic beside it.
-  float g[VALS], hy[VALS], u[VALS], h[VALS];
+  uint64_t g[PAIRS], hy[PAIRS], u[PAIRS], h[PAIRS];
   float s1x, s1y, s2x = 0.0f, s2y = 0.0f;          // partial sums, then the rows'
+  auto both = [](uint64_t v) {
+    const float2 f = apart(v);
+    return f.x + f.y;
+  };
   auto first = [&](const uint8_t* from, int64_t r, const Stats& st) {
     s1x = s1y = 0.0f;
     if (!has_y || r >= p.rows) return;
-    R::values(from + R::RING_BYTES, s_in, r, p.lds, n, t, hy);
-    R::values(from + 2 * R::RING_BYTES, dy_in, r, p.ldy, n, t, g);
+    float v[VALS], d[VALS];
+    R::values(from + R::RING_BYTES, s_in, r, p.lds, n, t, v);
+    R::values(from + 2 * R::RING_BYTES, dy_in, r, p.ldy, n, t, d);
     // the mean is subtracted before the scale: rows far from zero keep their
     // digits; columns outside the row have dY = gamma = 0 and add nothing
+    const uint64_t off = two(-st.my), scale = two(st.ry);
+    uint64_t a = two(0.0f), b = a;
 #pragma unroll
-    for (int j = 0; j < VALS; ++j) {
-      hy[j] = (hy[j] - st.my) * st.ry;
-      sum[2][j] = fmaf(g[j], hy[j], sum[2][j]);
-      sum[3][j] += g[j];
-      g[j] *= gy[j];
-      s1x += g[j];
-      s1y = fmaf(g[j], hy[j], s1y);
+    for (int j = 0; j < PAIRS; ++j) {
+      hy[j] = mul2(add2(two(v[2 * j], v[2 * j + 1]), off), scale);
+      const uint64_t dy = two(d[2 * j], d[2 * j + 1]);
+      sum[2][j] = fma2(dy, hy[j], sum[2][j]);
+      sum[3][j] = add2(sum[3][j], dy);
+      g[j] = mul2(dy, gy[j]);
+      a = add2(a, g[j]);
+      b = fma2(g[j], hy[j], b);
     }
+    s1x = both(a);
+    s1y = both(b);
   };
   auto exchange = [&](int flip) {
     const float4 v = warp_sum4(s1x, s1y, s2x, s2y, lane, WARPS > 1 ? reinterpret_cast<float*>(&slot[flip][team][w]) : nullptr);
@@ -491,12 +506,15 @@ __global__ void __launch_bounds__(kBwdThreads) residual_norm_backward_kernel(con
   };
   float last_rf = 0.0f;                            // of the row whose dF is left
   auto finish = [&](int64_t r) {
-    const float less = -s2x * layer_f * last_rf, slope = -s2y * p.inv_n * last_rf;
-    if (has_f) {
+    const uint64_t less = two(-s2x * layer_f * last_rf), slope = two(-s2y * p.inv_n * last_rf), scale = two(last_rf);
+    float v[VALS];
 #pragma unroll
-      for (int j = 0; j < VALS; ++j) u[j] = fmaf(h[j], slope, fmaf(u[j], last_rf, less));
+    for (int j = 0; j < PAIRS; ++j) {
+      const float2 f = apart(has_f ? fma2(h[j], slope, fma2(u[j], scale, less)) : u[j]);
+      v[2 * j] = f.x;
+      v[2 * j + 1] = f.y;
     }
-    R::store(df_out, r, p.ldf, n, t, u);
+    R::store(df_out, r, p.ldf, n, t, v);
   };
   const int64_t row0 = row;
   int at = 0, ahead = D - 1;
@@ -516,30 +534,33 @@ __global__ void __launch_bounds__(kBwdThreads) residual_norm_backward_kernel(con
     const uint8_t* from = ring + 4 * at * R::RING_BYTES;
     at = at + 1 == D ? 0 : at + 1;
     ahead = ahead + 1 == D ? 0 : ahead + 1;
-    float tt[VALS];
+    float tt[VALS], v[VALS];
     if (has_ds) {
       R::values(from + 3 * R::RING_BYTES, ds_in, row, p.lds, n, t, tt);
     } else {
 #pragma unroll
       for (int j = 0; j < VALS; ++j) tt[j] = 0.0f;
     }
-    if (has_y) {
-      const float less = -s1x * layer_y * now.ry, slope = -s1y * p.inv_n * now.ry;
+    R::values(from, f_in, row, p.ldf, n, t, v);
+    const uint64_t less = two(-s1x * layer_y * now.ry), slope = two(-s1y * p.inv_n * now.ry), ry = two(now.ry);
+    const uint64_t off = two(-now.mf), scale = two(now.rf), alpha = two(p.alpha);
+    uint64_t a = two(0.0f), b = a;
 #pragma unroll
-      for (int j = 0; j < VALS; ++j) tt[j] += fmaf(hy[j], slope, fmaf(g[j], now.ry, less));
+    for (int j = 0; j < PAIRS; ++j) {
+      uint64_t d = two(tt[2 * j], tt[2 * j + 1]);
+      if (has_y) d = add2(d, fma2(hy[j], slope, fma2(g[j], ry, less)));
+      h[j] = mul2(add2(two(v[2 * j], v[2 * j + 1]), off), scale);
+      sum[0][j] = fma2(d, h[j], sum[0][j]);
+      sum[1][j] = add2(sum[1][j], d);
+      u[j] = mul2(d, gf[j]);
+      a = add2(a, u[j]);
+      b = fma2(u[j], h[j], b);
+      const float2 f = apart(mul2(d, alpha));
+      tt[2 * j] = f.x;
+      tt[2 * j + 1] = f.y;
     }
-    R::values(from, f_in, row, p.ldf, n, t, h);
-    s2x = s2y = 0.0f;
-#pragma unroll
-    for (int j = 0; j < VALS; ++j) {
-      h[j] = (h[j] - now.mf) * now.rf;
-      sum[0][j] = fmaf(tt[j], h[j], sum[0][j]);
-      sum[1][j] += tt[j];
-      u[j] = tt[j] * gf[j];
-      s2x += u[j];
-      s2y = fmaf(u[j], h[j], s2y);
-      tt[j] *= p.alpha;
-    }
+    s2x = both(a);
+    s2y = both(b);
     R::store(dx_out, row, p.ldx, n, t, tt);
     last_rf = now.rf;
     now = next;
@@ -560,7 +581,10 @@ __global__ void __launch_bounds__(kBwdThreads) residual_norm_backward_kernel(con
 #pragma unroll
     for (int q = 0; q < kSums; ++q)
 #pragma unroll
-      for (int k = 0; k < R::PER; ++k) sums[(team * kSums + q) * ALL + R::col(i, t) + k] = sum[q][i * R::PER + k];
+      for (int k = 0; k < R::PER; ++k) {
+        const float2 f = apart(sum[q][(i * R::PER + k) / 2]);
+        sums[(team * kSums + q) * ALL + R::col(i, t) + k] = (i * R::PER + k) & 1 ? f.y : f.x;
+      }
   __syncthreads();
   float* to = p.part + int64_t(group) * kSums * p.n + c0;
   for (int c = threadIdx.x; c < n; c += kBwdThreads) {

@@ -4,11 +4,12 @@
 //   weight of a chosen expert e = scale exp(l_e - m) / sum exp(l - m),  m the row's largest logit
 //   dl_e = p_e (g_e - sum over e of g p),  p the softmax, g_e = scale * dweight where e was chosen, else 0
 //
-// A warp holds a row in registers, consecutive logits per lane, as unsigned
-// keys in the order of the numbers.  Each choice is one maximum over the warp;
-// the lowest lane that has it has the lowest index too.  Rows of more than 1024
-// logits are read again from the cache for every choice instead: the next one is
-// the largest (key, lowest index) behind the last.
+// Keys are unsigned integers in the order of the numbers.  Up to 8 of up to 256
+// experts: see below.  Otherwise a warp holds a row in registers, consecutive logits
+// per lane; each choice is one maximum over the warp, and the lowest lane that has
+// it has the lowest index too.  Rows of more than 1024 logits are read again from
+// the cache for every choice instead: the next one is the largest (key, lowest
+// index) behind the last.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -32,7 +33,8 @@ struct RouterParams {
   const float* dweights;     // backward
   void* dlogits;
   int64_t rows, ld, ldd;
-  int32_t experts, k, over, vec;
+  int32_t experts, k, over;
+  int32_t vec, vec_d;        // rows of logits, of dlogits, on vector boundaries
   float scale;
 };
 
@@ -92,79 +94,83 @@ __device__ __forceinline__ void load_row(const void* base, int64_t at, int exper
   }
 }
 
+// One row by a warp.
+template <typename T, int VPL>
+__device__ __forceinline__ void forward_row(const RouterParams& p, int64_t row, int lane) {
+  const int64_t at = row * p.ld;
+  uint32_t key[VPL > 0 ? VPL : 1];
+  float total = 0.0f;
+  if constexpr (VPL > 0) {
+    float f[VPL];
+    load_row<T, VPL>(p.logits, at, p.experts, lane, p.vec, f);
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) key[i] = key_of(f[i]);
+  }
+  uint32_t mine = kClosed, first = kClosed, last = 0xFFFFFFFFu;
+  int last_at = -1, found = 0;
+  for (int j = 0; j < p.k; ++j) {
+    uint32_t best = kClosed;
+    int best_at = 0;
+    if constexpr (VPL > 0) {
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) best = max(best, key[i]);
+    } else {
+      for (int c = lane; c < p.experts; c += 32) {
+        const uint32_t v = key_of(logit_at<T>(p.logits, at + c));
+        if ((v < last || (v == last && c > last_at)) && v > best) best = v, best_at = c;
+      }
+    }
+    const uint32_t m = __reduce_max_sync(kAll, best);
+    if (m <= kClosed) break;                     // no open expert is left
+    if (j == 0) {
+      first = m;
+      if (p.over == GOLDY_ROUTER_ALL) {
+        const float top = value_of(m);
+        if constexpr (VPL > 0) {
+#pragma unroll
+          for (int i = 0; i < VPL; ++i) total += expf(value_of(key[i]) - top);
+        } else {
+          for (int c = lane; c < p.experts; c += 32) total += expf(logit_at<T>(p.logits, at + c) - top);
+        }
+        total = sum_of(total);
+      }
+    }
+    if constexpr (VPL > 0) {
+      const int winner = __ffs(int(__ballot_sync(kAll, best == m))) - 1;
+      if (lane == winner) {
+        bool open = true;
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) {
+          if (open && key[i] == m) {
+            open = false;
+            key[i] = kClosed;
+            p.ids[row * p.k + j] = lane * VPL + i;
+          }
+        }
+      }
+    } else {
+      last = m;
+      last_at = int(__reduce_min_sync(kAll, best == m ? unsigned(best_at) : 0xFFFFFFFFu));
+      if (lane == 0) p.ids[row * p.k + j] = last_at;
+    }
+    if (lane == j) mine = m;
+    ++found;
+  }
+  float e = lane < found ? expf(value_of(mine) - value_of(first)) : 0.0f;
+  if (p.over == GOLDY_ROUTER_CHOSEN) total = sum_of(e);
+  if (lane < p.k) {
+    p.weights[row * p.k + lane] = lane < found ? p.scale * (e / total) : 0.0f;
+    if (lane >= found) p.ids[row * p.k + lane] = -1;
+  }
+}
+
 template <typename T, int VPL>
 __global__ void __launch_bounds__(kWarps * 32) router_forward_kernel(const RouterParams p) {
   ptx::griddep_launch_dependents();
   ptx::griddep_wait();
-  const int lane = threadIdx.x & 31;
   const int64_t step = int64_t(gridDim.x) * kWarps;
-  for (int64_t row = int64_t(blockIdx.x) * kWarps + (threadIdx.x >> 5); row < p.rows; row += step) {
-    const int64_t at = row * p.ld;
-    uint32_t key[VPL > 0 ? VPL : 1];
-    float total = 0.0f;
-    if constexpr (VPL > 0) {
-      float f[VPL];
-      load_row<T, VPL>(p.logits, at, p.experts, lane, p.vec, f);
-#pragma unroll
-      for (int i = 0; i < VPL; ++i) key[i] = key_of(f[i]);
-    }
-    uint32_t mine = kClosed, first = kClosed, last = 0xFFFFFFFFu;
-    int last_at = -1, found = 0;
-    for (int j = 0; j < p.k; ++j) {
-      uint32_t best = kClosed;
-      int best_at = 0;
-      if constexpr (VPL > 0) {
-#pragma unroll
-        for (int i = 0; i < VPL; ++i) best = max(best, key[i]);
-      } else {
-        for (int c = lane; c < p.experts; c += 32) {
-          const uint32_t v = key_of(logit_at<T>(p.logits, at + c));
-          if ((v < last || (v == last && c > last_at)) && v > best) best = v, best_at = c;
-        }
-      }
-      const uint32_t m = __reduce_max_sync(kAll, best);
-      if (m <= kClosed) break;                     // no open expert is left
-      if (j == 0) {
-        first = m;
-        if (p.over == GOLDY_ROUTER_ALL) {
-          const float top = value_of(m);
-          if constexpr (VPL > 0) {
-#pragma unroll
-            for (int i = 0; i < VPL; ++i) total += expf(value_of(key[i]) - top);
-          } else {
-            for (int c = lane; c < p.experts; c += 32) total += expf(logit_at<T>(p.logits, at + c) - top);
-          }
-          total = sum_of(total);
-        }
-      }
-      if constexpr (VPL > 0) {
-        const int winner = __ffs(int(__ballot_sync(kAll, best == m))) - 1;
-        if (lane == winner) {
-          bool open = true;
-#pragma unroll
-          for (int i = 0; i < VPL; ++i) {
-            if (open && key[i] == m) {
-              open = false;
-              key[i] = kClosed;
-              p.ids[row * p.k + j] = lane * VPL + i;
-            }
-          }
-        }
-      } else {
-        last = m;
-        last_at = int(__reduce_min_sync(kAll, best == m ? unsigned(best_at) : 0xFFFFFFFFu));
-        if (lane == 0) p.ids[row * p.k + j] = last_at;
-      }
-      if (lane == j) mine = m;
-      ++found;
-    }
-    float e = lane < found ? expf(value_of(mine) - value_of(first)) : 0.0f;
-    if (p.over == GOLDY_ROUTER_CHOSEN) total = sum_of(e);
-    if (lane < p.k) {
-      p.weights[row * p.k + lane] = lane < found ? p.scale * (e / total) : 0.0f;
-      if (lane >= found) p.ids[row * p.k + lane] = -1;
-    }
-  }
+  for (int64_t row = int64_t(blockIdx.x) * kWarps + (threadIdx.x >> 5); row < p.rows; row += step)
+    forward_row<T, VPL>(p, row, threadIdx.x & 31);
 }
 
 template <typename T, int VPL>
@@ -237,6 +243,262 @@ __global__ void __launch_bounds__(kWarps * 32) router_backward_kernel(const Rout
   }
 }
 
+// ---- up to 8 of up to 256 experts: eight lanes per row ---------------------------
+// Four rows per warp share every instruction.  A lane sorts its keys eight at a time,
+// and lists are merged (the larger of A[i] and B[7 - i] are the eight largest of
+// both, in an order that three steps of compare and exchange sort): first those of
+// a lane, then those of the eight lanes, after which every lane knows the row's
+// eight largest keys.  bf16 logits leave room for the index in the key; of fp32
+// logits, a lane that holds one of them finds its slot by its key, and rows in which
+// two of these are equal go the way above.
+
+constexpr int kTeam = 8;
+constexpr int kTop = 8;
+
+__device__ __forceinline__ void order(uint32_t& a, uint32_t& b) {
+  const uint32_t hi = max(a, b);
+  b = min(a, b);
+  a = hi;
+}
+// falling order of eight keys that rise and fall once
+__device__ __forceinline__ void sort_bitonic(uint32_t (&k)[kTop]) {
+#pragma unroll
+  for (int d = 4; d > 0; d /= 2)
+#pragma unroll
+    for (int i = 0; i < kTop; ++i)
+      if ((i & d) == 0) order(k[i], k[i + d]);
+}
+// falling order of eight keys (Batcher's merge exchange, 19 comparisons)
+__device__ __forceinline__ void sort8(uint32_t (&k)[kTop]) {
+  order(k[0], k[1]), order(k[2], k[3]), order(k[4], k[5]), order(k[6], k[7]);
+  order(k[0], k[2]), order(k[1], k[3]), order(k[4], k[6]), order(k[5], k[7]);
+  order(k[1], k[2]), order(k[5], k[6]);
+  order(k[0], k[4]), order(k[1], k[5]), order(k[2], k[6]), order(k[3], k[7]);
+  order(k[2], k[4]), order(k[3], k[5]);
+  order(k[1], k[2]), order(k[3], k[4]), order(k[5], k[6]);
+}
+
+// A lane's logits are those of pieces lane, lane + 8, ... of PIECE each.
+template <typename T, int VPL>
+struct Share {
+  static constexpr int PIECE = 16 / int(sizeof(T)) < VPL ? 16 / int(sizeof(T)) : VPL;
+  static __device__ __forceinline__ int index(int i, int lane) { return (i / PIECE * kTeam + lane) * PIECE + i % PIECE; }
+  static __device__ __forceinline__ void load(const void* base, int64_t at, int experts, int lane, int vec, float (&f)[VPL]) {
+#pragma unroll
+    for (int i = 0; i < VPL; i += PIECE) {
+      const int c = index(i, lane);
+      if (vec && c + PIECE <= experts) {
+        const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const char*>(base) + (at + c) * int64_t(sizeof(T)));
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int j = 0; j < PIECE; ++j)
+          f[i + j] = sizeof(T) == 4 ? __uint_as_float(w[j % 4]) : j & 1 ? bf16_hi(w[j / 2 % 4]) : bf16_lo(w[j / 2 % 4]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < PIECE; ++j) f[i + j] = c + j < experts ? logit_at<T>(base, at + c + j) : -INFINITY;
+      }
+    }
+  }
+  static __device__ __forceinline__ void store(void* base, int64_t at, int experts, int lane, int vec, const float (&f)[VPL]) {
+#pragma unroll
+    for (int i = 0; i < VPL; i += PIECE) {
+      const int c = index(i, lane);
+      if (vec && c + PIECE <= experts) {
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          w[j] = sizeof(T) == 4 ? __float_as_uint(f[i + j]) : pack_bf16(f[(i + 2 * j) % VPL], f[(i + 2 * j + 1) % VPL]);
+        *reinterpret_cast<uint4*>(static_cast<char*>(base) + (at + c) * int64_t(sizeof(T))) = make_uint4(w[0], w[1], w[2], w[3]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < PIECE; ++j)
+          if (c + j < experts) put_logit<T>(base, at + c + j, f[i + j]);
+      }
+    }
+  }
+};
+
+// exp(x) for x <= 0 (NaN stays NaN)
+__device__ __forceinline__ float exp_below(float x) { return fast_exp2(x * kLog2E); }
+// sum over a team's lanes, to all of them
+__device__ __forceinline__ float team_sum(float v) {
+#pragma unroll
+  for (int d = kTeam / 2; d > 0; d /= 2) v += __shfl_xor_sync(kAll, v, d);
+  return v;
+}
+
+template <typename T, int VPL>
+__global__ void __launch_bounds__(kWarps * 32) router_forward_small_kernel(const RouterParams p) {
+  using S = Share<T, VPL>;
+  constexpr bool INDEXED = sizeof(T) == 2;         // the key's lower half holds the index
+  ptx::griddep_launch_dependents();
+  ptx::griddep_wait();
+  const int lane = threadIdx.x & (kTeam - 1);
+  const int64_t step = int64_t(gridDim.x) * (kWarps * 32 / kTeam);
+  const int64_t first_row = int64_t(blockIdx.x) * (kWarps * 32 / kTeam) + (threadIdx.x / 32) * (32 / kTeam);
+  for (int64_t row4 = first_row; row4 < p.rows; row4 += step) {    // the warp's four rows
+    const int64_t row = row4 + (threadIdx.x & 31) / kTeam;
+    const bool there = row < p.rows;
+    const int64_t at = (there ? row : row4) * p.ld;
+    float f[VPL];
+    uint32_t key[VPL], best[kTop];
+    S::load(p.logits, at, p.experts, lane, p.vec, f);
+#pragma unroll
+    for (int i = 0; i < VPL; ++i)
+      key[i] = INDEXED ? (key_of(f[i]) & 0xFFFF0000u) | uint32_t(0xFFFF - S::index(i, lane)) : key_of(f[i]);
+#pragma unroll
+    for (int i0 = 0; i0 < VPL; i0 += kTop) {
+      uint32_t k[kTop];
+#pragma unroll
+      for (int i = 0; i < kTop; ++i) k[i] = key[i0 + i];
+      sort8(k);
+      if (i0 == 0) {
+#pragma unroll
+        for (int i = 0; i < kTop; ++i) best[i] = k[i];
+      } else {
+#pragma unroll
+        for (int i = 0; i < kTop; ++i) best[i] = max(best[i], k[kTop - 1 - i]);
+        sort_bitonic(best);
+      }
+    }
+#pragma unroll
+    for (int d = 1; d < kTeam; d *= 2) {
+      uint32_t k[kTop];
+#pragma unroll
+      for (int i = 0; i < kTop; ++i) k[i] = __shfl_xor_sync(kAll, best[kTop - 1 - i], d);
+#pragma unroll
+      for (int i = 0; i < kTop; ++i) best[i] = max(best[i], k[i]);
+      sort_bitonic(best);
+    }
+    // open ones among the first k
+    int found = 0;
+    uint32_t least = 0xFFFFFFFFu;                  // the smallest chosen key
+#pragma unroll
+    for (int j = 0; j < kTop; ++j) {
+      const bool open = j < p.k && (INDEXED ? best[j] >> 16 > kClosed >> 16 : best[j] > kClosed);
+      found += open;
+      least = open ? best[j] : least;
+    }
+    auto value = [](uint32_t k) {
+      return INDEXED ? __uint_as_float(__float_as_uint(value_of(k)) & 0xFFFF0000u) : value_of(k);
+    };
+    const float top = found ? value(best[0]) : 0.0f;
+    float total = 0.0f;
+    if (p.over == GOLDY_ROUTER_ALL) {
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) total += exp_below(f[i] - top);
+      total = team_sum(total);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kTop; ++j) total += j < found ? exp_below(value(best[j]) - top) : 0.0f;
+    }
+    const float share = p.scale / total;
+    int32_t* ids = p.ids + row * p.k;
+    float* weights = p.weights + row * p.k;
+    if constexpr (INDEXED) {
+      uint32_t k = best[0];
+#pragma unroll
+      for (int j = 1; j < kTop; ++j) k = lane == j ? best[j] : k;
+      if (there && lane < p.k) {
+        ids[lane] = lane < found ? int(0xFFFF - (k & 0xFFFFu)) : -1;
+        weights[lane] = lane < found ? exp_below(value(k) - top) * share : 0.0f;
+      }
+    } else {
+      uint32_t mine = 0;                           // this lane's chosen logits
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) mine |= uint32_t(found > 0 && key[i] >= least) << i;
+      int chosen = __popc(mine);
+#pragma unroll
+      for (int d = 1; d < kTeam; d *= 2) chosen += __shfl_xor_sync(kAll, chosen, d);
+      bool twice = chosen != found;
+#pragma unroll
+      for (int j = 0; j + 1 < kTop; ++j) twice |= j + 1 < found && best[j] == best[j + 1];
+      if (__any_sync(kAll, there && twice)) {
+        for (int r = 0; r < 32 / kTeam && row4 + r < p.rows; ++r) forward_row<T, 0>(p, row4 + r, threadIdx.x & 31);
+        continue;
+      }
+      if (!there) mine = 0;
+      while (mine) {
+        const int c = S::index(__ffs(int(mine)) - 1, lane);
+        mine &= mine - 1;
+        const float v = logit_at<T>(p.logits, at + c);
+        const uint32_t k = key_of(v);
+        int slot = 0;
+#pragma unroll
+        for (int j = 0; j < kTop; ++j) slot += best[j] > k;
+        ids[slot] = c;
+        weights[slot] = exp_below(v - top) * share;
+      }
+      if (there && lane >= found && lane < p.k) {
+        ids[lane] = -1;
+        weights[lane] = 0.0f;
+      }
+    }
+  }
+}
+
+template <typename T, int VPL>
+__global__ void __launch_bounds__(kWarps * 32) router_backward_small_kernel(const RouterParams p) {
+  using S = Share<T, VPL>;
+  ptx::griddep_launch_dependents();
+  ptx::griddep_wait();
+  const int lane = threadIdx.x & (kTeam - 1);
+  const int64_t step = int64_t(gridDim.x) * (kWarps * 32 / kTeam);
+  const int64_t first_row = int64_t(blockIdx.x) * (kWarps * 32 / kTeam) + (threadIdx.x / 32) * (32 / kTeam);
+  const bool all = p.over == GOLDY_ROUTER_ALL;
+  for (int64_t row4 = first_row; row4 < p.rows; row4 += step) {
+    const int64_t row = row4 + (threadIdx.x & 31) / kTeam;
+    const bool there = row < p.rows;
+    const int64_t at = (there ? row : row4) * p.ld;
+    // this lane's slot
+    int id = there && lane < p.k ? p.ids[row * p.k + lane] : -1;
+    if (id < 0 || id >= p.experts) id = -1;
+    float f[VPL];
+    if (all) S::load(p.logits, at, p.experts, lane, p.vec, f);
+    const float dw = id >= 0 ? p.scale * p.dweights[row * p.k + lane] : 0.0f;
+    const float l = id >= 0 ? logit_at<T>(p.logits, at + id) : -INFINITY;
+    // an expert that is named again: the lowest slot takes all its gradients
+    float g = 0.0f, top = -INFINITY;
+    bool owner = id >= 0;
+#pragma unroll
+    for (int j = 0; j < kTop; ++j) {
+      const bool same = __shfl_sync(kAll, id, j, kTeam) == id;
+      const float gj = __shfl_sync(kAll, dw, j, kTeam);
+      if (same) g += gj;
+      owner &= !(same && j < lane);
+    }
+    if (all) {
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) top = fmaxf(top, f[i]);
+    } else {
+      top = l;
+    }
+#pragma unroll
+    for (int d = 1; d < kTeam; d *= 2) top = fmaxf(top, __shfl_xor_sync(kAll, top, d));
+    const bool none = top == -INFINITY;            // (a NaN among the logits makes the sum NaN)
+    if (none) top = 0.0f;
+    const float e = owner ? exp_below(l - top) : 0.0f;
+    float total = e;
+    if (all) {
+      total = 0.0f;
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) {
+        f[i] = exp_below(f[i] - top);
+        total += f[i];
+      }
+    }
+    total = team_sum(total);
+    const float inv = none && total == 0.0f ? 0.0f : 1.0f / total, prob = e * inv;
+    const float dot = team_sum(owner ? g * prob : 0.0f), back = -dot * inv;
+    const int64_t to = row * p.ldd;
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) f[i] = all ? f[i] * back : 0.0f;
+    if (there) S::store(p.dlogits, to, p.experts, lane, p.vec_d, f);
+    __syncwarp();                                  // behind the others' values
+    if (owner) put_logit<T>(p.dlogits, to + id, prob * (g - dot));
+  }
+}
+
 template <typename T, int VPL>
 const void* pick(bool backward) {
   return backward ? reinterpret_cast<const void*>(&router_backward_kernel<T, VPL>)
@@ -255,15 +517,27 @@ const void* pick_width(int per_lane, bool backward) {
   }
 }
 
+template <typename T, int VPL>
+const void* pick_small(bool backward) {
+  return backward ? reinterpret_cast<const void*>(&router_backward_small_kernel<T, VPL>)
+                  : reinterpret_cast<const void*>(&router_forward_small_kernel<T, VPL>);
+}
+template <typename T>
+const void* pick_small_width(int experts, bool backward) {
+  if (experts <= 8 * kTeam) return pick_small<T, 8>(backward);
+  return experts <= 16 * kTeam ? pick_small<T, 16>(backward) : pick_small<T, 32>(backward);
+}
+
 struct RouterCall {
   RouterParams p;
   const void* fn;
+  int64_t per_cta;           // rows
   void* stream;
 };
 
 goldy_status launch_router(const LayerContext& ctx, void* arg) {
   RouterCall& call = *static_cast<RouterCall*>(arg);
-  const int64_t grid = std::min(ceil_div(call.p.rows, int64_t(kWarps)), int64_t(ctx.sm_count) * 8);
+  const int64_t grid = std::min(ceil_div(call.p.rows, call.per_cta), int64_t(ctx.sm_count) * 8);
   void* args[] = {&call.p};
   return launch_layer("router", call.fn, grid, kWarps * 32, 0, call.stream, args);
 }
@@ -284,10 +558,13 @@ goldy_status check_router(const goldy_router_desc* d) {
 }
 
 goldy_status run_router(const goldy_router_desc& d, RouterCall& call, const void* logits, bool backward, void* stream) {
+  const bool f32 = d.dtype == GOLDY_F32, small = d.k <= kTop && d.experts <= 32 * kTeam;
   int per_lane = 1;
   while (per_lane < 64 && per_lane * 32 < d.experts) per_lane *= 2;
-  call.fn = d.dtype == GOLDY_F32 ? pick_width<float>(per_lane, backward) : pick_width<uint16_t>(per_lane, backward);
-  const int64_t access = std::min<int64_t>(16, per_lane * int64_t(element_size(d.dtype)));
+  const int64_t es = int64_t(element_size(d.dtype)), access = small ? 16 : std::min<int64_t>(16, per_lane * es);
+  if (small) call.fn = f32 ? pick_small_width<float>(d.experts, backward) : pick_small_width<uint16_t>(d.experts, backward);
+  else call.fn = f32 ? pick_width<float>(per_lane, backward) : pick_width<uint16_t>(per_lane, backward);
+  call.per_cta = small ? kWarps * 32 / kTeam : kWarps;
   call.p.logits = logits;
   call.p.rows = d.rows;
   call.p.ld = d.ld;
@@ -296,7 +573,8 @@ goldy_status run_router(const goldy_router_desc& d, RouterCall& call, const void
   call.p.k = d.k;
   call.p.over = d.over;
   call.p.scale = d.scale;
-  call.p.vec = on_boundary(logits, size_t(access)) && d.ld * int64_t(element_size(d.dtype)) % access == 0;
+  call.p.vec = on_boundary(logits, size_t(access)) && d.ld * es % access == 0;
+  call.p.vec_d = on_boundary(call.p.dlogits, 16) && d.ldd * es % 16 == 0;
   call.stream = stream;
   const goldy_status st = with_layer_context(stream, launch_router, &call);
   return st == GOLDY_OK ? ok() : st;
