@@ -133,7 +133,9 @@ struct NormRow {
   }
 
   static __device__ __forceinline__ void fetch(uint8_t* ring, const void* base, int64_t row, int64_t ld, int n, int t) {
-    const T* at = static_cast<const T*>(base) + row * ld;
+    fetch(ring, static_cast<const T*>(base) + row * ld, n, t);
+  }
+  static __device__ __forceinline__ void fetch(uint8_t* ring, const T* at, int n, int t) {
     const int off = SHIFT ? shift(at) : 0;
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s)
@@ -160,8 +162,11 @@ struct NormRow {
   // the row's values, 0 outside it (SHIFT: behind the team's barrier)
   static __device__ __forceinline__ void values(const uint8_t* ring, const void* base, int64_t row, int64_t ld, int n,
                                                 int t, float (&f)[VALS]) {
+    values(ring, static_cast<const T*>(base) + row * ld, n, t, f);
+  }
+  static __device__ __forceinline__ void values(const uint8_t* ring, const T* at, int n, int t, float (&f)[VALS]) {
     if constexpr (SHIFT) {
-      switch (shift(static_cast<const T*>(base) + row * ld)) {
+      switch (shift(at)) {
         case 0: pick<0>(ring, n, t, f); break;
         case 1: pick<1>(ring, n, t, f); break;
         case 2: pick<2>(ring, n, t, f); break;
@@ -226,7 +231,9 @@ struct NormRow {
   }
   // the row's results (all lanes of a warp)
   static __device__ __forceinline__ void store(void* base, int64_t row, int64_t ld, int n, int t, const float (&f)[VALS]) {
-    T* at = static_cast<T*>(base) + row * ld;
+    store(static_cast<T*>(base) + row * ld, n, t, f);
+  }
+  static __device__ __forceinline__ void store(T* at, int n, int t, const float (&f)[VALS]) {
     if constexpr (SHIFT) {
       switch (shift(at)) {
         case 0: put<0>(at, n, t, f); break;

@@ -363,7 +363,8 @@ residual_norm_forward_kernel(const ResidualNormParams p) {
   }
 }
 
-template <typename T, int TEAM, bool VEC, bool WIDE>
+// FULL: both norms and dS are there.
+template <typename T, int TEAM, bool VEC, bool WIDE, bool FULL>
 __global__ void __launch_bounds__(kBwdThreads) residual_norm_backward_kernel(const ResidualNormParams p) {
   constexpr int TEAMS = kBwdThreads / TEAM, WARPS = TEAM / 32, VALS = kBwdVals, D = bwd_depth<T>();
   using R = NormRow<T, VALS, TEAM, kBwdThreads, VEC, WIDE>;
@@ -381,41 +382,51 @@ __global__ void __launch_bounds__(kBwdThreads) residual_norm_backward_kernel(con
   const T* const ds_in = static_cast<const T*>(p.ds) + c0;
   T* const dx_out = static_cast<T*>(p.s) + c0;
   T* const df_out = static_cast<T*>(p.y) + c0;
-  const bool has_y = p.norm_y != GOLDY_NORM_NONE, has_f = p.norm_f != GOLDY_NORM_NONE, has_ds = p.ds != nullptr;
+  const bool has_y = FULL || p.norm_y != GOLDY_NORM_NONE, has_f = FULL || p.norm_f != GOLDY_NORM_NONE;
+  const bool has_ds = FULL || p.ds != nullptr;
   const float layer_f = p.norm_f == GOLDY_NORM_LAYER ? p.inv_n : 0.0f, layer_y = p.norm_y == GOLDY_NORM_LAYER ? p.inv_n : 0.0f;
   if (WIDE) ptx::cluster_sync_all();               // the others have started
   ptx::griddep_launch_dependents();
   ptx::griddep_wait();
-  const int64_t step = int64_t(groups) * TEAMS;
-  int64_t row = int64_t(group) * TEAMS + team;
-  auto fetch = [&](int d, int64_t r) {
-    if (r < p.rows) {
+  const int64_t step = int64_t(groups) * TEAMS, row0 = int64_t(group) * TEAMS + team;
+  int left = row0 < p.rows ? int((p.rows - row0 - 1) / step) + 1 : 0;    // rows of this team (memory holds fewer than 2^31)
+  // pointers run along: of the row fetched next, of the row whose dX and dF are next
+  const T* f_at = f_in + row0 * p.ldf;
+  const T* s_at = s_in + row0 * p.lds;
+  const T* dy_at = dy_in + row0 * p.ldy;
+  const T* ds_at = ds_in + row0 * p.lds;
+  T* dx_at = dx_out + row0 * p.ldx;
+  T* df_at = df_out + row0 * p.ldf;
+  const int64_t step_f = step * p.ldf, step_s = step * p.lds, step_y = step * p.ldy, step_x = step * p.ldx;
+  auto fetch = [&](int d, bool there) {
+    if (there) {
       uint8_t* to = ring + 4 * d * R::RING_BYTES;
-      R::fetch(to, f_in, r, p.ldf, n, t);
+      R::fetch(to, f_at, n, t);
       if (has_y) {
-        R::fetch(to + R::RING_BYTES, s_in, r, p.lds, n, t);
-        R::fetch(to + 2 * R::RING_BYTES, dy_in, r, p.ldy, n, t);
+        R::fetch(to + R::RING_BYTES, s_at, n, t);
+        R::fetch(to + 2 * R::RING_BYTES, dy_at, n, t);
       }
-      if (has_ds) R::fetch(to + 3 * R::RING_BYTES, ds_in, r, p.lds, n, t);
+      if (has_ds) R::fetch(to + 3 * R::RING_BYTES, ds_at, n, t);
     }
+    f_at += step_f;
+    s_at += step_s;
+    dy_at += step_y;
+    ds_at += step_s;
     copy_commit();
   };
-  struct Stats {
-    float mf, rf, my, ry;
+  // a row's statistics, one per lane: mean and rstd of N_f, of N_y
+  const int which = lane & 3;
+  const bool mine = which == 0 ? p.norm_f == GOLDY_NORM_LAYER : which == 1 ? has_f : which == 2 ? p.norm_y == GOLDY_NORM_LAYER : has_y;
+  const float* stats_at = p.stats + which * p.rows + row0;
+  auto next_stats = [&](bool there) {
+    const float v = mine && there ? *stats_at : float(which & 1);
+    stats_at += step;
+    return v;
   };
-  auto stats_of = [&](int64_t r) {
-    Stats s = {0.0f, 1.0f, 0.0f, 1.0f};
-    if (r < p.rows) {
-      if (p.norm_f == GOLDY_NORM_LAYER) s.mf = p.stats[r];
-      if (has_f) s.rf = p.stats[p.rows + r];
-      if (p.norm_y == GOLDY_NORM_LAYER) s.my = p.stats[2 * p.rows + r];
-      if (has_y) s.ry = p.stats[3 * p.rows + r];
-    }
-    return s;
-  };
+  auto stat = [&](float v, int q) { return __shfl_sync(0xFFFFFFFFu, v, q); };
 #pragma unroll
-  for (int d = 0; d < D - 1; ++d) fetch(d, row + d * step);
-  Stats now = stats_of(row), next = stats_of(row + step);
+  for (int d = 0; d < D - 1; ++d) fetch(d, left > d);
+  float now = next_stats(left > 0), next = next_stats(left > 1);
   // values in pairs: half the instructions
   constexpr int PAIRS = VALS / 2;
   uint64_t gf[PAIRS], gy[PAIRS], sum[kSums][PAIRS];      // gate * gamma_f, gamma_y; 0 outside the row
@@ -452,15 +463,18 @@ __global__ void __launch_bounds__(kBwdThreads) residual_norm_backward_kernel(con
     const float2 f = apart(v);
     return f.x + f.y;
   };
-  auto first = [&](const uint8_t* from, int64_t r, const Stats& st) {
+  float ry = 1.0f;                                 // rstd of N_y of the row that first() has seen
+  int64_t row = row0;                              // (SHIFT: whose rows start anywhere)
+  auto first = [&](const uint8_t* from, bool there, int64_t r, float st) {
     s1x = s1y = 0.0f;
-    if (!has_y || r >= p.rows) return;
+    if (!has_y || !there) return;
     float v[VALS], d[VALS];
-    R::values(from + R::RING_BYTES, s_in, r, p.lds, n, t, v);
-    R::values(from + 2 * R::RING_BYTES, dy_in, r, p.ldy, n, t, d);
+    R::values(from + R::RING_BYTES, R::SHIFT ? s_in + r * p.lds : nullptr, n, t, v);
+    R::values(from + 2 * R::RING_BYTES, R::SHIFT ? dy_in + r * p.ldy : nullptr, n, t, d);
+    ry = stat(st, 3);
     // the mean is subtracted before the scale: rows far from zero keep their
     // digits; columns outside the row have dY = gamma = 0 and add nothing
-    const uint64_t off = two(-st.my), scale = two(st.ry);
+    const uint64_t off = two(-stat(st, 2)), scale = two(ry);
     uint64_t a = two(0.0f), b = a;
 #pragma unroll
     for (int j = 0; j < PAIRS; ++j) {
@@ -505,7 +519,7 @@ __global__ void __launch_bounds__(kBwdThreads) residual_norm_backward_kernel(con
     s1x = r.x, s1y = r.y, s2x = r.z, s2y = r.w;
   };
   float last_rf = 0.0f;                            // of the row whose dF is left
-  auto finish = [&](int64_t r) {
+  auto finish = [&]() {
     const uint64_t less = two(-s2x * layer_f * last_rf), slope = two(-s2y * p.inv_n * last_rf), scale = two(last_rf);
     float v[VALS];
 #pragma unroll
@@ -514,41 +528,44 @@ __global__ void __launch_bounds__(kBwdThreads) residual_norm_backward_kernel(con
       v[2 * j] = f.x;
       v[2 * j + 1] = f.y;
     }
-    R::store(df_out, r, p.ldf, n, t, v);
+    R::store(df_at, n, t, v);
+    df_at += step_f;
   };
-  const int64_t row0 = row;
   int at = 0, ahead = D - 1;
-  if (row < p.rows) {                              // whole teams, and whole clusters
+  bool begun = false;
+  if (left > 0) {                                  // whole teams, and whole clusters
     copy_wait<D - 2>();
     if (R::SHIFT) team_sync<TEAM, kBwdThreads>(team);
-    first(ring, row, now);
+    first(ring, true, row, now);
     exchange(1);
   }
-  for (int flip = 0; row < p.rows; row += step, flip ^= 1) {
-    fetch(ahead, row + (D - 1) * step);            // where the row before this one was
-    const Stats later = stats_of(row + 2 * step);
+  for (int flip = 0; left > 0; --left, row += step, flip ^= 1) {
+    fetch(ahead, left > D - 1);                    // where the row before this one was
+    const float later = next_stats(left > 2);
     copy_wait<D - 2>();
     if (R::SHIFT) team_sync<TEAM, kBwdThreads>(team);
-    if (row != row0) finish(row - step);
+    if (begun) finish();
+    begun = true;
     // T, dX, and what dF needs
     const uint8_t* from = ring + 4 * at * R::RING_BYTES;
     at = at + 1 == D ? 0 : at + 1;
     ahead = ahead + 1 == D ? 0 : ahead + 1;
     float tt[VALS], v[VALS];
     if (has_ds) {
-      R::values(from + 3 * R::RING_BYTES, ds_in, row, p.lds, n, t, tt);
+      R::values(from + 3 * R::RING_BYTES, R::SHIFT ? ds_in + row * p.lds : nullptr, n, t, tt);
     } else {
 #pragma unroll
       for (int j = 0; j < VALS; ++j) tt[j] = 0.0f;
     }
-    R::values(from, f_in, row, p.ldf, n, t, v);
-    const uint64_t less = two(-s1x * layer_y * now.ry), slope = two(-s1y * p.inv_n * now.ry), ry = two(now.ry);
-    const uint64_t off = two(-now.mf), scale = two(now.rf), alpha = two(p.alpha);
+    R::values(from, R::SHIFT ? f_in + row * p.ldf : nullptr, n, t, v);
+    last_rf = stat(now, 1);
+    const uint64_t less = two(-s1x * layer_y * ry), slope = two(-s1y * p.inv_n * ry), by = two(ry);
+    const uint64_t off = two(-stat(now, 0)), scale = two(last_rf), alpha = two(p.alpha);
     uint64_t a = two(0.0f), b = a;
 #pragma unroll
     for (int j = 0; j < PAIRS; ++j) {
       uint64_t d = two(tt[2 * j], tt[2 * j + 1]);
-      if (has_y) d = add2(d, fma2(hy[j], slope, fma2(g[j], ry, less)));
+      if (has_y) d = add2(d, fma2(hy[j], slope, fma2(g[j], by, less)));
       h[j] = mul2(add2(two(v[2 * j], v[2 * j + 1]), off), scale);
       sum[0][j] = fma2(d, h[j], sum[0][j]);
       sum[1][j] = add2(sum[1][j], d);
@@ -561,14 +578,14 @@ __global__ void __launch_bounds__(kBwdThreads) residual_norm_backward_kernel(con
     }
     s2x = both(a);
     s2y = both(b);
-    R::store(dx_out, row, p.ldx, n, t, tt);
-    last_rf = now.rf;
+    R::store(dx_at, n, t, tt);
+    dx_at += step_x;
     now = next;
     next = later;
-    first(ring + 4 * at * R::RING_BYTES, row + step, now);
+    first(ring + 4 * at * R::RING_BYTES, left > 1, row + step, now);
     exchange(flip);
   }
-  if (row != row0) finish(row - step);
+  if (begun) finish();
   if (!p.part) return;
   // the teams' sums go through shared memory, in column order, to be added in
   // team order
@@ -673,10 +690,11 @@ size_t backward_bytes(const goldy_residual_norm_desc& d) {
 }
 
 template <typename T, int TEAM, bool VEC, bool WIDE = false>
-NormKernel pick(bool backward) {
+NormKernel pick(bool backward, bool full) {
   if (backward) {
     using R = NormRow<T, kBwdVals, TEAM, kBwdThreads, VEC, WIDE>;
-    return {reinterpret_cast<const void*>(&residual_norm_backward_kernel<T, TEAM, VEC, WIDE>), kBwdThreads,
+    return {full ? reinterpret_cast<const void*>(&residual_norm_backward_kernel<T, TEAM, VEC, WIDE, VEC>)
+                 : reinterpret_cast<const void*>(&residual_norm_backward_kernel<T, TEAM, VEC, WIDE, false>), kBwdThreads,
             kBwdThreads / TEAM, 1,
             std::max(size_t(4) * bwd_depth<T>() * R::RING_BYTES, size_t(kSums) * kBwdThreads * kBwdVals * sizeof(float))};
   }
@@ -686,14 +704,14 @@ NormKernel pick(bool backward) {
           TEAM > kFwdThreads ? 1 : 2, size_t(2) * kFwdDepth * R::RING_BYTES};
 }
 template <typename T, bool VEC>
-NormKernel pick_shape(const NormShape& s, bool backward) {
-  if (s.cluster > 1) return pick<T, kMaxTeam, VEC, true>(backward);
+NormKernel pick_shape(const NormShape& s, bool backward, bool full) {
+  if (s.cluster > 1) return pick<T, kMaxTeam, VEC, true>(backward, full);
   switch (s.team) {
-    case 32: return pick<T, 32, VEC>(backward);
-    case 64: return pick<T, 64, VEC>(backward);
-    case 128: return pick<T, 128, VEC>(backward);
-    case 256: return pick<T, 256, VEC>(backward);
-    case 512: return pick<T, 512, VEC>(backward);
+    case 32: return pick<T, 32, VEC>(backward, full);
+    case 64: return pick<T, 64, VEC>(backward, full);
+    case 128: return pick<T, 128, VEC>(backward, full);
+    case 256: return pick<T, 256, VEC>(backward, full);
+    case 512: return pick<T, 512, VEC>(backward, full);
     default:
       return {backward ? reinterpret_cast<const void*>(&residual_norm_backward_stream_kernel<T>)
                        : reinterpret_cast<const void*>(&residual_norm_forward_stream_kernel<T>),
@@ -746,8 +764,12 @@ goldy_status launch_residual_norm(const LayerContext& ctx, void* arg) {
   if (!ctx.whole && shape.cluster > 1) shape = {0, 1, 0};
   const int cluster = shape.cluster;
   NormKernel k;
-  if (d.dtype == GOLDY_F32) k = call.vec ? pick_shape<float, true>(shape, call.backward) : pick_shape<float, false>(shape, call.backward);
-  else k = call.vec ? pick_shape<uint16_t, true>(shape, call.backward) : pick_shape<uint16_t, false>(shape, call.backward);
+  const bool full = call.vec && d.norm_f != GOLDY_NORM_NONE && d.norm_y != GOLDY_NORM_NONE && call.p.ds;
+  if (d.dtype == GOLDY_F32)
+    k = call.vec ? pick_shape<float, true>(shape, call.backward, full) : pick_shape<float, false>(shape, call.backward, full);
+  else
+    k = call.vec ? pick_shape<uint16_t, true>(shape, call.backward, full)
+                 : pick_shape<uint16_t, false>(shape, call.backward, full);
   cudaError_t e = allow_smem(ctx.device, k);
   if (e != cudaSuccess) return fail(GOLDY_ERR_CUDA, std::string("cudaFuncSetAttribute: ") + cudaGetErrorString(e));
   int64_t cap = int64_t(ctx.sm_count) * k.per_sm;              // CTAs, or clusters, resident at once
