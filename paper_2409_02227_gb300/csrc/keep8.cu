@@ -24,6 +24,7 @@ constexpr int kThreads = 256;
 constexpr int kBlock = GOLDY_KEEP8_BLOCK;
 constexpr int kPer = 8;                          // elements per thread
 constexpr int kShare = kBlock / kPer;            // threads per block
+constexpr int kUnroll = 4;                       // pieces of 8 per thread and step, packing; half as many back
 constexpr uint32_t kInfinity = 0x7F800000u;
 
 struct KeepParams {
@@ -33,8 +34,9 @@ struct KeepParams {
   void* z;
   void* h;
   int64_t rows, ldz, ldh;
-  int32_t n, blocks, vec;
+  int32_t n, blocks;
   int32_t lanes_log;     // threads per row, log2
+  int64_t pieces;        // of 8 elements, where rows follow one another without a gap
 };
 
 // 2^i for -127 <= i <= 127
@@ -53,38 +55,37 @@ __device__ __forceinline__ float2 from_e4m3x2(uint32_t v) {
   return f;
 }
 
-// 8 elements from column c on, 0 behind the row's end
-template <typename T>
-__device__ __forceinline__ void load8(const T* row, int c, int n, int vec, float (&f)[kPer]) {
-  using B = Block<T>;
+// Four lanes' 8 elements each as a block: this lane's bytes, and e.
+__device__ __forceinline__ uint2 quantise(float (&f)[kPer], int& e) {
+  uint32_t top = 0;
 #pragma unroll
-  for (int i = 0; i < kPer; i += B::PER) {
-    float g[B::PER];
-    B::unpack(vec && c + i + B::PER <= n ? B::template load<true>(row, c + i, n) : B::template load<false>(row, c + i, n), g);
+  for (int i = 0; i < kPer; ++i) top = max(top, __float_as_uint(f[i]) & 0x7FFFFFFFu);
+  if (top >= kInfinity) {                          // an infinity or NaN among them
+    top = 0;
 #pragma unroll
-    for (int j = 0; j < B::PER; ++j) f[i + j] = g[j];
-  }
-}
-template <typename T>
-__device__ __forceinline__ void store8(T* row, int c, int n, int vec, const float (&f)[kPer]) {
-  using B = Block<T>;
-#pragma unroll
-  for (int i = 0; i < kPer; i += B::PER) {
-    if (vec && c + i + B::PER <= n) {
-      float g[B::PER];
-#pragma unroll
-      for (int j = 0; j < B::PER; ++j) g[j] = f[i + j];
-      B::template store<true>(row, c + i, n, B::pack(g));
-    } else {
-#pragma unroll
-      for (int j = 0; j < B::PER; ++j)
-        if (c + i + j < n) B::put(row, c + i + j, f[i + j]);
+    for (int i = 0; i < kPer; ++i) {
+      const uint32_t b = __float_as_uint(f[i]) & 0x7FFFFFFFu;
+      if (b < kInfinity) top = max(top, b);
+      else f[i] = __uint_as_float(0x7FFFFFFFu);
     }
   }
+  top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+  top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+  e = max(-127, int(top >> 23) - 127 - 8 + ((top & 0x7FFFFFu) > 0x600000u));
+  const uint64_t scale = two(power(-e));
+  uint32_t w[kPer / 2];
+#pragma unroll
+  for (int i = 0; i < kPer / 2; ++i) {
+    const float2 v = apart(mul2(two(f[2 * i], f[2 * i + 1]), scale));
+    w[i] = to_e4m3x2(v.x, v.y);
+  }
+  return make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
 }
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads) keep8_pack_kernel(const KeepParams p) {
+  using B = Block<T>;
+  constexpr int LOADS = kPer / B::PER, UNROLL = 2;
   ptx::griddep_launch_dependents();
   ptx::griddep_wait();
   const int lanes = 1 << p.lanes_log, x = threadIdx.x & (lanes - 1);
@@ -94,91 +95,251 @@ __global__ void __launch_bounds__(kThreads) keep8_pack_kernel(const KeepParams p
   const int64_t rounds = (p.rows + per_cta - 1) / per_cta;
   for (int64_t r = blockIdx.x; r < rounds; r += gridDim.x) {
     const int64_t row = r * per_cta + (threadIdx.x >> p.lanes_log);
-    for (int trip = 0; trip < trips; ++trip) {      // every thread of a warp goes along: they trade maxima
-      const int at = trip * lanes + x;
-      const bool in = row < p.rows && at < per_row;
+    const typename B::Source source(static_cast<const T*>(p.z_in) + min(row, p.rows - 1) * p.ldz, p.n, 0);
+    for (int trip = 0; trip < trips; trip += UNROLL) {   // every thread of a warp goes along: they trade maxima
+      typename B::template Raw<false> raw[UNROLL][LOADS];
+#pragma unroll
+      for (int k = 0; k < UNROLL; ++k) {
+        const int c = ((trip + k) * lanes + x) * kPer;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+          if (c + i * B::PER < p.n) raw[k][i].load(source, c / B::PER + i);
+      }
+#pragma unroll
+      for (int k = 0; k < UNROLL; ++k) {
+        const int at = (trip + k) * lanes + x, c = at * kPer;
+        float f[kPer];
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+          float g[B::PER];
+          uint4 v = make_uint4(0, 0, 0, 0);
+          if (c + i * B::PER < p.n) {
+            v = raw[k][i].get(source.shift);
+            if (c + (i + 1) * B::PER > p.n) {
+              const uint4 m = B::inside(c + i * B::PER, p.n);
+              v.x &= m.x, v.y &= m.y, v.z &= m.z, v.w &= m.w;
+            }
+          }
+          B::unpack(v, g);
+#pragma unroll
+          for (int j = 0; j < B::PER; ++j) f[i * B::PER + j] = g[j];
+        }
+        int e;
+        const uint2 bytes = quantise(f, e);
+        if (row >= p.rows || at >= per_row) continue;
+        p.q[row * per_row + at] = bytes;
+        if ((at & (kShare - 1)) == 0) p.scales[row * p.blocks + at / kShare] = uint8_t(e + 127);
+      }
+    }
+  }
+}
+
+// Rows without gaps and of whole blocks are one long row: several pieces per
+// thread are on their way at once, and no index is more than a sum.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) keep8_pack_flat_kernel(const KeepParams p) {
+  using B = Block<T>;
+  constexpr int LOADS = kPer / B::PER;
+  ptx::griddep_launch_dependents();
+  ptx::griddep_wait();
+  const uint4* z = static_cast<const uint4*>(p.z_in);
+  const int64_t step = int64_t(gridDim.x) * kThreads * kUnroll;
+  for (int64_t u0 = int64_t(blockIdx.x) * kThreads * kUnroll + threadIdx.x; (u0 & ~int64_t(31)) < p.pieces; u0 += step) {
+    uint4 v[kUnroll][LOADS];
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) {
+      const int64_t u = u0 + k * kThreads;
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) v[k][i] = u < p.pieces ? __ldcs(z + u * LOADS + i) : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) {
+      const int64_t u = u0 + k * kThreads;
       float f[kPer];
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) f[i] = 0.0f;
-      if (in) load8<T>(static_cast<const T*>(p.z_in) + row * p.ldz, at * kPer, p.n, p.vec, f);
-      uint32_t top = 0;
+      for (int i = 0; i < LOADS; ++i) {
+        float g[B::PER];
+        B::unpack(v[k][i], g);
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) top = max(top, __float_as_uint(f[i]) & 0x7FFFFFFFu);
-      const bool odd = top >= kInfinity;            // an infinity or NaN among them
-      if (odd) {
-        top = 0;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-          const uint32_t b = __float_as_uint(f[i]) & 0x7FFFFFFFu;
-          if (b < kInfinity) top = max(top, b);
-          else f[i] = __uint_as_float(0x7FFFFFFFu);
-        }
+        for (int j = 0; j < B::PER; ++j) f[i * B::PER + j] = g[j];
       }
-      top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-      top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-      const int e = max(-127, int(top >> 23) - 127 - 8 + ((top & 0x7FFFFFu) > 0x600000u));
-      const float scale = power(-e);
-      uint32_t w[kPer / 2];
+      int e;
+      const uint2 q = quantise(f, e);
+      if (u >= p.pieces) continue;
+      p.q[u] = q;
+      if ((u & (kShare - 1)) == 0) p.scales[u / kShare] = uint8_t(e + 127);
+    }
+  }
+}
+
+__device__ __forceinline__ void restore(const uint2& v, int e, uint64_t (&f)[kPer / 2]) {
+  const uint64_t scale = two(power(e - 127));
+  const uint32_t w[4] = {v.x, v.x >> 16, v.y, v.y >> 16};
 #pragma unroll
-      for (int i = 0; i < kPer / 2; ++i) w[i] = to_e4m3x2(f[2 * i] * scale, f[2 * i + 1] * scale);
-      if (!in) continue;
-      p.q[row * per_row + at] = make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
-      if ((at & (kShare - 1)) == 0) p.scales[row * p.blocks + at / kShare] = uint8_t(e + 127);
+  for (int i = 0; i < kPer / 2; ++i) {
+    const float2 g = from_e4m3x2(w[i]);
+    f[i] = mul2(two(g.x, g.y), scale);
+  }
+}
+
+__device__ __forceinline__ void singles(const uint64_t (&v)[kPer / 2], float (&f)[kPer]) {
+#pragma unroll
+  for (int i = 0; i < kPer / 2; ++i) {
+    const float2 g = apart(v[i]);
+    f[2 * i] = g.x;
+    f[2 * i + 1] = g.y;
+  }
+}
+
+// Rows that start anywhere are written in blocks of their own address: the bytes of
+// a block lie in two neighbouring words of 8 (4, for fp32), under one scale or two.
+template <typename T, int ACT>
+__global__ void __launch_bounds__(kThreads) keep8_unpack_kernel(const KeepParams p) {
+  using B = Block<T>;
+  constexpr int PAIRS = B::PER / 2;
+  ptx::griddep_launch_dependents();
+  ptx::griddep_wait();
+  const int lanes = 1 << p.lanes_log, x = threadIdx.x & (lanes - 1), row_bytes = p.blocks * kBlock;
+  const int64_t step = int64_t(gridDim.x) * (kThreads >> p.lanes_log);
+  for (int64_t row = int64_t(blockIdx.x) * (kThreads >> p.lanes_log) + (threadIdx.x >> p.lanes_log); row < p.rows; row += step) {
+    const uint8_t* const q = reinterpret_cast<const uint8_t*>(p.q) + row * row_bytes;
+    const uint8_t* const scales = p.scales + row * p.blocks;
+    // values c .. c + PER - 1 of the row, in pairs (those outside it are anything)
+    auto values = [&](int c, uint64_t (&f)[PAIRS]) {
+      const int first = max(c, 0), last = min(c + B::PER, row_bytes) - 1;       // kept bytes, zeros behind the row's end
+      const int w0 = first / 4, w1 = last / 4, at = c >= 0 ? c : first;
+      uint32_t w[3];
+      if constexpr (B::PER == 8) {
+        const int mid = min(w0 + 1, w1);
+        w[0] = reinterpret_cast<const uint32_t*>(q)[w0];
+        w[1] = reinterpret_cast<const uint32_t*>(q)[mid];
+        w[2] = reinterpret_cast<const uint32_t*>(q)[w1];
+      } else {
+        w[0] = reinterpret_cast<const uint32_t*>(q)[w0];
+        w[1] = w[2] = reinterpret_cast<const uint32_t*>(q)[w1];
+      }
+      const uint32_t bits = uint32_t(at & 3) * 8u;
+      uint32_t lo = __funnelshift_r(w[0], w[1], bits), hi = __funnelshift_r(w[1], w[2], bits);
+      if (c < 0) {                                 // the row's first elements are the block's last
+        const uint32_t up = uint32_t(-c) * 8u;
+        const uint64_t v = up < 64 ? (uint64_t(w[1]) << 32 | w[0]) << up : 0;
+        lo = uint32_t(v), hi = uint32_t(v >> 32);
+      }
+      const int s0 = first / kBlock, change = (s0 + 1) * kBlock - c;            // elements under the first scale
+      const float a = power(int(scales[s0]) - 127), b = power(int(scales[last / kBlock]) - 127);
+      const uint32_t v[4] = {lo, lo >> 16, hi, hi >> 16};
+#pragma unroll
+      for (int i = 0; i < PAIRS; ++i) {
+        const float2 g = from_e4m3x2(v[i]);
+        f[i] = mul2(two(g.x, g.y), two(2 * i < change ? a : b, 2 * i + 1 < change ? a : b));
+      }
+    };
+    auto fill = [&](T* to, bool act) {
+      const int off = B::off(to), blocks = B::count(to, p.n);
+      for (int i = x; i < blocks; i += lanes) {
+        uint64_t f[PAIRS];
+        values(i * B::PER - off, f);
+        if (act) {
+#pragma unroll
+          for (int k = 0; k < PAIRS; ++k) f[k] = act_value2(f[k], ACT);
+        }
+        B::template store<false>(to, i * B::PER - off, p.n, B::pack(f));
+      }
+    };
+    T* const z = p.z ? static_cast<T*>(p.z) + row * p.ldz : nullptr;
+    T* const h = p.h ? static_cast<T*>(p.h) + row * p.ldh : nullptr;
+    if (z && h && B::off(z) == B::off(h)) {        // both from one reading
+      const int off = B::off(z), blocks = B::count(z, p.n);
+      for (int i = x; i < blocks; i += lanes) {
+        uint64_t f[PAIRS];
+        values(i * B::PER - off, f);
+        B::template store<false>(z, i * B::PER - off, p.n, B::pack(f));
+#pragma unroll
+        for (int k = 0; k < PAIRS; ++k) f[k] = act_value2(f[k], ACT);
+        B::template store<false>(h, i * B::PER - off, p.n, B::pack(f));
+      }
+    } else {
+      if (z) fill(z, false);
+      if (h) fill(h, true);
     }
   }
 }
 
 template <typename T, int ACT>
-__global__ void __launch_bounds__(kThreads) keep8_unpack_kernel(const KeepParams p) {
+__global__ void __launch_bounds__(kThreads) keep8_unpack_flat_kernel(const KeepParams p) {
+  using B = Block<T>;
+  constexpr int UNROLL = kUnroll / 2, STORES = kPer / B::PER;
   ptx::griddep_launch_dependents();
   ptx::griddep_wait();
-  const int lanes = 1 << p.lanes_log, x = threadIdx.x & (lanes - 1);
-  const int per_row = p.blocks * kShare, used = (p.n + kPer - 1) / kPer;
-  const int64_t step = int64_t(gridDim.x) * (kThreads >> p.lanes_log);
-  for (int64_t row = int64_t(blockIdx.x) * (kThreads >> p.lanes_log) + (threadIdx.x >> p.lanes_log); row < p.rows; row += step)
-    for (int at = x; at < used; at += lanes) {
-      const uint2 v = p.q[row * per_row + at];
-      const float scale = power(int(p.scales[row * p.blocks + at / kShare]) - 127);
-      const uint32_t w[4] = {v.x, v.x >> 16, v.y, v.y >> 16};
-      float f[kPer];
+  const int64_t step = int64_t(gridDim.x) * kThreads * UNROLL;
+  for (int64_t u0 = int64_t(blockIdx.x) * kThreads * UNROLL + threadIdx.x; u0 < p.pieces; u0 += step) {
+    uint2 q[UNROLL];
+    int e[UNROLL];
 #pragma unroll
-      for (int i = 0; i < kPer / 2; ++i) {
-        const float2 g = from_e4m3x2(w[i]);
-        f[2 * i] = g.x * scale;
-        f[2 * i + 1] = g.y * scale;
-      }
-      if (p.z) store8<T>(static_cast<T*>(p.z) + row * p.ldz, at * kPer, p.n, p.vec, f);
+    for (int k = 0; k < UNROLL; ++k) {
+      const int64_t u = min(u0 + k * kThreads, p.pieces - 1);
+      q[k] = __ldcs(p.q + u);
+      e[k] = p.scales[u / kShare];
+    }
+#pragma unroll
+    for (int k = 0; k < UNROLL; ++k) {
+      const int64_t u = u0 + k * kThreads;
+      if (u >= p.pieces) break;
+      uint64_t v[kPer / 2];
+      float f[kPer];
+      auto put = [&](void* base) {
+        singles(v, f);
+#pragma unroll
+        for (int i = 0; i < STORES; ++i) {
+          float g[B::PER];
+#pragma unroll
+          for (int j = 0; j < B::PER; ++j) g[j] = f[i * B::PER + j];
+          __stcs(static_cast<uint4*>(base) + u * STORES + i, B::pack(g));
+        }
+      };
+      restore(q[k], e[k], v);
+      if (p.z) put(p.z);
       if (!p.h) continue;
 #pragma unroll
-      for (int i = 0; i < kPer / 2; ++i) {
-        const float2 g = apart(act_value2(two(f[2 * i], f[2 * i + 1]), ACT));
-        f[2 * i] = g.x;
-        f[2 * i + 1] = g.y;
-      }
-      store8<T>(static_cast<T*>(p.h) + row * p.ldh, at * kPer, p.n, p.vec, f);
+      for (int i = 0; i < kPer / 2; ++i) v[i] = act_value2(v[i], ACT);
+      put(p.h);
     }
+  }
 }
 
+template <typename T, int ACT>
+const void* unpack_fn(bool flat) {
+  return flat ? reinterpret_cast<const void*>(&keep8_unpack_flat_kernel<T, ACT>)
+              : reinterpret_cast<const void*>(&keep8_unpack_kernel<T, ACT>);
+}
 template <typename T>
-const void* unpack_fn(int act) {
+const void* unpack_fn(int act, bool flat) {
   switch (act) {
-    case GOLDY_ACT_RELU: return reinterpret_cast<const void*>(&keep8_unpack_kernel<T, GOLDY_ACT_RELU>);
-    case GOLDY_ACT_GELU: return reinterpret_cast<const void*>(&keep8_unpack_kernel<T, GOLDY_ACT_GELU>);
-    case GOLDY_ACT_GELU_TANH: return reinterpret_cast<const void*>(&keep8_unpack_kernel<T, GOLDY_ACT_GELU_TANH>);
-    case GOLDY_ACT_SILU: return reinterpret_cast<const void*>(&keep8_unpack_kernel<T, GOLDY_ACT_SILU>);
-    default: return reinterpret_cast<const void*>(&keep8_unpack_kernel<T, GOLDY_ACT_NONE>);
+    case GOLDY_ACT_RELU: return unpack_fn<T, GOLDY_ACT_RELU>(flat);
+    case GOLDY_ACT_GELU: return unpack_fn<T, GOLDY_ACT_GELU>(flat);
+    case GOLDY_ACT_GELU_TANH: return unpack_fn<T, GOLDY_ACT_GELU_TANH>(flat);
+    case GOLDY_ACT_SILU: return unpack_fn<T, GOLDY_ACT_SILU>(flat);
+    default: return unpack_fn<T, GOLDY_ACT_NONE>(flat);
   }
+}
+template <typename T>
+const void* pack_fn(bool flat) {
+  return flat ? reinterpret_cast<const void*>(&keep8_pack_flat_kernel<T>) : reinterpret_cast<const void*>(&keep8_pack_kernel<T>);
 }
 
 struct KeepCall {
   KeepParams p;
   const void* fn;
+  bool flat;
+  int per_thread;        // pieces per step (flat)
   void* stream;
 };
 
 goldy_status launch_keep(const LayerContext& ctx, void* arg) {
   KeepCall& call = *static_cast<KeepCall*>(arg);
-  const int64_t grid = std::min(ceil_div(call.p.rows, int64_t(kThreads >> call.p.lanes_log)), int64_t(ctx.sm_count) * 32);
+  const int64_t units = call.flat ? ceil_div(call.p.pieces, int64_t(kThreads) * call.per_thread)
+                                  : ceil_div(call.p.rows, int64_t(kThreads >> call.p.lanes_log));
+  const int64_t grid = std::min(units, int64_t(ctx.sm_count) * 32);
   void* args[] = {&call.p};
   return launch_layer("keep8", call.fn, grid, kThreads, 0, call.stream, args);
 }
@@ -196,7 +357,7 @@ goldy_status check_keep(const goldy_keep8_desc* d) {
   return GOLDY_OK;
 }
 
-goldy_status run_keep(const goldy_keep8_desc& d, KeepCall& call, void* stream) {
+goldy_status run_keep(const goldy_keep8_desc& d, KeepCall& call, bool pack, void* stream) {
   KeepParams& p = call.p;
   p.rows = d.rows;
   p.ldz = d.ldz;
@@ -206,7 +367,13 @@ goldy_status run_keep(const goldy_keep8_desc& d, KeepCall& call, void* stream) {
   while ((1 << p.lanes_log) < kThreads && (1 << p.lanes_log) < p.blocks * kShare) ++p.lanes_log;
   const int64_t per = 16 / int64_t(element_size(d.dtype));
   auto whole = [&](const void* a, int64_t ld) { return !a || (on_boundary(a, 16) && ld % per == 0); };
-  p.vec = whole(p.z_in, d.ldz) && whole(p.z, d.ldz) && whole(p.h, d.ldh);
+  auto packed = [&](const void* a, int64_t ld) { return !a || ld == d.n; };
+  call.flat = whole(p.z_in, d.ldz) && whole(p.z, d.ldz) && whole(p.h, d.ldh) && d.n % kBlock == 0 && packed(p.z_in, d.ldz) && packed(p.z, d.ldz) && packed(p.h, d.ldh);
+  p.pieces = d.rows * (d.n / kPer);
+  call.per_thread = pack ? kUnroll : kUnroll / 2;
+  const bool f32 = d.dtype == GOLDY_F32;
+  if (pack) call.fn = f32 ? pack_fn<uint32_t>(call.flat) : pack_fn<uint16_t>(call.flat);
+  else call.fn = f32 ? unpack_fn<uint32_t>(d.act, call.flat) : unpack_fn<uint16_t>(d.act, call.flat);
   call.stream = stream;
   const goldy_status st = with_layer_context(stream, launch_keep, &call);
   return st == GOLDY_OK ? ok() : st;
@@ -239,9 +406,7 @@ extern "C" goldy_status goldy_keep8_pack(const goldy_keep8_desc* desc, const voi
   call.p.z_in = Z;
   call.p.q = static_cast<uint2*>(Q);
   call.p.scales = static_cast<uint8_t*>(scales);
-  call.fn = desc->dtype == GOLDY_F32 ? reinterpret_cast<const void*>(&keep8_pack_kernel<float>)
-                                     : reinterpret_cast<const void*>(&keep8_pack_kernel<uint16_t>);
-  return run_keep(*desc, call, stream);
+  return run_keep(*desc, call, true, stream);
 } catch (...) {
   return layer_exception();
 }
@@ -260,8 +425,7 @@ extern "C" goldy_status goldy_keep8_unpack(const goldy_keep8_desc* desc, const v
   call.p.scales = static_cast<uint8_t*>(const_cast<void*>(scales));
   call.p.z = Z;
   call.p.h = H;
-  call.fn = desc->dtype == GOLDY_F32 ? unpack_fn<float>(desc->act) : unpack_fn<uint16_t>(desc->act);
-  return run_keep(*desc, call, stream);
+  return run_keep(*desc, call, false, stream);
 } catch (...) {
   return layer_exception();
 }

@@ -35,8 +35,8 @@ constexpr unsigned kAll = 0xFFFFFFFFu;
 // ---- sort ---------------------------------------------------------------------
 
 constexpr int kSortThreads = 512;
-constexpr int kAlone = 4096;           // slots up to which one CTA sorts them
-constexpr int kChunk = 2048;           // slots per CTA otherwise
+constexpr int kAlone = 2048;           // slots up to which one CTA sorts them
+constexpr int kChunk = 1024;           // slots per CTA otherwise
 constexpr int kMostChunks = 304;       // at most, then chunks grow
 constexpr int kSortSmem = 200 * 1024;  // for the warps' counts
 
@@ -48,6 +48,7 @@ struct SortParams {
   int32_t* counts;       // [chunks][groups + 1]; null: one chunk
   int32_t slots, groups, chunk, chunks;
   int32_t warps;         // that walk a chunk
+  int32_t share_log;     // lanes per group that add up the chunks, log2
 };
 
 __device__ __forceinline__ int group_of(const SortParams& p, int slot) {
@@ -83,24 +84,48 @@ __global__ void __launch_bounds__(kSortThreads) route_place_kernel(const SortPar
   const int64_t from = min(hi, lo + warp * share), to = warp < p.warps ? min(hi, from + share) : from;
   for (int64_t s = from + lane; s < to; s += 32) atomicAdd(next + warp * bins + group_of(p, int(s)), 1);
   __syncthreads();
-  // all slots of a group, and those of the chunks before
-  for (int g = threadIdx.x; g < bins; g += kSortThreads) {
-    int total = 0, before = 0;
-    if (p.counts) {
-      for (int c = 0; c < p.chunks; ++c) {
-        const int n = p.counts[int64_t(c) * bins + g];
-        if (c < int(blockIdx.x)) before += n;
-        total += n;
+  // all slots of a group, and those of the chunks before: `share_log` lanes per
+  // group add up the chunks, four loads of each on their way at once
+  if (p.counts) {
+    const int lanes = 1 << p.share_log, x = threadIdx.x & (lanes - 1);
+    for (int g = threadIdx.x >> p.share_log; (g & ~31) < bins; g += kSortThreads >> p.share_log) {     // whole warps
+      int total = 0, before = 0;
+      for (int c0 = x; c0 < p.chunks; c0 += 4 * lanes) {
+        int n[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int c = c0 + i * lanes;
+          n[i] = c < p.chunks && g < bins ? p.counts[int64_t(c) * bins + g] : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (c0 + i * lanes < int(blockIdx.x)) before += n[i];
+          total += n[i];
+        }
       }
-    } else {
-      for (int w = 0; w < p.warps; ++w) total += next[w * bins + g];
+      for (int d = 1; d < lanes; d *= 2) {
+        total += __shfl_xor_sync(kAll, total, d);
+        before += __shfl_xor_sync(kAll, before, d);
+      }
+      if (g < bins && x == 0) {
+        start[g] = total;
+        int at = before;
+        for (int w = 0; w < p.warps; ++w) {
+          const int n = next[w * bins + g];
+          next[w * bins + g] = at;
+          at += n;
+        }
+      }
     }
-    start[g] = total;
-    int at = before;
-    for (int w = 0; w < p.warps; ++w) {
-      const int n = next[w * bins + g];
-      next[w * bins + g] = at;
-      at += n;
+  } else {
+    for (int g = threadIdx.x; g < bins; g += kSortThreads) {
+      int at = 0;
+      for (int w = 0; w < p.warps; ++w) {
+        const int n = next[w * bins + g];
+        next[w * bins + g] = at;
+        at += n;
+      }
+      start[g] = at;
     }
   }
   __syncthreads();
@@ -147,8 +172,13 @@ __global__ void __launch_bounds__(kSortThreads) route_place_kernel(const SortPar
 
 // ---- rows ---------------------------------------------------------------------
 
-constexpr int kRowThreads = 256;
-constexpr int kInFlight = 8;           // experts' rows that combine reads at once
+constexpr int kRowThreads = 256;       // at most
+constexpr int kDispatchBlocks = 2;     // of a row, on their way per thread
+constexpr int kDispatchCtas = 5;       // per SM, by registers
+constexpr int combine_ctas(int slots) { return slots > 2 ? 4 : 5; }
+constexpr int kGradBlocks = 2;         // of dY, and as many of E (4, with 2 CTAs per SM: 74 us for 30000 x 150 to
+                                       // four places, now 36)
+constexpr int kGradCtas = 4;
 
 struct RowParams {
   const void* tokens;    // X, or dY
@@ -160,139 +190,207 @@ struct RowParams {
   float* dweights;
   int64_t rows, ldx, lde, ldr;
   int32_t width, k, places;
-  int32_t lanes_log;     // threads per row, log2
+  int32_t lanes, per_cta;  // threads per row, rows per CTA
 };
 
-__device__ __forceinline__ int place_of(const RowParams& p, int64_t slot) {
-  const int at = p.place[slot];
-  return at >= 0 && at < p.places ? at : -1;
-}
-
-// Calls body(token, block) for this thread's blocks of its rows.
-template <typename T, bool ALIGNED, typename F>
-__device__ __forceinline__ void for_blocks(const RowParams& p, F body) {
-  const int lanes = 1 << p.lanes_log, x = threadIdx.x & (lanes - 1);
-  const int64_t per_cta = kRowThreads >> p.lanes_log;
-  // a row that starts inside a block touches one more
-  const int blocks = p.width / Block<T>::PER + (ALIGNED ? 0 : 2);
-  for (int64_t t = int64_t(blockIdx.x) * per_cta + (threadIdx.x >> p.lanes_log); t < p.rows; t += int64_t(gridDim.x) * per_cta)
-    for (int b = x; b < blocks; b += lanes) body(t, b);
-}
+__device__ __forceinline__ int valid_place(const RowParams& p, int at) { return unsigned(at) < unsigned(p.places) ? at : -1; }
 
 template <typename T, bool ALIGNED>
-__global__ void __launch_bounds__(kRowThreads) route_dispatch_kernel(const RowParams p) {
+__global__ void __launch_bounds__(kRowThreads, kDispatchCtas) route_dispatch_kernel(const RowParams p) {
   using B = Block<T>;
+  constexpr int BLOCKS = kDispatchBlocks;
   ptx::griddep_launch_dependents();
   ptx::griddep_wait();
-  for_blocks<T, ALIGNED>(p, [&](int64_t t, int b) {
-    const T* x = static_cast<const T*>(p.tokens) + t * p.ldx;
-    uint4 v;
-    if (ALIGNED) v = B::template load<true>(x, b * B::PER, p.width);
-    for (int j = 0; j < p.k; ++j) {
-      const int at = place_of(p, t * p.k + j);
-      if (at < 0) continue;
-      T* e = static_cast<T*>(p.out) + int64_t(at) * p.lde;
-      const int c = b * B::PER - (ALIGNED ? 0 : B::off(e));
-      if (!ALIGNED) {
-        if (c >= p.width) continue;
-        v = B::template load<false>(x, c, p.width);
-      }
-      B::template store<ALIGNED>(e, c, p.width, v);
-    }
-  });
-}
-
-template <typename T, bool ALIGNED>
-__global__ void __launch_bounds__(kRowThreads) route_combine_kernel(const RowParams p) {
-  using B = Block<T>;
-  ptx::griddep_launch_dependents();
-  ptx::griddep_wait();
-  for_blocks<T, ALIGNED>(p, [&](int64_t t, int b) {
-    T* y = static_cast<T*>(p.out) + t * p.ldx;
-    const int c = b * B::PER - (ALIGNED ? 0 : B::off(y));
-    if (!ALIGNED && c >= p.width) return;
-    float sum[B::PER], f[B::PER];
+  const int line = threadIdx.x / p.lanes, x = threadIdx.x % p.lanes, lanes = p.lanes;
+  for (int64_t t = int64_t(blockIdx.x) * p.per_cta + line; t < p.rows; t += int64_t(gridDim.x) * p.per_cta) {
+    const T* const from = static_cast<const T*>(p.tokens) + t * p.ldx;
+    const int32_t* const place = p.place + t * p.k;
+    if constexpr (ALIGNED) {
+      const int blocks = p.width / B::PER;
+      for (int b0 = x; b0 < blocks; b0 += lanes * BLOCKS) {
+        uint4 v[BLOCKS];
 #pragma unroll
-    for (int i = 0; i < B::PER; ++i) sum[i] = 0.0f;
-    for (int j0 = 0; j0 < p.k; j0 += kInFlight) {
-      uint4 v[kInFlight];
-      int at[kInFlight];
-      float w[kInFlight];
+        for (int u = 0; u < BLOCKS; ++u)
+          if (u == 0 || b0 + u * lanes < blocks) v[u] = reinterpret_cast<const uint4*>(from)[b0 + u * lanes];
+        for (int j = 0; j < p.k; ++j) {
+          const int at = valid_place(p, place[j]);
+          if (at < 0) continue;
+          uint4* e = reinterpret_cast<uint4*>(static_cast<T*>(p.out) + int64_t(at) * p.lde);
 #pragma unroll
-      for (int j = 0; j < kInFlight; ++j) {
-        const bool there = j0 + j < p.k;
-        at[j] = there ? place_of(p, t * p.k + j0 + j) : -1;
-        w[j] = there && p.weights ? p.weights[t * p.k + j0 + j] : 1.0f;
-      }
-#pragma unroll
-      for (int j = 0; j < kInFlight; ++j)
-        if (at[j] >= 0)
-          v[j] = B::template load<ALIGNED>(static_cast<const T*>(p.experts) + int64_t(at[j]) * p.lde, c, p.width);
-#pragma unroll
-      for (int j = 0; j < kInFlight; ++j) {
-        if (at[j] < 0) continue;
-        B::unpack(v[j], f);
-#pragma unroll
-        for (int i = 0; i < B::PER; ++i) sum[i] = fmaf(w[j], f[i], sum[i]);
-      }
-    }
-    if (p.res) {
-      B::unpack(B::template load<ALIGNED>(static_cast<const T*>(p.res) + t * p.ldr, c, p.width), f);
-#pragma unroll
-      for (int i = 0; i < B::PER; ++i) sum[i] += f[i];
-    }
-    B::template store<ALIGNED>(y, c, p.width, B::pack(sum));
-  });
-}
-
-template <typename T, bool ALIGNED, bool DOT>
-__global__ void __launch_bounds__(kRowThreads) route_combine_grad_kernel(const RowParams p) {
-  using B = Block<T>;
-  constexpr int UNROLL = 4;
-  ptx::griddep_launch_dependents();
-  ptx::griddep_wait();
-  const int lane = threadIdx.x & 31;
-  const int64_t slots = p.rows * p.k, step = int64_t(gridDim.x) * (kRowThreads / 32);
-  for (int64_t s = int64_t(blockIdx.x) * (kRowThreads / 32) + (threadIdx.x >> 5); s < slots; s += step) {
-    const int at = place_of(p, s);
-    if (at < 0) {
-      if (DOT && lane == 0) p.dweights[s] = 0.0f;
-      continue;
-    }
-    const T* dy = static_cast<const T*>(p.tokens) + s / p.k * p.ldx;
-    const T* e = static_cast<const T*>(p.experts) + int64_t(at) * p.lde;
-    T* de = static_cast<T*>(p.out) + int64_t(at) * p.lde;
-    const float w = p.weights ? p.weights[s] : 1.0f;
-    const int off = ALIGNED ? 0 : B::off(de);
-    float dot = 0.0f;
-    for (int c0 = lane * B::PER - off; c0 < p.width; c0 += UNROLL * 32 * B::PER) {
-      uint4 g[UNROLL], v[UNROLL];
-#pragma unroll
-      for (int u = 0; u < UNROLL; ++u) {
-        const int c = c0 + u * 32 * B::PER;
-        if (c >= p.width) continue;
-        g[u] = B::template load<ALIGNED>(dy, c, p.width);
-        if (DOT) v[u] = B::template load<ALIGNED>(e, c, p.width);
-      }
-#pragma unroll
-      for (int u = 0; u < UNROLL; ++u) {
-        const int c = c0 + u * 32 * B::PER;
-        if (c >= p.width) continue;
-        float f[B::PER], h[B::PER];
-        B::unpack(g[u], f);
-        if (DOT) B::unpack(v[u], h);
-#pragma unroll
-        for (int i = 0; i < B::PER; ++i) {
-          if (DOT) dot = fmaf(f[i], h[i], dot);
-          f[i] *= w;
+          for (int u = 0; u < BLOCKS; ++u)
+            if (u == 0 || b0 + u * lanes < blocks) e[b0 + u * lanes] = v[u];
         }
-        B::template store<ALIGNED>(de, c, p.width, B::pack(f));
+      }
+    } else {
+      // places start on any element: a block of any of them lies in three of X
+      const typename B::Source source(from, p.width, 0);
+      const int blocks = B::count(from, p.width) + 1;
+      for (int b = x; b < blocks; b += lanes) {
+        uint4 v[3];
+#pragma unroll
+        for (int i = 0; i < 3; ++i) v[i] = source.first[min(max(b + i - 1, 0), source.last)];
+        for (int j = 0; j < p.k; ++j) {
+          const int at = valid_place(p, place[j]);
+          if (at < 0) continue;
+          T* e = static_cast<T*>(p.out) + int64_t(at) * p.lde;
+          const typename B::Source s(from, p.width, B::off(e));
+          const int c = b * B::PER - B::off(e);
+          if (c >= p.width) continue;
+          B::template store<false>(e, c, p.width, shift_blocks(s.ahead ? v[0] : v[1], s.ahead ? v[1] : v[2], s.shift));
+        }
+      }
+    }
+  }
+}
+
+// SLOTS * BLOCKS blocks of experts' rows on their way at once.  (Copies of the next
+// tokens' rows into shared memory or the L2 cache meanwhile took 112 and 99 us for
+// 8192 tokens of 8 x 2048, this 52; 8 slots of one block 61.  Rows of 1111 elements,
+// which start anywhere: 46 us, twice the floor, by instructions.)
+template <typename T, bool ALIGNED, int SLOTS, int BLOCKS>
+__global__ void __launch_bounds__(kRowThreads, combine_ctas(SLOTS)) route_combine_kernel(const RowParams p) {
+  using B = Block<T>;
+  constexpr int PAIRS = B::PER / 2;
+  ptx::griddep_launch_dependents();
+  ptx::griddep_wait();
+  const int line = threadIdx.x / p.lanes, x = threadIdx.x % p.lanes, lanes = p.lanes;
+  for (int64_t t = int64_t(blockIdx.x) * p.per_cta + line; t < p.rows; t += int64_t(gridDim.x) * p.per_cta) {
+    T* const y = static_cast<T*>(p.out) + t * p.ldx;
+    const int32_t* const place = p.place + t * p.k;
+    const float* const weights = p.weights ? p.weights + t * p.k : nullptr;
+    const int off = ALIGNED ? 0 : B::off(y), blocks = ALIGNED ? p.width / B::PER : B::count(y, p.width);
+    auto source = [&](const T* row) {
+      if constexpr (!ALIGNED) return typename B::Source(row, p.width, off);
+      typename B::Source s;
+      s.first = reinterpret_cast<const uint4*>(row);
+      return s;
+    };
+    auto expert = [&](int at) { return source(static_cast<const T*>(p.experts) + int64_t(at) * p.lde); };
+    for (int b0 = x; b0 < blocks; b0 += lanes * BLOCKS) {
+      uint64_t sum[BLOCKS][PAIRS];
+#pragma unroll
+      for (int u = 0; u < BLOCKS; ++u)
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) sum[u][i] = two(0.0f);
+      auto inside = [&](int u) { return u == 0 || b0 + u * lanes < blocks; };
+      auto add = [&](int u, const uint4& v, float w) {
+        uint64_t f[PAIRS];
+        B::pairs(v, f);
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) sum[u][i] = fma2(two(w), f[i], sum[u][i]);
+      };
+      for (int j0 = 0; j0 < p.k; j0 += SLOTS) {
+        typename B::template Raw<ALIGNED> v[SLOTS][BLOCKS];
+        int at[SLOTS];
+        uint32_t shift[SLOTS];
+#pragma unroll
+        for (int j = 0; j < SLOTS; ++j) at[j] = j0 + j < p.k ? valid_place(p, place[j0 + j]) : -1;
+#pragma unroll
+        for (int j = 0; j < SLOTS; ++j) {
+          if (at[j] < 0) continue;
+          const typename B::Source s = expert(at[j]);
+          shift[j] = s.shift;
+#pragma unroll
+          for (int u = 0; u < BLOCKS; ++u)
+            if (inside(u)) v[j][u].load(s, b0 + u * lanes);
+        }
+#pragma unroll
+        for (int j = 0; j < SLOTS; ++j) {
+          if (at[j] < 0) continue;
+          const float w = weights ? weights[j0 + j] : 1.0f;
+#pragma unroll
+          for (int u = 0; u < BLOCKS; ++u) add(u, v[j][u].get(shift[j]), w);
+        }
+      }
+      if (p.res) {
+        const typename B::Source s = source(static_cast<const T*>(p.res) + t * p.ldr);
+        typename B::template Raw<ALIGNED> v[BLOCKS];
+#pragma unroll
+        for (int u = 0; u < BLOCKS; ++u)
+          if (inside(u)) v[u].load(s, b0 + u * lanes);
+#pragma unroll
+        for (int u = 0; u < BLOCKS; ++u) add(u, v[u].get(s.shift), 1.0f);
+      }
+#pragma unroll
+      for (int u = 0; u < BLOCKS; ++u)
+        if (inside(u)) B::template store<ALIGNED>(y, (b0 + u * lanes) * B::PER - off, p.width, B::pack(sum[u]));
+    }
+  }
+}
+
+// LANES threads per slot.
+template <typename T, bool ALIGNED, bool DOT, int LANES>
+__global__ void __launch_bounds__(kRowThreads, kGradCtas) route_combine_grad_kernel(const RowParams p) {
+  using B = Block<T>;
+  constexpr int BLOCKS = kGradBlocks, PAIRS = B::PER / 2, TEAMS = kRowThreads / LANES;
+  ptx::griddep_launch_dependents();
+  ptx::griddep_wait();
+  const int lane = threadIdx.x % LANES, slots = p.places;
+  const int64_t step = int64_t(gridDim.x) * TEAMS;
+  int64_t s = int64_t(blockIdx.x) * TEAMS + threadIdx.x / LANES;
+  auto slot = [&](int64_t i, int& at, float& w) {
+    at = i < slots ? valid_place(p, p.place[i]) : -1;
+    w = i < slots && p.weights ? p.weights[i] : 1.0f;
+  };
+  int at, next_at;
+  float w, next_w;
+  slot(s, at, w);
+  for (; __any_sync(kAll, s < slots); s += step, at = next_at, w = next_w) {       // whole warps: they add up together
+    slot(s + step, next_at, next_w);
+    uint64_t dot2 = two(0.0f);
+    if (at >= 0) {
+      const T* dy_row = static_cast<const T*>(p.tokens) + int64_t(uint32_t(s) / uint32_t(p.k)) * p.ldx;
+      const T* e_row = static_cast<const T*>(p.experts) + int64_t(at) * p.lde;
+      T* const de = static_cast<T*>(p.out) + int64_t(at) * p.lde;
+      const int off = ALIGNED ? 0 : B::off(de), blocks = ALIGNED ? p.width / B::PER : B::count(de, p.width);
+      typename B::Source dy, e;
+      if constexpr (ALIGNED) {
+        dy.first = reinterpret_cast<const uint4*>(dy_row);
+        e.first = reinterpret_cast<const uint4*>(e_row);
+      } else {
+        dy = typename B::Source(dy_row, p.width, off);
+        if (DOT) e = typename B::Source(e_row, p.width, off);
+      }
+      for (int b0 = lane; b0 < blocks; b0 += BLOCKS * LANES) {
+        typename B::template Raw<ALIGNED> g[BLOCKS], v[BLOCKS];
+#pragma unroll
+        for (int u = 0; u < BLOCKS; ++u) {
+          const int b = b0 + u * LANES;
+          if (u > 0 && b >= blocks) continue;
+          g[u].load(dy, b);
+          if (DOT) v[u].load(e, b);
+        }
+#pragma unroll
+        for (int u = 0; u < BLOCKS; ++u) {
+          const int b = b0 + u * LANES, c = b * B::PER - off;
+          if (u > 0 && b >= blocks) continue;
+          uint64_t f[PAIRS], h[PAIRS];
+          uint4 gv = g[u].get(dy.shift);
+          if (DOT) {
+            uint4 ev = v[u].get(e.shift);
+            if (!ALIGNED && (c < 0 || c + B::PER > p.width)) {
+              const uint4 m = B::inside(c, p.width);
+              gv.x &= m.x, gv.y &= m.y, gv.z &= m.z, gv.w &= m.w;
+              ev.x &= m.x, ev.y &= m.y, ev.z &= m.z, ev.w &= m.w;
+            }
+            B::pairs(ev, h);
+          }
+          B::pairs(gv, f);
+#pragma unroll
+          for (int i = 0; i < PAIRS; ++i) {
+            if (DOT) dot2 = fma2(f[i], h[i], dot2);
+            f[i] = mul2(f[i], two(w));
+          }
+          B::template store<ALIGNED>(de, c, p.width, B::pack(f));
+        }
       }
     }
     if (DOT) {
+      const float2 d2 = apart(dot2);
+      float dot = d2.x + d2.y;
 #pragma unroll
-      for (int d = 16; d > 0; d >>= 1) dot += __shfl_xor_sync(kAll, dot, d);
-      if (lane == 0) p.dweights[s] = dot;
+      for (int d = LANES / 2; d > 0; d >>= 1) dot += __shfl_xor_sync(kAll, dot, d);
+      if (lane == 0 && s < slots) p.dweights[s] = dot;
     }
   }
 }
@@ -358,18 +456,20 @@ goldy_status launch_sort(const LayerContext& ctx, void* arg) {
 struct RowCall {
   RowParams p;
   const void* fn;
-  bool warp_per_slot;
+  int64_t units;         // rows, or slots
+  int per_cta, threads;
+  int per_sm;            // CTAs, at most
   void* stream;
 };
 
 goldy_status launch_rows(const LayerContext& ctx, void* arg) {
   RowCall& call = *static_cast<RowCall*>(arg);
-  const int64_t per_cta = call.warp_per_slot ? kRowThreads / 32 : kRowThreads >> call.p.lanes_log;
-  const int64_t units = call.warp_per_slot ? call.p.rows * call.p.k : call.p.rows;
-  const int64_t grid = std::min(ceil_div(units, per_cta), int64_t(ctx.sm_count) * 64);
+  const int64_t grid = std::min(ceil_div(call.units, int64_t(call.per_cta)), int64_t(ctx.sm_count) * call.per_sm);
   void* args[] = {&call.p};
-  return launch_layer("route", call.fn, grid, kRowThreads, 0, call.stream, args);
+  return launch_layer("route", call.fn, grid, call.threads, 0, call.stream, args);
 }
+
+int64_t row_blocks(const goldy_route_desc& d) { return std::max<int64_t>(1, ceil_div(d.width, 16 / int64_t(element_size(d.dtype)))); }
 
 goldy_status run_rows(const goldy_route_desc& d, RowCall& call, void* stream) {
   RowParams& p = call.p;
@@ -380,11 +480,23 @@ goldy_status run_rows(const goldy_route_desc& d, RowCall& call, void* stream) {
   p.width = int32_t(d.width);
   p.k = d.k;
   p.places = int32_t(slots_of(d));
-  const int64_t blocks = d.width / (16 / int64_t(element_size(d.dtype))) + 2;
-  while ((1 << p.lanes_log) < kRowThreads && (int64_t(1) << p.lanes_log) + 2 < blocks) ++p.lanes_log;
   call.stream = stream;
   const goldy_status st = with_layer_context(stream, launch_rows, &call);
   return st == GOLDY_OK ? ok() : st;
+}
+
+// Threads that share a token's row, each with `per_thread` blocks at once: equal
+// shares, whatever their number (a row of 139 blocks in twos: 70 threads, three
+// rows per CTA), not powers of two.  A row off its blocks' boundaries has one more.
+void share_rows(const goldy_route_desc& d, RowCall& call, int per_thread, bool aligned) {
+  const int64_t blocks = row_blocks(d) + (aligned ? 0 : 1), rounds = ceil_div(blocks, int64_t(kRowThreads) * per_thread);
+  call.p.lanes = int32_t(ceil_div(blocks, rounds * per_thread));
+  call.p.per_cta = kRowThreads / call.p.lanes;
+  call.units = d.rows;
+  call.per_cta = call.p.per_cta;
+  call.threads = call.p.lanes * call.p.per_cta;
+  // more CTAs than fit (16384 x 4096 to two places: 67 us, resident ones alone 75)
+  call.per_sm = 64;
 }
 
 // every row whole blocks on their boundaries
@@ -402,17 +514,28 @@ const void* dispatch_fn(bool aligned) {
                  : reinterpret_cast<const void*>(&route_dispatch_kernel<T, false>);
 }
 template <typename T>
-const void* combine_fn(bool aligned) {
-  return aligned ? reinterpret_cast<const void*>(&route_combine_kernel<T, true>)
-                 : reinterpret_cast<const void*>(&route_combine_kernel<T, false>);
+const void* combine_fn(bool aligned, int k) {
+  if (!aligned) return reinterpret_cast<const void*>(&route_combine_kernel<T, false, 4, 1>);
+  return k > 2 ? reinterpret_cast<const void*>(&route_combine_kernel<T, true, 4, 2>)
+               : reinterpret_cast<const void*>(&route_combine_kernel<T, true, 2, 2>);
 }
-template <typename T>
+// Threads per slot: few blocks leave no work for a whole warp.
+int grad_lanes(const goldy_route_desc& d) { return row_blocks(d) > 48 ? 32 : row_blocks(d) > 16 ? 16 : 8; }
+template <typename T, int LANES>
 const void* grad_fn(bool aligned, bool dot) {
   if (dot)
-    return aligned ? reinterpret_cast<const void*>(&route_combine_grad_kernel<T, true, true>)
-                   : reinterpret_cast<const void*>(&route_combine_grad_kernel<T, false, true>);
-  return aligned ? reinterpret_cast<const void*>(&route_combine_grad_kernel<T, true, false>)
-                 : reinterpret_cast<const void*>(&route_combine_grad_kernel<T, false, false>);
+    return aligned ? reinterpret_cast<const void*>(&route_combine_grad_kernel<T, true, true, LANES>)
+                   : reinterpret_cast<const void*>(&route_combine_grad_kernel<T, false, true, LANES>);
+  return aligned ? reinterpret_cast<const void*>(&route_combine_grad_kernel<T, true, false, LANES>)
+                 : reinterpret_cast<const void*>(&route_combine_grad_kernel<T, false, false, LANES>);
+}
+template <typename T>
+const void* grad_fn(bool aligned, bool dot, int lanes) {
+  switch (lanes) {
+    case 32: return grad_fn<T, 32>(aligned, dot);
+    case 16: return grad_fn<T, 16>(aligned, dot);
+    default: return grad_fn<T, 8>(aligned, dot);
+  }
 }
 
 }  // namespace
@@ -456,6 +579,7 @@ extern "C" goldy_status goldy_route_sort(const goldy_route_desc* desc, const int
   p.chunks = int32_t(chunks_of(p.slots));
   p.chunk = int32_t(ceil_div(std::max<int64_t>(1, ceil_div(p.slots, int64_t(p.chunks))), 32) * 32);
   p.warps = int32_t(std::min<int64_t>(kSortThreads / 32, kSortSmem / ((p.groups + 1) * int64_t(sizeof(int32_t)))));
+  while (p.share_log < 5 && (int64_t(p.groups + 1) << p.share_log) < kSortThreads && (1 << p.share_log) < p.chunks) ++p.share_log;
   call.stream = stream;
   st = with_layer_context(stream, launch_sort, &call);
   return st == GOLDY_OK ? ok() : st;
@@ -476,7 +600,8 @@ extern "C" goldy_status goldy_route_dispatch(const goldy_route_desc* desc, const
   call.p.place = place;
   call.p.out = E;
   const bool aligned = in_blocks(*desc, {{X, desc->ldx}, {E, desc->lde}});
-  call.fn = desc->dtype == GOLDY_F32 ? dispatch_fn<float>(aligned) : dispatch_fn<uint16_t>(aligned);
+  call.fn = desc->dtype == GOLDY_F32 ? dispatch_fn<uint32_t>(aligned) : dispatch_fn<uint16_t>(aligned);
+  share_rows(*desc, call, aligned ? kDispatchBlocks : 1, aligned);
   return run_rows(*desc, call, stream);
 } catch (...) {
   return layer_exception();
@@ -499,7 +624,8 @@ extern "C" goldy_status goldy_route_combine(const goldy_route_desc* desc, const 
   call.p.res = R;
   call.p.out = Y;
   const bool aligned = in_blocks(*desc, {{E, desc->lde}, {R, desc->ldr}, {Y, desc->ldx}});
-  call.fn = desc->dtype == GOLDY_F32 ? combine_fn<float>(aligned) : combine_fn<uint16_t>(aligned);
+  call.fn = desc->dtype == GOLDY_F32 ? combine_fn<uint32_t>(aligned, desc->k) : combine_fn<uint16_t>(aligned, desc->k);
+  share_rows(*desc, call, aligned ? 2 : 1, aligned);
   return run_rows(*desc, call, stream);
 } catch (...) {
   return layer_exception();
@@ -524,10 +650,16 @@ extern "C" goldy_status goldy_route_combine_grad(const goldy_route_desc* desc, c
   call.p.weights = weights;
   call.p.out = dE;
   call.p.dweights = dweights;
-  call.warp_per_slot = true;
-  const bool aligned = in_blocks(*desc, {{dY, desc->ldx}, {dweights ? E : nullptr, desc->lde}, {dE, desc->lde}});
+  // (rows of no elements: only the zeros of dweights are written)
+  const bool aligned =
+      desc->width == 0 || in_blocks(*desc, {{dY, desc->ldx}, {dweights ? E : nullptr, desc->lde}, {dE, desc->lde}});
   const bool dot = dweights != nullptr;
-  call.fn = desc->dtype == GOLDY_F32 ? grad_fn<float>(aligned, dot) : grad_fn<uint16_t>(aligned, dot);
+  const int lanes = grad_lanes(*desc);
+  call.fn = desc->dtype == GOLDY_F32 ? grad_fn<uint32_t>(aligned, dot, lanes) : grad_fn<uint16_t>(aligned, dot, lanes);
+  call.units = slots_of(*desc);
+  call.per_cta = kRowThreads / lanes;
+  call.threads = kRowThreads;
+  call.per_sm = kGradCtas;                         // resident: the next slot's place is read ahead
   return run_rows(*desc, call, stream);
 } catch (...) {
   return layer_exception();

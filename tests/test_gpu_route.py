@@ -45,7 +45,7 @@ def check_sort(ids, rows, k, groups):
 
 
 @pytest.mark.parametrize("rows,k,groups", [(1, 1, 1), (1, 8, 64), (5, 3, 7), (16, 6, 64), (100, 2, 8), (511, 8, 31), (512, 8, 16),
-                                           (513, 8, 16), (4096, 1, 256), (4097, 1, 256), (1366, 3, 60), (3000, 32, 128),
+                                           (513, 8, 16), (1024, 2, 16), (683, 3, 5), (4096, 1, 256), (4097, 1, 256), (1366, 3, 60), (3000, 32, 128),
                                            (700, 6, 2000), (1000, 5, 4096), (2, 1, 4096), (160001, 4, 33)])
 def test_sort(cuda_ok, rows, k, groups):
     ids = torch.randint(-1, groups + 1, (rows, k), generator=gen_of(rows), device="cuda").int()
@@ -209,6 +209,16 @@ def test_dispatch_gradient_is_combine(cuda_ok):
     G.goldy_route_combine(c.d, g.data_ptr(), c.place.data_ptr(), dx.data_ptr())
     torch.cuda.synchronize()
     assert float((e * g).sum()) == float((x * dx).sum())
+
+
+def test_rows_without_elements(cuda_ok):
+    """Only the weights' gradient has something to write: zeros."""
+    d, place = G.route_desc(6, 2, 3, 0), torch.arange(12, dtype=torch.int32, device="cuda")
+    dw = torch.full((12,), 5.0, device="cuda")
+    odd = torch.zeros(8, dtype=torch.uint16, device="cuda").data_ptr() + 2
+    G.goldy_route_combine_grad(d, odd, odd, place.data_ptr(), 0, odd, dw.data_ptr())
+    torch.cuda.synchronize()
+    assert (dw == 0).all()
 
 
 def test_places_out_of_range(cuda_ok):
