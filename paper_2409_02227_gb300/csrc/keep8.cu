@@ -85,51 +85,44 @@ __device__ __forceinline__ uint2 quantise(float (&f)[kPer], int& e) {
 template <typename T>
 __global__ void __launch_bounds__(kThreads) keep8_pack_kernel(const KeepParams p) {
   using B = Block<T>;
-  constexpr int LOADS = kPer / B::PER, UNROLL = 2;
+  constexpr int LOADS = kPer / B::PER;
   ptx::griddep_launch_dependents();
   ptx::griddep_wait();
   const int lanes = 1 << p.lanes_log, x = threadIdx.x & (lanes - 1);
   const int per_row = p.blocks * kShare;
   const int64_t per_cta = kThreads >> p.lanes_log;
-  const int trips = (per_row + lanes - 1) >> p.lanes_log;
   const int64_t rounds = (p.rows + per_cta - 1) / per_cta;
   for (int64_t r = blockIdx.x; r < rounds; r += gridDim.x) {
     const int64_t row = r * per_cta + (threadIdx.x >> p.lanes_log);
     const typename B::Source source(static_cast<const T*>(p.z_in) + min(row, p.rows - 1) * p.ldz, p.n, 0);
-    for (int trip = 0; trip < trips; trip += UNROLL) {   // every thread of a warp goes along: they trade maxima
-      typename B::template Raw<false> raw[UNROLL][LOADS];
+    for (int at0 = 0; at0 < per_row; at0 += lanes) {     // every thread of a warp goes along: they trade maxima
+      const int at = at0 + x;
+      typename B::template Raw<false> raw[LOADS];
 #pragma unroll
-      for (int k = 0; k < UNROLL; ++k) {
-        const int c = ((trip + k) * lanes + x) * kPer;
+      for (int i = 0; i < LOADS; ++i)
+        if (at * kPer + i * B::PER < p.n) raw[i].load(source, at * LOADS + i);
+      float f[kPer];
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i)
-          if (c + i * B::PER < p.n) raw[k][i].load(source, c / B::PER + i);
-      }
-#pragma unroll
-      for (int k = 0; k < UNROLL; ++k) {
-        const int at = (trip + k) * lanes + x, c = at * kPer;
-        float f[kPer];
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-          float g[B::PER];
-          uint4 v = make_uint4(0, 0, 0, 0);
-          if (c + i * B::PER < p.n) {
-            v = raw[k][i].get(source.shift);
-            if (c + (i + 1) * B::PER > p.n) {
-              const uint4 m = B::inside(c + i * B::PER, p.n);
-              v.x &= m.x, v.y &= m.y, v.z &= m.z, v.w &= m.w;
-            }
+      for (int i = 0; i < LOADS; ++i) {
+        const int c = at * kPer + i * B::PER;
+        float g[B::PER];
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (c < p.n) {
+          v = raw[i].get(source.shift);
+          if (c + B::PER > p.n) {
+            const uint4 m = B::inside(c, p.n);
+            v.x &= m.x, v.y &= m.y, v.z &= m.z, v.w &= m.w;
           }
-          B::unpack(v, g);
-#pragma unroll
-          for (int j = 0; j < B::PER; ++j) f[i * B::PER + j] = g[j];
         }
-        int e;
-        const uint2 bytes = quantise(f, e);
-        if (row >= p.rows || at >= per_row) continue;
-        p.q[row * per_row + at] = bytes;
-        if ((at & (kShare - 1)) == 0) p.scales[row * p.blocks + at / kShare] = uint8_t(e + 127);
+        B::unpack(v, g);
+#pragma unroll
+        for (int j = 0; j < B::PER; ++j) f[i * B::PER + j] = g[j];
       }
+      int e;
+      const uint2 bytes = quantise(f, e);
+      if (row >= p.rows || at >= per_row) continue;
+      p.q[row * per_row + at] = bytes;
+      if ((at & (kShare - 1)) == 0) p.scales[row * p.blocks + at / kShare] = uint8_t(e + 127);
     }
   }
 }
@@ -193,7 +186,7 @@ __device__ __forceinline__ void singles(const uint64_t (&v)[kPer / 2], float (&f
 
 // Rows that start anywhere are written in blocks of their own address: the bytes of
 // a block lie in two neighbouring words of 8 (4, for fp32), under one scale or two.
-template <typename T, int ACT>
+template <typename T, int ACT, bool ALIGNED>
 __global__ void __launch_bounds__(kThreads) keep8_unpack_kernel(const KeepParams p) {
   using B = Block<T>;
   constexpr int PAIRS = B::PER / 2;
@@ -206,6 +199,18 @@ __global__ void __launch_bounds__(kThreads) keep8_unpack_kernel(const KeepParams
     const uint8_t* const scales = p.scales + row * p.blocks;
     // values c .. c + PER - 1 of the row, in pairs (those outside it are anything)
     auto values = [&](int c, uint64_t (&f)[PAIRS]) {
+      if constexpr (ALIGNED) {                     // whole words under one scale
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(q + c);
+        const uint32_t lo = w[0], hi = B::PER == 8 ? w[B::PER / 4 - 1] : lo;
+        const uint64_t scale = two(power(int(scales[c / kBlock]) - 127));
+        const uint32_t v[4] = {lo, lo >> 16, hi, hi >> 16};
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) {
+          const float2 g = from_e4m3x2(v[i]);
+          f[i] = mul2(two(g.x, g.y), scale);
+        }
+        return;
+      }
       const int first = max(c, 0), last = min(c + B::PER, row_bytes) - 1;       // kept bytes, zeros behind the row's end
       const int w0 = first / 4, w1 = last / 4, at = c >= 0 ? c : first;
       uint32_t w[3];
@@ -235,7 +240,7 @@ __global__ void __launch_bounds__(kThreads) keep8_unpack_kernel(const KeepParams
       }
     };
     auto fill = [&](T* to, bool act) {
-      const int off = B::off(to), blocks = B::count(to, p.n);
+      const int off = ALIGNED ? 0 : B::off(to), blocks = B::count(to, p.n);
       for (int i = x; i < blocks; i += lanes) {
         uint64_t f[PAIRS];
         values(i * B::PER - off, f);
@@ -248,8 +253,8 @@ __global__ void __launch_bounds__(kThreads) keep8_unpack_kernel(const KeepParams
     };
     T* const z = p.z ? static_cast<T*>(p.z) + row * p.ldz : nullptr;
     T* const h = p.h ? static_cast<T*>(p.h) + row * p.ldh : nullptr;
-    if (z && h && B::off(z) == B::off(h)) {        // both from one reading
-      const int off = B::off(z), blocks = B::count(z, p.n);
+    if (z && h && (ALIGNED || B::off(z) == B::off(h))) {       // both from one reading
+      const int off = ALIGNED ? 0 : B::off(z), blocks = B::count(z, p.n);
       for (int i = x; i < blocks; i += lanes) {
         uint64_t f[PAIRS];
         values(i * B::PER - off, f);
@@ -308,18 +313,19 @@ __global__ void __launch_bounds__(kThreads) keep8_unpack_flat_kernel(const KeepP
 }
 
 template <typename T, int ACT>
-const void* unpack_fn(bool flat) {
-  return flat ? reinterpret_cast<const void*>(&keep8_unpack_flat_kernel<T, ACT>)
-              : reinterpret_cast<const void*>(&keep8_unpack_kernel<T, ACT>);
+const void* unpack_fn(bool flat, bool aligned) {
+  if (flat) return reinterpret_cast<const void*>(&keep8_unpack_flat_kernel<T, ACT>);
+  return aligned ? reinterpret_cast<const void*>(&keep8_unpack_kernel<T, ACT, true>)
+                 : reinterpret_cast<const void*>(&keep8_unpack_kernel<T, ACT, false>);
 }
 template <typename T>
-const void* unpack_fn(int act, bool flat) {
+const void* unpack_fn(int act, bool flat, bool aligned) {
   switch (act) {
-    case GOLDY_ACT_RELU: return unpack_fn<T, GOLDY_ACT_RELU>(flat);
-    case GOLDY_ACT_GELU: return unpack_fn<T, GOLDY_ACT_GELU>(flat);
-    case GOLDY_ACT_GELU_TANH: return unpack_fn<T, GOLDY_ACT_GELU_TANH>(flat);
-    case GOLDY_ACT_SILU: return unpack_fn<T, GOLDY_ACT_SILU>(flat);
-    default: return unpack_fn<T, GOLDY_ACT_NONE>(flat);
+    case GOLDY_ACT_RELU: return unpack_fn<T, GOLDY_ACT_RELU>(flat, aligned);
+    case GOLDY_ACT_GELU: return unpack_fn<T, GOLDY_ACT_GELU>(flat, aligned);
+    case GOLDY_ACT_GELU_TANH: return unpack_fn<T, GOLDY_ACT_GELU_TANH>(flat, aligned);
+    case GOLDY_ACT_SILU: return unpack_fn<T, GOLDY_ACT_SILU>(flat, aligned);
+    default: return unpack_fn<T, GOLDY_ACT_NONE>(flat, aligned);
   }
 }
 template <typename T>
@@ -368,12 +374,13 @@ goldy_status run_keep(const goldy_keep8_desc& d, KeepCall& call, bool pack, void
   const int64_t per = 16 / int64_t(element_size(d.dtype));
   auto whole = [&](const void* a, int64_t ld) { return !a || (on_boundary(a, 16) && ld % per == 0); };
   auto packed = [&](const void* a, int64_t ld) { return !a || ld == d.n; };
-  call.flat = whole(p.z_in, d.ldz) && whole(p.z, d.ldz) && whole(p.h, d.ldh) && d.n % kBlock == 0 && packed(p.z_in, d.ldz) && packed(p.z, d.ldz) && packed(p.h, d.ldh);
+  const bool aligned = whole(p.z_in, d.ldz) && whole(p.z, d.ldz) && whole(p.h, d.ldh);
+  call.flat = aligned && d.n % kBlock == 0 && packed(p.z_in, d.ldz) && packed(p.z, d.ldz) && packed(p.h, d.ldh);
   p.pieces = d.rows * (d.n / kPer);
   call.per_thread = pack ? kUnroll : kUnroll / 2;
   const bool f32 = d.dtype == GOLDY_F32;
   if (pack) call.fn = f32 ? pack_fn<uint32_t>(call.flat) : pack_fn<uint16_t>(call.flat);
-  else call.fn = f32 ? unpack_fn<uint32_t>(d.act, call.flat) : unpack_fn<uint16_t>(d.act, call.flat);
+  else call.fn = f32 ? unpack_fn<uint32_t>(d.act, call.flat, aligned) : unpack_fn<uint16_t>(d.act, call.flat, aligned);
   call.stream = stream;
   const goldy_status st = with_layer_context(stream, launch_keep, &call);
   return st == GOLDY_OK ? ok() : st;

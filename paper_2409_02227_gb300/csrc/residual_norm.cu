@@ -348,7 +348,9 @@ residual_norm_forward_kernel(const ResidualNormParams p) {
     float v[VALS], x[VALS];
     R::values(ring + 2 * at * R::RING_BYTES, f_in, row, p.ldf, n, t, v);
     R::values(ring + (2 * at + 1) * R::RING_BYTES, x_in, row, p.ldx, n, t, x);
-    if (R::SHIFT) team_sync<TEAM, THREADS>(team);  // the ring's place is used again: every piece has been read
+    // (SHIFT: the ring's place is used again when every piece has been read, which
+    // the barriers of the norms make sure of, if there is one)
+    if (R::SHIFT && (WARPS == 1 || (p.norm_f == GOLDY_NORM_NONE && p.norm_y == GOLDY_NORM_NONE))) team_sync<TEAM, THREADS>(team);
     at = at + 1 == D ? 0 : at + 1;
     ahead = ahead + 1 == D ? 0 : ahead + 1;
     normalise(p.norm_f, 0, v);
