@@ -39,6 +39,7 @@ class Case:
                  far=0.0, seed=0):
         gen, t = gen_of(rows + n + seed), TYPES[dtype][0]
         rnd = lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731
+        self.stream = 0
         self.rows, self.n, self.t, self.norm_f, self.norm_y, self.alpha = rows, n, t, norm_f, norm_y, alpha
         self.ld, self.start = [n + m for m in more], start
         self.x, self.f = self.new(0, rnd(rows, n) + far), self.new(1, 0.5 * rnd(rows, n) + 0.3 * rnd(n) + far)
@@ -73,7 +74,9 @@ class Case:
     def check_forward(self):
         s, y = self.new(2), self.new(3)
         stats = torch.full((4, self.rows), 55.0, device="cuda")
-        G.goldy_residual_norm_forward(self.d, self.params, self.x.ptr, self.f.ptr, s.ptr, y.ptr if self.norm_y else 0, stats.data_ptr())
+        torch.cuda.synchronize()                            # the call may go to another stream
+        G.goldy_residual_norm_forward(self.d, self.params, self.x.ptr, self.f.ptr, s.ptr, y.ptr if self.norm_y else 0, stats.data_ptr(),
+                                      self.stream)
         torch.cuda.synchronize()
         rs, size_s, ry, size_y, want = self.forward64(self.x.t.double(), self.f.t.double())
         k = steps(self.n) * U
@@ -131,10 +134,11 @@ class Case:
         grads = {k: torch.full((self.n,), 3.0, device="cuda") for k in (names if wanted is None else wanted)}
         need = G.goldy_residual_norm_query(self.d)
         ws = workspace(need)
+        torch.cuda.synchronize()
         G.goldy_residual_norm_backward(self.d, self.params, dy.ptr if self.norm_y else 0, ds.ptr if ds else 0, self.f.ptr, s.ptr,
                                        stats.data_ptr(), dx.ptr, df.ptr,
                                        G.residual_norm_params(**{k: g.data_ptr() for k, g in grads.items()}) if grads else None,
-                                       ws.data_ptr() if grads else 0, need if grads else 0, accumulate=accumulate)
+                                       ws.data_ptr() if grads else 0, need if grads else 0, self.stream, accumulate)
         torch.cuda.synchronize()
         assert not ws[:65536].any()
         return grads
@@ -192,6 +196,19 @@ def test_strides(cuda_ok, n, more, start, dtype):
 def test_rows(cuda_ok, rows):
     Case(rows, 128, "bf16", RMS, LAYER).check_backward()
     Case(rows, 1031, "f32", RMS, RMS).check_backward()
+
+
+@pytest.mark.parametrize("rows,n", [(70, 300), (9, 5000), (5, 9001), (3, 20000)])
+def test_inside_a_partition(cuda_ok, rows, n):
+    """A quarter of the SMs, where long rows are read several times instead of being
+    shared by clusters."""
+    part = G.goldy_partition_create(32, 1)
+    _, (stream,) = G.goldy_partition_query(part, 1)
+    for dtype in ("bf16", "f32"):
+        c = Case(rows, n, dtype, LAYER, RMS)
+        c.stream = stream
+        torch.cuda.synchronize()
+        c.check_backward()
 
 
 def test_many_rows(cuda_ok):
