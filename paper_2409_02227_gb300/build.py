@@ -5,7 +5,8 @@ parallel: ``planner.cpp`` (host C++), ``runtime.cu`` (launch manager),
 ``noalloc.cu`` (the entry point with a compiled-in scratch array),
 ``kernels.cu`` once per GO-Kernel kind (``-DGOLDY_KIND=k``), the layer
 operators (``linear.cu``, ``repack.cu``, ``bias_grad.cu``, ``layernorm.cu``,
-``router.cu``, ``route.cu``, ``residual_norm.cu``, ``keep8.cu``) and
+``router.cu``, ``route.cu``, ``residual_norm.cu``, ``keep8.cu``),
+``residual_norm_kernels.cu`` once per type and direction, and
 ``linear_kernels.cu`` once per pass and activation.  Objects go to
 ``_build/`` next to this file and the library to
 ``paper_2409_02227_gb300/libgoldy.so``; both are git-ignored.  A rebuild is
@@ -60,6 +61,11 @@ def _jobs(ptxas_verbose: bool):
     jobs.append(("ewise", cu + ["-c", os.path.join(CSRC, "ewise.cu")]))
     for name in ("linear", "repack", "bias_grad", "layernorm", "router", "route", "residual_norm", "keep8"):
         jobs.append((name, cu + ["-c", os.path.join(CSRC, name + ".cu")]))
+    for f32 in range(2):
+        for backward in range(2):
+            jobs.append((f"residual_norm_kernels_{'f32' if f32 else 'bf16'}_{'backward' if backward else 'forward'}",
+                         cu + [f"-DGOLDY_NORM_F32={f32}", f"-DGOLDY_NORM_BACKWARD={backward}", "-c",
+                               os.path.join(CSRC, "residual_norm_kernels.cu")]))
     for k, a in LINEAR_KERNELS:
         jobs.append((f"linear_kernels_p{k}_a{a}", cu + [f"-DGOLDY_LINEAR_PASS={k}", f"-DGOLDY_LINEAR_ACT={a}", "-c",
                                                         os.path.join(CSRC, "linear_kernels.cu")]))

@@ -59,7 +59,7 @@ __device__ __forceinline__ float lanes_sum(float v) {
   return v;
 }
 
-// PER parameters from index c on, 0 from n on; VEC: c + PER <= n, on a vector's
+// PER parameters from index c on, 0 from n on and before 0; VEC: c + PER <= n, on a vector's
 // boundary.  Plain loads, as of mean and rstd: the kernel before this one may have
 // written them after this one began, which the read-only data path does not allow.
 template <int PER, bool VEC>
@@ -67,7 +67,7 @@ __device__ __forceinline__ void load_params(const void* p, int f32, int c, int n
   if (!VEC || !p) {
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
-      if (!VEC && c + k >= n) f[k] = 0.0f;
+      if (!VEC && (c + k >= n || c + k < 0)) f[k] = 0.0f;
       else if (!p) f[k] = absent;
       else f[k] = f32 ? static_cast<const float*>(p)[c + k] : load_bf16(p, c + k);
     }
@@ -111,7 +111,10 @@ __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group 
 // backwards 50; in blocks 30 and 55).
 // SURE: the first half of the pieces is inside whatever the row's length, as the
 // host takes the smallest team that holds the row: no tests for those.
-template <typename T, int VALS, int TEAM, int THREADS, bool VEC, bool WIDE>
+// FRAME (with VEC): the row starts `lo` elements behind a block's start, and so do
+// all rows of the team and all arrays; columns are counted from the block's start,
+// n is the row's end in that count, and only its first and last block are not whole.
+template <typename T, int VALS, int TEAM, int THREADS, bool VEC, bool WIDE, bool FRAME = false>
 struct NormRow {
   static constexpr bool SHIFT = !VEC && sizeof(T) == 2;
   static constexpr int PER = VEC ? 16 / int(sizeof(T)) : SHIFT ? 8 : 1;
@@ -119,11 +122,21 @@ struct NormRow {
   static constexpr int PIECE = VEC || SHIFT ? 16 : 4;
   static constexpr int BLOCKS = SLOTS * TEAM + 1;  // SHIFT: of one row
   static constexpr int RING_BYTES = SHIFT ? THREADS / TEAM * BLOCKS * 16 : SLOTS * THREADS * PIECE;   // of one row per team
-  static constexpr int SURE = TEAM > 32 && !WIDE ? SLOTS / 2 : 0;
+  static constexpr int SURE = TEAM > 32 && !WIDE && !FRAME ? SLOTS / 2 : 0;
   static __device__ __forceinline__ int col(int slot, int t) { return (slot * TEAM + t) * PER; }
   static __device__ __forceinline__ bool in(int slot, int t, int n) { return slot < SURE || col(slot, t) < n; }
   static __device__ __forceinline__ bool whole(int slot, int t, int n) {
     return !SHIFT || slot < SURE || col(slot, t) + PER <= n;
+  }
+  // elements lo <= col + k < n of a piece, and how many there are
+  static __device__ __forceinline__ bool inside(int slot, int k, int t, int n, int lo) {
+    return col(slot, t) + k < n && (!FRAME || col(slot, t) + k >= lo);
+  }
+  static __device__ __forceinline__ bool complete(int slot, int t, int n, int lo) {
+    return FRAME ? col(slot, t) >= lo && col(slot, t) + PER <= n : whole(slot, t, n);
+  }
+  static __device__ __forceinline__ int count(int slot, int t, int n, int lo) {
+    return complete(slot, t, n, lo) ? PER : min(col(slot, t) + PER, n) - (FRAME ? max(col(slot, t), lo) : col(slot, t));
   }
   // SHIFT: elements by which a row starts behind a block's start
   static __device__ __forceinline__ int shift(const T* at) { return int(reinterpret_cast<uintptr_t>(at) & 15) / 2; }
@@ -164,7 +177,7 @@ struct NormRow {
                                                 int t, float (&f)[VALS]) {
     values(ring, static_cast<const T*>(base) + row * ld, n, t, f);
   }
-  static __device__ __forceinline__ void values(const uint8_t* ring, const T* at, int n, int t, float (&f)[VALS]) {
+  static __device__ __forceinline__ void values(const uint8_t* ring, const T* at, int n, int t, float (&f)[VALS], int lo = 0) {
     if constexpr (SHIFT) {
       switch (shift(at)) {
         case 0: pick<0>(ring, n, t, f); break;
@@ -192,6 +205,11 @@ struct NormRow {
             o[4 % PER] = bf16_lo(v.z), o[5 % PER] = bf16_hi(v.z), o[6 % PER] = bf16_lo(v.w), o[7 % PER] = bf16_hi(v.w);
           } else {
             o[0] = __uint_as_float(v.x), o[1] = __uint_as_float(v.y), o[2] = __uint_as_float(v.z), o[3] = __uint_as_float(v.w);
+          }
+          if (FRAME && !complete(s, t, n, lo)) {
+#pragma unroll
+            for (int k = 0; k < PER; ++k)
+              if (!inside(s, k, t, n, lo)) o[k] = 0.0f;
           }
         }
       }
@@ -233,7 +251,7 @@ struct NormRow {
   static __device__ __forceinline__ void store(void* base, int64_t row, int64_t ld, int n, int t, const float (&f)[VALS]) {
     store(static_cast<T*>(base) + row * ld, n, t, f);
   }
-  static __device__ __forceinline__ void store(T* at, int n, int t, const float (&f)[VALS]) {
+  static __device__ __forceinline__ void store(T* at, int n, int t, const float (&f)[VALS], int lo = 0) {
     if constexpr (SHIFT) {
       switch (shift(at)) {
         case 0: put<0>(at, n, t, f); break;
@@ -251,7 +269,14 @@ struct NormRow {
         if (!in(s, t, n)) continue;
         T* to = at + col(s, t);
         const float* v = f + s * PER;
-        if (!VEC) {
+        if (FRAME && !complete(s, t, n, lo)) {
+#pragma unroll
+          for (int k = 0; k < PER; ++k) {
+            if (!inside(s, k, t, n, lo)) continue;
+            if (sizeof(T) == 2) store_bf16(to, k, v[k]);
+            else reinterpret_cast<float*>(to)[k] = v[k];
+          }
+        } else if (!VEC) {
           *reinterpret_cast<float*>(to) = v[0];
         } else if (sizeof(T) == 2) {
           __stcs(reinterpret_cast<uint4*>(to), make_uint4(pack_bf16(v[0], v[1 % PER]), pack_bf16(v[2 % PER], v[3 % PER]),
@@ -274,6 +299,21 @@ __device__ __forceinline__ void tell_cluster(float4* to, int rank, int cluster, 
                  : "memory");
   ptx::cluster_sync_all();
 }
+
+// The same from warp to warp: warp w of CTA `rank` tells every CTA of the cluster
+// its value (the same in all lanes), which one barrier later each has in
+// slots[rank][w] of its own shared memory.  Work may lie between the two calls.
+template <int WARPS>
+__device__ __forceinline__ void tell_cluster_begin(float4* slots, int rank, int cluster, int w, int lane, float4 v) {
+  if (lane < cluster)
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(
+                     ptx::map_to_rank(ptx::smem_u32(slots + rank * WARPS + w), uint32_t(lane))),
+                 "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w)
+                 : "memory");
+  __syncwarp();
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tell_cluster_end() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 // Barrier of one team: a warp needs none, the whole CTA has barrier 0.
 template <int TEAM, int THREADS>

@@ -6,6 +6,20 @@
 //   T = dS + N_y'(dY gamma_y),  dX = alpha T,  dF = N_f'(T gate gamma_f)
 //   A = sum over rows of T xhat_f,  B = sum of T,  C = sum of dY xhat_y,  D = sum of dY:
 //   dgate = gamma_f A + beta_f B,  dgamma_f = gate A,  dbeta_f = gate B,  dgamma_y = C,  dbeta_y = D
+//
+// HBM-bound: two arrays are read and two written (backwards four and two), each
+// once.  As in the layer norm, teams of 32 to 512 threads hold rows in registers (16
+// values per thread, backwards 8: four sums per column stay there too) with the
+// next rows on their way into shared memory, and rows too long for a team are
+// shared by clusters.  Forwards the parameters are folded, gate gamma_f and gate
+// beta_f, so that four vectors fit the registers (16384 x 4096 bf16: 89 us, 6.0
+// TB/s).  Backwards the second sums of a row and the first of the next one are
+// exchanged at one barrier (16384 x 2048 bf16: 77 us, 5.2 TB/s; with a barrier for
+// each 110), and the arithmetic is in pairs (one by one: 90); what bounds it is
+// instructions, 16 warps per SM being all that the sums leave room for.  A cluster's
+// warps tell one another their sums directly, and the next row is asked for before
+// the answer is waited for (4096 x 8192 backwards: 104 us; sums joined in each CTA
+// first: 123).  The CTAs' partial rows are summed in CTA order by a second kernel.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -14,47 +28,13 @@
 #include <string>
 #include <utility>
 
-#include "layer_launch.h"
-#include "layer_math.cuh"
-#include "norm_launch.h"
-#include "norm_rows.cuh"
-#include "sm103_ptx.cuh"
+#include "residual_norm_kernel.cuh"
 
 namespace goldy {
 namespace {
 
 constexpr int kStreamThreads = 512;
 constexpr int kBwdCtas = 152;          // CTAs of a backward launch, at most: one partial row each
-constexpr int kSums = 4;               // A, B, C, D
-
-struct ResidualNormParams {
-  const void* x;
-  const void* f;
-  const void* dy;            // backward, null without a norm
-  const void* ds;            // may be null
-  const void* s_in;          // backward
-  void* s;                   // S, or dX
-  void* y;                   // Y, or dF
-  const void* gate;
-  const void* gamma_f;
-  const void* beta_f;
-  const void* gamma_y;
-  const void* beta_y;
-  float* stats;              // [4][rows], may be null forwards
-  float* part;               // backward: [CTA][kSums][n]
-  int64_t rows, ldx, ldf, lds, ldy;
-  int32_t n, param_f32, norm_f, norm_y;
-  float eps, alpha, inv_n;
-  int32_t cluster;           // CTAs that share a row, each with `seg` of its columns (the last with the rest)
-  int32_t seg;
-  // the parameters' gradients (backward)
-  float* dgate;
-  float* dgamma_f;
-  float* dbeta_f;
-  float* dgamma_y;
-  float* dbeta_y;
-  int32_t accumulate, parts;
-};
 
 template <typename T>
 __device__ __forceinline__ float elem(const void* base, int64_t i) {
@@ -199,429 +179,7 @@ __global__ void __launch_bounds__(kStreamThreads) residual_norm_backward_stream_
   }
 }
 
-// ---- rows in registers ----------------------------------------------------------
-
-constexpr int kMaxTeam = 512;
-constexpr int kFwdThreads = 256;       // per CTA, at least the team
-constexpr int kBwdThreads = 512;
-constexpr int kFwdVals = 16;           // values of a row per thread
-constexpr int kBwdVals = 8;
-constexpr int kFwdDepth = 3;           // rows in a thread's ring
-// (backwards a row's F and dS stay until the row after it has come in)
-template <typename T> __host__ __device__ constexpr int bwd_depth() { return sizeof(T) == 2 ? 4 : 3; }
-
-// The parameters' gradients of column c from its four sums.
-__device__ __forceinline__ void give_gradients(const ResidualNormParams& p, int64_t c, float a, float b, float cc, float d) {
-  const float gate = param_at(p.gate, p.param_f32, int(c), 1.0f);
-  auto give = [&](float* to, float g) {
-    if (to) to[c] = p.accumulate ? to[c] + g : g;
-  };
-  give(p.dgate, fmaf(param_at(p.gamma_f, p.param_f32, int(c), 1.0f), a, param_at(p.beta_f, p.param_f32, int(c), 0.0f) * b));
-  give(p.dgamma_f, gate * a);
-  give(p.dbeta_f, gate * b);
-  give(p.dgamma_y, cc);
-  give(p.dbeta_y, d);
-}
-
-template <typename T, int TEAM, bool VEC, bool WIDE>
-__global__ void __launch_bounds__(TEAM > kFwdThreads ? TEAM : kFwdThreads, TEAM > kFwdThreads ? 1 : 2)
-residual_norm_forward_kernel(const ResidualNormParams p) {
-  constexpr int THREADS = TEAM > kFwdThreads ? TEAM : kFwdThreads, TEAMS = THREADS / TEAM, VALS = kFwdVals;
-  constexpr int WARPS = TEAM / 32, D = kFwdDepth;
-  using R = NormRow<T, VALS, TEAM, THREADS, VEC, WIDE>;
-  __shared__ float4 slot[2][2][TEAMS][WARPS];      // per row, norm and warp: sum, M2, elements, mean
-  __shared__ float4 part[2][2][WIDE ? kMaxCluster : 1];
-  extern __shared__ __align__(16) uint8_t ring[];  // D rows of F, D of X
-  const int team = threadIdx.x / TEAM, t = threadIdx.x % TEAM, w = t >> 5, lane = t & 31;
-  // WIDE: this CTA's n columns from c0 on, of rows that a cluster shares
-  const int rank = WIDE ? int(ptx::cluster_ctarank()) : 0, c0 = WIDE ? rank * p.seg : 0;
-  const int n = WIDE ? min(p.seg, p.n - c0) : p.n;
-  const int group = WIDE ? int(blockIdx.x) / p.cluster : int(blockIdx.x);
-  const int groups = WIDE ? int(gridDim.x) / p.cluster : int(gridDim.x);
-  const T* const f_in = static_cast<const T*>(p.f) + c0;
-  const T* const x_in = static_cast<const T*>(p.x) + c0;
-  T* const s_out = static_cast<T*>(p.s) + c0;
-  T* const y_out = static_cast<T*>(p.y) + c0;
-  if (WIDE) ptx::cluster_sync_all();               // the others have started
-  ptx::griddep_launch_dependents();
-  ptx::griddep_wait();
-  const int64_t step = int64_t(groups) * TEAMS;
-  int64_t row = int64_t(group) * TEAMS + team;
-  if (row >= p.rows) return;                       // whole teams only
-  auto fetch = [&](int d, int64_t r) {
-    if (r < p.rows) {
-      R::fetch(ring + 2 * d * R::RING_BYTES, f_in, r, p.ldf, n, t);
-      R::fetch(ring + (2 * d + 1) * R::RING_BYTES, x_in, r, p.ldx, n, t);
-    }
-    copy_commit();
-  };
-#pragma unroll
-  for (int d = 0; d < D - 1; ++d) fetch(d, row + d * step);
-  // gate * N_f(v) = xhat * a + b: two parameters instead of three
-  float a[VALS], b[VALS], gamma[VALS], beta[VALS];
-  int mine = 0;                                    // values this thread has
-#pragma unroll
-  for (int i = 0; i < R::SLOTS; ++i) {
-    if (!R::in(i, t, n)) {
-#pragma unroll
-      for (int k = i * R::PER; k < (i + 1) * R::PER; ++k) a[k] = b[k] = gamma[k] = beta[k] = 0.0f;
-      continue;
-    }
-    const int c = c0 + R::col(i, t), k0 = i * R::PER;
-    load_params<R::PER, VEC>(p.gate, p.param_f32, c, c0 + n, 1.0f, gamma + k0);
-    load_params<R::PER, VEC>(p.gamma_f, p.param_f32, c, c0 + n, 1.0f, a + k0);
-    load_params<R::PER, VEC>(p.beta_f, p.param_f32, c, c0 + n, 0.0f, b + k0);
-#pragma unroll
-    for (int k = k0; k < k0 + R::PER; ++k) a[k] *= gamma[k], b[k] *= gamma[k];
-    load_params<R::PER, VEC>(p.gamma_y, p.param_f32, c, c0 + n, 1.0f, gamma + k0);
-    load_params<R::PER, VEC>(p.beta_y, p.param_f32, c, c0 + n, 0.0f, beta + k0);
-    mine += R::whole(i, t, n) ? R::PER : n - R::col(i, t);
-  }
-  const float warp_n = warp_sum(float(mine));
-  const float warp_inv = warp_n > 0.0f ? 1.0f / warp_n : 0.0f;
-  int at = 0, ahead = D - 1;                       // ring places of this row and of the one fetched now
-  for (int flip = 0; row < p.rows; row += step, flip ^= 1) {
-    // xhat of the values in v, which are 0 outside the row and stay 0 there
-    // (a layer norm's as differences from the warp's mean first)
-    auto normalise = [&](int kind, int which, float (&v)[VALS]) {
-      if (kind == GOLDY_NORM_NONE) return;
-      float s = 0.0f, wm = 0.0f;
-      if (kind == GOLDY_NORM_LAYER) {
-#pragma unroll
-        for (int j = 0; j < VALS; ++j) s += v[j];
-        s = warp_sum(s);
-        wm = s * warp_inv;
-#pragma unroll
-        for (int i = 0; i < R::SLOTS; ++i) {
-          if (!R::in(i, t, n)) continue;
-#pragma unroll
-          for (int k = 0; k < R::PER; ++k) {
-            float& e = v[i * R::PER + k];
-            e = R::whole(i, t, n) || R::col(i, t) + k < n ? e - wm : 0.0f;
-          }
-        }
-      }
-      float m2 = 0.0f;
-#pragma unroll
-      for (int j = 0; j < VALS; ++j) m2 = fmaf(v[j], v[j], m2);
-      m2 = warp_sum(m2);
-      float mean = wm;
-      if (WARPS > 1) {
-        if (lane == 0) slot[flip][which][team][w] = make_float4(s, m2, warp_n, wm);
-        team_sync<TEAM, THREADS>(team);
-        const float4 o = slot[flip][which][team][lane & (WARPS - 1)];
-        float total = 0.0f;
-        if (kind == GOLDY_NORM_LAYER) {
-          total = lanes_sum<WARPS>(o.x);
-          mean = total * (WIDE ? 1.0f / float(n) : p.inv_n);
-        }
-        const float d = o.w - mean;
-        m2 = lanes_sum<WARPS>(fmaf(o.z * d, d, o.y));
-        if (WIDE) {                                // the same once more, over the cluster's CTAs in order
-          tell_cluster(part[flip][which], rank, p.cluster, make_float4(total, m2, float(n), mean));
-          float all = 0.0f;
-          for (int k = 0; k < p.cluster; ++k) all += part[flip][which][k].x;
-          mean = all * p.inv_n;
-          m2 = 0.0f;
-          for (int k = 0; k < p.cluster; ++k) {
-            const float4 q = part[flip][which][k];
-            const float e = q.w - mean;
-            m2 += fmaf(q.z * e, e, q.y);
-          }
-        }
-      }
-      const float rstd = rsqrtf(fmaf(m2, p.inv_n, p.eps)), shift = (wm - mean) * rstd;
-#pragma unroll
-      for (int i = 0; i < R::SLOTS; ++i) {
-        if (!R::in(i, t, n)) continue;
-#pragma unroll
-        for (int j = i * R::PER; j < (i + 1) * R::PER; ++j) v[j] = fmaf(v[j], rstd, shift);
-      }
-      if (t == 0 && rank == 0 && p.stats) {
-        if (kind == GOLDY_NORM_LAYER) p.stats[2 * which * p.rows + row] = mean;
-        p.stats[(2 * which + 1) * p.rows + row] = rstd;
-      }
-    };
-    fetch(ahead, row + (D - 1) * step);
-    copy_wait<D - 1>();
-    if (R::SHIFT) team_sync<TEAM, THREADS>(team);
-    float v[VALS], x[VALS];
-    R::values(ring + 2 * at * R::RING_BYTES, f_in, row, p.ldf, n, t, v);
-    R::values(ring + (2 * at + 1) * R::RING_BYTES, x_in, row, p.ldx, n, t, x);
-    // (SHIFT: the ring's place is used again when every piece has been read, which
-    // the barriers of the norms make sure of, if there is one)
-    if (R::SHIFT && (WARPS == 1 || (p.norm_f == GOLDY_NORM_NONE && p.norm_y == GOLDY_NORM_NONE))) team_sync<TEAM, THREADS>(team);
-    at = at + 1 == D ? 0 : at + 1;
-    ahead = ahead + 1 == D ? 0 : ahead + 1;
-    normalise(p.norm_f, 0, v);
-#pragma unroll
-    for (int j = 0; j < VALS; ++j) v[j] = fmaf(v[j], a[j], fmaf(p.alpha, x[j], b[j]));
-    R::store(s_out, row, p.lds, n, t, v);
-    if (p.norm_y == GOLDY_NORM_NONE) continue;
-    normalise(p.norm_y, 1, v);
-#pragma unroll
-    for (int j = 0; j < VALS; ++j) v[j] = fmaf(v[j], gamma[j], beta[j]);
-    R::store(y_out, row, p.ldy, n, t, v);
-  }
-}
-
-// FULL: both norms and dS are there.
-template <typename T, int TEAM, bool VEC, bool WIDE, bool FULL>
-__global__ void __launch_bounds__(kBwdThreads) residual_norm_backward_kernel(const ResidualNormParams p) {
-  constexpr int TEAMS = kBwdThreads / TEAM, WARPS = TEAM / 32, VALS = kBwdVals, D = bwd_depth<T>();
-  using R = NormRow<T, VALS, TEAM, kBwdThreads, VEC, WIDE>;
-  __shared__ float4 slot[2][TEAMS][WARPS];
-  __shared__ float4 part[2][WIDE ? kMaxCluster : 1];
-  extern __shared__ __align__(16) uint8_t ring[];  // D rows of F, S, dY and dS each; at the end the CTA's sums
-  const int team = threadIdx.x / TEAM, t = threadIdx.x % TEAM, w = t >> 5, lane = t & 31;
-  const int rank = WIDE ? int(ptx::cluster_ctarank()) : 0, c0 = WIDE ? rank * p.seg : 0;
-  const int n = WIDE ? min(p.seg, p.n - c0) : p.n;
-  const int group = WIDE ? int(blockIdx.x) / p.cluster : int(blockIdx.x);
-  const int groups = WIDE ? int(gridDim.x) / p.cluster : int(gridDim.x);
-  const T* const f_in = static_cast<const T*>(p.f) + c0;
-  const T* const s_in = static_cast<const T*>(p.s_in) + c0;
-  const T* const dy_in = static_cast<const T*>(p.dy) + c0;
-  const T* const ds_in = static_cast<const T*>(p.ds) + c0;
-  T* const dx_out = static_cast<T*>(p.s) + c0;
-  T* const df_out = static_cast<T*>(p.y) + c0;
-  const bool has_y = FULL || p.norm_y != GOLDY_NORM_NONE, has_f = FULL || p.norm_f != GOLDY_NORM_NONE;
-  const bool has_ds = FULL || p.ds != nullptr;
-  const float layer_f = p.norm_f == GOLDY_NORM_LAYER ? p.inv_n : 0.0f, layer_y = p.norm_y == GOLDY_NORM_LAYER ? p.inv_n : 0.0f;
-  if (WIDE) ptx::cluster_sync_all();               // the others have started
-  ptx::griddep_launch_dependents();
-  ptx::griddep_wait();
-  const int64_t step = int64_t(groups) * TEAMS, row0 = int64_t(group) * TEAMS + team;
-  int left = row0 < p.rows ? int((p.rows - row0 - 1) / step) + 1 : 0;    // rows of this team (memory holds fewer than 2^31)
-  // pointers run along: of the row fetched next, of the row whose dX and dF are next
-  const T* f_at = f_in + row0 * p.ldf;
-  const T* s_at = s_in + row0 * p.lds;
-  const T* dy_at = dy_in + row0 * p.ldy;
-  const T* ds_at = ds_in + row0 * p.lds;
-  T* dx_at = dx_out + row0 * p.ldx;
-  T* df_at = df_out + row0 * p.ldf;
-  const int64_t step_f = step * p.ldf, step_s = step * p.lds, step_y = step * p.ldy, step_x = step * p.ldx;
-  auto fetch = [&](int d, bool there) {
-    if (there) {
-      uint8_t* to = ring + 4 * d * R::RING_BYTES;
-      R::fetch(to, f_at, n, t);
-      if (has_y) {
-        R::fetch(to + R::RING_BYTES, s_at, n, t);
-        R::fetch(to + 2 * R::RING_BYTES, dy_at, n, t);
-      }
-      if (has_ds) R::fetch(to + 3 * R::RING_BYTES, ds_at, n, t);
-    }
-    f_at += step_f;
-    s_at += step_s;
-    dy_at += step_y;
-    ds_at += step_s;
-    copy_commit();
-  };
-  // a row's statistics, one per lane: mean and rstd of N_f, of N_y
-  const int which = lane & 3;
-  const bool mine = which == 0 ? p.norm_f == GOLDY_NORM_LAYER : which == 1 ? has_f : which == 2 ? p.norm_y == GOLDY_NORM_LAYER : has_y;
-  const float* stats_at = p.stats + which * p.rows + row0;
-  auto next_stats = [&](bool there) {
-    const float v = mine && there ? *stats_at : float(which & 1);
-    stats_at += step;
-    return v;
-  };
-  auto stat = [&](float v, int q) { return __shfl_sync(0xFFFFFFFFu, v, q); };
-#pragma unroll
-  for (int d = 0; d < D - 1; ++d) fetch(d, left > d);
-  float now = next_stats(left > 0), next = next_stats(left > 1);
-  // values in pairs: half the instructions
-  constexpr int PAIRS = VALS / 2;
-  uint64_t gf[PAIRS], gy[PAIRS], sum[kSums][PAIRS];      // gate * gamma_f, gamma_y; 0 outside the row
-  {
-    float a[VALS], b[VALS], c[VALS];
-#pragma unroll
-    for (int i = 0; i < R::SLOTS; ++i) {
-      const int k0 = i * R::PER, at = c0 + R::col(i, t);
-      if (R::in(i, t, n)) {
-        load_params<R::PER, VEC>(p.gate, p.param_f32, at, c0 + n, 1.0f, a + k0);
-        load_params<R::PER, VEC>(p.gamma_f, p.param_f32, at, c0 + n, 1.0f, b + k0);
-        load_params<R::PER, VEC>(p.gamma_y, p.param_f32, at, c0 + n, 1.0f, c + k0);
-      } else {
-#pragma unroll
-        for (int k = k0; k < k0 + R::PER; ++k) a[k] = b[k] = c[k] = 0.0f;
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < PAIRS; ++j) {
-      gf[j] = mul2(two(a[2 * j], a[2 * j + 1]), two(b[2 * j], b[2 * j + 1]));
-      gy[j] = two(c[2 * j], c[2 * j + 1]);
-#pragma unroll
-      for (int q = 0; q < kSums; ++q) sum[q][j] = two(0.0f);
-    }
-  }
-  // A row takes two sums one after the other: (1) of dY gamma_y and its product
-  // with xhat_y, which T needs, (2) of T gate gamma_f and its product with xhat_f,
-  // which dF needs.  The second ones of a row and the first ones of the next row
-  // are exchanged together: one barrier per row, and each phase has another row's
-  // arithmetic beside it.
-  uint64_t g[PAIRS], hy[PAIRS], u[PAIRS], h[PAIRS];
-  float s1x, s1y, s2x = 0.0f, s2y = 0.0f;          // partial sums, then the rows'
-  auto both = [](uint64_t v) {
-    const float2 f = apart(v);
-    return f.x + f.y;
-  };
-  float ry = 1.0f;                                 // rstd of N_y of the row that first() has seen
-  int64_t row = row0;                              // (SHIFT: whose rows start anywhere)
-  auto first = [&](const uint8_t* from, bool there, int64_t r, float st) {
-    s1x = s1y = 0.0f;
-    if (!has_y || !there) return;
-    float v[VALS], d[VALS];
-    R::values(from + R::RING_BYTES, R::SHIFT ? s_in + r * p.lds : nullptr, n, t, v);
-    R::values(from + 2 * R::RING_BYTES, R::SHIFT ? dy_in + r * p.ldy : nullptr, n, t, d);
-    ry = stat(st, 3);
-    // the mean is subtracted before the scale: rows far from zero keep their
-    // digits; columns outside the row have dY = gamma = 0 and add nothing
-    const uint64_t off = two(-stat(st, 2)), scale = two(ry);
-    uint64_t a = two(0.0f), b = a;
-#pragma unroll
-    for (int j = 0; j < PAIRS; ++j) {
-      hy[j] = mul2(add2(two(v[2 * j], v[2 * j + 1]), off), scale);
-      const uint64_t dy = two(d[2 * j], d[2 * j + 1]);
-      sum[2][j] = fma2(dy, hy[j], sum[2][j]);
-      sum[3][j] = add2(sum[3][j], dy);
-      g[j] = mul2(dy, gy[j]);
-      a = add2(a, g[j]);
-      b = fma2(g[j], hy[j], b);
-    }
-    s1x = both(a);
-    s1y = both(b);
-  };
-  auto exchange = [&](int flip) {
-    const float4 v = warp_sum4(s1x, s1y, s2x, s2y, lane, WARPS > 1 ? reinterpret_cast<float*>(&slot[flip][team][w]) : nullptr);
-    float4 r = v;
-    if (WARPS > 1) {
-      team_sync<TEAM, kBwdThreads>(team);
-      if (WARPS <= 4) {
-        r = slot[flip][team][0];
-#pragma unroll
-        for (int k = 1; k < WARPS; ++k) {
-          const float4 o = slot[flip][team][k];
-          r.x += o.x, r.y += o.y, r.z += o.z, r.w += o.w;
-        }
-      } else {
-        const float4 o = slot[flip][team][lane & (WARPS - 1)];
-        r = make_float4(lanes_sum<WARPS>(o.x), lanes_sum<WARPS>(o.y), lanes_sum<WARPS>(o.z), lanes_sum<WARPS>(o.w));
-      }
-      if (WIDE) {
-        tell_cluster(part[flip], rank, p.cluster, r);
-        r = part[flip][0];
-        for (int k = 1; k < p.cluster; ++k) {
-          const float4 o = part[flip][k];
-          r.x += o.x, r.y += o.y, r.z += o.z, r.w += o.w;
-        }
-      }
-    } else if (R::SHIFT) {
-      __syncwarp();
-    }
-    s1x = r.x, s1y = r.y, s2x = r.z, s2y = r.w;
-  };
-  float last_rf = 0.0f;                            // of the row whose dF is left
-  auto finish = [&]() {
-    const uint64_t less = two(-s2x * layer_f * last_rf), slope = two(-s2y * p.inv_n * last_rf), scale = two(last_rf);
-    float v[VALS];
-#pragma unroll
-    for (int j = 0; j < PAIRS; ++j) {
-      const float2 f = apart(has_f ? fma2(h[j], slope, fma2(u[j], scale, less)) : u[j]);
-      v[2 * j] = f.x;
-      v[2 * j + 1] = f.y;
-    }
-    R::store(df_at, n, t, v);
-    df_at += step_f;
-  };
-  int at = 0, ahead = D - 1;
-  bool begun = false;
-  if (left > 0) {                                  // whole teams, and whole clusters
-    copy_wait<D - 2>();
-    if (R::SHIFT) team_sync<TEAM, kBwdThreads>(team);
-    first(ring, true, row, now);
-    exchange(1);
-  }
-  for (int flip = 0; left > 0; --left, row += step, flip ^= 1) {
-    fetch(ahead, left > D - 1);                    // where the row before this one was
-    const float later = next_stats(left > 2);
-    copy_wait<D - 2>();
-    if (R::SHIFT) team_sync<TEAM, kBwdThreads>(team);
-    if (begun) finish();
-    begun = true;
-    // T, dX, and what dF needs
-    const uint8_t* from = ring + 4 * at * R::RING_BYTES;
-    at = at + 1 == D ? 0 : at + 1;
-    ahead = ahead + 1 == D ? 0 : ahead + 1;
-    float tt[VALS], v[VALS];
-    if (has_ds) {
-      R::values(from + 3 * R::RING_BYTES, R::SHIFT ? ds_in + row * p.lds : nullptr, n, t, tt);
-    } else {
-#pragma unroll
-      for (int j = 0; j < VALS; ++j) tt[j] = 0.0f;
-    }
-    R::values(from, R::SHIFT ? f_in + row * p.ldf : nullptr, n, t, v);
-    last_rf = stat(now, 1);
-    const uint64_t less = two(-s1x * layer_y * ry), slope = two(-s1y * p.inv_n * ry), by = two(ry);
-    const uint64_t off = two(-stat(now, 0)), scale = two(last_rf), alpha = two(p.alpha);
-    uint64_t a = two(0.0f), b = a;
-#pragma unroll
-    for (int j = 0; j < PAIRS; ++j) {
-      uint64_t d = two(tt[2 * j], tt[2 * j + 1]);
-      if (has_y) d = add2(d, fma2(hy[j], slope, fma2(g[j], by, less)));
-      h[j] = mul2(add2(two(v[2 * j], v[2 * j + 1]), off), scale);
-      sum[0][j] = fma2(d, h[j], sum[0][j]);
-      sum[1][j] = add2(sum[1][j], d);
-      u[j] = mul2(d, gf[j]);
-      a = add2(a, u[j]);
-      b = fma2(u[j], h[j], b);
-      const float2 f = apart(mul2(d, alpha));
-      tt[2 * j] = f.x;
-      tt[2 * j + 1] = f.y;
-    }
-    s2x = both(a);
-    s2y = both(b);
-    R::store(dx_at, n, t, tt);
-    dx_at += step_x;
-    now = next;
-    next = later;
-    first(ring + 4 * at * R::RING_BYTES, left > 1, row + step, now);
-    exchange(flip);
-  }
-  if (begun) finish();
-  if (!p.part) return;
-  // the teams' sums go through shared memory, in column order, to be added in
-  // team order
-  float* sums = reinterpret_cast<float*>(ring);    // [teams][kSums][column]
-  constexpr int ALL = TEAM * VALS;
-  copy_wait<0>();
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < R::SLOTS; ++i)
-#pragma unroll
-    for (int q = 0; q < kSums; ++q)
-#pragma unroll
-      for (int k = 0; k < R::PER; ++k) {
-        const float2 f = apart(sum[q][(i * R::PER + k) / 2]);
-        sums[(team * kSums + q) * ALL + R::col(i, t) + k] = (i * R::PER + k) & 1 ? f.y : f.x;
-      }
-  __syncthreads();
-  float* to = p.part + int64_t(group) * kSums * p.n + c0;
-  for (int c = threadIdx.x; c < n; c += kBwdThreads) {
-    float v[kSums];
-#pragma unroll
-    for (int q = 0; q < kSums; ++q) {
-      v[q] = 0.0f;
-#pragma unroll
-      for (int k = 0; k < TEAMS; ++k) v[q] += sums[(k * kSums + q) * ALL + c];
-    }
-    if (groups > 1) {
-#pragma unroll
-      for (int q = 0; q < kSums; ++q) __stcg(to + int64_t(q) * p.n + c, v[q]);
-    } else {                                       // this CTA's sums are the result
-      give_gradients(p, c0 + c, v[0], v[1], v[2], v[3]);
-    }
-  }
-}
+// ---- gradients of the parameters --------------------------------------------------
 
 // The parameters' gradients from the CTAs' partial rows, in CTA order: of 32
 // columns, eight warps per sum take every eighth row, all in flight together, and
@@ -657,15 +215,15 @@ __global__ void __launch_bounds__(kSums * kReduceWarps * 32) residual_norm_reduc
 
 // ---- host ---------------------------------------------------------------------
 
-// Threads per row; 0: the row streams.  `cluster` CTAs of kMaxTeam threads share
-// a row that is too long for one.
-struct NormShape {
-  int team, cluster, seg;
-};
-NormShape shape_for(const goldy_residual_norm_desc& d, bool backward) {
+ResidualNormShape shape_for(const goldy_residual_norm_desc& d, bool backward, bool framed) {
   const int64_t vals = backward ? kBwdVals : kFwdVals;
+  // (a framed row begins inside its first block)
+  const int64_t wide = d.n + (framed ? 16 / int64_t(element_size(d.dtype)) - 1 : 0);
   int team = 32;
-  while (team < kMaxTeam && team * vals < d.n) team *= 2;
+  while (team < kMaxTeam && team * vals < wide) team *= 2;
+  // one that the few elements more would give half-empty teams does not pay (1000
+  // rows of 1023 in fp32 backwards: 16 us, otherwise 14)
+  if (framed) return team * vals < wide || (team > 32 && team / 2 * vals >= d.n) ? ResidualNormShape{0, 1, 0} : ResidualNormShape{team, 1, int(wide)};
   int cluster = 1;
   while (cluster < kMaxCluster && cluster * team * vals < d.n) cluster *= 2;
   if (cluster * team * vals < d.n) return {0, 1, 0};
@@ -679,46 +237,17 @@ int64_t stream_parts(const goldy_residual_norm_desc& d) {
 // Rows per team up to which one CTA does them all: a further kernel that sums
 // partial rows costs more.
 constexpr int kAloneRows = 2;
-int64_t team_parts(const goldy_residual_norm_desc& d, const NormShape& s) {
+int64_t team_parts(const goldy_residual_norm_desc& d, const ResidualNormShape& s) {
   const int64_t teams = s.cluster > 1 ? 1 : kBwdThreads / s.team;
   if (d.rows <= kAloneRows * teams) return 1;      // no second kernel
   return std::min<int64_t>(kBwdCtas / s.cluster, ceil_div(d.rows, teams));
 }
 size_t backward_bytes(const goldy_residual_norm_desc& d) {
-  const NormShape s = shape_for(d, true);
+  const ResidualNormShape s = shape_for(d, true, false), f = shape_for(d, true, true);
   // (inside an SM partition rows stream where clusters would share them)
-  const int64_t parts = s.team == 0 || s.cluster > 1 ? stream_parts(d) : team_parts(d, s);
+  int64_t parts = s.team == 0 || s.cluster > 1 ? stream_parts(d) : team_parts(d, s);
+  if (f.team > 0) parts = std::max(parts, team_parts(d, f));
   return kLayerCounterBytes + size_t(parts) * kSums * size_t(d.n) * sizeof(float);
-}
-
-template <typename T, int TEAM, bool VEC, bool WIDE = false>
-NormKernel pick(bool backward, bool full) {
-  if (backward) {
-    using R = NormRow<T, kBwdVals, TEAM, kBwdThreads, VEC, WIDE>;
-    return {full ? reinterpret_cast<const void*>(&residual_norm_backward_kernel<T, TEAM, VEC, WIDE, VEC>)
-                 : reinterpret_cast<const void*>(&residual_norm_backward_kernel<T, TEAM, VEC, WIDE, false>), kBwdThreads,
-            kBwdThreads / TEAM, 1,
-            std::max(size_t(4) * bwd_depth<T>() * R::RING_BYTES, size_t(kSums) * kBwdThreads * kBwdVals * sizeof(float))};
-  }
-  constexpr int THREADS = TEAM > kFwdThreads ? TEAM : kFwdThreads;
-  using R = NormRow<T, kFwdVals, TEAM, THREADS, VEC, WIDE>;
-  return {reinterpret_cast<const void*>(&residual_norm_forward_kernel<T, TEAM, VEC, WIDE>), THREADS, THREADS / TEAM,
-          TEAM > kFwdThreads ? 1 : 2, size_t(2) * kFwdDepth * R::RING_BYTES};
-}
-template <typename T, bool VEC>
-NormKernel pick_shape(const NormShape& s, bool backward, bool full) {
-  if (s.cluster > 1) return pick<T, kMaxTeam, VEC, true>(backward, full);
-  switch (s.team) {
-    case 32: return pick<T, 32, VEC>(backward, full);
-    case 64: return pick<T, 64, VEC>(backward, full);
-    case 128: return pick<T, 128, VEC>(backward, full);
-    case 256: return pick<T, 256, VEC>(backward, full);
-    case 512: return pick<T, 512, VEC>(backward, full);
-    default:
-      return {backward ? reinterpret_cast<const void*>(&residual_norm_backward_stream_kernel<T>)
-                       : reinterpret_cast<const void*>(&residual_norm_forward_stream_kernel<T>),
-              kStreamThreads, 1, 4, 0};
-  }
 }
 
 bool is_kind(int k) { return k == GOLDY_NORM_NONE || k == GOLDY_NORM_LAYER || k == GOLDY_NORM_RMS; }
@@ -754,44 +283,71 @@ goldy_status check_params(const goldy_residual_norm_desc& d, const goldy_residua
 struct ResidualNormCall {
   ResidualNormParams p;
   const goldy_residual_norm_desc* d;
-  bool backward, vec;
+  bool backward;
+  RowMode mode;
+  int period;            // framed rows: that many rows apart they begin alike
   void* stream;
 };
+
+NormKernel kernel_for(const ResidualNormCall& call, const ResidualNormShape& shape, RowMode mode) {
+  const goldy_residual_norm_desc& d = *call.d;
+  const bool f32 = d.dtype == GOLDY_F32, full = d.norm_f != GOLDY_NORM_NONE && d.norm_y != GOLDY_NORM_NONE && call.p.ds;
+  if (shape.team == 0)
+    return {call.backward ? (f32 ? reinterpret_cast<const void*>(&residual_norm_backward_stream_kernel<float>)
+                                 : reinterpret_cast<const void*>(&residual_norm_backward_stream_kernel<uint16_t>))
+                          : (f32 ? reinterpret_cast<const void*>(&residual_norm_forward_stream_kernel<float>)
+                                 : reinterpret_cast<const void*>(&residual_norm_forward_stream_kernel<uint16_t>)),
+            kStreamThreads, 1, 4, 0};
+  if (call.backward)
+    return f32 ? residual_norm_backward_f32(shape, mode, full) : residual_norm_backward_bf16(shape, mode, full);
+  return f32 ? residual_norm_forward_f32(shape, mode) : residual_norm_forward_bf16(shape, mode);
+}
+
+// CTAs, or clusters of them, all resident (`cap` are), every team with rows of its own
+int64_t groups_for(const ResidualNormCall& call, const ResidualNormShape& shape, const NormKernel& k, int64_t cap) {
+  const goldy_residual_norm_desc& d = *call.d;
+  int64_t groups = std::min(cap, ceil_div(d.rows, int64_t(k.teams)));
+  if (call.backward) groups = shape.team == 0 ? stream_parts(d) : team_parts(d, shape);
+  if (shape.cluster > 1) groups = std::min(groups, cap);
+  return std::max<int64_t>(1, groups);
+}
 
 goldy_status launch_residual_norm(const LayerContext& ctx, void* arg) {
   ResidualNormCall& call = *static_cast<ResidualNormCall*>(arg);
   const goldy_residual_norm_desc& d = *call.d;
-  NormShape shape = shape_for(d, call.backward);
-  // which SMs a partition has, and so whether a cluster fits into it, is not known
-  if (!ctx.whole && shape.cluster > 1) shape = {0, 1, 0};
-  const int cluster = shape.cluster;
-  NormKernel k;
-  const bool full = call.vec && d.norm_f != GOLDY_NORM_NONE && d.norm_y != GOLDY_NORM_NONE && call.p.ds;
-  if (d.dtype == GOLDY_F32)
-    k = call.vec ? pick_shape<float, true>(shape, call.backward, full) : pick_shape<float, false>(shape, call.backward, full);
-  else
-    k = call.vec ? pick_shape<uint16_t, true>(shape, call.backward, full)
-                 : pick_shape<uint16_t, false>(shape, call.backward, full);
+  RowMode mode = call.mode;
+  ResidualNormShape shape = shape_for(d, call.backward, mode == kFramedRows);
+  NormKernel k = kernel_for(call, shape, mode);
+  int64_t groups = 0;
+  if (mode == kFramedRows && shape.team > 0) {
+    groups = groups_for(call, shape, k, int64_t(ctx.sm_count) * k.per_sm);
+    // a team with several rows has them a whole number of periods apart
+    while (groups > 0 && groups * k.teams < d.rows && groups * k.teams % call.period != 0) --groups;
+  }
+  if (groups == 0) {
+    if (mode == kFramedRows) mode = kAnyRows;
+    shape = shape_for(d, call.backward, false);
+    // which SMs a partition has, and so whether a cluster fits into it, is not known
+    if (!ctx.whole && shape.cluster > 1) shape = {0, 1, 0};
+    k = kernel_for(call, shape, mode);
+    int64_t cap = int64_t(ctx.sm_count) * k.per_sm;            // CTAs, or clusters, resident at once
+    if (shape.cluster > 1) {
+      cudaError_t e = allow_smem(ctx.device, k);
+      int most = 0;
+      if (e == cudaSuccess) e = resident_clusters(ctx.device, k, shape.cluster, &most);
+      if (e == cudaSuccess && most < 1) e = cudaErrorInvalidClusterSize;
+      if (e != cudaSuccess) return fail(GOLDY_ERR_CUDA, std::string("residual norm, clusters: ") + cudaGetErrorString(e));
+      cap = std::min<int64_t>(cap / shape.cluster, most);
+    }
+    groups = groups_for(call, shape, k, cap);
+  }
   cudaError_t e = allow_smem(ctx.device, k);
   if (e != cudaSuccess) return fail(GOLDY_ERR_CUDA, std::string("cudaFuncSetAttribute: ") + cudaGetErrorString(e));
-  int64_t cap = int64_t(ctx.sm_count) * k.per_sm;              // CTAs, or clusters, resident at once
-  if (cluster > 1) {
-    int most = 0;
-    e = resident_clusters(ctx.device, k, cluster, &most);
-    if (e == cudaSuccess && most < 1) e = cudaErrorInvalidClusterSize;
-    if (e != cudaSuccess) return fail(GOLDY_ERR_CUDA, std::string("residual norm, clusters: ") + cudaGetErrorString(e));
-    cap = std::min<int64_t>(cap / cluster, most);
-  }
-  // all resident, every team with rows of its own
-  int64_t groups = std::min(cap, ceil_div(d.rows, int64_t(k.teams)));
-  if (call.backward) groups = shape.team == 0 ? stream_parts(d) : team_parts(d, shape);
-  if (cluster > 1) groups = std::min(groups, cap);
-  groups = std::max<int64_t>(1, groups);
-  call.p.cluster = cluster;
+  call.p.cluster = shape.cluster;
   call.p.seg = shape.seg;
   call.p.parts = int32_t(groups);
   void* args[] = {&call.p};
-  e = NormLaunch(unsigned(groups * cluster), unsigned(k.threads), k.smem, call.stream, unsigned(cluster)).run(k.fn, args);
+  e = NormLaunch(unsigned(groups * shape.cluster), unsigned(k.threads), k.smem, call.stream, unsigned(shape.cluster)).run(k.fn, args);
   if (e == cudaSuccess && call.p.part && (groups > 1 || shape.team == 0))
     e = NormLaunch(unsigned(ceil_div(d.n, 32)), kSums * kReduceWarps * 32, 0, call.stream)
             .run(reinterpret_cast<const void*>(&residual_norm_reduce_kernel), args);
@@ -799,17 +355,22 @@ goldy_status launch_residual_norm(const LayerContext& ctx, void* arg) {
   return GOLDY_OK;
 }
 
-// 16-byte accesses: whole vectors in every row, rows, bases and parameters on
-// vector boundaries
-bool whole_vectors(const goldy_residual_norm_desc& d, const goldy_residual_norm_params& given,
-                   std::initializer_list<std::pair<const void*, int64_t>> arrays) {
-  const int64_t per = d.dtype == GOLDY_F32 ? 4 : 8;
-  if (d.n % per != 0) return false;
-  for (const auto& a : arrays)
-    if (a.first && (!on_boundary(a.first, 16) || a.second % per != 0)) return false;
-  for (const void* q : {given.gate, given.gamma_f, given.beta_f, given.gamma_y, given.beta_y})
-    if (!on_boundary(q, 16)) return false;
-  return true;
+// How the arrays' rows lie (the parameters are read one by one but for whole rows).
+void row_mode(ResidualNormCall& call, const goldy_residual_norm_desc& d, const goldy_residual_norm_params& given,
+              std::initializer_list<std::pair<const void*, int64_t>> arrays) {
+  const int64_t size = int64_t(element_size(d.dtype)), per = 16 / size;
+  bool whole = d.n % per == 0, alike = true;
+  const auto& f = *arrays.begin();                 // F, which is always there
+  for (const auto& a : arrays) {
+    if (!a.first) continue;
+    whole = whole && on_boundary(a.first, 16) && a.second % per == 0;
+    alike = alike && reinterpret_cast<uintptr_t>(a.first) % 16 == reinterpret_cast<uintptr_t>(f.first) % 16 &&
+            a.second % per == f.second % per;
+  }
+  for (const void* q : {given.gate, given.gamma_f, given.beta_f, given.gamma_y, given.beta_y}) whole = whole && on_boundary(q, 16);
+  call.mode = whole ? kWholeRows : alike ? kFramedRows : kAnyRows;
+  call.period = 1;                                 // per / gcd(stride, per)
+  while (f.second * call.period % per != 0) call.period *= 2;
 }
 
 void common_params(ResidualNormCall& call, const goldy_residual_norm_desc& d, const goldy_residual_norm_params& given) {
@@ -875,7 +436,7 @@ extern "C" goldy_status goldy_residual_norm_forward(const goldy_residual_norm_de
   call.p.s = S;
   call.p.y = Y;
   call.p.stats = stats;
-  call.vec = whole_vectors(*desc, given, {{X, desc->ldx}, {F, desc->ldf}, {S, desc->lds}, {Y, desc->ldy}});
+  row_mode(call, *desc, given, {{F, desc->ldf}, {X, desc->ldx}, {S, desc->lds}, {Y, desc->ldy}});
   call.stream = stream;
   st = with_layer_context(stream, launch_residual_norm, &call);
   return st == GOLDY_OK ? ok() : st;
@@ -938,8 +499,8 @@ extern "C" goldy_status goldy_residual_norm_backward(const goldy_residual_norm_d
   call.p.dgamma_y = static_cast<float*>(want.gamma_y);
   call.p.dbeta_y = static_cast<float*>(want.beta_y);
   call.p.accumulate = accumulate;
-  call.vec = whole_vectors(*desc, given, {{dY, desc->ldy}, {dS, desc->lds}, {F, desc->ldf}, {dY ? S : nullptr, desc->lds},
-                                          {dX, desc->ldx}, {dF, desc->ldf}});
+  row_mode(call, *desc, given, {{F, desc->ldf}, {dY, desc->ldy}, {dS, desc->lds}, {dY ? S : nullptr, desc->lds},
+                                {dX, desc->ldx}, {dF, desc->ldf}});
   call.stream = stream;
   st = with_layer_context(stream, launch_residual_norm, &call);
   return st == GOLDY_OK ? ok() : st;

@@ -10,6 +10,10 @@
 // it has the lowest index too.  Rows of more than 1024 logits are read again from
 // the cache for every choice instead: the next one is the largest (key, lowest
 // index) behind the last.
+//
+// A row is read once (and its gradient written once), but what bounds the kernels is
+// arithmetic: comparisons for the choice, exponentials backwards (32768 x 128 fp32,
+// 8 chosen: 11 us forwards and 8 backwards, floors 2.8 and 5.2).
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -244,7 +248,8 @@ __global__ void __launch_bounds__(kWarps * 32) router_backward_kernel(const Rout
 }
 
 // ---- up to 8 of up to 256 experts: eight lanes per row ---------------------------
-// Four rows per warp share every instruction.  A lane sorts its keys eight at a time,
+// Four rows per warp share every instruction (a warp per row: 32768 x 128 forwards
+// and backwards 32 us, now 18).  A lane sorts its keys eight at a time,
 // and lists are merged (the larger of A[i] and B[7 - i] are the eight largest of
 // both, in an order that three steps of compare and exchange sort): first those of
 // a lane, then those of the eight lanes, after which every lane knows the row's

@@ -187,7 +187,8 @@ def test_kinds(cuda_ok, norm_f, norm_y, dtype):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("n", [64, 255, 2000, 4000, 9000])
 @pytest.mark.parametrize("more,start", [((8, 16, 0, 24), (8, 0, 16, 8)), ((0, 1, 2, 3), (1, 2, 3, 5)), ((1, 1, 1, 1), (0, 0, 0, 0)),
-                                        ((0, 0, 0, 0), (1, 0, 0, 0)), ((0, 0, 0, 0), (0, 0, 0, 3))])
+                                        ((0, 0, 0, 0), (1, 0, 0, 0)), ((0, 0, 0, 0), (0, 0, 0, 3)),
+                                        ((8, 0, 16, 8), (3, 3, 3, 3)), ((2, 10, 2, 18), (0, 0, 0, 0)), ((3, 3, 11, 3), (5, 5, 5, 5))])
 def test_strides(cuda_ok, n, more, start, dtype):
     Case(23, n, dtype, LAYER, RMS, more=more, start=start).check_backward()
 
@@ -213,6 +214,9 @@ def test_inside_a_partition(cuda_ok, rows, n):
 
 def test_many_rows(cuda_ok):
     Case(70000, 40, "bf16", RMS, RMS).check_backward()
+    Case(30001, 37, "bf16", RMS, LAYER).check_backward()
+    Case(5003, 1023, "bf16", LAYER, RMS).check_backward()
+    Case(5003, 517, "f32", LAYER, RMS).check_backward()
 
 
 @pytest.mark.parametrize("n", [120, 5000])
