@@ -6,7 +6,7 @@ parallel: ``planner.cpp`` (host C++), ``runtime.cu`` (launch manager),
 ``kernels.cu`` once per GO-Kernel kind (``-DGOLDY_KIND=k``), the layer
 operators (``linear.cu``, ``repack.cu``, ``bias_grad.cu``, ``layernorm.cu``,
 ``router.cu``, ``route.cu``, ``residual_norm.cu``, ``keep8.cu``),
-``residual_norm_kernels.cu`` once per type and direction, and
+``residual_norm_kernels.cu`` once per direction, type and row layout, and
 ``linear_kernels.cu`` once per pass and activation.  Objects go to
 ``_build/`` next to this file and the library to
 ``paper_2409_02227_gb300/libgoldy.so``; both are git-ignored.  A rebuild is
@@ -61,11 +61,14 @@ def _jobs(ptxas_verbose: bool):
     jobs.append(("ewise", cu + ["-c", os.path.join(CSRC, "ewise.cu")]))
     for name in ("linear", "repack", "bias_grad", "layernorm", "router", "route", "residual_norm", "keep8"):
         jobs.append((name, cu + ["-c", os.path.join(CSRC, name + ".cu")]))
-    for f32 in range(2):
-        for backward in range(2):
-            jobs.append((f"residual_norm_kernels_{'f32' if f32 else 'bf16'}_{'backward' if backward else 'forward'}",
-                         cu + [f"-DGOLDY_NORM_F32={f32}", f"-DGOLDY_NORM_BACKWARD={backward}", "-c",
-                               os.path.join(CSRC, "residual_norm_kernels.cu")]))
+    for direction in ("forward", "backward"):
+        for kind in ("bf16", "f32"):
+            for mode in range(3):
+                name = f"residual_norm_{direction}_{kind}_{mode}"
+                jobs.append((name, cu + [f"-DGOLDY_NORM_KERNEL={name}", f"-DGOLDY_NORM_F32={int(kind == 'f32')}",
+                                         f"-DGOLDY_NORM_BACKWARD={int(direction == 'backward')}",
+                                         f"-DGOLDY_NORM_MODE=RowMode({mode})", "-c",
+                                         os.path.join(CSRC, "residual_norm_kernels.cu")]))
     for k, a in LINEAR_KERNELS:
         jobs.append((f"linear_kernels_p{k}_a{a}", cu + [f"-DGOLDY_LINEAR_PASS={k}", f"-DGOLDY_LINEAR_ACT={a}", "-c",
                                                         os.path.join(CSRC, "linear_kernels.cu")]))

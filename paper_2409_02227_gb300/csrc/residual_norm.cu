@@ -215,19 +215,23 @@ __global__ void __launch_bounds__(kSums * kReduceWarps * 32) residual_norm_reduc
 
 // ---- host ---------------------------------------------------------------------
 
-ResidualNormShape shape_for(const goldy_residual_norm_desc& d, bool backward, bool framed) {
-  const int64_t vals = backward ? kBwdVals : kFwdVals;
+// Threads per row; 0: the row streams.  `cluster` CTAs of kMaxTeam threads share a
+// row that is too long for one.
+ResidualNormShape shape_for(const goldy_residual_norm_desc& d, bool backward, RowMode mode) {
+  const int64_t vals = backward ? kBwdVals : kFwdVals, most = kMaxTeam * vals;
   // (a framed row begins inside its first block)
-  const int64_t wide = d.n + (framed ? 16 / int64_t(element_size(d.dtype)) - 1 : 0);
-  int team = 32;
-  while (team < kMaxTeam && team * vals < wide) team *= 2;
-  // one that the few elements more would give half-empty teams does not pay (1000
-  // rows of 1023 in fp32 backwards: 16 us, otherwise 14)
-  if (framed) return team * vals < wide || (team > 32 && team / 2 * vals >= d.n) ? ResidualNormShape{0, 1, 0} : ResidualNormShape{team, 1, int(wide)};
-  int cluster = 1;
-  while (cluster < kMaxCluster && cluster * team * vals < d.n) cluster *= 2;
-  if (cluster * team * vals < d.n) return {0, 1, 0};
-  return {team, cluster, int(ceil_div(ceil_div(d.n, cluster), 8) * 8)};     // whole pieces
+  const int64_t wide = d.n + (mode == kFramedRows ? 16 / int64_t(element_size(d.dtype)) - 1 : 0);
+  int team = int(std::max<int64_t>(1, ceil_div(wide, 32 * vals))) * 32, cluster = 1;
+  // as many warps as the row takes up to 8, then 16 (16384 x 1111 bf16: 42 us, backwards
+  // 77; with powers of two 65 and 112); forwards 7 leave too little of the SM (8192 x
+  // 3333: 58 us, with 8 53); a power of two for rows that lie anyhow
+  if (team > 256) team = kMaxTeam;
+  if (team == 224 && !backward) team = 256;
+  if (mode == kAnyRows)
+    while (team & (team - 1)) team += 32;
+  while (cluster < kMaxCluster && cluster * most < wide) cluster *= 2;
+  if (cluster * most < wide) return {0, 1, 0};
+  return {cluster > 1 ? kMaxTeam : team, cluster, int(ceil_div(ceil_div(wide, cluster), 8) * 8)};      // whole pieces
 }
 
 // Partial rows of a backward launch, at most: CTAs, or clusters of them.
@@ -238,15 +242,17 @@ int64_t stream_parts(const goldy_residual_norm_desc& d) {
 // partial rows costs more.
 constexpr int kAloneRows = 2;
 int64_t team_parts(const goldy_residual_norm_desc& d, const ResidualNormShape& s) {
-  const int64_t teams = s.cluster > 1 ? 1 : kBwdThreads / s.team;
+  const int64_t teams = s.cluster > 1 ? 1 : bwd_threads(s.team) / s.team;
   if (d.rows <= kAloneRows * teams) return 1;      // no second kernel
   return std::min<int64_t>(kBwdCtas / s.cluster, ceil_div(d.rows, teams));
 }
 size_t backward_bytes(const goldy_residual_norm_desc& d) {
-  const ResidualNormShape s = shape_for(d, true, false), f = shape_for(d, true, true);
-  // (inside an SM partition rows stream where clusters would share them)
-  int64_t parts = s.team == 0 || s.cluster > 1 ? stream_parts(d) : team_parts(d, s);
-  if (f.team > 0) parts = std::max(parts, team_parts(d, f));
+  int64_t parts = 0;
+  for (const RowMode mode : {kWholeRows, kFramedRows, kAnyRows}) {
+    const ResidualNormShape s = shape_for(d, true, mode);
+    // (inside an SM partition rows stream where clusters would share them)
+    parts = std::max(parts, s.team == 0 || s.cluster > 1 ? stream_parts(d) : team_parts(d, s));
+  }
   return kLayerCounterBytes + size_t(parts) * kSums * size_t(d.n) * sizeof(float);
 }
 
@@ -298,9 +304,12 @@ NormKernel kernel_for(const ResidualNormCall& call, const ResidualNormShape& sha
                           : (f32 ? reinterpret_cast<const void*>(&residual_norm_forward_stream_kernel<float>)
                                  : reinterpret_cast<const void*>(&residual_norm_forward_stream_kernel<uint16_t>)),
             kStreamThreads, 1, 4, 0};
-  if (call.backward)
-    return f32 ? residual_norm_backward_f32(shape, mode, full) : residual_norm_backward_bf16(shape, mode, full);
-  return f32 ? residual_norm_forward_f32(shape, mode) : residual_norm_forward_bf16(shape, mode);
+  static ResidualNormPick* const picks[2][2][3] = {
+      {{residual_norm_forward_bf16_0, residual_norm_forward_bf16_1, residual_norm_forward_bf16_2},
+       {residual_norm_forward_f32_0, residual_norm_forward_f32_1, residual_norm_forward_f32_2}},
+      {{residual_norm_backward_bf16_0, residual_norm_backward_bf16_1, residual_norm_backward_bf16_2},
+       {residual_norm_backward_f32_0, residual_norm_backward_f32_1, residual_norm_backward_f32_2}}};
+  return picks[call.backward][f32][mode](shape, full);
 }
 
 // CTAs, or clusters of them, all resident (`cap` are), every team with rows of its own
@@ -316,19 +325,19 @@ goldy_status launch_residual_norm(const LayerContext& ctx, void* arg) {
   ResidualNormCall& call = *static_cast<ResidualNormCall*>(arg);
   const goldy_residual_norm_desc& d = *call.d;
   RowMode mode = call.mode;
-  ResidualNormShape shape = shape_for(d, call.backward, mode == kFramedRows);
-  NormKernel k = kernel_for(call, shape, mode);
+  ResidualNormShape shape;
+  NormKernel k;
   int64_t groups = 0;
-  if (mode == kFramedRows && shape.team > 0) {
-    groups = groups_for(call, shape, k, int64_t(ctx.sm_count) * k.per_sm);
-    // a team with several rows has them a whole number of periods apart
-    while (groups > 0 && groups * k.teams < d.rows && groups * k.teams % call.period != 0) --groups;
-  }
-  if (groups == 0) {
-    if (mode == kFramedRows) mode = kAnyRows;
-    shape = shape_for(d, call.backward, false);
+  for (;; mode = kAnyRows) {
+    shape = shape_for(d, call.backward, mode);
     // which SMs a partition has, and so whether a cluster fits into it, is not known
     if (!ctx.whole && shape.cluster > 1) shape = {0, 1, 0};
+    if (mode == kFramedRows) {
+      // a frame that takes larger teams or clusters than the row leaves them half
+      // empty (1000 rows of 1023 in fp32 backwards: 16 us, otherwise 14)
+      const ResidualNormShape any = shape_for(d, call.backward, kAnyRows);
+      if (shape.team == 0 || shape.team * shape.cluster > any.team * any.cluster) continue;
+    }
     k = kernel_for(call, shape, mode);
     int64_t cap = int64_t(ctx.sm_count) * k.per_sm;            // CTAs, or clusters, resident at once
     if (shape.cluster > 1) {
@@ -340,6 +349,10 @@ goldy_status launch_residual_norm(const LayerContext& ctx, void* arg) {
       cap = std::min<int64_t>(cap / shape.cluster, most);
     }
     groups = groups_for(call, shape, k, cap);
+    if (mode != kFramedRows) break;
+    // a team with several rows has them a whole number of periods apart
+    while (groups > 0 && groups * k.teams < d.rows && groups * k.teams % call.period != 0) --groups;
+    if (groups > 0) break;
   }
   cudaError_t e = allow_smem(ctx.device, k);
   if (e != cudaSuccess) return fail(GOLDY_ERR_CUDA, std::string("cudaFuncSetAttribute: ") + cudaGetErrorString(e));

@@ -58,18 +58,20 @@ struct ResidualNormShape {
 // lie anyhow 79 and 185; of 201: 16 and 25, then 34 and 34); or anyhow.
 enum RowMode { kWholeRows = 0, kFramedRows = 1, kAnyRows = 2 };
 
-// The kernel for a shape (residual_norm_kernels.cu, once per type and direction).
+// The kernel for a shape, per direction, type and mode (residual_norm_kernels.cu).
 // full: both norms and dS are there (backwards).
-NormKernel residual_norm_forward_bf16(const ResidualNormShape& s, RowMode mode);
-NormKernel residual_norm_forward_f32(const ResidualNormShape& s, RowMode mode);
-NormKernel residual_norm_backward_bf16(const ResidualNormShape& s, RowMode mode, bool full);
-NormKernel residual_norm_backward_f32(const ResidualNormShape& s, RowMode mode, bool full);
+using ResidualNormPick = NormKernel(const ResidualNormShape& s, bool full);
+ResidualNormPick residual_norm_forward_bf16_0, residual_norm_forward_bf16_1, residual_norm_forward_bf16_2;
+ResidualNormPick residual_norm_forward_f32_0, residual_norm_forward_f32_1, residual_norm_forward_f32_2;
+ResidualNormPick residual_norm_backward_bf16_0, residual_norm_backward_bf16_1, residual_norm_backward_bf16_2;
+ResidualNormPick residual_norm_backward_f32_0, residual_norm_backward_f32_1, residual_norm_backward_f32_2;
 
 constexpr int kMaxTeam = 512;
-constexpr int kFwdThreads = 256;       // per CTA, at least the team
-constexpr int kBwdThreads = 512;
 constexpr int kFwdVals = 16;           // values of a row per thread
 constexpr int kBwdVals = 8;
+// Threads of a CTA: whole teams, 512 per SM together (128 registers each).
+__host__ __device__ constexpr int fwd_threads(int team) { return team > 256 ? team : 256 % team ? team : 256; }
+__host__ __device__ constexpr int bwd_threads(int team) { return team * (512 / team); }
 
 constexpr int kFwdDepth = 3;           // rows in a thread's ring
 // (backwards a row's F and dS stay until the row after it has come in)
@@ -95,9 +97,9 @@ __device__ __forceinline__ int frame_of(const void* base, int64_t row, int64_t l
 }
 
 template <typename T, int TEAM, RowMode MODE, bool WIDE>
-__global__ void __launch_bounds__(TEAM > kFwdThreads ? TEAM : kFwdThreads, TEAM > kFwdThreads ? 1 : 2)
+__global__ void __launch_bounds__(fwd_threads(TEAM), 512 / fwd_threads(TEAM))
 residual_norm_forward_kernel(const ResidualNormParams p) {
-  constexpr int THREADS = TEAM > kFwdThreads ? TEAM : kFwdThreads, TEAMS = THREADS / TEAM, VALS = kFwdVals;
+  constexpr int THREADS = fwd_threads(TEAM), TEAMS = THREADS / TEAM, VALS = kFwdVals;
   constexpr int WARPS = TEAM / 32, D = kFwdDepth;
   constexpr bool VEC = MODE == kWholeRows, FRAME = MODE == kFramedRows;
   using R = NormRow<T, VALS, TEAM, THREADS, VEC || FRAME, WIDE, FRAME>;
@@ -105,16 +107,18 @@ residual_norm_forward_kernel(const ResidualNormParams p) {
   __shared__ float4 slot[2][2][WIDE ? kMaxCluster : TEAMS][WARPS];
   extern __shared__ __align__(16) uint8_t ring[];  // D rows of F, D of X
   const int team = threadIdx.x / TEAM, t = threadIdx.x % TEAM, w = t >> 5, lane = t & 31;
-  // WIDE: this CTA's n columns from c0 on, of rows that a cluster shares
-  const int rank = WIDE ? int(ptx::cluster_ctarank()) : 0, c0 = WIDE ? rank * p.seg : 0;
+  const int rank = WIDE ? int(ptx::cluster_ctarank()) : 0;
   const int group = WIDE ? int(blockIdx.x) / p.cluster : int(blockIdx.x);
   const int groups = WIDE ? int(gridDim.x) / p.cluster : int(gridDim.x);
-  const int lo = FRAME ? frame_of<T>(p.f, int64_t(group) * TEAMS + team, p.ldf) : 0;
-  const int n = WIDE ? min(p.seg, p.n - c0) : p.n + lo;      // the row's end, counted from its first block
-  const T* const f_in = static_cast<const T*>(p.f) + c0 - lo;
-  const T* const x_in = static_cast<const T*>(p.x) + c0 - lo;
-  T* const s_out = static_cast<T*>(p.s) + c0 - lo;
-  T* const y_out = static_cast<T*>(p.y) + c0 - lo;
+  // this CTA's n columns, from column c0 of the row on (of a frame: from its first
+  // block on, the row's first element being the frame's element lo)
+  const int frame = FRAME ? frame_of<T>(p.f, int64_t(group) * TEAMS + team, p.ldf) : 0;
+  const int c0 = (WIDE ? rank * p.seg : 0) - frame, lo = rank == 0 ? frame : 0;
+  const int n = WIDE ? min(p.seg, p.n - c0) : p.n - c0;
+  const T* const f_in = static_cast<const T*>(p.f) + c0;
+  const T* const x_in = static_cast<const T*>(p.x) + c0;
+  T* const s_out = static_cast<T*>(p.s) + c0;
+  T* const y_out = static_cast<T*>(p.y) + c0;
   if (WIDE) ptx::cluster_sync_all();               // the others have started
   ptx::griddep_launch_dependents();
   ptx::griddep_wait();
@@ -140,7 +144,7 @@ residual_norm_forward_kernel(const ResidualNormParams p) {
       for (int k = i * R::PER; k < (i + 1) * R::PER; ++k) a[k] = b[k] = gamma[k] = beta[k] = 0.0f;
       continue;
     }
-    const int c = c0 + R::col(i, t) - lo, k0 = i * R::PER, end = c0 + n - lo;
+    const int c = c0 + R::col(i, t), k0 = i * R::PER, end = c0 + n;
     load_params<R::PER, VEC>(p.gate, p.param_f32, c, end, 1.0f, gamma + k0);
     load_params<R::PER, VEC>(p.gamma_f, p.param_f32, c, end, 1.0f, a + k0);
     load_params<R::PER, VEC>(p.beta_f, p.param_f32, c, end, 0.0f, b + k0);
@@ -200,10 +204,25 @@ residual_norm_forward_kernel(const ResidualNormParams p) {
         } else {
           if (lane == 0) slot[flip][which][team][w] = o;
           team_sync<TEAM, THREADS>(team);
-          const float4 q = slot[flip][which][team][lane & (WARPS - 1)];
-          if (kind == GOLDY_NORM_LAYER) mean = lanes_sum<WARPS>(q.x) * p.inv_n;
-          const float d = q.w - mean;
-          m2 = lanes_sum<WARPS>(fmaf(q.z * d, d, q.y));
+          if constexpr ((WARPS & (WARPS - 1)) == 0) {
+            const float4 q = slot[flip][which][team][lane & (WARPS - 1)];
+            if (kind == GOLDY_NORM_LAYER) mean = lanes_sum<WARPS>(q.x) * p.inv_n;
+            const float d = q.w - mean;
+            m2 = lanes_sum<WARPS>(fmaf(q.z * d, d, q.y));
+          } else {
+            if (kind == GOLDY_NORM_LAYER) {
+#pragma unroll
+              for (int k = 0; k < WARPS; ++k) total += slot[flip][which][team][k].x;
+              mean = total * p.inv_n;
+            }
+            m2 = 0.0f;
+#pragma unroll
+            for (int k = 0; k < WARPS; ++k) {
+              const float4 q = slot[flip][which][team][k];
+              const float d = q.w - mean;
+              m2 += fmaf(q.z * d, d, q.y);
+            }
+          }
         }
       }
       const float rstd = rsqrtf(fmaf(m2, p.inv_n, p.eps)), shift = (wm - mean) * rstd;
@@ -243,24 +262,25 @@ residual_norm_forward_kernel(const ResidualNormParams p) {
 
 // FULL: both norms and dS are there.
 template <typename T, int TEAM, RowMode MODE, bool WIDE, bool FULL>
-__global__ void __launch_bounds__(kBwdThreads) residual_norm_backward_kernel(const ResidualNormParams p) {
-  constexpr int TEAMS = kBwdThreads / TEAM, WARPS = TEAM / 32, VALS = kBwdVals, D = bwd_depth<T>();
+__global__ void __launch_bounds__(bwd_threads(TEAM)) residual_norm_backward_kernel(const ResidualNormParams p) {
+  constexpr int THREADS = bwd_threads(TEAM), TEAMS = THREADS / TEAM, WARPS = TEAM / 32, VALS = kBwdVals, D = bwd_depth<T>();
   constexpr bool VEC = MODE == kWholeRows, FRAME = MODE == kFramedRows;
-  using R = NormRow<T, VALS, TEAM, kBwdThreads, VEC || FRAME, WIDE, FRAME>;
+  using R = NormRow<T, VALS, TEAM, THREADS, VEC || FRAME, WIDE, FRAME>;
   __shared__ float4 slot[2][WIDE ? kMaxCluster : TEAMS][WARPS];
   extern __shared__ __align__(16) uint8_t ring[];  // D rows of F, S, dY and dS each; at the end the CTA's sums
   const int team = threadIdx.x / TEAM, t = threadIdx.x % TEAM, w = t >> 5, lane = t & 31;
-  const int rank = WIDE ? int(ptx::cluster_ctarank()) : 0, c0 = WIDE ? rank * p.seg : 0;
+  const int rank = WIDE ? int(ptx::cluster_ctarank()) : 0;
   const int group = WIDE ? int(blockIdx.x) / p.cluster : int(blockIdx.x);
   const int groups = WIDE ? int(gridDim.x) / p.cluster : int(gridDim.x);
-  const int lo = FRAME ? frame_of<T>(p.f, int64_t(group) * TEAMS + team, p.ldf) : 0;
-  const int n = WIDE ? min(p.seg, p.n - c0) : p.n + lo;      // the row's end, counted from its first block
-  const T* const f_in = static_cast<const T*>(p.f) + c0 - lo;
-  const T* const s_in = static_cast<const T*>(p.s_in) + c0 - lo;
-  const T* const dy_in = static_cast<const T*>(p.dy) + c0 - lo;
-  const T* const ds_in = static_cast<const T*>(p.ds) + c0 - lo;
-  T* const dx_out = static_cast<T*>(p.s) + c0 - lo;
-  T* const df_out = static_cast<T*>(p.y) + c0 - lo;
+  const int frame = FRAME ? frame_of<T>(p.f, int64_t(group) * TEAMS + team, p.ldf) : 0;
+  const int c0 = (WIDE ? rank * p.seg : 0) - frame, lo = rank == 0 ? frame : 0;     // as forwards
+  const int n = WIDE ? min(p.seg, p.n - c0) : p.n - c0;
+  const T* const f_in = static_cast<const T*>(p.f) + c0;
+  const T* const s_in = static_cast<const T*>(p.s_in) + c0;
+  const T* const dy_in = static_cast<const T*>(p.dy) + c0;
+  const T* const ds_in = static_cast<const T*>(p.ds) + c0;
+  T* const dx_out = static_cast<T*>(p.s) + c0;
+  T* const df_out = static_cast<T*>(p.y) + c0;
   const bool has_y = FULL || p.norm_y != GOLDY_NORM_NONE, has_f = FULL || p.norm_f != GOLDY_NORM_NONE;
   const bool has_ds = FULL || p.ds != nullptr;
   const float layer_f = p.norm_f == GOLDY_NORM_LAYER ? p.inv_n : 0.0f, layer_y = p.norm_y == GOLDY_NORM_LAYER ? p.inv_n : 0.0f;
@@ -313,7 +333,7 @@ __global__ void __launch_bounds__(kBwdThreads) residual_norm_backward_kernel(con
     float a[VALS], b[VALS], c[VALS];
 #pragma unroll
     for (int i = 0; i < R::SLOTS; ++i) {
-      const int k0 = i * R::PER, at = c0 + R::col(i, t) - lo, end = c0 + n - lo;
+      const int k0 = i * R::PER, at = c0 + R::col(i, t), end = c0 + n;
       if (R::in(i, t, n)) {
         load_params<R::PER, VEC>(p.gate, p.param_f32, at, end, 1.0f, a + k0);
         load_params<R::PER, VEC>(p.gamma_f, p.param_f32, at, end, 1.0f, b + k0);
@@ -394,8 +414,8 @@ __global__ void __launch_bounds__(kBwdThreads) residual_norm_backward_kernel(con
       }
       r = make_float4(warp_sum(r.x), warp_sum(r.y), warp_sum(r.z), warp_sum(r.w));
     } else {
-      team_sync<TEAM, kBwdThreads>(team);
-      if (WARPS <= 4) {
+      team_sync<TEAM, THREADS>(team);
+      if (WARPS < 8) {
         r = slot[flip][team][0];
 #pragma unroll
         for (int k = 1; k < WARPS; ++k) {
@@ -429,7 +449,7 @@ __global__ void __launch_bounds__(kBwdThreads) residual_norm_backward_kernel(con
   bool begun = false;
   if (left > 0) {                                  // whole teams, and whole clusters
     copy_wait<D - 2>();
-    if (R::SHIFT) team_sync<TEAM, kBwdThreads>(team);
+    if (R::SHIFT) team_sync<TEAM, THREADS>(team);
     first(ring, true, row, now);
     send(1);
     if (!LATE) receive(1);
@@ -439,7 +459,7 @@ __global__ void __launch_bounds__(kBwdThreads) residual_norm_backward_kernel(con
     fetch(ahead, left > D - 1);                    // where the row before this one was
     const float later = next_stats(left > 2);
     copy_wait<D - 2>();
-    if (R::SHIFT) team_sync<TEAM, kBwdThreads>(team);
+    if (R::SHIFT) team_sync<TEAM, THREADS>(team);
     if (LATE) receive(flip ^ 1);
     if (begun) finish();
     begun = true;
@@ -504,11 +524,12 @@ __global__ void __launch_bounds__(kBwdThreads) residual_norm_backward_kernel(con
         sums[(team * kSums + q) * ALL + R::col(i, t) + k] = (i * R::PER + k) & 1 ? f.y : f.x;
       }
   __syncthreads();
-  float* to = p.part + int64_t(group) * kSums * p.n + c0;
-  int from[TEAMS];                                 // where the teams' rows begin in their sums
+  float* to = p.part + int64_t(group) * kSums * p.n;
+  int from[TEAMS];                                 // where column 0 of the teams' rows is in their sums
 #pragma unroll
-  for (int k = 0; k < TEAMS; ++k) from[k] = FRAME ? frame_of<T>(p.f, int64_t(group) * TEAMS + k, p.ldf) : 0;
-  for (int c = threadIdx.x; c < n - lo; c += kBwdThreads) {
+  for (int k = 0; k < TEAMS; ++k)
+    from[k] = (FRAME ? frame_of<T>(p.f, int64_t(group) * TEAMS + k, p.ldf) : 0) - (WIDE ? rank * p.seg : 0);
+  for (int c = max(c0, 0) + int(threadIdx.x); c < c0 + n; c += THREADS) {
     float v[kSums];
 #pragma unroll
     for (int q = 0; q < kSums; ++q) {
@@ -520,7 +541,7 @@ __global__ void __launch_bounds__(kBwdThreads) residual_norm_backward_kernel(con
 #pragma unroll
       for (int q = 0; q < kSums; ++q) __stcg(to + int64_t(q) * p.n + c, v[q]);
     } else {                                       // this CTA's sums are the result
-      give_gradients(p, c0 + c, v[0], v[1], v[2], v[3]);
+      give_gradients(p, c, v[0], v[1], v[2], v[3]);
     }
   }
 }
