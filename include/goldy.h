@@ -617,7 +617,8 @@ goldy_status goldy_layernorm_backward(const goldy_layernorm_desc* desc, const vo
  *   GOLDY_ROUTER_CHOSEN  scale * exp(l_e) / sum of exp(l) over the chosen ones
  * computed in fp32 from the logits less their largest.  Logits and dlogits have
  * `dtype`, any row strides >= experts, element alignment; ids (int32) and
- * weights (fp32) are packed rows x k. */
+ * weights (fp32) are packed rows x k.  Results must not overlap inputs unless
+ * stated. */
 typedef enum goldy_router_over { GOLDY_ROUTER_ALL = 0, GOLDY_ROUTER_CHOSEN = 1 } goldy_router_over;
 
 #define GOLDY_MAX_SLOTS 32      /* experts per token */
@@ -765,7 +766,8 @@ goldy_status goldy_residual_norm_backward(const goldy_residual_norm_desc* desc,
  * is held as NaN.  Q holds the blocks of a row one after another, each of
  * GOLDY_KEEP8_BLOCK bytes (zeros behind the row's end), rows packed: rows * blocks *
  * GOLDY_KEEP8_BLOCK bytes, 16-byte aligned; scales holds e + 127 per block, one
- * byte each, packed. */
+ * byte each, packed.  The aligned 16-byte blocks that a row of Z begins and ends in
+ * may be read whole; of Z and H only rows are written.  No array may overlap another. */
 #define GOLDY_KEEP8_BLOCK 32
 
 typedef struct goldy_keep8_desc {

@@ -70,13 +70,6 @@ struct Block {
     }
     return pack(v);
   }
-  static __device__ __forceinline__ float at(const T* row, int64_t c) {
-    return sizeof(T) == 2 ? load_bf16(row, c) : __uint_as_float(uint32_t(row[c]));
-  }
-  static __device__ __forceinline__ void put(T* row, int64_t c, float v) {
-    if (sizeof(T) == 2) store_bf16(row, c, v);
-    else row[c] = T(__float_as_uint(v));
-  }
   // A row of n elements as the source of a result whose row starts `off` elements
   // behind a block's start: block b of the result holds the row's elements from
   // b * PER - off on, which lie in two neighbouring blocks of the source.

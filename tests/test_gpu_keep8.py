@@ -117,6 +117,23 @@ def test_act(cuda_ok, act, dtype):
     assert torch.equal(h.t, h2.t)
 
 
+def test_far_apart(cuda_ok):
+    """Rows of Z and H more than 2^32 elements apart."""
+    rows, n, ld = 70000, 40, 70000
+    z = Rows(rows, n, torch.bfloat16, ld, 0, torch.randn(rows, n, generator=gen_of(1), device="cuda"))
+    packed = z.t.contiguous()
+    d, dense = G.keep8_desc(rows, n, ldz=ld, ldh=ld, act=G.GOLDY_ACT_SILU), G.keep8_desc(rows, n, act=G.GOLDY_ACT_SILU)
+    q_bytes, s_bytes = G.goldy_keep8_query(d)
+    (q, s), (q2, s2) = ([torch.zeros(b, dtype=torch.uint8, device="cuda") for b in (q_bytes, s_bytes)] for _ in range(2))
+    G.goldy_keep8_pack(d, z.ptr, q.data_ptr(), s.data_ptr())
+    G.goldy_keep8_pack(dense, packed.data_ptr(), q2.data_ptr(), s2.data_ptr())
+    h, z2, h2 = Rows(rows, n, torch.bfloat16, ld), torch.empty_like(packed), torch.empty_like(packed)
+    G.goldy_keep8_unpack(d, q.data_ptr(), s.data_ptr(), z.ptr, h.ptr)
+    G.goldy_keep8_unpack(dense, q2.data_ptr(), s2.data_ptr(), z2.data_ptr(), h2.data_ptr())
+    torch.cuda.synchronize()
+    assert torch.equal(q, q2) and torch.equal(s, s2) and torch.equal(z.t, z2) and torch.equal(h.t, h2)
+
+
 def test_edges(cuda_ok):
     """The largest value at, just below and just above 448 powers; ties; zeros;
     the smallest and largest numbers."""

@@ -229,6 +229,28 @@ def test_some_gradients(cuda_ok, n):
     Case(30, n, "f32", LAYER, LAYER).check_backward(accumulate=True)
 
 
+def test_far_apart(cuda_ok):
+    """Rows more than 2^32 bytes, and elements, apart from the first: 70000 rows of a
+    stride of 70000."""
+    rows, n, ld = 70000, 16, 70000
+    make = lambda fill=None: Rows(rows, n, torch.bfloat16, ld, 0, fill)  # noqa: E731
+    gen = gen_of(1)
+    x, f = (make(torch.randn(rows, n, generator=gen, device="cuda")) for _ in range(2))
+    s, y, near = make(), make(), Case(rows, n, "bf16", LAYER, RMS)
+    d = G.residual_norm_desc(rows, n, LAYER, RMS, alpha=0.75, ldx=ld, ldf=ld, lds=ld, ldy=ld)
+    near.x.t.copy_(x.t)
+    near.f.t.copy_(f.t)
+    s2, y2, stats = near.check_forward()
+    G.goldy_residual_norm_forward(d, near.params, x.ptr, f.ptr, s.ptr, y.ptr)
+    torch.cuda.synchronize()
+    assert torch.equal(s.t, s2.t) and torch.equal(y.t, y2.t)
+    dx, df, dx2, df2 = make(), make(), near.new(0), near.new(1)
+    near.backward(y2, s2, s2, stats, dx2, df2, wanted=[])
+    G.goldy_residual_norm_backward(d, near.params, y.ptr, s.ptr, f.ptr, s.ptr, stats.data_ptr(), dx.ptr, df.ptr)
+    torch.cuda.synchronize()
+    assert torch.equal(dx.t, dx2.t) and torch.equal(df.t, df2.t)
+
+
 def test_no_rows(cuda_ok):
     c = Case(0, 50, "f32", RMS, RMS)
     rows = [c.new(0) for _ in range(5)]
@@ -238,7 +260,7 @@ def test_no_rows(cuda_ok):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("n", [100, 1001, 6000, 9001])
+@pytest.mark.parametrize("n", [100, 1001, 6000, 9001, 33000, 66001])
 def test_in_place(cuda_ok, n, dtype):
     """Results over inputs give the same bits."""
     make = lambda: Case(25, n, dtype, RMS, LAYER)  # noqa: E731

@@ -211,6 +211,25 @@ def test_dispatch_gradient_is_combine(cuda_ok):
     assert float((e * g).sum()) == float((x * dx).sum())
 
 
+def test_far_apart(cuda_ok):
+    """Experts' rows more than 2^32 elements apart."""
+    rows, k, width, lde = 40000, 2, 24, 60000
+    d = G.route_desc(rows, k, 8, width, lde=lde)
+    ids = torch.randint(0, 8, (rows, k), generator=gen_of(1), device="cuda").int()
+    offsets, place, _ = sort(d, ids)
+    x = torch.randn(rows, width, generator=gen_of(2), device="cuda").bfloat16()
+    e = torch.zeros(rows * k, lde, dtype=torch.bfloat16, device="cuda")
+    G.goldy_route_dispatch(d, x.data_ptr(), place.data_ptr(), e.data_ptr())
+    y, dw = torch.empty_like(x), torch.empty(rows, k, device="cuda")
+    G.goldy_route_combine(d, e.data_ptr(), place.data_ptr(), y.data_ptr())
+    torch.cuda.synchronize()
+    assert torch.equal(e[place.long(), :width], x.repeat_interleave(k, 0)) and torch.equal(y, 2 * x)
+    G.goldy_route_combine_grad(d, x.data_ptr(), e.data_ptr(), place.data_ptr(), 0, e.data_ptr(), dw.data_ptr())
+    torch.cuda.synchronize()
+    assert torch.equal(dw[:, 0], dw[:, 1]) and torch.equal(e[place.long(), :width], x.repeat_interleave(k, 0))
+    assert not e[:, width:].any()
+
+
 def test_rows_without_elements(cuda_ok):
     """Only the weights' gradient has something to write: zeros."""
     d, place = G.route_desc(6, 2, 3, 0), torch.arange(12, dtype=torch.int32, device="cuda")

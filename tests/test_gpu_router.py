@@ -1,9 +1,11 @@
 """The router against its definition in fp64.
 
-Bounds.  A weight is scale e_j / sum(e), e = exp(l - m): the subtraction rounds the
-exponent by |l - m| u, expf is good to 2 units in the last place (4 u), the sum
-has experts / 32 + 5 steps, the division and the scale one rounding each: with
-logits that spread over `spread`, (2 spread + experts / 32 + 16) u of the weight.
+Bounds.  A weight is scale e_j / sum(e), e = exp(l - m) = 2^((l - m) log2 e): the
+difference, the constant and their product are rounded, 2.3 |l - m| u of e
+together, and the power is good to 2 units in the last place (4 u).  In the sum
+that is 2.3 sum(p |l - m|) u, and sum(p |l - m|) is at most ln(experts) < 8.4, so 20
+u; the sum has experts / 8 + 5 steps, the division and the scale one rounding each:
+with logits that spread over `spread`, (2.3 spread + experts / 8 + 36) u of the weight.
 dl_e = p_e (g_e - sum g p): p as above, the dot product over at most k terms has 6
 steps more, so twice that bound of p_e (|g_e| + sum |g| p), then one rounding to
 the logits' type."""
@@ -64,7 +66,7 @@ def against_fp64(l, k, over, dtype, scale, ids, weights, dl, dw, forward_ids=Non
     rows, experts = l.shape
     finite = torch.where(torch.isfinite(l.double()), l.double(), 0.0)
     spread = float((finite.max(1).values - finite.min(1).values).max()) if rows else 0.0
-    eps = (2 * spread + experts / 32 + 16) * U
+    eps = (2.3 * spread + experts / 8 + 36) * U
     want = choose(l, k)
     if forward_ids is None:
         assert torch.equal(ids.long(), want)
@@ -127,16 +129,17 @@ def test_ties(cuda_ok, experts, k):
         against_fp64(l.t, k, ALL, dtype, 1.0, ids, weights, dl, dw)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("experts", [20, 300, 1300])
-def test_infinite_and_nan(cuda_ok, experts):
+def test_infinite_and_nan(cuda_ok, experts, dtype):
     """A NaN or +infinity is chosen first; its row's weights are NaN, others' are not."""
     v = torch.randn(6, experts, generator=gen_of(5), device="cuda")
     v[1, 13], v[1, 4] = math.nan, math.inf
     v[2, 9] = math.inf
     v.view(torch.int32)[3, 2] = -1                          # a NaN with its sign set
     v[4] = math.nan
-    l = Rows(6, experts, torch.float32, fill=v)
-    ids, weights, dl, _ = check(l, 6, experts, 3, ALL, "f32", 1.0, True)
+    l = Rows(6, experts, TYPES[dtype][0], fill=v)
+    ids, weights, dl, _ = check(l, 6, experts, 3, ALL, dtype, 1.0, True)
     assert ids[1, :2].tolist() == [13, 4] and ids[2, 0] == 9 and ids[3, 0] == 2 and ids[4].tolist() == [0, 1, 2]
     clean = torch.tensor([0, 5], device="cuda")
     assert torch.isnan(weights[1:5]).any(1).all() and torch.isfinite(weights[clean]).all()
