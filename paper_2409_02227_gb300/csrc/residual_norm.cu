@@ -333,10 +333,13 @@ goldy_status launch_residual_norm(const LayerContext& ctx, void* arg) {
     // which SMs a partition has, and so whether a cluster fits into it, is not known
     if (!ctx.whole && shape.cluster > 1) shape = {0, 1, 0};
     if (mode == kFramedRows) {
-      // a frame that takes larger teams or clusters than the row leaves them half
-      // empty (1000 rows of 1023 in fp32 backwards: 16 us, otherwise 14)
+      // a frame may take a larger team than the row: in bf16 it pays all the same
+      // (16384 x 1023 backwards 74 us, in the general way 96; x 511 49 and 59), and
+      // forwards in fp32 (8192 x 511 17 and 26), but not backwards in fp32, where
+      // single elements cost less (8192 x 1023 62 and 51)
       const ResidualNormShape any = shape_for(d, call.backward, kAnyRows);
-      if (shape.team == 0 || shape.team * shape.cluster > any.team * any.cluster) continue;
+      const bool grown = shape.team > any.team && call.backward && d.dtype == GOLDY_F32;
+      if (shape.team == 0 || shape.cluster > any.cluster || grown) continue;
     }
     k = kernel_for(call, shape, mode);
     int64_t cap = int64_t(ctx.sm_count) * k.per_sm;            // CTAs, or clusters, resident at once
