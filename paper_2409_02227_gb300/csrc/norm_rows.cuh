@@ -138,6 +138,24 @@ struct NormRow {
   static __device__ __forceinline__ int count(int slot, int t, int n, int lo) {
     return complete(slot, t, n, lo) ? PER : min(col(slot, t) + PER, n) - (FRAME ? max(col(slot, t), lo) : col(slot, t));
   }
+  // FRAME: ones in the place of a thread's elements, for its pieces' words
+  struct Masks {
+    uint4 m[FRAME ? SLOTS : 1];
+    __device__ __forceinline__ Masks(int t, int n, int lo) {
+      if constexpr (FRAME) {
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s) {
+          uint32_t w[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            if (sizeof(T) == 4) w[k] = inside(s, k, t, n, lo) ? 0xFFFFFFFFu : 0u;
+            else w[k] = (inside(s, 2 * k, t, n, lo) ? 0xFFFFu : 0u) | (inside(s, 2 * k + 1, t, n, lo) ? 0xFFFF0000u : 0u);
+          }
+          m[s] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+      }
+    }
+  };
   // SHIFT: elements by which a row starts behind a block's start
   static __device__ __forceinline__ int shift(const T* at) { return int(reinterpret_cast<uintptr_t>(at) & 15) / 2; }
   // place in the ring of a thread's piece, or block
@@ -175,9 +193,13 @@ struct NormRow {
   // the row's values, 0 outside it (SHIFT: behind the team's barrier)
   static __device__ __forceinline__ void values(const uint8_t* ring, const void* base, int64_t row, int64_t ld, int n,
                                                 int t, float (&f)[VALS]) {
-    values(ring, static_cast<const T*>(base) + row * ld, n, t, f);
+    values(ring, static_cast<const T*>(base) + row * ld, n, t, f, 0);
   }
-  static __device__ __forceinline__ void values(const uint8_t* ring, const T* at, int n, int t, float (&f)[VALS], int lo = 0) {
+  // OUTSIDE: what tells the elements outside a frame's row, `lo` or masks (which cost
+  // registers, but no way apart for the threads at the row's ends: backwards 16384 x
+  // 1999 104 us, with lo 110; forwards 8192 x 3333 57, with lo 53)
+  template <typename OUTSIDE>
+  static __device__ __forceinline__ void values(const uint8_t* ring, const T* at, int n, int t, float (&f)[VALS], const OUTSIDE& out) {
     if constexpr (SHIFT) {
       switch (shift(at)) {
         case 0: pick<0>(ring, n, t, f); break;
@@ -198,7 +220,9 @@ struct NormRow {
         } else if (!VEC) {
           f[s] = *reinterpret_cast<const float*>(ring + place(s, t));
         } else {
-          const uint4 v = *reinterpret_cast<const uint4*>(ring + place(s, t));
+          uint4 v = *reinterpret_cast<const uint4*>(ring + place(s, t));
+          if constexpr (FRAME && sizeof(OUTSIDE) > sizeof(int))
+            v.x &= out.m[s].x, v.y &= out.m[s].y, v.z &= out.m[s].z, v.w &= out.m[s].w;
           float* o = f + s * PER;
           if (sizeof(T) == 2) {
             o[0] = bf16_lo(v.x), o[1] = bf16_hi(v.x), o[2] = bf16_lo(v.y), o[3] = bf16_hi(v.y);
@@ -206,10 +230,12 @@ struct NormRow {
           } else {
             o[0] = __uint_as_float(v.x), o[1] = __uint_as_float(v.y), o[2] = __uint_as_float(v.z), o[3] = __uint_as_float(v.w);
           }
-          if (FRAME && !complete(s, t, n, lo)) {
+          if constexpr (FRAME && sizeof(OUTSIDE) == sizeof(int)) {
+            if (!complete(s, t, n, out)) {
 #pragma unroll
-            for (int k = 0; k < PER; ++k)
-              if (!inside(s, k, t, n, lo)) o[k] = 0.0f;
+              for (int k = 0; k < PER; ++k)
+                if (!inside(s, k, t, n, out)) o[k] = 0.0f;
+            }
           }
         }
       }

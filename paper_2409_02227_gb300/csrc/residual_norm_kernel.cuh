@@ -287,6 +287,7 @@ __global__ void __launch_bounds__(bwd_threads(TEAM)) residual_norm_backward_kern
   if (WIDE) ptx::cluster_sync_all();               // the others have started
   ptx::griddep_launch_dependents();
   ptx::griddep_wait();
+  const typename R::Masks masks(t, n, lo);
   const int64_t step = int64_t(groups) * TEAMS, row0 = int64_t(group) * TEAMS + team;
   int left = row0 < p.rows ? int((p.rows - row0 - 1) / step) + 1 : 0;    // rows of this team (memory holds fewer than 2^31)
   // pointers run along: of the row fetched next, of the row whose dX and dF are next
@@ -368,8 +369,8 @@ __global__ void __launch_bounds__(bwd_threads(TEAM)) residual_norm_backward_kern
     s1x = s1y = 0.0f;
     if (!has_y || !there) return;
     float v[VALS], d[VALS];
-    R::values(from + R::RING_BYTES, R::SHIFT ? s_in + r * p.lds : nullptr, n, t, v, lo);
-    R::values(from + 2 * R::RING_BYTES, R::SHIFT ? dy_in + r * p.ldy : nullptr, n, t, d, lo);
+    R::values(from + R::RING_BYTES, R::SHIFT ? s_in + r * p.lds : nullptr, n, t, v, masks);
+    R::values(from + 2 * R::RING_BYTES, R::SHIFT ? dy_in + r * p.ldy : nullptr, n, t, d, masks);
     ry = stat(st, 3);
     // the mean is subtracted before the scale: rows far from zero keep their
     // digits; columns outside the row have dY = gamma = 0 and add nothing
@@ -469,12 +470,12 @@ __global__ void __launch_bounds__(bwd_threads(TEAM)) residual_norm_backward_kern
     ahead = ahead + 1 == D ? 0 : ahead + 1;
     float tt[VALS], v[VALS];
     if (has_ds) {
-      R::values(from + 3 * R::RING_BYTES, R::SHIFT ? ds_in + row * p.lds : nullptr, n, t, tt, lo);
+      R::values(from + 3 * R::RING_BYTES, R::SHIFT ? ds_in + row * p.lds : nullptr, n, t, tt, masks);
     } else {
 #pragma unroll
       for (int j = 0; j < VALS; ++j) tt[j] = 0.0f;
     }
-    R::values(from, R::SHIFT ? f_in + row * p.ldf : nullptr, n, t, v, lo);
+    R::values(from, R::SHIFT ? f_in + row * p.ldf : nullptr, n, t, v, masks);
     last_rf = stat(now, 1);
     const uint64_t less = two(-s1x * layer_y * ry), slope = two(-s1y * p.inv_n * ry), by = two(ry);
     const uint64_t off = two(-stat(now, 0)), scale = two(last_rf), alpha = two(p.alpha);
