@@ -328,14 +328,16 @@ __device__ __forceinline__ void tell_cluster(float4* to, int rank, int cluster, 
 
 // The same from warp to warp: warp w of CTA `rank` tells every CTA of the cluster
 // its value (the same in all lanes), which one barrier later each has in
-// slots[rank][w] of its own shared memory.  Work may lie between the two calls.
+// slots[rank][w] of its own shared memory.  Work may lie between begin and end.
 template <int WARPS>
-__device__ __forceinline__ void tell_cluster_begin(float4* slots, int rank, int cluster, int w, int lane, float4 v) {
+__device__ __forceinline__ void tell_cluster_warp(float4* slots, int rank, int cluster, int w, int lane, float4 v) {
   if (lane < cluster)
     asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(
                      ptx::map_to_rank(ptx::smem_u32(slots + rank * WARPS + w), uint32_t(lane))),
                  "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w)
                  : "memory");
+}
+__device__ __forceinline__ void tell_cluster_begin() {
   __syncwarp();
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
 }

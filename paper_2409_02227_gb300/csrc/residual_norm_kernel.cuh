@@ -74,8 +74,8 @@ __host__ __device__ constexpr int fwd_threads(int team) { return team > 256 ? te
 __host__ __device__ constexpr int bwd_threads(int team) { return team * (512 / team); }
 
 constexpr int kFwdDepth = 3;           // rows in a thread's ring
-// (backwards a row's F and dS stay until the row after it has come in)
-template <typename T> __host__ __device__ constexpr int bwd_depth() { return sizeof(T) == 2 ? 4 : 3; }
+// where the row after one has to come in before its place is used again
+template <typename T> __host__ __device__ constexpr int norm_depth() { return sizeof(T) == 2 ? 4 : 3; }
 
 // The parameters' gradients of column c from its four sums.
 __device__ __forceinline__ void give_gradients(const ResidualNormParams& p, int64_t c, float a, float b, float cc, float d) {
@@ -100,7 +100,7 @@ template <typename T, int TEAM, RowMode MODE, bool WIDE>
 __global__ void __launch_bounds__(fwd_threads(TEAM), 512 / fwd_threads(TEAM))
 residual_norm_forward_kernel(const ResidualNormParams p) {
   constexpr int THREADS = fwd_threads(TEAM), TEAMS = THREADS / TEAM, VALS = kFwdVals;
-  constexpr int WARPS = TEAM / 32, D = kFwdDepth;
+  constexpr int WARPS = TEAM / 32, D = WIDE ? norm_depth<T>() : kFwdDepth;
   constexpr bool VEC = MODE == kWholeRows, FRAME = MODE == kFramedRows;
   using R = NormRow<T, VALS, TEAM, THREADS, VEC || FRAME, WIDE, FRAME>;
   // per row, norm and warp (WIDE: of all CTAs that share the row): sum, M2, elements, mean
@@ -156,52 +156,37 @@ residual_norm_forward_kernel(const ResidualNormParams p) {
   }
   const float warp_n = warp_sum(float(mine));
   const float warp_inv = warp_n > 0.0f ? 1.0f / warp_n : 0.0f;
-  int at = 0, ahead = D - 1;                       // ring places of this row and of the one fetched now
-  for (int flip = 0; row < p.rows; row += step, flip ^= 1) {
-    // xhat of the values in v, which are 0 outside the row and stay 0 there
-    // (a layer norm's as differences from the warp's mean first)
-    auto normalise = [&](int kind, int which, float (&v)[VALS]) {
-      if (kind == GOLDY_NORM_NONE) return;
-      float s = 0.0f, wm = 0.0f;
-      if (kind == GOLDY_NORM_LAYER) {
+  if constexpr (!WIDE) {
+    int at = 0, ahead = D - 1;                       // ring places of this row and of the one fetched now
+    for (int flip = 0; row < p.rows; row += step, flip ^= 1) {
+      // xhat of the values in v, which are 0 outside the row and stay 0 there
+      // (a layer norm's as differences from the warp's mean first)
+      auto normalise = [&](int kind, int which, float (&v)[VALS]) {
+        if (kind == GOLDY_NORM_NONE) return;
+        float s = 0.0f, wm = 0.0f;
+        if (kind == GOLDY_NORM_LAYER) {
 #pragma unroll
-        for (int j = 0; j < VALS; ++j) s += v[j];
-        s = warp_sum(s);
-        wm = s * warp_inv;
+          for (int j = 0; j < VALS; ++j) s += v[j];
+          s = warp_sum(s);
+          wm = s * warp_inv;
 #pragma unroll
-        for (int i = 0; i < R::SLOTS; ++i) {
-          if (!R::in(i, t, n)) continue;
+          for (int i = 0; i < R::SLOTS; ++i) {
+            if (!R::in(i, t, n)) continue;
 #pragma unroll
-          for (int k = 0; k < R::PER; ++k) {
-            float& e = v[i * R::PER + k];
-            e = R::complete(i, t, n, lo) || R::inside(i, k, t, n, lo) ? e - wm : 0.0f;
+            for (int k = 0; k < R::PER; ++k) {
+              float& e = v[i * R::PER + k];
+              e = R::complete(i, t, n, lo) || R::inside(i, k, t, n, lo) ? e - wm : 0.0f;
+            }
           }
         }
-      }
-      float m2 = 0.0f;
+        float m2 = 0.0f;
 #pragma unroll
-      for (int j = 0; j < VALS; ++j) m2 = fmaf(v[j], v[j], m2);
-      m2 = warp_sum(m2);
-      float mean = wm;
-      if (WARPS > 1) {
-        const float4 o = make_float4(s, m2, warp_n, wm);
-        float total = 0.0f;
-        if (WIDE) {
-          tell_cluster_begin<WARPS>(&slot[flip][which][0][0], rank, p.cluster, w, lane, o);
-          tell_cluster_end();
-          const float4* all = &slot[flip][which][0][0];
-          if (kind == GOLDY_NORM_LAYER) {
-            for (int k = lane; k < p.cluster * WARPS; k += 32) total += all[k].x;
-            mean = warp_sum(total) * p.inv_n;
-          }
-          m2 = 0.0f;
-          for (int k = lane; k < p.cluster * WARPS; k += 32) {
-            const float4 q = all[k];
-            const float d = q.w - mean;
-            m2 += fmaf(q.z * d, d, q.y);
-          }
-          m2 = warp_sum(m2);
-        } else {
+        for (int j = 0; j < VALS; ++j) m2 = fmaf(v[j], v[j], m2);
+        m2 = warp_sum(m2);
+        float mean = wm;
+        if (WARPS > 1) {
+          const float4 o = make_float4(s, m2, warp_n, wm);
+          [[maybe_unused]] float total = 0.0f;
           if (lane == 0) slot[flip][which][team][w] = o;
           team_sync<TEAM, THREADS>(team);
           if constexpr ((WARPS & (WARPS - 1)) == 0) {
@@ -224,46 +209,162 @@ residual_norm_forward_kernel(const ResidualNormParams p) {
             }
           }
         }
-      }
-      const float rstd = rsqrtf(fmaf(m2, p.inv_n, p.eps)), shift = (wm - mean) * rstd;
+        const float rstd = rsqrtf(fmaf(m2, p.inv_n, p.eps)), shift = (wm - mean) * rstd;
 #pragma unroll
-      for (int i = 0; i < R::SLOTS; ++i) {
-        if (!R::in(i, t, n)) continue;
+        for (int i = 0; i < R::SLOTS; ++i) {
+          if (!R::in(i, t, n)) continue;
 #pragma unroll
-        for (int j = i * R::PER; j < (i + 1) * R::PER; ++j) v[j] = fmaf(v[j], rstd, shift);
-      }
-      if (t == 0 && rank == 0 && p.stats) {
-        if (kind == GOLDY_NORM_LAYER) p.stats[2 * which * p.rows + row] = mean;
-        p.stats[(2 * which + 1) * p.rows + row] = rstd;
-      }
+          for (int j = i * R::PER; j < (i + 1) * R::PER; ++j) v[j] = fmaf(v[j], rstd, shift);
+        }
+        if (t == 0 && rank == 0 && p.stats) {
+          if (kind == GOLDY_NORM_LAYER) p.stats[2 * which * p.rows + row] = mean;
+          p.stats[(2 * which + 1) * p.rows + row] = rstd;
+        }
+      };
+      fetch(ahead, row + (D - 1) * step);
+      copy_wait<D - 1>();
+      if (R::SHIFT) team_sync<TEAM, THREADS>(team);
+      float v[VALS], x[VALS];
+      R::values(ring + 2 * at * R::RING_BYTES, f_in + row * p.ldf, n, t, v, lo);
+      R::values(ring + (2 * at + 1) * R::RING_BYTES, x_in + row * p.ldx, n, t, x, lo);
+      // (SHIFT: the ring's place is used again when every piece has been read, which
+      // the barriers of the norms make sure of, if there is one)
+      if (R::SHIFT && (WARPS == 1 || (p.norm_f == GOLDY_NORM_NONE && p.norm_y == GOLDY_NORM_NONE))) team_sync<TEAM, THREADS>(team);
+      at = at + 1 == D ? 0 : at + 1;
+      ahead = ahead + 1 == D ? 0 : ahead + 1;
+      normalise(p.norm_f, 0, v);
+#pragma unroll
+      for (int j = 0; j < VALS; ++j) v[j] = fmaf(v[j], a[j], fmaf(p.alpha, x[j], b[j]));
+      R::store(s_out + row * p.lds, n, t, v, lo);
+      if (p.norm_y == GOLDY_NORM_NONE) continue;
+      normalise(p.norm_y, 1, v);
+#pragma unroll
+      for (int j = 0; j < VALS; ++j) v[j] = fmaf(v[j], gamma[j], beta[j]);
+      R::store(y_out + row * p.ldy, n, t, v, lo);
+    }
+  } else {
+    // A row takes the statistics of F, then those of S.  The first of a row and the
+    // second of the row before it are exchanged together: one cluster barrier per row,
+    // and each phase has another row's arithmetic beside it (8192 x 12288 bf16: 261 us,
+    // one after the other 334; a team's own barrier is not worth it: 16384 x 2048 48
+    // and 44, 16384 x 1999 85 and 66).
+    struct Sums {
+      float s, m2, wm;                               // of a warp: sum, squares about its mean, mean (RMS: about 0)
     };
-    fetch(ahead, row + (D - 1) * step);
-    copy_wait<D - 1>();
+    auto sums_of = [&](int kind, const float (&v)[VALS]) {
+      Sums r = {0.0f, 0.0f, 0.0f};
+      if (kind == GOLDY_NORM_NONE) return r;
+      if (kind == GOLDY_NORM_RMS) {                  // (zeros outside the row)
+#pragma unroll
+        for (int j = 0; j < VALS; ++j) r.m2 = fmaf(v[j], v[j], r.m2);
+      } else {
+#pragma unroll
+        for (int j = 0; j < VALS; ++j) r.s += v[j];
+        r.s = warp_sum(r.s);
+        r.wm = r.s * warp_inv;
+#pragma unroll
+        for (int i = 0; i < R::SLOTS; ++i) {
+          if (!R::in(i, t, n)) continue;
+          const bool complete = R::complete(i, t, n, lo);
+#pragma unroll
+          for (int k = 0; k < R::PER; ++k) {
+            const float d = complete || R::inside(i, k, t, n, lo) ? v[i * R::PER + k] - r.wm : 0.0f;
+            r.m2 = fmaf(d, d, r.m2);
+          }
+        }
+      }
+      r.m2 = warp_sum(r.m2);
+      return r;
+    };
+    Sums sf = {0.0f, 0.0f, 0.0f}, sy = sf;           // what is sent
+    float2 of = make_float2(0.0f, 1.0f), oy = of;    // mean and rstd that come of it
+    auto send = [&](int flip) {
+      tell_cluster_warp<WARPS>(&slot[flip][0][0][0], rank, p.cluster, w, lane, make_float4(sf.s, sf.m2, warp_n, sf.wm));
+      tell_cluster_warp<WARPS>(&slot[flip][1][0][0], rank, p.cluster, w, lane, make_float4(sy.s, sy.m2, warp_n, sy.wm));
+      tell_cluster_begin();
+    };
+    auto receive = [&](int flip) {
+      tell_cluster_end();
+      auto joined = [&](int kind, int which) {
+        if (kind == GOLDY_NORM_NONE) return make_float2(0.0f, 1.0f);
+        const float4* all = &slot[flip][which][0][0];
+        float mean = 0.0f, m2 = 0.0f;
+        if (kind == GOLDY_NORM_LAYER) {
+          for (int k = lane; k < p.cluster * WARPS; k += 32) mean += all[k].x;
+          mean = warp_sum(mean) * p.inv_n;
+        }
+        for (int k = lane; k < p.cluster * WARPS; k += 32) {
+          const float4 q = all[k];
+          const float d = q.w - mean;
+          m2 += fmaf(q.z * d, d, q.y);
+        }
+        return make_float2(mean, rsqrtf(fmaf(warp_sum(m2), p.inv_n, p.eps)));
+      };
+      of = joined(p.norm_f, 0);
+      oy = joined(p.norm_y, 1);
+    };
+    auto keep = [&](int kind, int which, int64_t r, const float2& o) {
+      if (t != 0 || rank != 0 || !p.stats || kind == GOLDY_NORM_NONE) return;
+      if (kind == GOLDY_NORM_LAYER) p.stats[2 * which * p.rows + r] = o.x;
+      p.stats[(2 * which + 1) * p.rows + r] = o.y;
+    };
+    float v[VALS];                                   // S of the row whose Y is left
+    auto finish = [&](int64_t r) {
+      if (p.norm_y == GOLDY_NORM_NONE) return;
+      keep(p.norm_y, 1, r, oy);
+      const float shift = -oy.x;
+#pragma unroll
+      for (int j = 0; j < VALS; ++j) v[j] = fmaf((v[j] + shift) * oy.y, gamma[j], beta[j]);
+      R::store(y_out + r * p.ldy, n, t, v, lo);
+    };
+    auto first = [&](const uint8_t* from, int64_t r) {
+      if (p.norm_f == GOLDY_NORM_NONE || r >= p.rows) return;
+      float f[VALS];
+      R::values(from, f_in + r * p.ldf, n, t, f, lo);
+      sf = sums_of(p.norm_f, f);
+    };
+    // where threads read one another's pieces of the row that makes place for the next
+    // one, the barrier has to lie before that is asked for
+    constexpr bool LATE = !R::SHIFT;
+    const int64_t row0 = row;
+    int at = 0, ahead = D - 1, last_flip = 0;
+    copy_wait<D - 2>();
     if (R::SHIFT) team_sync<TEAM, THREADS>(team);
-    float v[VALS], x[VALS];
-    R::values(ring + 2 * at * R::RING_BYTES, f_in + row * p.ldf, n, t, v, lo);
-    R::values(ring + (2 * at + 1) * R::RING_BYTES, x_in + row * p.ldx, n, t, x, lo);
-    // (SHIFT: the ring's place is used again when every piece has been read, which
-    // the barriers of the norms make sure of, if there is one)
-    if (R::SHIFT && (WARPS == 1 || (p.norm_f == GOLDY_NORM_NONE && p.norm_y == GOLDY_NORM_NONE))) team_sync<TEAM, THREADS>(team);
-    at = at + 1 == D ? 0 : at + 1;
-    ahead = ahead + 1 == D ? 0 : ahead + 1;
-    normalise(p.norm_f, 0, v);
+    first(ring, row);
+    send(1);
+    if (!LATE) receive(1);
+    for (int flip = 0; row < p.rows; row += step, last_flip = flip, flip ^= 1) {
+      fetch(ahead, row + (D - 1) * step);            // where the row before this one was
+      copy_wait<D - 2>();
+      if (R::SHIFT) team_sync<TEAM, THREADS>(team);
+      if (LATE) receive(flip ^ 1);
+      if (row != row0) finish(row - step);
+      keep(p.norm_f, 0, row, of);
+      const uint8_t* from = ring + 2 * at * R::RING_BYTES;
+      at = at + 1 == D ? 0 : at + 1;
+      ahead = ahead + 1 == D ? 0 : ahead + 1;
+      float x[VALS];
+      R::values(from, f_in + row * p.ldf, n, t, v, lo);
+      R::values(from + R::RING_BYTES, x_in + row * p.ldx, n, t, x, lo);
+      // (the mean is subtracted before the scale: rows far from zero keep their digits)
+      const float shift = -of.x;
 #pragma unroll
-    for (int j = 0; j < VALS; ++j) v[j] = fmaf(v[j], a[j], fmaf(p.alpha, x[j], b[j]));
-    R::store(s_out + row * p.lds, n, t, v, lo);
-    if (p.norm_y == GOLDY_NORM_NONE) continue;
-    normalise(p.norm_y, 1, v);
-#pragma unroll
-    for (int j = 0; j < VALS; ++j) v[j] = fmaf(v[j], gamma[j], beta[j]);
-    R::store(y_out + row * p.ldy, n, t, v, lo);
+      for (int j = 0; j < VALS; ++j) v[j] = fmaf((v[j] + shift) * of.y, a[j], fmaf(p.alpha, x[j], b[j]));
+      R::store(s_out + row * p.lds, n, t, v, lo);
+      sy = sums_of(p.norm_y, v);
+      first(ring + 2 * at * R::RING_BYTES, row + step);
+      send(flip);
+      if (!LATE) receive(flip);
+    }
+    if (LATE) receive(last_flip);
+    finish(row - step);
   }
 }
 
 // FULL: both norms and dS are there.
 template <typename T, int TEAM, RowMode MODE, bool WIDE, bool FULL>
 __global__ void __launch_bounds__(bwd_threads(TEAM)) residual_norm_backward_kernel(const ResidualNormParams p) {
-  constexpr int THREADS = bwd_threads(TEAM), TEAMS = THREADS / TEAM, WARPS = TEAM / 32, VALS = kBwdVals, D = bwd_depth<T>();
+  constexpr int THREADS = bwd_threads(TEAM), TEAMS = THREADS / TEAM, WARPS = TEAM / 32, VALS = kBwdVals, D = norm_depth<T>();
   constexpr bool VEC = MODE == kWholeRows, FRAME = MODE == kFramedRows;
   using R = NormRow<T, VALS, TEAM, THREADS, VEC || FRAME, WIDE, FRAME>;
   __shared__ float4 slot[2][WIDE ? kMaxCluster : TEAMS][WARPS];
@@ -391,7 +492,8 @@ __global__ void __launch_bounds__(bwd_threads(TEAM)) residual_norm_backward_kern
   };
   auto send = [&](int flip) {
     if (WIDE) {
-      tell_cluster_begin<WARPS>(&slot[flip][0][0], rank, p.cluster, w, lane, warp_sum4(s1x, s1y, s2x, s2y, lane, nullptr));
+      tell_cluster_warp<WARPS>(&slot[flip][0][0], rank, p.cluster, w, lane, warp_sum4(s1x, s1y, s2x, s2y, lane, nullptr));
+      tell_cluster_begin();
     } else if (WARPS > 1) {
       warp_sum4(s1x, s1y, s2x, s2y, lane, reinterpret_cast<float*>(&slot[flip][team][w]));
     } else {

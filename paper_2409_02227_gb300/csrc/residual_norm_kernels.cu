@@ -21,12 +21,12 @@ NormKernel pick(bool full) {
   return {full ? reinterpret_cast<const void*>(&residual_norm_backward_kernel<T, TEAM, MODE, WIDE, ALL>)
                : reinterpret_cast<const void*>(&residual_norm_backward_kernel<T, TEAM, MODE, WIDE, false>),
           THREADS, THREADS / TEAM, 1,
-          std::max(size_t(4) * bwd_depth<T>() * R::RING_BYTES, size_t(kSums) * THREADS * kBwdVals * sizeof(float))};
+          std::max(size_t(4) * norm_depth<T>() * R::RING_BYTES, size_t(kSums) * THREADS * kBwdVals * sizeof(float))};
 #else
   constexpr int THREADS = fwd_threads(TEAM);
   using R = NormRow<T, kFwdVals, TEAM, THREADS, MODE != kAnyRows, WIDE, MODE == kFramedRows>;
   return {reinterpret_cast<const void*>(&residual_norm_forward_kernel<T, TEAM, MODE, WIDE>), THREADS, THREADS / TEAM,
-          512 / THREADS, size_t(2) * kFwdDepth * R::RING_BYTES};
+          512 / THREADS, size_t(2) * (WIDE ? norm_depth<T>() : kFwdDepth) * R::RING_BYTES};
 #endif
 }
 
