@@ -54,8 +54,8 @@ struct ResidualNormShape {
 // How rows lie: in whole blocks of 16 bytes; all arrays' rows r the same number of
 // elements behind a block's start, a number that comes again every few rows, so that
 // a team whose rows are that far apart has its parameters, sums and data in one
-// frame (bf16, 16384 rows of 1999: 66 us, backwards 110, in the ways for rows that
-// lie anyhow 79 and 185; of 201: 16 and 25, then 34 and 34); or anyhow.
+// frame (bf16, 16384 rows of 1999: 66 us, backwards 104, in the ways for rows that
+// lie anyhow 78 and 184; of 201: 16 and 23, then 34 and 34); or anyhow.
 enum RowMode { kWholeRows = 0, kFramedRows = 1, kAnyRows = 2 };
 
 // The kernel for a shape, per direction, type and mode (residual_norm_kernels.cu).
