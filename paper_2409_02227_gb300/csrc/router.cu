@@ -17,6 +17,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <climits>
 #include <cmath>
 
 #include "layer_launch.h"
@@ -254,8 +255,9 @@ __global__ void __launch_bounds__(kWarps * 32) router_backward_kernel(const Rout
 // both, in an order that three steps of compare and exchange sort): first those of
 // a lane, then those of the eight lanes, after which every lane knows the row's
 // eight largest keys.  bf16 logits leave room for the index in the key; of fp32
-// logits, a lane that holds one of them finds its slot by its key, and rows in which
-// two of these are equal go the way above.
+// logits, a lane that holds one of them finds its slot by its key, and where two of
+// these are equal the team looks for the lowest index slot by slot (32768 x 128
+// fp32 forwards: 10.2 us, logits that hold bf16 values 14.2).
 
 constexpr int kTeam = 8;
 constexpr int kTop = 8;
@@ -333,7 +335,7 @@ __device__ __forceinline__ float team_sum(float v) {
 }
 
 template <typename T, int VPL>
-__global__ void __launch_bounds__(kWarps * 32) router_forward_small_kernel(const RouterParams p) {
+__global__ void __launch_bounds__(kWarps * 32, VPL > 16 ? 2 : 4) router_forward_small_kernel(const RouterParams p) {
   using S = Share<T, VPL>;
   constexpr bool INDEXED = sizeof(T) == 2;         // the key's lower half holds the index
   ptx::griddep_launch_dependents();
@@ -418,9 +420,30 @@ __global__ void __launch_bounds__(kWarps * 32) router_forward_small_kernel(const
       bool twice = chosen != found;
 #pragma unroll
       for (int j = 0; j + 1 < kTop; ++j) twice |= j + 1 < found && best[j] == best[j + 1];
+      // slots of equal logits, and the last one where more logits than slots have its
+      // key: by index, the lowest behind the one before
+      uint32_t shared = 0;
       if (__any_sync(kAll, there && twice)) {
-        for (int r = 0; r < 32 / kTeam && row4 + r < p.rows; ++r) forward_row<T, 0>(p, row4 + r, threadIdx.x & 31);
-        continue;
+        int last = -1;
+#pragma unroll
+        for (int j = 0; j < kTop; ++j) {
+          const bool again = j > 0 && best[j] == best[j > 0 ? j - 1 : 0];
+          const bool is = j < found && (again || (j + 1 < found ? best[j] == best[j + 1 < kTop ? j + 1 : j] : chosen > found));
+          if (!__any_sync(kAll, is)) continue;
+          shared |= uint32_t(is) << j;
+          if (!again) last = -1;
+          int c = INT_MAX;
+#pragma unroll
+          for (int i = VPL - 1; i >= 0; --i)
+            if (key[i] == best[j] && S::index(i, lane) > last) c = S::index(i, lane);
+#pragma unroll
+          for (int d = 1; d < kTeam; d *= 2) c = min(c, __shfl_xor_sync(kAll, c, d));
+          last = c;
+          if (there && is && lane == j) {
+            ids[j] = c;
+            weights[j] = exp_below(value(best[j]) - top) * share;
+          }
+        }
       }
       if (!there) mine = 0;
       while (mine) {
@@ -431,6 +454,7 @@ __global__ void __launch_bounds__(kWarps * 32) router_forward_small_kernel(const
         int slot = 0;
 #pragma unroll
         for (int j = 0; j < kTop; ++j) slot += best[j] > k;
+        if (shared >> slot & 1) continue;
         ids[slot] = c;
         weights[slot] = exp_below(v - top) * share;
       }
