@@ -250,14 +250,14 @@ __global__ void __launch_bounds__(kWarps * 32) router_backward_kernel(const Rout
 
 // ---- up to 8 of up to 256 experts: eight lanes per row ---------------------------
 // Four rows per warp share every instruction (a warp per row: 32768 x 128 forwards
-// and backwards 32 us, now 18).  A lane sorts its keys eight at a time,
+// and backwards 32 us, now 17).  A lane sorts its keys eight at a time,
 // and lists are merged (the larger of A[i] and B[7 - i] are the eight largest of
 // both, in an order that three steps of compare and exchange sort): first those of
 // a lane, then those of the eight lanes, after which every lane knows the row's
 // eight largest keys.  bf16 logits leave room for the index in the key; of fp32
 // logits, a lane that holds one of them finds its slot by its key, and where two of
 // these are equal the team looks for the lowest index slot by slot (32768 x 128
-// fp32 forwards: 10.2 us, logits that hold bf16 values 14.2).
+// fp32 forwards: 10.4 us, logits that hold bf16 values 14.7).
 
 constexpr int kTeam = 8;
 constexpr int kTop = 8;
@@ -325,8 +325,37 @@ struct Share {
   }
 };
 
-// exp(x) for x <= 0 (NaN stays NaN)
-__device__ __forceinline__ float exp_below(float x) { return fast_exp2(x * kLog2E); }
+// exp(x) for x <= 0 (NaN stays NaN): exp(x) = 2^y exp(x - y ln 2) for any y, here x
+// log2 e as it is rounded, which alone would cost |x| u and more.  What is left, r,
+// is below 2^-15, so that 1 + r is its exponential; ln 2 is taken in two parts.
+// Where r is no such number, x being infinite or far down, the power is 0.
+// (32768 x 128 fp32: 10.4 us and, backwards, 6.2; without r 10.2 and 6.0, with expf 11.1 and 6.5.)
+constexpr float kLn2 = 0.693147180559945309f, kLn2Rest = float(0.693147180559945309 - double(kLn2));
+__device__ __forceinline__ uint64_t exp_below2(uint64_t x) {
+  const uint64_t y = mul2(x, two(kLog2E));
+  const float2 p = apart(y), r = apart(fma2(y, two(-kLn2Rest), fma2(y, two(-kLn2), x)));
+  const uint64_t e = two(fast_exp2(p.x), fast_exp2(p.y));
+  return fma2(e, two(fminf(r.x, 1.0f), fminf(r.y, 1.0f)), e);
+}
+__device__ __forceinline__ float exp_below(float x) {
+  const float y = x * kLog2E, r = fmaf(y, -kLn2Rest, fmaf(y, -kLn2, x)), e = fast_exp2(y);
+  return fmaf(e, fminf(r, 1.0f), e);
+}
+// f = exp(f - top), and their sum
+template <int N>
+__device__ __forceinline__ float exp_all(float (&f)[N], float top) {
+  uint64_t sum = two(0.0f);
+#pragma unroll
+  for (int i = 0; i < N; i += 2) {
+    const uint64_t e = exp_below2(add2(two(f[i], f[i + 1]), two(-top)));
+    sum = add2(sum, e);
+    const float2 v = apart(e);
+    f[i] = v.x;
+    f[i + 1] = v.y;
+  }
+  const float2 v = apart(sum);
+  return v.x + v.y;
+}
 // sum over a team's lanes, to all of them
 __device__ __forceinline__ float team_sum(float v) {
 #pragma unroll
@@ -392,9 +421,7 @@ __global__ void __launch_bounds__(kWarps * 32, VPL > 16 ? 2 : 4) router_forward_
     const float top = found ? value(best[0]) : 0.0f;
     float total = 0.0f;
     if (p.over == GOLDY_ROUTER_ALL) {
-#pragma unroll
-      for (int i = 0; i < VPL; ++i) total += exp_below(f[i] - top);
-      total = team_sum(total);
+      total = team_sum(exp_all(f, top));
     } else {
 #pragma unroll
       for (int j = 0; j < kTop; ++j) total += j < found ? exp_below(value(best[j]) - top) : 0.0f;
@@ -467,7 +494,7 @@ __global__ void __launch_bounds__(kWarps * 32, VPL > 16 ? 2 : 4) router_forward_
 }
 
 template <typename T, int VPL>
-__global__ void __launch_bounds__(kWarps * 32) router_backward_small_kernel(const RouterParams p) {
+__global__ void __launch_bounds__(kWarps * 32, VPL > 16 ? 2 : VPL > 8 ? 4 : 6) router_backward_small_kernel(const RouterParams p) {
   using S = Share<T, VPL>;
   ptx::griddep_launch_dependents();
   ptx::griddep_wait();
@@ -508,14 +535,7 @@ __global__ void __launch_bounds__(kWarps * 32) router_backward_small_kernel(cons
     if (none) top = 0.0f;
     const float e = owner ? exp_below(l - top) : 0.0f;
     float total = e;
-    if (all) {
-      total = 0.0f;
-#pragma unroll
-      for (int i = 0; i < VPL; ++i) {
-        f[i] = exp_below(f[i] - top);
-        total += f[i];
-      }
-    }
+    if (all) total = exp_all(f, top);
     total = team_sum(total);
     const float inv = none && total == 0.0f ? 0.0f : 1.0f / total, prob = e * inv;
     const float dot = team_sum(owner ? g * prob : 0.0f), back = -dot * inv;
