@@ -615,7 +615,8 @@ goldy_status goldy_layernorm_backward(const goldy_layernorm_desc* desc, const vo
  * expert e is
  *   GOLDY_ROUTER_ALL     scale * exp(l_e) / sum of exp(l) over all experts
  *   GOLDY_ROUTER_CHOSEN  scale * exp(l_e) / sum of exp(l) over the chosen ones
- * computed in fp32 from the logits less their largest.  Logits and dlogits have
+ * computed in fp32 from the logits less their largest; a row's results are the same
+ * bits whatever the other rows hold.  Logits and dlogits have
  * `dtype`, any row strides >= experts, element alignment; ids (int32) and
  * weights (fp32) are packed rows x k.  Results must not overlap inputs unless
  * stated. */

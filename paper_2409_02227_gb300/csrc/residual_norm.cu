@@ -15,8 +15,9 @@
 // beta_f, so that four vectors fit the registers (16384 x 4096 bf16: 89 us, 6.0
 // TB/s).  Backwards the second sums of a row and the first of the next one are
 // exchanged at one barrier (16384 x 2048 bf16: 77 us, 5.2 TB/s; with a barrier for
-// each 110), and the arithmetic is in pairs (one by one: 90); what bounds it is
-// instructions, 16 warps per SM being all that the sums leave room for.  A cluster's
+// each 110), and the arithmetic is in pairs (one by one: 90); instructions issue in
+// 59% of the slots, and the 16 warps per SM that the sums leave room for do not hide
+// the rest, their own latencies.  A cluster's
 // warps tell one another their sums directly, and the next row is asked for before
 // the answer is waited for (4096 x 8192 backwards: 104 us; sums joined in each CTA
 // first: 123).  The CTAs' partial rows are summed in CTA order by a second kernel.

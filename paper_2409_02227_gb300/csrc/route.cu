@@ -16,10 +16,14 @@
 // its places (dispatch: X is read once) or from all of them (combine).  The
 // gradient takes 8 to 32 lanes per slot, which also sum the dot product.  bf16: 16384
 // x 4096 to two places 57 us (7.0 TB/s, with the sort before it 66), 8192 x 8 x 2048
-// back with weights and residual 54 (6.2 TB/s).  Rows that start on any element take
-// two blocks of the source per block of the result: 4 to 6 more instructions per
-// element pair, which then bound them (8192 x 8 x 1111: 46, 47 and 73 us, twice the
-// floors).
+// back with weights and residual 54 (6.2 TB/s), its gradient 88 (6.5 TB/s).  Rows that
+// start on any element take two blocks of the source per block of the result, 4 to 6
+// more instructions per element pair, and partly written blocks (8192 x 8 x 1111: 46,
+// 47 and 74 us, floors 27, 24 and 46).  The gradient's lanes also take a row in whole
+// steps of 64 blocks and the slots in whole rounds (5000 x 3 x 1111: 21 us, floor
+// 11.5; 72% of the lanes and 77% of the rounds are filled).  The placing kernel's
+// every CTA adds up all chunks' counts, so that many slots over many experts cost by
+// chunks x chunks x experts (262144 slots over 64 experts 18 us, 256 41, 4096 599).
 #include <cuda_runtime.h>
 
 #include <algorithm>

@@ -256,6 +256,7 @@ class RoutedFeedForward(FeedForward):
         G.goldy_route_combine(self.route, de.data_ptr(), self.place.data_ptr(), dn.data_ptr(), stream=stream)
         dlogits = torch.empty_like(self.logits)
         G.goldy_router_backward(self.router, self.logits.data_ptr(), self.ids.data_ptr(), dw.data_ptr(), dlogits.data_ptr(), stream)
+        # the products take bf16 rows: a rounding of the gradient that reaches wr and the normed rows
         dlogits = dlogits.bfloat16()
         G.goldy_linear_weight_grad(self.scores, self.normed.data_ptr(), dlogits.data_ptr(), g["wr"].data_ptr(), **dense)
         G.goldy_linear_input_grad(self.scores, dlogits.data_ptr(), p["wr"].data_ptr(), dn.data_ptr(), residual=dn.data_ptr(), **dense)
